@@ -70,6 +70,9 @@ typedef enum { UC_POLICY_PROTECTED = -1, UC_POLICY_EVICT = 0, UC_POLICY_QUANT = 
 #define UC_MAX_SEGMENTS 8 /* segments per attend call / types per table */
 #define UC_MAX_QTOKENS 8  /* decode-shaped attend calls; more take the dense path */
 #define UC_MAX_CALLS 8    /* decode calls per uc_attend_batch launch */
+#define UC_MAX_LINEAR_HEADS 64 /* KV heads per uc_linear_attend call */
+#define UC_MAX_BEAMS 32   /* beams per request in uc_beam_select */
+#define UC_MAX_BEAM_OUT 32 /* continuations per request in uc_beam_select */
 
 /*
  * One compressed segment: one cache type of one layer, for B sequences and
@@ -613,6 +616,107 @@ uc_status uc_append(uc_segment* seg, const void* k_new, const void* v_new, int32
  */
 uc_status uc_append_next(uc_segment* seg, const void* k_new, const void* v_new, int32_t base_position,
                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------- layers with a state of constant size */
+
+/* bf16 rows of UC_HEAD_DIM contiguous elements: row (b, h, t) starts at
+ * ptr + b*stride_b + h*stride_h + t*stride_t (strides in elements, multiples
+ * of 8; the stride of an extent of 1 is not used). Both [B, H, T, 128] and
+ * [B, T, H, 128] memory are described this way. */
+typedef struct uc_rows {
+  void* ptr;
+  int64_t stride_b, stride_h, stride_t;
+} uc_rows;
+
+/*
+ * Linear attention with a decay for each KV head, for layers whose cache is a
+ * state of constant size (no counterpart in the paper, whose models attend
+ * with softmax throughout; it serves models that mix both kinds of layer).
+ * Per sequence b and KV head j, with gamma_j = exp(log_decay[j]) <= 1:
+ *   S_t = gamma_j S_{t-1} + k_t v_t^T     (row: key channel, column: value channel)
+ *   o_t = S_t^T q_t / sqrt(128)           for every query head of KV head j
+ * for t = 0 .. lengths[b] - 1, starting from state_in (NULL: zeros), and
+ * state_out = S after the sequence's last token. Rows of out from lengths[b]
+ * on are written as zeros; rows of q, k and v there may hold anything.
+ *   q, out     n_q_heads heads of n_tok rows, k and v n_kv_heads
+ *   lengths    host int32 [B], 0 .. n_tok; NULL: n_tok for every sequence
+ *   log_decay  host float [n_kv_heads], finite, <= 0
+ *   state_in, state_out  fp32 [B, Hkv, 128, 128]; they may be the same array
+ *              (the state is then updated in place) but not overlap otherwise
+ * Query head h reads KV head h / (Hq / Hkv). fp32 throughout but for the
+ * outputs' rounding. 1 <= B <= UC_MAX_BATCH, Hkv <= UC_MAX_LINEAR_HEADS,
+ * n_tok >= 1. out must not overlap q, k or v.
+ * workspace: uc_linear_workspace_size() bytes, 16-byte aligned.
+ */
+uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v, int32_t batch, int32_t n_q_heads,
+                           int32_t n_kv_heads, int32_t n_tok, const int32_t* lengths, const float* log_decay,
+                           const float* state_in, float* state_out, const uc_rows* out, void* workspace,
+                           size_t workspace_bytes, void* stream);
+size_t uc_linear_workspace_size(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_tok);
+
+/* ---------------------------------- several continuations (beams) per request */
+
+typedef enum { UC_FP32 = 0, UC_BF16 = 1, UC_FP16 = 2 } uc_dtype;
+
+/*
+ * The best n continuations of every request over its beams and the
+ * vocabulary. A continuation of beam k by token v scores
+ *   c = scores[b, k] + log softmax(logits[b, k])_v
+ * and the n best come out by descending c; equal c by ascending beam, then
+ * descending logit, then ascending token, so the result is unique. fp32
+ * arithmetic whatever the logits' type.
+ *   logits    [B, K, V] of `dtype`, row (b, k) at b*stride_b + k*stride_k
+ *             elements, V contiguous; -inf bans a token. NaN or +inf sets
+ *             UC_ERR_RANGE in the status word (and counts as -inf)
+ *   scores    fp32 [B, K], -inf for a beam that is not alive yet; NaN or +inf
+ *             sets UC_ERR_RANGE
+ *   finished  uint8 [B, K], nullable: a finished beam has one continuation,
+ *             token `eos`, that keeps its score; its logits are not read
+ *   eos       the end token, or -1 for none (finished must then be NULL)
+ *   out_scores fp32, out_parent (the beam), out_token int32 [B, n]
+ *   out_finished uint8 [B, n], nullable: 1 where the token is eos or the
+ *             parent was finished
+ * Where fewer than n continuations have a finite score the rest follow with
+ * -inf in the same order. 1 <= K <= UC_MAX_BEAMS, 1 <= n <= UC_MAX_BEAM_OUT,
+ * n <= K * V, B * K <= 65535. workspace: uc_beam_workspace_size() bytes,
+ * 16-byte aligned.
+ */
+uc_status uc_beam_select(const void* logits, int32_t dtype, int64_t stride_b, int64_t stride_k, int32_t batch,
+                         int32_t n_beams, int32_t vocab, const float* scores, const uint8_t* finished, int32_t eos,
+                         int32_t n, float* out_scores, int32_t* out_parent, int32_t* out_token,
+                         uint8_t* out_finished, void* workspace, size_t workspace_bytes, void* stream);
+size_t uc_beam_workspace_size(int32_t batch, int32_t n_beams, int32_t vocab, int32_t n);
+
+/* One cache to reorder: a segment pair (src, dst non-NULL) or a pair of
+ * arrays of `state_bytes` per sequence (a multiple of 4, 4-byte aligned),
+ * for example the states of uc_linear_attend. */
+typedef struct uc_reorder_item {
+  const uc_segment* src;
+  uc_segment* dst;
+  const void* state_src;
+  void* state_dst;
+  uint64_t state_bytes;
+} uc_reorder_item;
+
+/*
+ * Caches follow the beams that were chosen: sequence g*n_to + i of every
+ * target becomes a copy of sequence g*n_from + parent[g, i] of its source
+ * (g < n_groups; parent device int32 [n_groups, n_to], 0 <= parent < n_from).
+ * With n_from = 1 this expands a request's prompt caches to its beams; with
+ * n_from = n_to it reorders them after a selection. Of a segment only what a
+ * sequence holds is copied (rows, codes, parameters, tail, indices, count).
+ * src and dst share kind, bits, n_kv_heads and n_src, dst->cap >= src->cap,
+ * src->batch = n_groups * n_from, dst->batch = n_groups * n_to; FULL targets
+ * are views of the caller's rows, which are written. Sources and targets must
+ * not share storage. The sequences of one group hold the same number of
+ * tokens (src->n_kept_host); dst->n_kept_host takes it over. All items of a
+ * call go in as few launches as their number of arrays allows. A parent out
+ * of range sets UC_ERR_RANGE in the status word, a device count beyond src's
+ * capacity UC_ERR_BUDGET; that sequence is then not written. workspace: >= 256 bytes
+ * (status word).
+ */
+uc_status uc_reorder(const uc_reorder_item* items, int32_t n_items, const int32_t* parent, int32_t n_groups,
+                     int32_t n_from, int32_t n_to, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -26,10 +26,12 @@ Modules and the passages they follow:
                   decode tokens (§3.4, App. E).
 * ``attention`` — one shared softmax over all segments, with log-sum-exp and
                   per-segment attention mass (App. E, Eq. 1).
+* ``linear``    — linear attention with a decay for each KV head.
+* ``beams``     — beam selection and the reordering of sequences.
 
 Parity status of each function is stated in its module docstring. The only
 unpinned item is whether Gaussian synthetic attention resembles a trained
 model's (no model weights or datasets exist here): "parity unpinned" for
 workload realism, not for any function below.
 """
-from . import scores, policy, select, quant, segment, attention  # noqa: F401
+from . import scores, policy, select, quant, segment, attention, linear, beams  # noqa: F401

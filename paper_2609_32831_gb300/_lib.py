@@ -75,7 +75,20 @@ class UcAttendLaunchInfo(C.Structure):
     _fields_ = [("cluster", C.c_int32), ("ctas", C.c_int32), ("stages", C.c_int32), ("merge_width", C.c_int32)]
 
 
+class UcRows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("stride_t", C.c_int64)]
+
+
+class UcReorderItem(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("state_src", C.c_void_p), ("state_dst", C.c_void_p),
+                ("state_bytes", C.c_uint64)]
+
+
 MAX_CALLS = 8
+MAX_LINEAR_HEADS = 64
+MAX_BEAMS = 32
+MAX_BEAM_OUT = 32
+FP32, BF16, FP16 = range(3)
 
 # uc_allocator: stream-ordered device memory hooks for library-owned segments
 ALLOC_FN = C.CFUNCTYPE(C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p)
@@ -132,6 +145,13 @@ _SIGS = {
     "uc_attend_batch": (C.c_int, [_P, C.c_int32, _P, C.c_size_t, _P]),
     "uc_attend_batch_workspace_size": (C.c_size_t, [_P, C.c_int32]),
     "uc_attend_static": (C.c_int, [_P, C.c_int32, C.c_int32, _P, C.c_int32, _P, _P, _P, _P]),
+    "uc_linear_attend": (C.c_int, [_P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P, _P, _P, _P,
+                                   C.c_size_t, _P]),
+    "uc_linear_workspace_size": (C.c_size_t, [C.c_int32] * 4),
+    "uc_beam_select": (C.c_int, [_P, C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, _P, _P,
+                                 C.c_int32, C.c_int32, _P, _P, _P, _P, _P, C.c_size_t, _P]),
+    "uc_beam_workspace_size": (C.c_size_t, [C.c_int32] * 4),
+    "uc_reorder": (C.c_int, [_P, C.c_int32, _P, C.c_int32, C.c_int32, C.c_int32, _P, C.c_size_t, _P]),
     "uc_append": (C.c_int, [C.POINTER(UcSegment), _P, _P, C.c_int32, _P, C.c_size_t, _P]),
     "uc_append_next": (C.c_int, [C.POINTER(UcSegment), _P, _P, C.c_int32, _P, C.c_size_t, _P]),
 }

@@ -593,6 +593,128 @@ def append_next(seg: Segment, k_new: torch.Tensor, v_new: torch.Tensor, base_pos
         C.byref(seg.c), _ptr(k_new), _ptr(v_new), int(base_position), wp, wn, _stream(stream)))
 
 
+# -------------------------------------- layers with a state of constant size
+
+def _rows(t: torch.Tensor) -> "_lib.UcRows":
+    sb, sh, st, _ = t.stride()
+    return _lib.UcRows(t.data_ptr(), sb, sh, st)
+
+
+def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: Sequence[float],
+                  state: Optional[torch.Tensor] = None, out_state: Optional[torch.Tensor] = None,
+                  lengths: Optional[Sequence[int]] = None, out: Optional[torch.Tensor] = None,
+                  ws: Optional[Workspace] = None, stream=None):
+    """Linear attention with a decay for each KV head (uc_linear_attend):
+    S_t = exp(log_decay) S_{t-1} + k_t v_t^T, o_t = S_t^T q_t / sqrt(128).
+
+    q [B, Hq, T, 128], k, v [B, Hkv, T, 128] bf16 with contiguous rows and any
+    strides that are multiples of 8 (so [B, T, H, 128] memory transposed to
+    [B, H, T, 128] works). log_decay: Hkv host floats <= 0. state [B, Hkv,
+    128, 128] fp32: what earlier tokens left (None: zeros). out_state: where
+    the new state goes (may be ``state``: in place). lengths: host tokens per
+    sequence (None: T); outputs behind them are zero. Returns (out, out_state),
+    out with q's shape and strides."""
+    B, hq, T, d = q.shape
+    hkv = k.shape[1]
+    if q.dtype != torch.bfloat16 or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16 or d != HEAD_DIM:
+        raise ValueError("linear_attend: q, k and v are bf16 with 128 channels")
+    if k.shape != (B, hkv, T, d) or v.shape != k.shape or q.stride(3) != 1 or k.stride(3) != 1 or v.stride(3) != 1:
+        raise ValueError("linear_attend: k and v are [B, Hkv, T, 128], every row contiguous")
+    if len(log_decay) != hkv or (lengths is not None and len(lengths) != B):
+        raise ValueError("linear_attend: one log_decay per KV head, one length per sequence")
+    if out is None:
+        out = torch.empty_like(q)
+        if stream is not None:
+            out.record_stream(stream)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.stride(3) != 1:
+        raise ValueError("linear_attend: out has q's shape and type, every row contiguous")
+    if out_state is None:
+        out_state = torch.empty((B, hkv, d, d), dtype=torch.float32, device=q.device)
+        if stream is not None:
+            out_state.record_stream(stream)
+    for s in (state, out_state):
+        if s is not None and (s.shape != (B, hkv, d, d) or s.dtype != torch.float32 or not s.is_contiguous()):
+            raise ValueError("linear_attend: states are contiguous fp32 [B, Hkv, 128, 128]")
+    ws = ws or default_workspace(q.device)
+    L = lib()
+    wp, wn = ws.get(L.uc_linear_workspace_size(B, hq, hkv, T))
+    check("uc_linear_attend", L.uc_linear_attend(
+        C.byref(_rows(q)), C.byref(_rows(k)), C.byref(_rows(v)), B, hq, hkv, T,
+        None if lengths is None else (C.c_int32 * B)(*lengths), (C.c_float * hkv)(*log_decay), _ptr(state),
+        out_state.data_ptr(), C.byref(_rows(out)), wp, wn, _stream(stream)))
+    return out, out_state
+
+
+# ----------------------------------- several continuations (beams) per request
+
+_LOGIT_TYPES = {torch.float32: _lib.FP32, torch.bfloat16: _lib.BF16, torch.float16: _lib.FP16}
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int, finished: Optional[torch.Tensor] = None,
+                eos: int = -1, ws: Optional[Workspace] = None, stream=None):
+    """The best n continuations of every request (uc_beam_select): logits [B,
+    K, V] fp32, bf16 or fp16 (rows contiguous), scores [B, K] fp32, finished
+    [B, K] bool or None -> (scores fp32, parent int32, token int32, finished
+    bool), each [B, n], best first."""
+    B, K, V = logits.shape
+    if logits.dtype not in _LOGIT_TYPES or logits.stride(2) != 1:
+        raise ValueError("beam_select: logits are fp32, bf16 or fp16 with contiguous rows")
+    if scores.shape != (B, K) or scores.dtype != torch.float32 or not scores.is_contiguous():
+        raise ValueError("beam_select: scores are contiguous fp32 [B, K]")
+    if finished is not None and (finished.shape != (B, K) or finished.dtype not in (torch.bool, torch.uint8)
+                                 or not finished.is_contiguous()):
+        raise ValueError("beam_select: finished is contiguous bool [B, K]")
+    dev = logits.device
+    best = torch.empty((B, n), dtype=torch.float32, device=dev)
+    at = torch.empty((2, B, n), dtype=torch.int32, device=dev)
+    done = torch.empty((B, n), dtype=torch.bool, device=dev)
+    if stream is not None:
+        for t in (best, at, done):
+            t.record_stream(stream)
+    parent, token = at.unbind(0)
+    ws = ws or default_workspace(dev)
+    L = lib()
+    wp, wn = ws.get(L.uc_beam_workspace_size(B, K, V, n))
+    check("uc_beam_select", L.uc_beam_select(
+        logits.data_ptr(), _LOGIT_TYPES[logits.dtype], logits.stride(0), logits.stride(1), B, K, V, scores.data_ptr(),
+        _ptr(finished), eos, n, best.data_ptr(), parent.data_ptr(), token.data_ptr(), done.data_ptr(), wp, wn,
+        _stream(stream)))
+    return best, parent, token, done
+
+
+def reorder(pairs, parent: torch.Tensor, ws: Optional[Workspace] = None, stream=None) -> None:
+    """Caches follow their beams (uc_reorder). ``pairs``: (source, target)
+    pairs of Segments, or of contiguous tensors [sequences, ...] such as the
+    states of ``linear_attend``. parent [groups, n_to] int32: sequence g * n_to
+    + i of a target becomes sequence g * n_from + parent[g, i] of its source,
+    n_from = the sources' sequences / groups. Sources and targets share no
+    storage: callers keep two of each and use them in turn."""
+    if parent.dtype != torch.int32 or parent.dim() != 2 or not parent.is_contiguous():
+        raise ValueError("reorder: parent is a contiguous int32 [groups, n_to]")
+    groups, n_to = parent.shape
+    items, n_seq = [], None
+    for src, dst in pairs:
+        if isinstance(src, Segment):
+            have = src.batch
+            items.append(_lib.UcReorderItem(C.addressof(src.c), C.addressof(dst.c), None, None, 0))
+        else:
+            have = src.shape[0]
+            if not (src.is_contiguous() and dst.is_contiguous()) or src.dtype != dst.dtype \
+                    or src.shape[1:] != dst.shape[1:] or dst.shape[0] != groups * n_to:
+                raise ValueError("reorder: tensors are contiguous [sequences, ...] of one type and shape per sequence")
+            items.append(_lib.UcReorderItem(None, None, src.data_ptr(), dst.data_ptr(),
+                                            src.element_size() * (src.numel() // have if have else 0)))
+        if n_seq not in (None, have):
+            raise ValueError("reorder: the sources hold different numbers of sequences")
+        n_seq = have
+    if n_seq is None or groups == 0 or n_seq % groups:
+        raise ValueError("reorder: the sources' sequences are a multiple of the groups")
+    ws = ws or default_workspace(parent.device)
+    wp, wn = ws.get(256)
+    check("uc_reorder", lib().uc_reorder((_lib.UcReorderItem * len(items))(*items), len(items), parent.data_ptr(),
+                                         groups, n_seq // groups, n_to, wp, wn, _stream(stream)))
+
+
 def set_dense_serial_pv(serial: bool) -> bool:
     """A setting of the dense attention kernel kept for its callers, without
     effect any more (see unicache.h); returns the previous one."""

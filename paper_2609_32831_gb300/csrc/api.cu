@@ -28,7 +28,7 @@ void set_error(const char* fmt, ...) {
 
 void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 
-static uc_status cuda_check(const char* where) {
+uc_status cuda_check(const char* where) {
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) {
     set_error("%s: %s", where, cudaGetErrorString(e));
@@ -125,7 +125,7 @@ static uc_status segment_maps(const uc_segment* seg, CUtensorMap* mk, CUtensorMa
   return UC_OK;
 }
 
-static int num_sms() {
+int num_sms() {
   static int n = 0;
   if (n == 0) {
     int dev = 0;
@@ -139,7 +139,7 @@ static int num_sms() {
 static bool is_quant(int kind) { return kind == UC_KIND_QUANT || kind == UC_KIND_EVICT_QUANT; }
 
 // Validates the descriptor of a segment (storage pointers included).
-static uc_status check_segment(const uc_segment* s, const char* fn) {
+uc_status check_segment(const uc_segment* s, const char* fn) {
   if (s == nullptr) {
     set_error("%s: null segment", fn);
     return UC_ERR_ARG;

@@ -1,0 +1,372 @@
+// C-ABI entry points of generation beside the segment cache: linear attention
+// over a constant-size state, beam selection, and the reordering of caches
+// and states. Argument validation and launches; nothing here allocates.
+#include <climits>
+#include <cmath>
+#include <cstring>
+
+#include "common.cuh"
+#include "internal.h"
+
+namespace uc {
+namespace {
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+// Do [a, a + an) and [b, b + bn) share a byte?
+bool overlap(const void* a, uint64_t an, const void* b, uint64_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return an != 0 && bn != 0 && x < y + bn && y < x + an;
+}
+
+uc_status check_workspace(const void* workspace, size_t bytes, size_t need, const char* fn) {
+  if (workspace == nullptr || !aligned(workspace, 16)) {
+    set_error("%s: workspace must be non-null and 16-byte aligned", fn);
+    return UC_ERR_ARG;
+  }
+  if (bytes < need) {
+    set_error("%s: workspace of %zu bytes, %zu needed", fn, bytes, need);
+    return UC_ERR_OOM;
+  }
+  return UC_OK;
+}
+
+// Rows of `heads` heads of `n_tok` tokens: strides in the kernels' form (0
+// where the extent is 1) and the bytes from the first row to the last's end.
+uc_status check_rows(const uc_rows* r, const char* what, int batch, int heads, int n_tok, RowsDev* out,
+                     uint64_t* extent) {
+  if (r == nullptr || r->ptr == nullptr || !aligned(r->ptr, 16)) {
+    set_error("uc_linear_attend: %s must be non-null and 16-byte aligned", what);
+    return UC_ERR_ARG;
+  }
+  const int64_t stride[3] = {batch > 1 ? r->stride_b : 0, heads > 1 ? r->stride_h : 0, n_tok > 1 ? r->stride_t : 0};
+  const int size[3] = {batch, heads, n_tok};
+  int64_t last = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (size[i] > 1 && (stride[i] < UC_HEAD_DIM || stride[i] % 8 != 0 || stride[i] > (int64_t(1) << 37))) {
+      set_error("uc_linear_attend: strides of %s must be multiples of 8 elements, at least %d and below 2^37", what,
+                UC_HEAD_DIM);
+      return UC_ERR_SHAPE;
+    }
+    last += stride[i] * (size[i] - 1);
+  }
+  *out = RowsDev{static_cast<__nv_bfloat16*>(r->ptr), stride[0], stride[1], stride[2]};
+  *extent = 2ull * (uint64_t)(last + UC_HEAD_DIM);
+  return UC_OK;
+}
+
+}  // namespace
+}  // namespace uc
+
+using namespace uc;
+
+extern "C" {
+
+// ------------------------------------------------------- linear attention
+size_t uc_linear_workspace_size(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_tok) {
+  UC_TRACE();
+  if (batch < 1 || n_q_heads < 1 || n_kv_heads < 1 || n_tok < 1) return 0;
+  return 256;
+}
+
+uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v, int32_t batch, int32_t n_q_heads,
+                           int32_t n_kv_heads, int32_t n_tok, const int32_t* lengths, const float* log_decay,
+                           const float* state_in, float* state_out, const uc_rows* out, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  UC_TRACE();
+  if (batch < 1 || batch > UC_MAX_BATCH || n_kv_heads < 1 || n_kv_heads > UC_MAX_LINEAR_HEADS ||
+      n_q_heads < n_kv_heads || n_q_heads % n_kv_heads != 0 || n_q_heads > 65535 || n_tok < 1) {
+    set_error("uc_linear_attend: unsupported shape (batch %d, query heads %d, kv heads %d, tokens %d)", batch,
+              n_q_heads, n_kv_heads, n_tok);
+    return UC_ERR_SHAPE;
+  }
+  LinearParams p;
+  memset(&p, 0, sizeof(p));
+  uint64_t nq, nk, nv, no;
+  uc_status st = check_rows(q, "q", batch, n_q_heads, n_tok, &p.q, &nq);
+  if (st == UC_OK) st = check_rows(k, "k", batch, n_kv_heads, n_tok, &p.k, &nk);
+  if (st == UC_OK) st = check_rows(v, "v", batch, n_kv_heads, n_tok, &p.v, &nv);
+  if (st == UC_OK) st = check_rows(out, "out", batch, n_q_heads, n_tok, &p.out, &no);
+  if (st != UC_OK) return st;
+  if (log_decay == nullptr || state_out == nullptr || !aligned(state_out, 16) || !aligned(state_in, 16)) {
+    set_error("uc_linear_attend: log_decay and state_out must be non-null, states 16-byte aligned");
+    return UC_ERR_ARG;
+  }
+  const uint64_t ns = 4ull * batch * n_kv_heads * UC_HEAD_DIM * UC_HEAD_DIM;
+  // (rows of different tensors may interleave in one buffer, so only equal
+  // bases and the dense state arrays are compared)
+  if (out->ptr == q->ptr || out->ptr == k->ptr || out->ptr == v->ptr ||
+      (state_in != state_out && overlap(state_in, state_in ? ns : 0, state_out, ns))) {
+    set_error("uc_linear_attend: outputs overlap inputs");
+    return UC_ERR_ARG;
+  }
+  for (int j = 0; j < n_kv_heads; ++j) {
+    if (!std::isfinite(log_decay[j]) || log_decay[j] > 0.f) {
+      set_error("uc_linear_attend: log_decay[%d] must be finite and <= 0", j);
+      return UC_ERR_ARG;
+    }
+    p.log2_decay[j] = (double)log_decay[j] * 1.4426950408889634074;
+  }
+  for (int b = 0; b < batch; ++b) {
+    p.lengths[b] = lengths ? lengths[b] : n_tok;
+    if (p.lengths[b] < 0 || p.lengths[b] > n_tok) {
+      set_error("uc_linear_attend: lengths[%d] = %d outside [0, %d]", b, p.lengths[b], n_tok);
+      return UC_ERR_SHAPE;
+    }
+  }
+  st = check_workspace(workspace, workspace_bytes, uc_linear_workspace_size(batch, n_q_heads, n_kv_heads, n_tok),
+                       "uc_linear_attend");
+  if (st != UC_OK) return st;
+  p.state_in = state_in;
+  p.state_out = state_out;
+  p.batch = batch;
+  p.n_q_heads = n_q_heads;
+  p.n_kv_heads = n_kv_heads;
+  p.group = n_q_heads / n_kv_heads;
+  p.n_tok = n_tok;
+  p.scale = (float)(1.0 / std::sqrt((double)UC_HEAD_DIM));
+  launch_linear(p, reinterpret_cast<cudaStream_t>(stream));
+  return cuda_check("uc_linear_attend");
+}
+
+// --------------------------------------------------------- beam selection
+static int64_t beam_tiles(int32_t vocab) { return ((int64_t)vocab + kBeamTile - 1) / kBeamTile; }
+
+size_t uc_beam_workspace_size(int32_t batch, int32_t n_beams, int32_t vocab, int32_t n) {
+  UC_TRACE();
+  if (batch < 1 || n_beams < 1 || vocab < 1 || n < 1) return 0;
+  const uint64_t lists = (uint64_t)batch * n_beams * beam_tiles(vocab);
+  return 256 + lists * (sizeof(float2) + (uint64_t)n * 8);
+}
+
+uc_status uc_beam_select(const void* logits, int32_t dtype, int64_t stride_b, int64_t stride_k, int32_t batch,
+                         int32_t n_beams, int32_t vocab, const float* scores, const uint8_t* finished, int32_t eos,
+                         int32_t n, float* out_scores, int32_t* out_parent, int32_t* out_token,
+                         uint8_t* out_finished, void* workspace, size_t workspace_bytes, void* stream) {
+  UC_TRACE();
+  if (dtype != UC_FP32 && dtype != UC_BF16 && dtype != UC_FP16) {
+    set_error("uc_beam_select: bad logits type %d", dtype);
+    return UC_ERR_ARG;
+  }
+  if (batch < 1 || n_beams < 1 || n_beams > UC_MAX_BEAMS || vocab < 1 || n < 1 || n > UC_MAX_BEAM_OUT ||
+      (int64_t)batch * n_beams > 65535 || n > (int64_t)n_beams * vocab) {
+    set_error("uc_beam_select: unsupported shape (batch %d, beams %d, vocabulary %d, n %d)", batch, n_beams, vocab, n);
+    return UC_ERR_SHAPE;
+  }
+  if ((n_beams > 1 && stride_k < vocab) || (batch > 1 && stride_b < 1)) {
+    set_error("uc_beam_select: logits rows overlap (strides %lld, %lld)", (long long)stride_b, (long long)stride_k);
+    return UC_ERR_SHAPE;
+  }
+  if (logits == nullptr || scores == nullptr || out_scores == nullptr || out_parent == nullptr ||
+      out_token == nullptr || !aligned(logits, dtype == UC_FP32 ? 4 : 2) || !aligned(scores, 4) ||
+      !aligned(out_scores, 4) || !aligned(out_parent, 4) || !aligned(out_token, 4)) {
+    set_error("uc_beam_select: null or misaligned argument");
+    return UC_ERR_ARG;
+  }
+  if (eos < -1 || eos >= vocab || (finished != nullptr && eos < 0)) {
+    set_error("uc_beam_select: end token %d outside the vocabulary (%d), or finished beams without one", eos, vocab);
+    return UC_ERR_ARG;
+  }
+  const uc_status st = check_workspace(workspace, workspace_bytes, uc_beam_workspace_size(batch, n_beams, vocab, n),
+                                       "uc_beam_select");
+  if (st != UC_OK) return st;
+  BeamParams p;
+  memset(&p, 0, sizeof(p));
+  p.logits = logits;
+  p.stride_b = batch > 1 ? stride_b : 0;
+  p.stride_k = n_beams > 1 ? stride_k : 0;
+  p.scores = scores;
+  p.finished = finished;
+  p.out_scores = out_scores;
+  p.out_parent = out_parent;
+  p.out_token = out_token;
+  p.out_finished = out_finished;
+  p.batch = batch;
+  p.beams = n_beams;
+  p.vocab = vocab;
+  p.n = n;
+  p.tiles = (int)beam_tiles(vocab);
+  p.eos = eos;
+  p.status = static_cast<DevStatus*>(workspace);
+  const size_t lists = (size_t)batch * n_beams * p.tiles;
+  p.part_ms = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + 256);
+  p.part_x = reinterpret_cast<float*>(p.part_ms + lists);
+  p.part_tok = reinterpret_cast<int32_t*>(p.part_x + lists * n);
+  launch_beam(p, dtype, reinterpret_cast<cudaStream_t>(stream));
+  return cuda_check("uc_beam_select");
+}
+
+// ---------------------------------------------------------------- reorder
+namespace {
+
+struct ReorderList {
+  ReorderParams p;
+  cudaStream_t stream;
+  int64_t units = 0;
+  bool launched = false;
+
+  void flush() {
+    if (p.n_arrays == 0) return;
+    p.n_units = (int32_t)units;
+    launch_reorder(p, stream);
+    p.n_arrays = 0;
+    units = 0;
+  }
+  void add(const void* src, void* dst, int64_t src_block, int64_t dst_block, int heads, int unit, int live,
+           int max_units, const int32_t* n_kept, int max_kept) {
+    const int64_t parts = ((int64_t)max_units * unit + kReorderBytes - 1) / kReorderBytes;
+    const int64_t more = parts * heads * p.n_seq;
+    if (more == 0) return;
+    if (p.n_arrays == kReorderArrays || units + more > INT32_MAX) flush();
+    ReorderArray& a = p.a[p.n_arrays++];
+    a.src = static_cast<const uint8_t*>(src);
+    a.dst = static_cast<uint8_t*>(dst);
+    a.src_block = src_block;
+    a.dst_block = dst_block;
+    a.n_kept = n_kept;
+    a.heads = heads;
+    a.unit = unit;
+    a.live = live;
+    a.max_units = max_units;
+    a.max_kept = max_kept;
+    a.parts = (int32_t)parts;
+    a.begin = (int32_t)units;
+    units += more;
+  }
+};
+
+bool packed(const uc_segment* s) { return s->kind == UC_KIND_QUANT || s->kind == UC_KIND_EVICT_QUANT; }
+
+// Tokens a block of the segment can hold.
+int capacity(const uc_segment* s) { return s->kind == UC_KIND_FULL ? s->n_src : s->cap; }
+
+uc_status check_item(const uc_reorder_item& it, int i, int n_groups, int n_from, int n_to) {
+  if ((it.src == nullptr) != (it.dst == nullptr) || (it.state_src == nullptr) != (it.state_dst == nullptr) ||
+      (it.src == nullptr) == (it.state_src == nullptr)) {
+    set_error("uc_reorder: item %d is neither a pair of segments nor a pair of arrays", i);
+    return UC_ERR_ARG;
+  }
+  if (it.src == nullptr) {
+    if (it.state_bytes == 0 || it.state_bytes % 4 != 0 || it.state_bytes > INT32_MAX || !aligned(it.state_src, 4) ||
+        !aligned(it.state_dst, 4)) {
+      set_error("uc_reorder: item %d: %llu bytes per sequence (a multiple of 4 below 2^31, 4-byte aligned arrays)", i,
+                (unsigned long long)it.state_bytes);
+      return UC_ERR_SHAPE;
+    }
+    if (overlap(it.state_src, it.state_bytes * n_groups * n_from, it.state_dst, it.state_bytes * n_groups * n_to)) {
+      set_error("uc_reorder: item %d: source and target overlap", i);
+      return UC_ERR_ARG;
+    }
+    return UC_OK;
+  }
+  const uc_segment *s = it.src, *d = it.dst;
+  uc_status st = check_segment(s, "uc_reorder");
+  if (st == UC_OK) st = check_segment(d, "uc_reorder");
+  if (st != UC_OK) return st;
+  if (s->kind != d->kind || s->bits != d->bits || s->n_kv_heads != d->n_kv_heads || s->n_src != d->n_src ||
+      capacity(d) < capacity(s) || s->batch != n_groups * n_from || d->batch != n_groups * n_to) {
+    set_error("uc_reorder: item %d: segments differ (kind, bits, heads or source length), the target is smaller, or "
+              "their batches are not %d x %d and %d x %d", i, n_groups, n_from, n_groups, n_to);
+    return UC_ERR_SHAPE;
+  }
+  for (int g = 0; g < n_groups; ++g)
+    for (int j = 1; j < n_from; ++j)
+      if (s->n_kept_host[g * n_from + j] != s->n_kept_host[g * n_from]) {
+        set_error("uc_reorder: item %d: the sequences of group %d hold different numbers of tokens", i, g);
+        return UC_ERR_SHAPE;
+      }
+  for (const uc_segment* x : {s, d}) {
+    const int64_t last = ((int64_t)x->batch * x->n_kv_heads - 1) * x->row_stride + x->row_offset +
+                         (packed(x) ? UC_GROUP : capacity(x));
+    if (last > x->rows_total || x->row_stride < (packed(x) ? UC_GROUP : capacity(x))) {
+      set_error("uc_reorder: item %d: rows run past rows_total, or blocks overlap", i);
+      return UC_ERR_SHAPE;
+    }
+  }
+  uc_segment_sizes zs, zd;
+  st = uc_segment_sizes_of(s, &zs);
+  if (st == UC_OK) st = uc_segment_sizes_of(d, &zd);
+  if (st != UC_OK) return st;
+  const uint64_t ns = (uint64_t)s->rows_total * UC_HEAD_DIM * 2, nd = (uint64_t)d->rows_total * UC_HEAD_DIM * 2;
+  if (overlap(s->k, ns, d->k, nd) || overlap(s->v, ns, d->v, nd) || overlap(s->n_kept, zs.n_kept, d->n_kept, zd.n_kept) ||
+      overlap(s->kept_idx, zs.kept_idx, d->kept_idx, zd.kept_idx) ||
+      overlap(s->k_codes, zs.k_codes, d->k_codes, zd.k_codes) ||
+      overlap(s->v_codes, zs.v_codes, d->v_codes, zd.v_codes) ||
+      overlap(s->k_params, zs.k_params, d->k_params, zd.k_params) ||
+      overlap(s->v_params, zs.v_params, d->v_params, zd.v_params)) {
+    set_error("uc_reorder: item %d: source and target share storage", i);
+    return UC_ERR_ARG;
+  }
+  return UC_OK;
+}
+
+}  // namespace
+
+uc_status uc_reorder(const uc_reorder_item* items, int32_t n_items, const int32_t* parent, int32_t n_groups,
+                     int32_t n_from, int32_t n_to, void* workspace, size_t workspace_bytes, void* stream) {
+  UC_TRACE();
+  if (items == nullptr || parent == nullptr || !aligned(parent, 4)) {
+    set_error("uc_reorder: null or misaligned argument");
+    return UC_ERR_ARG;
+  }
+  if (n_items < 1 || n_groups < 1 || n_from < 1 || n_to < 1 || (int64_t)n_groups * n_from > 65535 ||
+      (int64_t)n_groups * n_to > 65535) {
+    set_error("uc_reorder: bad sizes (%d items, %d groups, %d -> %d)", n_items, n_groups, n_from, n_to);
+    return UC_ERR_SHAPE;
+  }
+  uc_status st = check_workspace(workspace, workspace_bytes, 256, "uc_reorder");
+  if (st != UC_OK) return st;
+  for (int i = 0; i < n_items; ++i) {
+    st = check_item(items[i], i, n_groups, n_from, n_to);
+    if (st != UC_OK) return st;
+  }
+  ReorderList list;
+  list.stream = reinterpret_cast<cudaStream_t>(stream);
+  list.p.parent = parent;
+  list.p.status = static_cast<DevStatus*>(workspace);
+  list.p.n_arrays = 0;
+  list.p.n_seq = n_groups * n_to;
+  list.p.n_from = n_from;
+  list.p.n_to = n_to;
+  for (int i = 0; i < n_items; ++i) {
+    const uc_reorder_item& it = items[i];
+    if (it.src == nullptr) {
+      const int bytes = (int)it.state_bytes;
+      list.add(it.state_src, it.state_dst, bytes, bytes, 1, 4, kLiveAll, bytes / 4, nullptr, 0);
+      continue;
+    }
+    const uc_segment* s = it.src;
+    uc_segment* d = it.dst;
+    const int h = s->n_kv_heads, cap = capacity(s);
+    constexpr int kRow = UC_HEAD_DIM * 2;
+    const int64_t so = s->row_offset * kRow, dof = d->row_offset * kRow;
+    const int64_t sb = s->row_stride * kRow, db = d->row_stride * kRow;
+    auto shifted = [](void* p, int64_t off) { return static_cast<void*>(static_cast<uint8_t*>(p) + off); };
+    if (packed(s)) {
+      const int codes = UC_GROUP * UC_HEAD_DIM * s->bits / 8, groups = cap / UC_GROUP;
+      const int64_t sg = s->cap / UC_GROUP, dg = d->cap / UC_GROUP;
+      list.add(s->k_codes, d->k_codes, sg * codes, dg * codes, h, codes, kLiveGroups, groups, s->n_kept, cap);
+      list.add(s->v_codes, d->v_codes, sg * codes, dg * codes, h, codes, kLiveGroups, groups, s->n_kept, cap);
+      list.add(s->k_params, d->k_params, sg * 512, dg * 512, h, 512, kLiveGroups, groups, s->n_kept, cap);
+      list.add(s->v_params, d->v_params, sg * 512, dg * 512, h, 512, kLiveGroups, groups, s->n_kept, cap);
+      list.add(s->k, d->k, sb, db, h, kRow, kLiveTail, UC_GROUP - 1, s->n_kept, cap);
+      list.add(s->v, d->v, sb, db, h, kRow, kLiveTail, UC_GROUP - 1, s->n_kept, cap);
+    } else {
+      list.add(shifted(s->k, so), shifted(d->k, dof), sb, db, h, kRow, kLiveTokens, cap, s->n_kept, cap);
+      list.add(shifted(s->v, so), shifted(d->v, dof), sb, db, h, kRow, kLiveTokens, cap, s->n_kept, cap);
+    }
+    if (s->kind != UC_KIND_FULL)
+      list.add(s->kept_idx, d->kept_idx, 4ll * s->cap, 4ll * d->cap, h, 4, kLiveTokens, cap, s->n_kept, cap);
+    list.add(s->n_kept, d->n_kept, 4, 4, 1, 4, kLiveCount, 1, s->n_kept, cap);
+  }
+  list.flush();
+  st = cuda_check("uc_reorder");
+  if (st == UC_OK)
+    for (int i = 0; i < n_items; ++i)
+      if (items[i].src != nullptr)
+        for (int j = 0; j < n_groups * n_to; ++j)
+          items[i].dst->n_kept_host[j] = items[i].src->n_kept_host[j / n_to * n_from];
+  return st;
+}
+
+}  // extern "C"

@@ -284,6 +284,78 @@ struct DenseParams {
 size_t dense_smem_bytes();
 void launch_dense(const DenseParams& p, cudaStream_t st);
 
+// ------------------------------------------- linear attention with decay
+// bf16 rows of 128 elements at (sequence, head, token), strides in elements.
+struct RowsDev {
+  __nv_bfloat16* base;
+  int64_t sb, sh, st;
+#if defined(__CUDACC__)
+  __device__ __forceinline__ __nv_bfloat16* at(int b, int h, int t) const { return base + b * sb + h * sh + t * st; }
+#endif
+};
+
+struct LinearParams {
+  RowsDev q, k, v, out;
+  const float* state_in;  // [B, Hkv, 128, 128] or null: zeros
+  float* state_out;
+  int batch, n_q_heads, n_kv_heads, group, n_tok;
+  float scale;
+  int32_t lengths[UC_MAX_BATCH];
+  double log2_decay[UC_MAX_LINEAR_HEADS];
+};
+void launch_linear(const LinearParams& p, cudaStream_t st);
+
+// ------------------------------------------------- beam selection, reorder
+constexpr int kBeamTile = 8192;  // logits of a row that one CTA selects from
+
+struct BeamParams {
+  const void* logits;
+  int64_t stride_b, stride_k;  // elements between requests / beams
+  const float* scores;         // [B, K]
+  const uint8_t* finished;     // [B, K] or null
+  float* out_scores;           // [B, n]
+  int32_t* out_parent;
+  int32_t* out_token;
+  uint8_t* out_finished;       // may be null
+  float2* part_ms;             // [B * K][tiles]: max, sum of exp(x - max)
+  float* part_x;               // [B * K][tiles][n]: the tile's best logits
+  int32_t* part_tok;           // and their tokens
+  DevStatus* status;
+  int batch, beams, vocab, n, tiles, eos;
+};
+void launch_beam(const BeamParams& p, int dtype, cudaStream_t st);
+
+// One array of one item to reorder. Sequence i of the target (request
+// i / n_to) takes the blocks of sequence (i / n_to) n_from + parent[i] of the
+// source: `heads` blocks of live(n) units of `unit` bytes, n the source
+// sequence's kept count (kLiveCount: the count itself, one unit).
+enum ReorderLive { kLiveAll = 0, kLiveTokens = 1, kLiveGroups = 2, kLiveTail = 3, kLiveCount = 4 };
+struct ReorderArray {
+  const uint8_t* src;
+  uint8_t* dst;
+  int64_t src_block, dst_block;  // bytes between consecutive (sequence, head) blocks
+  const int32_t* n_kept;         // source counts, null for kLiveAll
+  int32_t heads, unit, live;
+  int32_t max_units;             // units of a block at most
+  int32_t max_kept;              // tokens a sequence may hold
+  int32_t parts;                 // work units per block
+  int32_t begin;                 // first work unit of this array
+};
+constexpr int kReorderArrays = 256;  // arrays of one launch
+constexpr int kReorderBytes = 16384;  // bytes of a work unit
+struct ReorderParams {
+  ReorderArray a[kReorderArrays];
+  const int32_t* parent;
+  DevStatus* status;
+  int32_t n_arrays, n_seq, n_from, n_to, n_units;
+};
+void launch_reorder(const ReorderParams& p, cudaStream_t st);
+
+// Shared by the files with C-ABI entry points (defined in api.cu).
+uc_status cuda_check(const char* where);
+uc_status check_segment(const uc_segment* s, const char* fn);
+int num_sms();
+
 int attend_ctas_per_sm(int ntiles);
 constexpr int kMaxClusterItems = 16;  // CTAs of the largest cluster
 int attend_clusters(int c);
