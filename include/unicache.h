@@ -185,8 +185,8 @@ int32_t uc_set_dense_serial_pv(int32_t serial);
 
 /* Limit, in nanoseconds, of every bounded wait inside the decode attention
  * kernels (a producer waiting for a free ring slot, consumers waiting for a
- * tile or a work item) and the quantizer (a warp waiting for its staged
- * rows), process-wide; a wait that runs out records UC_ERR_TIMEOUT in the
+ * tile or a work item), the quantizer (a warp waiting for its staged rows)
+ * and the chunked linear attention, process-wide; a wait that runs out records UC_ERR_TIMEOUT in the
  * call's workspace status word and the kernel returns without hanging. 0 restores the default (2 s). Read when a call is built
  * (a captured graph keeps the value of its capture). Returns the previous
  * value. */
@@ -643,9 +643,11 @@ typedef struct uc_rows {
  *   log_decay  host float [n_kv_heads], finite, <= 0
  *   state_in, state_out  fp32 [B, Hkv, 128, 128]; they may be the same array
  *              (the state is then updated in place) but not overlap otherwise
- * Query head h reads KV head h / (Hq / Hkv). fp32 throughout but for the
- * outputs' rounding. 1 <= B <= UC_MAX_BATCH, Hkv <= UC_MAX_LINEAR_HEADS,
- * n_tok >= 1. out must not overlap q, k or v.
+ * Query head h reads KV head h / (Hq / Hkv). n_tok <= UC_MAX_QTOKENS (decode)
+ * takes the recurrence token by token in fp32; more take chunks of 128 tokens
+ * on the tensor cores, with the decayed q.k and the state that q multiplies
+ * rounded to bf16 and sums and states in fp32. 1 <= B <= UC_MAX_BATCH, Hkv <= UC_MAX_LINEAR_HEADS,
+ * 1 <= n_tok <= 2^28. out must not overlap q, k or v.
  * workspace: uc_linear_workspace_size() bytes, 16-byte aligned.
  */
 uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v, int32_t batch, int32_t n_q_heads,

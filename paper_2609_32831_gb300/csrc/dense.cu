@@ -34,31 +34,6 @@
 
 namespace uc {
 
-// S_x = Q_x K^T over the 8 K steps of d = 128 (16 channels each): the A
-// (Q) and B (K) offsets step 32 B inside a 128-B swizzled row, then 16 KB
-// to the second 64-channel block.
-template <int ACC0>
-__device__ __forceinline__ void issue_qk(uint32_t lead, uint32_t d, uint32_t q_lo, uint32_t k_lo, uint32_t hi,
-                                         uint32_t idesc) {
-  umma_ss_lead<0, 0, ACC0>(lead, d, q_lo, k_lo, hi, idesc);
-  umma_ss_lead<2, 2, 1>(lead, d, q_lo, k_lo, hi, idesc);
-  umma_ss_lead<4, 4, 1>(lead, d, q_lo, k_lo, hi, idesc);
-  umma_ss_lead<6, 6, 1>(lead, d, q_lo, k_lo, hi, idesc);
-  umma_ss_lead<1024, 1024, 1>(lead, d, q_lo, k_lo, hi, idesc);
-  umma_ss_lead<1026, 1026, 1>(lead, d, q_lo, k_lo, hi, idesc);
-  umma_ss_lead<1028, 1028, 1>(lead, d, q_lo, k_lo, hi, idesc);
-  umma_ss_lead<1030, 1030, 1>(lead, d, q_lo, k_lo, hi, idesc);
-}
-
-template <int N>
-__device__ __forceinline__ void setmaxnreg_inc() {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-template <int N>
-__device__ __forceinline__ void setmaxnreg_dec() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-}
-
 // Named barrier over the 256 softmax threads (warps 0-7).
 __device__ __forceinline__ void softmax_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
@@ -98,21 +73,6 @@ struct DenseSmem {
   uint32_t tmem_base;
 };
 static_assert(sizeof(DenseSmem) + 1024 <= 232448, "dense kernel shared memory");
-
-__device__ __forceinline__ bool dwait(uint64_t* bar, uint32_t parity, DevStatus* st, int where, bool& aborted) {
-  if (aborted) return false;
-  if (!mbar_wait(bar, parity, st, where)) aborted = true;
-  return !aborted;
-}
-
-// The same for all 32 lanes of a warp: the outcome is made warp-uniform, so
-// the warp-collective tcgen05.ld / st that follow never run divergently.
-__device__ __forceinline__ bool dwait_warp(uint64_t* bar, uint32_t parity, DevStatus* st, int where,
-                                           bool& aborted) {
-  if (!aborted && !mbar_wait(bar, parity, st, where)) aborted = true;
-  aborted = __any_sync(0xffffffffu, aborted);
-  return !aborted;
-}
 
 // ------------------------------------------------------------ materialize
 // Writes fp16 K hi / K lo / V rows of every tile of every (b, kvh). One CTA

@@ -1,6 +1,7 @@
 // C-ABI entry points of generation beside the segment cache: linear attention
 // over a constant-size state, beam selection, and the reordering of caches
 // and states. Argument validation and launches; nothing here allocates.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstring>
@@ -29,6 +30,11 @@ uc_status check_workspace(const void* workspace, size_t bytes, size_t need, cons
     return UC_ERR_OOM;
   }
   return UC_OK;
+}
+
+float2 two_floats(double x) {
+  const float hi = (float)x;
+  return make_float2(hi, std::isfinite(hi) ? (float)(x - (double)hi) : 0.f);
 }
 
 // Rows of `heads` heads of `n_tok` tokens: strides in the kernels' form (0
@@ -63,10 +69,48 @@ using namespace uc;
 extern "C" {
 
 // ------------------------------------------------------- linear attention
+// Decode-shaped calls take the recurrence token by token.
+static bool linear_steps(int n_q_heads, int n_kv_heads, int n_tok) {
+  return n_tok <= UC_MAX_QTOKENS;
+}
+
+// How a prompt is cut: over query heads and over tokens where the (sequence,
+// KV head) pairs alone leave SMs idle. Either costs a pass over k and v before
+// (the states that the runs start from) and two launches. Costs in clocks of a
+// CTA.
+static LinearPlan plan_linear(int batch, int n_q_heads, int n_kv_heads, int n_tok) {
+  constexpr double kTile = 3200, kChunkCost = 1500, kCta = 6000, kFirstChunk = 3000, kFirstPass = 12000;
+  const int pairs = batch * n_kv_heads, g = n_q_heads / n_kv_heads, sms = num_sms();
+  const int chunks = (n_tok + kChunk - 1) / kChunk;
+  LinearPlan best;
+  memset(&best, 0, sizeof(best));
+  double least = 0;
+  for (int per = 1; per <= g; ++per) {
+    const int parts = (g + per - 1) / per;
+    for (int waves = 0; waves <= 4; ++waves) {
+      // one run, or as many as fill so many rounds of CTAs
+      const int64_t want = waves == 0 ? 1 : (int64_t)waves * sms / ((int64_t)pairs * parts);
+      if (want < 1 || (waves > 0 && want == 1)) continue;
+      const int cpr = (int)((chunks + want - 1) / want), runs = (chunks + cpr - 1) / cpr;
+      const bool two = runs > 1 || parts > 1;
+      double cost = std::ceil((double)pairs * runs * parts / sms) * (kCta + cpr * (kChunkCost + per * kTile));
+      if (two) cost += kFirstPass + std::ceil((double)pairs * runs / sms) * cpr * kFirstChunk + runs * 200.0;
+      if (least == 0 || cost < least) {
+        least = cost;
+        best = LinearPlan{chunks, runs, cpr, parts, per, two};
+      }
+    }
+  }
+  return best;
+}
+
 size_t uc_linear_workspace_size(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_tok) {
   UC_TRACE();
-  if (batch < 1 || n_q_heads < 1 || n_kv_heads < 1 || n_tok < 1) return 0;
-  return 256;
+  if (batch < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || n_tok < 1) return 0;
+  if (linear_steps(n_q_heads, n_kv_heads, n_tok)) return 256;
+  const LinearPlan plan = plan_linear(batch, n_q_heads, n_kv_heads, n_tok);
+  if (!plan.two_pass) return 256;
+  return 256 + 2ull * plan.runs * batch * n_kv_heads * UC_HEAD_DIM * UC_HEAD_DIM * sizeof(float);
 }
 
 uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v, int32_t batch, int32_t n_q_heads,
@@ -75,7 +119,7 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
                            size_t workspace_bytes, void* stream) {
   UC_TRACE();
   if (batch < 1 || batch > UC_MAX_BATCH || n_kv_heads < 1 || n_kv_heads > UC_MAX_LINEAR_HEADS ||
-      n_q_heads < n_kv_heads || n_q_heads % n_kv_heads != 0 || n_q_heads > 65535 || n_tok < 1) {
+      n_q_heads < n_kv_heads || n_q_heads % n_kv_heads != 0 || n_q_heads > 65535 || n_tok < 1 || n_tok > (1 << 28)) {
     set_error("uc_linear_attend: unsupported shape (batch %d, query heads %d, kv heads %d, tokens %d)", batch,
               n_q_heads, n_kv_heads, n_tok);
     return UC_ERR_SHAPE;
@@ -105,7 +149,9 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
       set_error("uc_linear_attend: log_decay[%d] must be finite and <= 0", j);
       return UC_ERR_ARG;
     }
-    p.log2_decay[j] = (double)log_decay[j] * 1.4426950408889634074;
+    const double g = std::exp((double)log_decay[j]), l = (double)log_decay[j] * 1.4426950408889634074;
+    p.decay[j] = two_floats(g);
+    p.log2_decay[j] = two_floats(std::max(l, -1e30));  // (finite: 0 times it is 0)
   }
   for (int b = 0; b < batch; ++b) {
     p.lengths[b] = lengths ? lengths[b] : n_tok;
@@ -125,7 +171,24 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
   p.group = n_q_heads / n_kv_heads;
   p.n_tok = n_tok;
   p.scale = (float)(1.0 / std::sqrt((double)UC_HEAD_DIM));
-  launch_linear(p, reinterpret_cast<cudaStream_t>(stream));
+  const cudaStream_t cs = reinterpret_cast<cudaStream_t>(stream);
+  if (linear_steps(n_q_heads, n_kv_heads, n_tok)) {
+    launch_linear_step(p, cs);
+    return cuda_check("uc_linear_attend");
+  }
+  LinearChunkParams c;
+  memset(&c, 0, sizeof(c));
+  c.p = p;
+  st = encode_rows_4d(&c.tq, p.q, n_tok, n_q_heads, batch, kChunk);
+  if (st == UC_OK) st = encode_rows_4d(&c.tk, p.k, n_tok, n_kv_heads, batch, kChunk);
+  if (st == UC_OK) st = encode_rows_4d(&c.tv, p.v, n_tok, n_kv_heads, batch, kChunk);
+  if (st != UC_OK) return st;
+  c.plan = plan_linear(batch, n_q_heads, n_kv_heads, n_tok);
+  c.local = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 256);
+  c.start = c.local + (size_t)c.plan.runs * batch * n_kv_heads * UC_HEAD_DIM * UC_HEAD_DIM;
+  c.status = static_cast<DevStatus*>(workspace);
+  c.wait_ns = wait_limit_ns();
+  launch_linear_chunks(c, cs);
   return cuda_check("uc_linear_attend");
 }
 

@@ -301,9 +301,31 @@ struct LinearParams {
   int batch, n_q_heads, n_kv_heads, group, n_tok;
   float scale;
   int32_t lengths[UC_MAX_BATCH];
-  double log2_decay[UC_MAX_LINEAR_HEADS];
+  float2 decay[UC_MAX_LINEAR_HEADS];       // gamma and what fp32 leaves of it
+  float2 log2_decay[UC_MAX_LINEAR_HEADS];  // log2(gamma), the same
 };
-void launch_linear(const LinearParams& p, cudaStream_t st);
+void launch_linear_step(const LinearParams& p, cudaStream_t st);
+
+// Prompts in chunks of kChunk tokens. The chunks of a sequence are cut into
+// `runs` runs of chunks_per_run, the query heads of a KV head into
+// `head_parts` parts; one CTA takes (sequence, KV head, run, part). With more
+// than one of either, the states that the runs start from are formed first
+// (`runs` > 1: sums of the runs' own tokens, then joined).
+constexpr int kChunk = 128;
+struct LinearPlan {
+  int chunks, runs, chunks_per_run, head_parts, heads_per_part;
+  bool two_pass;
+};
+struct LinearChunkParams {
+  LinearParams p;
+  CUtensorMap tq, tk, tv;  // bf16 [128, T, H, B], box 64 x kChunk, 128B swizzle
+  LinearPlan plan;
+  float* local;            // [runs][B * Hkv][128][128]: a run's own sum, fp32
+  float* start;            // the same: the state a run starts from
+  DevStatus* status;
+  uint64_t wait_ns;
+};
+void launch_linear_chunks(const LinearChunkParams& p, cudaStream_t st);
 
 // ------------------------------------------------- beam selection, reorder
 constexpr int kBeamTile = 8192;  // logits of a row that one CTA selects from
@@ -355,6 +377,8 @@ void launch_reorder(const ReorderParams& p, cudaStream_t st);
 uc_status cuda_check(const char* where);
 uc_status check_segment(const uc_segment* s, const char* fn);
 int num_sms();
+// bf16 rows as a 4D tensor map [128, T, H, B], box 64 x `rows`.
+uc_status encode_rows_4d(CUtensorMap* map, const RowsDev& r, int n_tok, int heads, int batch, int rows);
 
 int attend_ctas_per_sm(int ntiles);
 constexpr int kMaxClusterItems = 16;  // CTAs of the largest cluster

@@ -210,4 +210,46 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
   return d;
 }
 
+// S = Q K^T over the 8 K steps of d = 128 (16 channels each): the A
+// (Q) and B (K) offsets step 32 B inside a 128-B swizzled row, then 16 KB
+// to the second 64-channel block.
+template <int ACC0>
+__device__ __forceinline__ void issue_qk(uint32_t lead, uint32_t d, uint32_t q_lo, uint32_t k_lo, uint32_t hi,
+                                         uint32_t idesc) {
+  umma_ss_lead<0, 0, ACC0>(lead, d, q_lo, k_lo, hi, idesc);
+  umma_ss_lead<2, 2, 1>(lead, d, q_lo, k_lo, hi, idesc);
+  umma_ss_lead<4, 4, 1>(lead, d, q_lo, k_lo, hi, idesc);
+  umma_ss_lead<6, 6, 1>(lead, d, q_lo, k_lo, hi, idesc);
+  umma_ss_lead<1024, 1024, 1>(lead, d, q_lo, k_lo, hi, idesc);
+  umma_ss_lead<1026, 1026, 1>(lead, d, q_lo, k_lo, hi, idesc);
+  umma_ss_lead<1028, 1028, 1>(lead, d, q_lo, k_lo, hi, idesc);
+  umma_ss_lead<1030, 1030, 1>(lead, d, q_lo, k_lo, hi, idesc);
+}
+
+template <int N>
+__device__ __forceinline__ void setmaxnreg_inc() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void setmaxnreg_dec() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// A bounded wait that records its outcome (see mbar_wait).
+__device__ __forceinline__ bool dwait(uint64_t* bar, uint32_t parity, DevStatus* st, int where, bool& aborted,
+                                      uint64_t limit_ns = kWaitLimitNs) {
+  if (aborted) return false;
+  if (!mbar_wait(bar, parity, st, where, limit_ns)) aborted = true;
+  return !aborted;
+}
+
+// The same for all 32 lanes of a warp: the outcome is made warp-uniform, so
+// the warp-collective tcgen05.ld / st that follow never run divergently.
+__device__ __forceinline__ bool dwait_warp(uint64_t* bar, uint32_t parity, DevStatus* st, int where,
+                                           bool& aborted, uint64_t limit_ns = kWaitLimitNs) {
+  if (!aborted && !mbar_wait(bar, parity, st, where, limit_ns)) aborted = true;
+  aborted = __any_sync(0xffffffffu, aborted);
+  return !aborted;
+}
+
 }  // namespace uc
