@@ -79,52 +79,87 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 // ----------------------------------------------------------------- chunks
 // Prompts. With S the state before a chunk of kChunk tokens, i, j positions in
 // it and nv its valid tokens,
-//   o_i  = (gamma^{i+1} S^T q_i + sum_{j <= i} gamma^{i-j} (q_i . k_j) v_j) / sqrt(128)
+//   o_i  = a_i (q_i S + sum_{j <= i} (q_i . k_j) gamma^{-(j+1)} v_j) / sqrt(128),  a_i = gamma^{i+1}
 //   S'   = gamma^nv S + sum_j k_j (gamma^{nv-1-j} v_j)^T
-// so a chunk costs three 128^3 products per query head (Q K^T, Q S, P V) and
-// one per KV head for the state. Bound by HBM: 64 KB of q and o per head and
-// chunk against 3 x 512 cycles of the tensor pipe.
+// so a chunk costs three 128^3 products per query head (Q K^T, Q S and P V, the
+// last two into one accumulator) and one per KV head for the state. Bound by
+// HBM: 64 KB of q and o per head and chunk, 1.5 us of an SM's share, against
+// 3 x 512 cycles of the tensor pipe.
 //
 // One CTA per (sequence, KV head, run of chunks, part of its query heads):
-//   warp 8   TMA producer: k and v tiles per chunk, a q tile per head, two slots of each
-//   warp 9   issues every tcgen05.mma
-//   warp 10  zeroes the k and v rows behind the sequence's end in its last
-//            chunk (they may hold NaN, and 0 x NaN is not 0)
-//   WG0, WG1 (warps 0-7) halves of the columns of every product: the decay mask on Q K^T (P,
-//            bf16, back to tensor memory), the epilogue, the decayed values
-//            of the state's update and the state itself, which stays in their
-//            registers in fp32 (64 columns of one key channel per thread).
-// The jobs of a run are its tiles (chunk, head) in order and, after a chunk's
-// last tile, the update of the state. Q K^T of the next tile is issued before
-// the current one's other products.
+//   WG0, WG1 (warps 0-7) halves of the columns of Q K^T: P = mask and weights,
+//            bf16, back to tensor memory
+//   WG2, WG3 (8-15) the epilogue, halves of the channels: o scaled, rounded and
+//            stored, turned around in shared memory so that two lanes write a
+//            32-byte sector of a row
+//   WG4      (16-19) the state. It stays in tensor memory in fp32; per chunk
+//            its bf16 copy goes to shared memory for Q S, it is scaled by
+//            gamma^nv in place, and the chunk's decayed values are formed in
+//            slices of 16 tokens that accumulate on it while the chunk's tiles run
+//   warp 20  TMA producer: k and v tiles per chunk and a q tile per head, in the
+//            order they are needed, each into whichever slot is free
+//   warp 21  issues Q K^T, one tile ahead
+//   warp 22  issues Q S and P V
+//   warp 23  issues the slices' products and releases the chunk's k and v slots
+//            (one warp for all of it: its own waits and issues took 3500 cycles a tile)
+// In a sequence's last chunk, warps 21 and 22 first zero the k and v rows behind
+// its end: they may hold NaN, and 0 x NaN is not 0.
+// Order of the products: Q K^T of the next tile while the epilogue reads the
+// last one's o, then Q S and P V. (With the epilogue and the update on the
+// warps that form P, and rows stored from registers, 32 lines per instruction,
+// a tile took 4900 cycles and an update of the state 6500.)
 //
 // Roundings to bf16: P and the copy of S that Q multiplies (each about as
-// large as the output's own rounding), and none of the state's path: the
-// decayed values enter as two bf16 parts (v gamma^n to 2^-17), the update
-// accumulates in fp32.
-constexpr int kLThreads = 384;
-constexpr int kLRegCompute = 216;  // 256 x 216 + 128 x 56 registers <= 384 x 168
-constexpr int kLRegOther = 56;
-static_assert(256 * kLRegCompute + 128 * kLRegOther <= kLThreads * 168, "register split");
+// large as the output's own rounding), and none on the state's path: the
+// decayed values enter as three bf16 parts (v gamma^n to 2^-25; two parts left
+// the state 2.7e-6 off), the update accumulates in fp32.
+//
+// a_i and gamma^{-(j+1)} take the row's common factor out of both products.
+// Where gamma^128 < 2^-64 (a memory of under two tokens) a_i stops at 2^-64 and
+// P carries gamma^{i-j} / a_i instead; Q S is then kept 2^-64 of its size where
+// it should be less still.
+constexpr int kLThreads = 768;
+constexpr int kLRegLaunch = 80;  // registers per thread at launch, and after the warpgroups rebalance
+constexpr int kLRegP = 88;
+constexpr int kLRegEpilogue = 80;
+constexpr int kLRegState = 72;
+constexpr int kLRegOther = 72;
+static_assert(256 * (kLRegP + kLRegEpilogue) + 128 * (kLRegState + kLRegOther) <= kLThreads * kLRegLaunch, "register split");
+constexpr int kWarpEpilogue = 8, kWarpState = 16, kWarpTma = 20, kWarpQk = 21, kWarpMma = 22, kWarpSlice = 23;
 constexpr uint32_t kTmemLinear = 512;
-constexpr uint32_t kColState = 256;  // O1 = Q S
-constexpr uint32_t kColOut = 384;    // O2 = P V; the S slots are columns 0 and 128
+constexpr uint32_t kColOut = 256;    // o; the S slots are columns 0 and 128
+constexpr uint32_t kColState = 384;
 constexpr uint32_t kTileBytes = kChunk * kHeadDim * 2;
+constexpr int kSlice = 16;  // tokens of one slice of decayed values
+constexpr int kSlices = kChunk / kSlice;
+constexpr uint32_t kSliceBytes = kSlice * kHeadDim * 2;
+constexpr float kLeastScale = 5.421010862427522e-20f;  // 2^-64
+constexpr int kLSlots = 5;
+constexpr int kLFull = 8;  // "arrived" barriers, by load number: more than loads in flight
+
+template <int N>
+__device__ __forceinline__ void rebalance() {
+  if constexpr (N < kLRegLaunch) setmaxnreg_dec<N>();
+  if constexpr (N > kLRegLaunch) setmaxnreg_inc<N>();
+}
 
 struct LinearSmem {
-  uint8_t k[2][kTileBytes];  // [2 x 64 channels][128 tokens][128 B], 128B swizzle; V becomes the decayed values' hi part
-  uint8_t v[2][kTileBytes];
-  uint8_t q[2][kTileBytes];  // the slot of a chunk's last tile then takes the lo part
-  uint8_t s[kTileBytes];     // the chunk's state, bf16 [2 x 64 value channels][128 key channels][128 B]
-  float pw[kChunk + 4];      // gamma^n
-  float cf[32];              // gamma^{31 - n}
-  uint64_t k_full[2], v_full[2], kv_empty[2], q_full[2], q_empty[2];
-  uint64_t s_full[2], p_full[2], o_full, o_free, vt_full, st_ready, last_issued, fixed;
+  uint8_t slot[kLSlots][kTileBytes];   // [2 x 64 channels][128 tokens][128 B], 128B swizzle
+  uint8_t s[kTileBytes];               // the chunk's state, bf16 [2 x 64 value channels][128 key channels][128 B]
+  uint8_t part[2][3][kSliceBytes];     // decayed values, three parts: [2 x 64 channels][16 tokens][128 B]
+  uint4 turn[8][32 * 2];               // per epilogue warp: 32 rows of 32 B
+  float pw[kChunk + 4];                // gamma^n
+  float cj[kChunk];                    // gamma^{-(n + 1)}
+  uint64_t full[kLFull], empty[kLSlots];
+  uint64_t s_full[2], p_full[2], o_full, o_free;
+  uint64_t st_ready, s_free, chunk_go, k_done[2], v_done[2], kv_done, part_full[2], part_free[2];
   uint32_t tmem_base;
+  uint32_t ks[2], vs;                  // slots of a chunk's k (by parity) and v
+  uint8_t slot_of[16];                 // slot of load L at L mod 16
 };
 static_assert(sizeof(LinearSmem) + 1024 <= 232448, "linear attention shared memory");
 
-// gamma^n, n >= 0, to fp32 rounding: the exponent n log2(gamma) is formed from
+// gamma^n to fp32 rounding (n < 0 only where it stays finite): the exponent n log2(gamma) is formed from
 // two fp32 parts of log2(gamma) and split into its whole part and a rest of at
 // most 1/2 (in one fp32 number its error grows with n). n = 0 gives 1, also
 // where gamma is 0.
@@ -135,6 +170,13 @@ __device__ __forceinline__ float decay_pow(float2 log2_gamma, int n) {
   const float w = rintf(x);
   const float rest = (x - w) + fmaf(log2_gamma.y, m, fmaf(log2_gamma.x, m, -x));
   return ldexpf(exp2f(rest), (int)w);
+}
+
+// One arrival for a warp whose lanes have all done their part: 32 arrivals of
+// one instruction are taken one after the other.
+__device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
 }
 
 __device__ __forceinline__ void tma_load_rows(void* dst, const CUtensorMap* map, int c0, int t, int h, int b,
@@ -153,74 +195,95 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, 
   tma_load_rows(dst + kTileBytes / 2, map, 64, t, h, b, bar);
 }
 
-// D (+)= A B over 128 rows of both operands in shared memory, K (tokens or key
-// channels) along the rows of B: A K-major (q) or along its rows too (k).
-template <int KK, int ACC>
-__device__ __forceinline__ void issue_q_s_step(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id) {
-  umma_ss_lead<(KK < 4 ? 2 * KK : 1024 + 2 * (KK - 4)), 128 * KK, ACC>(lead, d, a, b, hi, id);
+// One K = 16 step: D (+)= A B, descriptors as the low words of their bases.
+__device__ __forceinline__ void issue_ss(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id,
+                                         uint32_t acc) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      ".reg .b64 da, db;\n"
+      "setp.ne.b32 q, %6, 0;\n"
+      "setp.ne.b32 p, %5, 0;\n"
+      "mov.b64 da, {%1, %3};\n"
+      "mov.b64 db, {%2, %3};\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n"
+      "}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc), "r"(lead)
+      : "memory");
 }
+__device__ __forceinline__ void issue_ts(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      ".reg .b64 db;\n"
+      "setp.ne.b32 q, %5, 0;\n"
+      "setp.eq.b32 p, 0, 0;\n"
+      "mov.b64 db, {%2, %3};\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n"
+      "}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(hi), "r"(id), "r"(lead)
+      : "memory");
+}
+// The three products of a tile, in loops of one step each: 24 warps share the
+// instruction caches, and straight-line issues were fetched anew every time.
+// S = Q K^T: both along their 128-B rows (32 B per step, then the second 64 channels).
+__device__ __forceinline__ void issue_q_k(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id) {
+#pragma unroll 1
+  for (uint32_t k = 0; k < 8; ++k) {
+    const uint32_t off = (k & 3) * 2 + (k >> 2) * (kTileBytes >> 5);
+    issue_ss(lead, d, a + off, b + off, hi, id, k);
+  }
+}
+// O = Q S: the state's key channels along its rows (16 rows of 128 B per step).
 __device__ __forceinline__ void issue_q_s(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id) {
-  issue_q_s_step<0, 0>(lead, d, a, b, hi, id);
-  issue_q_s_step<1, 1>(lead, d, a, b, hi, id);
-  issue_q_s_step<2, 1>(lead, d, a, b, hi, id);
-  issue_q_s_step<3, 1>(lead, d, a, b, hi, id);
-  issue_q_s_step<4, 1>(lead, d, a, b, hi, id);
-  issue_q_s_step<5, 1>(lead, d, a, b, hi, id);
-  issue_q_s_step<6, 1>(lead, d, a, b, hi, id);
-  issue_q_s_step<7, 1>(lead, d, a, b, hi, id);
+#pragma unroll 1
+  for (uint32_t k = 0; k < 8; ++k)
+    issue_ss(lead, d, a + (k & 3) * 2 + (k >> 2) * (kTileBytes >> 5), b + 128 * k, hi, id, k);
 }
-template <int ACC0>
-__device__ __forceinline__ void issue_k_v(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id) {
-  umma_ss_lead<0, 0, ACC0>(lead, d, a, b, hi, id);
-  umma_ss_lead<128, 128, 1>(lead, d, a, b, hi, id);
-  umma_ss_lead<256, 256, 1>(lead, d, a, b, hi, id);
-  umma_ss_lead<384, 384, 1>(lead, d, a, b, hi, id);
-  umma_ss_lead<512, 512, 1>(lead, d, a, b, hi, id);
-  umma_ss_lead<640, 640, 1>(lead, d, a, b, hi, id);
-  umma_ss_lead<768, 768, 1>(lead, d, a, b, hi, id);
-  umma_ss_lead<896, 896, 1>(lead, d, a, b, hi, id);
-}
-// O2 = P V: P of keys 0-63 in the slot's columns 0-31, of keys 64-127 in 64-95
+// O += P V: P of keys 0-63 in the slot's columns 0-31, of keys 64-127 in 64-95
 // (each warpgroup's P lies in the columns that it alone read).
 __device__ __forceinline__ void issue_p_v(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id) {
-  umma_ts_lead<0>(lead, d, a, b, hi, id, 0u);
-  umma_ts_lead<1>(lead, d, a, b, hi, id, 1u);
-  umma_ts_lead<2>(lead, d, a, b, hi, id, 1u);
-  umma_ts_lead<3>(lead, d, a, b, hi, id, 1u);
-  umma_ts_lead<4>(lead, d, a + 32, b, hi, id, 1u);
-  umma_ts_lead<5>(lead, d, a + 32, b, hi, id, 1u);
-  umma_ts_lead<6>(lead, d, a + 32, b, hi, id, 1u);
-  umma_ts_lead<7>(lead, d, a + 32, b, hi, id, 1u);
+#pragma unroll 1
+  for (uint32_t k = 0; k < 8; ++k) issue_ts(lead, d, a + 8 * k + 32 * (k >> 2), b + 128 * k, hi, id);
 }
 
-// The decayed values of a chunk as two bf16 parts: hi over V in place, lo into
-// `lo`, by `threads` threads. Row j's weight w(j), 0 from row nv on (whatever
-// the row holds).
-template <typename W>
-__device__ __forceinline__ void decay_values(uint8_t* v, uint8_t* lo, int nv, int thread, int threads, const W& weight) {
-#pragma unroll 2
-  for (int i = thread; i < (int)kTileBytes / 16; i += threads) {
-    const int j = (i >> 3) & (kChunk - 1);
-    uint4* at = reinterpret_cast<uint4*>(v) + i;
-    uint4 h = make_uint4(0, 0, 0, 0), l = h;
+// The decayed values of tokens 16 sl .. 16 sl + 15 of a chunk as three bf16
+// parts, by `threads` threads (a divisor of 256). Token j's weight w(j), 0 from
+// nv on (whatever the row holds).
+template <int THREADS, typename W>
+__device__ __forceinline__ void decay_slice(const uint8_t* v, uint8_t (*parts)[kSliceBytes], int sl, int nv, int thread,
+                                            const W& weight) {
+#pragma unroll
+  for (int i = thread; i < 2 * kSlice * 8; i += THREADS) {
+    const int half = i / (8 * kSlice), in = i % (8 * kSlice), j = kSlice * sl + (in >> 3);
+    uint32_t part[3][4] = {};
     if (j < nv) {
       const float w = weight(j);
-      const uint4 x = *at;
-      const uint32_t in[4] = {x.x, x.y, x.z, x.w};
-      uint32_t hi[4], rest[4];
+      const uint4 x = *(reinterpret_cast<const uint4*>(v + half * (kTileBytes / 2) + kSlice * sl * 128) + in);
+      const uint32_t bits[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float a = bf16_lo(in[e]) * w, b = bf16_hi(in[e]) * w;
-        hi[e] = pack_bf16(a, b);
-        rest[e] = pack_bf16(a - bf16_lo(hi[e]), b - bf16_hi(hi[e]));
+        float a = bf16_lo(bits[e]) * w, b = bf16_hi(bits[e]) * w;
+#pragma unroll
+        for (int u = 0; u < 3; ++u) {
+          part[u][e] = pack_bf16(a, b);
+          a -= bf16_lo(part[u][e]);
+          b -= bf16_hi(part[u][e]);
+        }
       }
-      h = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      l = make_uint4(rest[0], rest[1], rest[2], rest[3]);
     }
-    *at = h;
-    reinterpret_cast<uint4*>(lo)[i] = l;
+#pragma unroll
+    for (int u = 0; u < 3; ++u)
+      reinterpret_cast<uint4*>(parts[u])[i] = make_uint4(part[u][0], part[u][1], part[u][2], part[u][3]);
   }
   __syncwarp();
+}
+
+// D += K^T V over one slice: A the slice's rows of k, B its three parts.
+__device__ __forceinline__ void issue_slice(uint32_t lead, uint32_t d, uint32_t k, uint32_t parts, uint32_t hi, uint32_t id,
+                                            bool first) {
+#pragma unroll 1
+  for (uint32_t u = 0; u < 3; ++u) issue_ss(lead, d, k, parts + u * (kSliceBytes >> 4), hi, id, !first || u > 0);
 }
 
 // Zeroes rows nv .. 127 of a tile, by one warp.
@@ -228,6 +291,8 @@ __device__ __forceinline__ void zero_rows(uint8_t* tile, int nv, int lane) {
   for (int half = 0; half < 2; ++half)
     for (int i = nv * 8 + lane; i < kChunk * 8; i += 32)
       reinterpret_cast<uint4*>(tile + half * (kTileBytes / 2))[i] = make_uint4(0, 0, 0, 0);
+  fence_proxy_async_smem();
+  __syncwarp();
 }
 
 __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid_constant__ LinearChunkParams c) {
@@ -246,34 +311,41 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
   const int c0 = run * c.plan.chunks_per_run;
   const int n_all = (len + kChunk - 1) / kChunk;  // chunks with a valid token
   const int nc = max(0, min(c.plan.chunks_per_run, n_all - c0));
+  const int tiles = nc * nh;
   // the state behind the last chunk is needed where this launch writes it
   const bool last_state = !c.plan.two_pass;
   auto valid = [&](int ci) { return min(kChunk, len - (c0 + ci) * kChunk); };
-
+  // loads in order, nh + 2 per chunk: k, the first head's q, v, the other heads' q
+  auto load_k = [&](int ci) { return ci * (nh + 2); };
+  auto load_v = [&](int ci) { return ci * (nh + 2) + 2; };
+  auto load_q = [&](int ci, int h) { return ci * (nh + 2) + (h == 0 ? 1 : h + 2); };
   if (threadIdx.x == 0) {
+    for (int s = 0; s < kLFull; ++s) mbar_init(&sm.full[s], 1);
+    for (int s = 0; s < kLSlots; ++s) mbar_init(&sm.empty[s], 1);
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&sm.k_full[s], 1);
-      mbar_init(&sm.v_full[s], 1);
-      mbar_init(&sm.kv_empty[s], 1);
-      mbar_init(&sm.q_full[s], 1);
-      mbar_init(&sm.q_empty[s], 1);
       mbar_init(&sm.s_full[s], 1);
-      mbar_init(&sm.p_full[s], 256);
+      mbar_init(&sm.p_full[s], 8);     // (arrivals: one per warp)
+      mbar_init(&sm.part_full[s], 4);
+      mbar_init(&sm.part_free[s], 1);
+      mbar_init(&sm.k_done[s], 1);
+      mbar_init(&sm.v_done[s], 1);
     }
     mbar_init(&sm.o_full, 1);
-    mbar_init(&sm.o_free, 256);
-    mbar_init(&sm.vt_full, 256);
-    mbar_init(&sm.st_ready, 256);
-    mbar_init(&sm.last_issued, 1);
-    mbar_init(&sm.fixed, 32);
+    mbar_init(&sm.o_free, 8);
+    mbar_init(&sm.st_ready, 4);
+    mbar_init(&sm.s_free, 1);
+    mbar_init(&sm.kv_done, 1);
+    mbar_init(&sm.chunk_go, 1);
     fence_barrier_init();
   }
+  const float2 l2 = p.log2_decay[kvh];
+  const bool strong = l2.x * kChunk < -64.f;
   if (threadIdx.x <= kChunk) {
-    const float w = decay_pow(p.log2_decay[kvh], threadIdx.x);
+    const float w = decay_pow(l2, threadIdx.x);
     sm.pw[threadIdx.x] = w;
-    if (threadIdx.x < 32) sm.cf[31 - threadIdx.x] = w;
+    if (threadIdx.x < kChunk) sm.cj[threadIdx.x] = strong ? 0.f : decay_pow(l2, -1 - (int)threadIdx.x);
   }
-  if (warp == 9) tmem_alloc(&sm.tmem_base, kTmemLinear);
+  if (warp == kWarpMma) tmem_alloc(&sm.tmem_base, kTmemLinear);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -282,274 +354,355 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
   DevStatus* const st = c.status;
   const uint64_t lim = c.wait_ns;
 
-  if (warp >= 8) {
-    setmaxnreg_dec<kLRegOther>();
-    if (warp == 8 && lane == 0) {
+  if (warp >= kWarpTma) {
+    rebalance<kLRegOther>();
+    if (warp == kWarpTma && lane == 0) {
       // ------------------------------------------------------ TMA producer
       prefetch_tmap(&c.tq);
       prefetch_tmap(&c.tk);
       prefetch_tmap(&c.tv);
-      int ti = 0, loaded = 0;
-      for (int ci = 0; ci < nc && !aborted; ++ci) {
-        const int s = ci & 1, t0 = (c0 + ci) * kChunk;
-        if (ci >= 2 && !dwait(&sm.kv_empty[s], ((ci >> 1) - 1) & 1, st, 50, aborted, lim)) break;
-        load_tile(sm.k[s], &c.tk, t0, kvh, b, &sm.k_full[s]);
-        load_tile(sm.v[s], &c.tv, t0, kvh, b, &sm.v_full[s]);
-        loaded = ci + 1;
-        if (loaded == nc) mbar_arrive(&sm.last_issued);
-        for (int h = 0; h < nh; ++h, ++ti) {
-          const int qs = ti & 1;
-          if (ti >= 2 && !dwait(&sm.q_empty[qs], ((ti >> 1) - 1) & 1, st, 51, aborted, lim)) break;
-          load_tile(sm.q[qs], &c.tq, t0, kvh * p.group + h0 + h, b, &sm.q_full[qs]);
+      uint32_t used = 0, phase = 0;  // by slot: taken before; parity of the release waited for
+      int L = 0;
+      const int n_loads = nc * (nh + 2);
+      for (int ci = 0, in = 0; L < n_loads; ++L) {
+        int s = -1;
+        const uint64_t t0 = global_ns();
+        for (uint32_t it = 0; s < 0; ++it) {
+          for (int i = 0; i < kLSlots && s < 0; ++i)
+            if (!((used >> i) & 1u) || mbar_test(&sm.empty[i], (phase >> i) & 1u)) s = i;
+          if (s < 0 && (it & 15u) == 15u && global_ns() - t0 > lim) {
+            set_status(st, UC_ERR_TIMEOUT, 50);
+            aborted = true;
+            break;
+          }
+        }
+        if (aborted) break;
+        if ((used >> s) & 1u) phase ^= 1u << s;
+        used |= 1u << s;
+        sm.slot_of[L & 15] = (uint8_t)s;
+        uint64_t* bar = &sm.full[L % kLFull];
+        const int t = (c0 + ci) * kChunk;
+        if (in == 0)
+          load_tile(sm.slot[s], &c.tk, t, kvh, b, bar);
+        else if (in == 2)
+          load_tile(sm.slot[s], &c.tv, t, kvh, b, bar);
+        else
+          load_tile(sm.slot[s], &c.tq, t, kvh * p.group + h0 + (in == 1 ? 0 : in - 2), b, bar);
+        if (++in == nh + 2) {
+          in = 0;
+          ++ci;
         }
       }
       if (aborted) {
         // no copy may land in shared memory that is no longer this CTA's
         bool gone = false;
-        for (int i = max(0, loaded - 2); i < loaded; ++i) {
-          dwait(&sm.k_full[i & 1], (i >> 1) & 1, st, 52, gone, lim);
-          dwait(&sm.v_full[i & 1], (i >> 1) & 1, st, 52, gone, lim);
-        }
-        for (int i = max(0, ti - 2); i < ti; ++i) dwait(&sm.q_full[i & 1], (i >> 1) & 1, st, 52, gone, lim);
+        for (int i = max(0, L - kLSlots); i < L; ++i)
+          dwait(&sm.full[i % kLFull], (i / kLFull) & 1, st, 52, gone, lim);
       }
-    } else if (warp == 10) {
-      // ------------------------------------- rows behind the sequence's end
-      if (nc > 0 && valid(nc - 1) < kChunk) {
-        const int s = (nc - 1) & 1, ph = ((nc - 1) >> 1) & 1, nv = valid(nc - 1);
-        // (once the last copies are issued, the slots' current phase is theirs)
-        if (dwait_warp(&sm.last_issued, 0, st, 53, aborted, lim) &&
-            dwait_warp(&sm.k_full[s], ph, st, 53, aborted, lim) && dwait_warp(&sm.v_full[s], ph, st, 53, aborted, lim)) {
-          zero_rows(sm.k[s], nv, lane);
-          zero_rows(sm.v[s], nv, lane);
-          fence_proxy_async_smem();
-          mbar_arrive(&sm.fixed);
-        }
-      }
-    } else if (warp == 9) {
-      // -------------------------------------------------------- MMA issuer
+    } else if (warp == kWarpQk) {
+      // ---------------------------------------------------------- Q K^T
       const uint32_t lead = elect_one();
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-      constexpr uint32_t id_qk = idesc_bf16(128, 128, 0, 0);
-      constexpr uint32_t id_b = idesc_bf16(128, 128, 0, 1);   // B along its rows
-      constexpr uint32_t id_ab = idesc_bf16(128, 128, 1, 1);  // A and B along their rows
+      const uint32_t dhi = (uint32_t)(smem_desc_sw128(0, 16) >> 32);
+      const uint32_t row_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.slot[0]), 16);
+      for (int ci = 0, t = 0; ci < nc && !aborted; ++ci) {
+        uint32_t ks = 0;
+        for (int h = 0; h < nh; ++h, ++t) {
+          // P of the tile before the last has been read: its slot is free
+          if (t > 1 && !dwait_warp(&sm.o_full, t & 1, st, 58, aborted, lim)) break;
+          if (h == 0) {
+            const int L = load_k(ci);
+            if (!dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, 54, aborted, lim)) break;
+            ks = __shfl_sync(0xffffffffu, (uint32_t)sm.slot_of[L & 15], 0);
+            if (valid(ci) < kChunk) zero_rows(sm.slot[ks], valid(ci), lane);
+            if (lane == 0) sm.ks[ci & 1] = ks;
+          }
+          const int L = load_q(ci, h);
+          if (!dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, 56, aborted, lim)) break;
+          const uint32_t qs = __shfl_sync(0xffffffffu, (uint32_t)sm.slot_of[L & 15], 0);
+          tc_fence_after();
+          issue_q_k(lead, tm + 128 * (t & 1), row_lo + qs * (kTileBytes >> 4), row_lo + ks * (kTileBytes >> 4), dhi,
+                    idesc_bf16(128, 128, 0, 0));
+          umma_commit_lead(lead, &sm.s_full[t & 1]);
+          if (h == nh - 1) umma_commit_lead(lead, &sm.k_done[ci & 1]);
+        }
+      }
+    } else if (warp == kWarpMma) {
+      // ------------------------------------------------------ Q S and P V
+      const uint32_t lead = elect_one();
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      constexpr uint32_t id_b = idesc_bf16(128, 128, 0, 1);  // B along its rows
       const uint32_t dhi = (uint32_t)(smem_desc_sw128(0, 16) >> 32);
       constexpr uint32_t kStep = kTileBytes >> 4;
-      const uint32_t q_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.q[0]), 16);
-      const uint32_t k_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.k[0]), 16);
-      const uint32_t kt_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.k[0]), kTileBytes / 2);
-      const uint32_t v_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.v[0]), kTileBytes / 2);
+      // a slot as an operand along its 128-B rows (q) or across them (v)
+      const uint32_t row_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.slot[0]), 16);
+      const uint32_t col_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.slot[0]), kTileBytes / 2);
       const uint32_t s_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.s), kTileBytes / 2);
-      const uint32_t lq_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.q[0]), kTileBytes / 2);
-      // Q K^T of tile (ci, h), which is job n and tile ti of the run
-      auto issue_scores = [&](int n, int ti, int ci, int h) -> bool {
-        if (h == 0) {
-          if (!dwait_warp(&sm.k_full[ci & 1], (ci >> 1) & 1, st, 54, aborted, lim)) return false;
-          if (ci == nc - 1 && valid(ci) < kChunk && !dwait_warp(&sm.fixed, 0, st, 55, aborted, lim)) return false;
-        }
-        if (!dwait_warp(&sm.q_full[ti & 1], (ti >> 1) & 1, st, 56, aborted, lim)) return false;
-        tc_fence_after();
-        issue_qk<0>(lead, tm + 128 * (n & 1), q_lo + (ti & 1) * kStep, k_lo + (ci & 1) * kStep, dhi, id_qk);
-        umma_commit_lead(lead, &sm.s_full[n & 1]);
-        return true;
+      auto take = [&](int L, int where) -> uint32_t {  // waits for load L; its slot
+        dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, where, aborted, lim);
+        return __shfl_sync(0xffffffffu, (uint32_t)sm.slot_of[L & 15], 0);
       };
-      int n = 0, ti = 0;
-      bool ok = nc > 0 && issue_scores(0, 0, 0, 0);
-      for (int ci = 0; ci < nc && ok; ++ci) {
-        const bool update = ci + 1 < nc || last_state;
-        for (int h = 0; h < nh && ok; ++h, ++n, ++ti) {
+      for (int ci = 0, t = 0; ci < nc && !aborted; ++ci) {
+        uint32_t vs = 0;
+        for (int h = 0; h < nh; ++h, ++t) {
           const bool last = h == nh - 1;
-          ok = false;
+          const uint32_t qs = take(load_q(ci, h), 56);
           if (h == 0) {
-            // the chunk's state is in shared memory, the update's sums are read
+            vs = take(load_v(ci), 60);
+            if (!aborted && valid(ci) < kChunk) zero_rows(sm.slot[vs], valid(ci), lane);
+            // the chunk's state is in shared memory, the next scaled in place
             if (!dwait_warp(&sm.st_ready, ci & 1, st, 57, aborted, lim)) break;
-          } else if (!dwait_warp(&sm.o_full, (ti - 1) & 1, st, 58, aborted, lim)) {
-            break;  // (the other S slot's P is consumed)
           }
-          if (!last && !issue_scores(n + 1, ti + 1, ci, h + 1)) break;
-          if (ti > 0 && !dwait_warp(&sm.o_free, (ti - 1) & 1, st, 59, aborted, lim)) break;
+          if (t > 0 && !dwait_warp(&sm.o_free, (t - 1) & 1, st, 59, aborted, lim)) break;
           tc_fence_after();
-          issue_q_s(lead, tm + kColState, q_lo + (ti & 1) * kStep, s_lo, dhi, id_b);
-          if (!(last && update)) umma_commit_lead(lead, &sm.q_empty[ti & 1]);
-          if (h == 0 && !dwait_warp(&sm.v_full[ci & 1], (ci >> 1) & 1, st, 60, aborted, lim)) break;
-          if (!dwait_warp(&sm.p_full[ti & 1], (ti >> 1) & 1, st, 61, aborted, lim)) break;
+          issue_q_s(lead, tm + kColOut, row_lo + qs * kStep, s_lo, dhi, id_b);
+          if (last) umma_commit_lead(lead, &sm.s_free);
+          if (!dwait_warp(&sm.p_full[t & 1], (t >> 1) & 1, st, 61, aborted, lim)) break;
           tc_fence_after();
-          issue_p_v(lead, tm + kColOut, tm + 128 * (n & 1), v_lo + (ci & 1) * kStep, dhi, id_b);
+          umma_commit_lead(lead, &sm.empty[qs]);  // Q S is issued, and Q K^T was done before P
+          issue_p_v(lead, tm + kColOut, tm + 128 * (t & 1), col_lo + vs * kStep, dhi, id_b);
           umma_commit_lead(lead, &sm.o_full);
-          ok = true;
-        }
-        if (!ok) break;
-        if (update) {
-          ok = false;
-          if (!dwait_warp(&sm.o_full, (ti - 1) & 1, st, 62, aborted, lim)) break;
-          if (ci + 1 < nc && !issue_scores(n + 1, ti, ci + 1, 0)) break;
-          if (!dwait_warp(&sm.vt_full, ci & 1, st, 63, aborted, lim)) break;
-          tc_fence_after();
-          const uint32_t d = tm + 128 * (n & 1), a = kt_lo + (ci & 1) * kStep;
-          issue_k_v<0>(lead, d, a, v_lo + (ci & 1) * kStep, dhi, id_ab);
-          issue_k_v<1>(lead, d, a, lq_lo + ((ti - 1) & 1) * kStep, dhi, id_ab);
-          umma_commit_lead(lead, &sm.s_full[n & 1]);
-          umma_commit_lead(lead, &sm.kv_empty[ci & 1]);
-          umma_commit_lead(lead, &sm.q_empty[(ti - 1) & 1]);
-          ++n;
-          ok = true;
-        }
-      }
-    }
-  } else {
-    setmaxnreg_inc<kLRegCompute>();
-    // -------------------------------------------------------------- compute
-    const int x = warp >> 2;          // half of the columns
-    const int r = threadIdx.x & 127;  // TMEM lane: token of the tile, or key channel of the state
-    const int wr = 32 * (warp & 3);   // the warp's first row
-    const uint32_t lane_off = (uint32_t)wr << 16;
-    const int tid = threadIdx.x;
-    // state row r (key channel), value channels 64 x .. 64 x + 63
-    float sreg[64];
-    {
-      if (c.plan.two_pass) griddep_wait();
-      const float* src = c.plan.two_pass ? c.start + ((size_t)run * p.batch * p.n_kv_heads + bh) * kHeadDim * kHeadDim
-                                         : (p.state_in ? p.state_in + (size_t)bh * kHeadDim * kHeadDim : nullptr);
-#pragma unroll
-      for (int e = 0; e < 64; e += 4) {
-        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (src) w = *reinterpret_cast<const float4*>(src + (size_t)r * kHeadDim + 64 * x + e);
-        sreg[e] = w.x;
-        sreg[e + 1] = w.y;
-        sreg[e + 2] = w.z;
-        sreg[e + 3] = w.w;
-      }
-    }
-    auto store_state = [&]() {  // bf16 copy for Q S
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint4 w = make_uint4(pack_bf16(sreg[8 * e], sreg[8 * e + 1]), pack_bf16(sreg[8 * e + 2], sreg[8 * e + 3]),
-                                   pack_bf16(sreg[8 * e + 4], sreg[8 * e + 5]), pack_bf16(sreg[8 * e + 6], sreg[8 * e + 7]));
-        *reinterpret_cast<uint4*>(sm.s + x * (kTileBytes / 2) + r * 128 + ((e ^ (r & 7)) << 4)) = w;
-      }
-      fence_proxy_async_smem();
-      mbar_arrive(&sm.st_ready);
-    };
-    if (nc > 0) store_state();
-    // P of job n, tile ti: gamma^{i-j} (q_i . k_j) for j <= i, 32 columns at a time
-    auto scores = [&](int n, int ti) -> bool {
-      if (!dwait_warp(&sm.s_full[n & 1], (n >> 1) & 1, st, 64, aborted, lim)) return false;
-      tc_fence_after();
-      const uint32_t slot = tmem + lane_off + 128 * (n & 1) + 64 * x;
-      uint32_t pk[2][16];
-#pragma unroll
-      for (int blk = 0; blk < 2; ++blk) {
-        const int j0 = 64 * x + 32 * blk;
-        if (j0 > wr) {  // above the diagonal
-#pragma unroll
-          for (int e = 0; e < 16; ++e) pk[blk][e] = 0u;
-          continue;
-        }
-        uint32_t sr[32];
-        tmem_ld32(slot + 32 * blk, sr);
-        tmem_wait_ld();
-        if (j0 < wr) {
-          const float rowf = sm.pw[r - j0 - 31];
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            pk[blk][e] = pack_bf16(__uint_as_float(sr[2 * e]) * (sm.cf[2 * e] * rowf),
-                                   __uint_as_float(sr[2 * e + 1]) * (sm.cf[2 * e + 1] * rowf));
-        } else {
-          // the diagonal block: lane i, column j (masked entries may hold anything)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float a = 2 * e <= lane ? __uint_as_float(sr[2 * e]) * sm.pw[max(0, lane - 2 * e)] : 0.f;
-            const float bb = 2 * e + 1 <= lane ? __uint_as_float(sr[2 * e + 1]) * sm.pw[max(0, lane - 2 * e - 1)] : 0.f;
-            pk[blk][e] = pack_bf16(a, bb);
+          if (last) umma_commit_lead(lead, &sm.v_done[ci & 1]);
+          if (h == 0 && lane == 0) {
+            sm.vs = vs;
+            mbar_arrive(&sm.chunk_go);  // the chunk's k and v are there
           }
         }
       }
-      tmem_st16(slot, pk[0]);
-      tmem_st16(slot + 16, pk[1]);
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(&sm.p_full[ti & 1]);
-      return true;
-    };
-    // o of tile ti = (ci, h)
-    auto epilogue = [&](int ti, int ci, int h) -> bool {
-      if (!dwait_warp(&sm.o_full, ti & 1, st, 65, aborted, lim)) return false;
-      tc_fence_after();
-      const int nv = valid(ci), t = (c0 + ci) * kChunk + r;
-      const float f1 = sm.pw[r + 1] * p.scale, f2 = p.scale;
-      __nv_bfloat16* o = t < p.n_tok ? p.out.at(b, kvh * p.group + h0 + h, t) + 64 * x : nullptr;
-      uint32_t a[2][32], d[2][32];
-#pragma unroll
-      for (int blk = 0; blk < 2; ++blk) {
-        tmem_ld32(tmem + lane_off + kColState + 64 * x + 32 * blk, a[blk]);
-        tmem_ld32(tmem + lane_off + kColOut + 64 * x + 32 * blk, d[blk]);
+    } else if (warp == kWarpSlice) {
+      // ---------------------------------------------------- slices' products
+      const uint32_t lead = elect_one();
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      constexpr uint32_t id_ab = idesc_bf16(128, 128, 1, 1);  // A and B along their rows
+      const uint32_t dhi = (uint32_t)(smem_desc_sw128(0, 16) >> 32);
+      const uint32_t col_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.slot[0]), kTileBytes / 2);
+      const uint32_t part_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.part[0][0]), kSliceBytes / 2);
+      int n = 0;
+      for (int ci = 0; ci < (last_state ? nc : nc - 1) && !aborted; ++ci) {
+        // (the state is scaled for this chunk before the chunk's first tile goes)
+        if (!dwait_warp(&sm.chunk_go, ci & 1, st, 62, aborted, lim)) break;
+        const uint32_t ks = __shfl_sync(0xffffffffu, sm.ks[ci & 1], 0), vs = __shfl_sync(0xffffffffu, sm.vs, 0);
+        for (int sl = 0; sl < kSlices; ++sl, ++n) {
+          const int buf = n & 1;
+          if (!dwait_warp(&sm.part_full[buf], (n >> 1) & 1, st, 62, aborted, lim)) break;
+          tc_fence_after();
+          issue_slice(lead, tm + kColState, col_lo + ks * (kTileBytes >> 4) + 128 * sl,
+                      part_lo + buf * (3 * kSliceBytes >> 4), dhi, id_ab, false);
+          umma_commit_lead(lead, &sm.part_free[buf]);
+        }
+        umma_commit_lead(lead, &sm.kv_done);
+        if (!dwait_warp(&sm.kv_done, ci & 1, st, 62, aborted, lim)) break;
+        // (two barriers each: the tiles of the next chunk may be done before this is looked at)
+        if (!dwait_warp(&sm.k_done[ci & 1], (ci >> 1) & 1, st, 62, aborted, lim)) break;
+        if (lane == 0) mbar_arrive(&sm.empty[ks]);
+        if (!dwait_warp(&sm.v_done[ci & 1], (ci >> 1) & 1, st, 62, aborted, lim)) break;
+        if (lane == 0) mbar_arrive(&sm.empty[vs]);
       }
-      tmem_wait_ld();
-      tc_fence_before();
-      mbar_arrive(&sm.o_free);
-      if (o != nullptr) {
+    }
+  } else if (warp >= kWarpState) {
+    rebalance<kLRegState>();
+    // ---------------------------------------------------------------- state
+    const int r = threadIdx.x & 127;  // key channel = TMEM lane
+    const uint32_t s_addr = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColState;
+    if (c.plan.two_pass) griddep_wait();
+    const size_t row = ((size_t)bh * kHeadDim + r) * kHeadDim;
+    const float* src = c.plan.two_pass ? c.start + (size_t)run * p.batch * p.n_kv_heads * kHeadDim * kHeadDim + row
+                                       : (p.state_in ? p.state_in + row : nullptr);
+#pragma unroll 1
+    for (int blk = 0; blk < 4; ++blk) {
+      uint32_t w[32];
 #pragma unroll
-        for (int u8 = 0; u8 < 8; ++u8) {
-          const int blk = u8 >> 2, e = 8 * (u8 & 3);
+      for (int e = 0; e < 32; e += 4) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (src) x = *reinterpret_cast<const uint4*>(src + 32 * blk + e);
+        w[e] = x.x;
+        w[e + 1] = x.y;
+        w[e + 2] = x.z;
+        w[e + 3] = x.w;
+      }
+      tmem_st32(s_addr + 32 * blk, w);
+    }
+    tmem_wait_st();
+    int n_slice = 0;
+    for (int ci = 0; ci < nc && !aborted; ++ci) {
+      const bool update = ci + 1 < nc || last_state;
+      const int nv = valid(ci);
+      if (ci > 0 && !(dwait_warp(&sm.kv_done, (ci - 1) & 1, st, 66, aborted, lim) &&
+                      dwait_warp(&sm.s_free, (ci - 1) & 1, st, 66, aborted, lim)))
+        break;
+      tc_fence_after();
+      const float g = sm.pw[nv];
+#pragma unroll
+      for (int blk = 0; blk < 4; ++blk) {
+        uint32_t x[32];
+        tmem_ld32(s_addr + 32 * blk, x);
+        tmem_wait_ld32(x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
           uint32_t w[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int i = e + 2 * u;
-            const float y0 = fmaf(__uint_as_float(a[blk][i]), f1, __uint_as_float(d[blk][i]) * f2);
-            const float y1 = fmaf(__uint_as_float(a[blk][i + 1]), f1, __uint_as_float(d[blk][i + 1]) * f2);
-            w[u] = r < nv ? pack_bf16(y0, y1) : 0u;
-          }
-          *reinterpret_cast<uint4*>(o + 32 * blk + e) = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int u = 0; u < 4; ++u)
+            w[u] = pack_bf16(__uint_as_float(x[8 * e + 2 * u]), __uint_as_float(x[8 * e + 2 * u + 1]));
+          const int chunk16 = 4 * (blk & 1) + e;  // 16 bytes of the row's half
+          *reinterpret_cast<uint4*>(sm.s + (blk >> 1) * (kTileBytes / 2) + r * 128 + ((chunk16 ^ (r & 7)) << 4)) =
+              make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        if (update) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * g);
+          tmem_st32(s_addr + 32 * blk, x);
         }
       }
-      __syncwarp();
-      return true;
-    };
-    int n = 0, ti = 0;
-    bool ok = true;
-    for (int ci = 0; ci < nc && ok; ++ci) {
-      const bool update = ci + 1 < nc || last_state;
-      for (int h = 0; h < nh && ok; ++h, ++n, ++ti) {
-        ok = scores(n, ti);
-        if (ok && h > 0) ok = epilogue(ti - 1, ci, h - 1);
-      }
-      if (!ok) break;
-      if (update) {
-        const int s = ci & 1, nv = valid(ci);
-        // the chunk's products are complete: V and the last q tile's slot are free to be written
-        ok = dwait_warp(&sm.o_full, (ti - 1) & 1, st, 66, aborted, lim) &&
-             dwait_warp(&sm.v_full[s], (ci >> 1) & 1, st, 67, aborted, lim);
-        if (!ok) break;
-        decay_values(sm.v[s], sm.q[(ti - 1) & 1], nv, tid, 256, [&](int j) { return sm.pw[nv - 1 - j]; });
+      tmem_wait_st();
+      tc_fence_before();
+      fence_proxy_async_smem();
+      warp_arrive(&sm.st_ready, lane);
+      if (!update) break;
+      if (!dwait_warp(&sm.chunk_go, ci & 1, st, 67, aborted, lim)) break;  // V is there
+      const uint8_t* v = sm.slot[sm.vs];
+      for (int sl = 0; sl < kSlices; ++sl, ++n_slice) {
+        const int buf = n_slice & 1;
+        if (n_slice >= 2 && !dwait_warp(&sm.part_free[buf], ((n_slice >> 1) - 1) & 1, st, 68, aborted, lim)) break;
+        decay_slice<128>(v, sm.part[buf], sl, nv, r, [&](int j) { return sm.pw[nv - 1 - j]; });
         fence_proxy_async_smem();
-        mbar_arrive(&sm.vt_full);
-        ok = epilogue(ti - 1, ci, nh - 1) && dwait_warp(&sm.s_full[n & 1], (n >> 1) & 1, st, 68, aborted, lim);
-        if (!ok) break;
-        tc_fence_after();
-        const float g = sm.pw[nv];
-#pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-          uint32_t kv[32];
-          tmem_ld32(tmem + lane_off + 128 * (n & 1) + 64 * x + 32 * blk, kv);
-          tmem_wait_ld();
-#pragma unroll
-          for (int e = 0; e < 32; ++e) sreg[32 * blk + e] = fmaf(sreg[32 * blk + e], g, __uint_as_float(kv[e]));
-        }
-        tc_fence_before();
-        ++n;
-        store_state();
-      } else {
-        ok = epilogue(ti - 1, ci, nh - 1);
+        warp_arrive(&sm.part_full[buf], lane);
       }
     }
-    if (last_state && !aborted) {
-      float* dst = p.state_out + ((size_t)bh * kHeadDim + r) * kHeadDim + 64 * x;
+    if (last_state && !aborted && (nc == 0 || dwait_warp(&sm.kv_done, (nc - 1) & 1, st, 66, aborted, lim))) {
+      tc_fence_after();
+      float* dst = p.state_out + row;
+#pragma unroll 1
+      for (int blk = 0; blk < 4; ++blk) {
+        uint32_t x[32];
+        tmem_ld32(s_addr + 32 * blk, x);
+        tmem_wait_ld32(x);
 #pragma unroll
-      for (int e = 0; e < 64; e += 4)
-        *reinterpret_cast<float4*>(dst + e) = make_float4(sreg[e], sreg[e + 1], sreg[e + 2], sreg[e + 3]);
+        for (int e = 0; e < 32; e += 4)
+          *reinterpret_cast<uint4*>(dst + 32 * blk + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+      }
+    }
+    tc_fence_before();
+  } else if (warp >= kWarpEpilogue) {
+    rebalance<kLRegEpilogue>();
+    // ------------------------------------------------------------- epilogue
+    const int r = threadIdx.x & 127;  // TMEM lane: token of the tile
+    const int half = (warp - kWarpEpilogue) >> 2;  // of the channels
+    const uint32_t o_addr = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColOut + 64 * half;
+    const float f = fmaxf(sm.pw[r + 1], strong ? kLeastScale : 0.f) * p.scale;
+    const uint64_t ff = f2_pack(f, f);
+    uint4* const turn = sm.turn[warp - kWarpEpilogue];
+    for (int ci = 0, t = 0; ci < nc && !aborted; ++ci) {
+      const int nv = valid(ci);
+      for (int h = 0; h < nh; ++h, ++t) {
+        if (!dwait_warp(&sm.o_full, t & 1, st, 65, aborted, lim)) break;
+        tc_fence_after();
+        // o leaves tensor memory before anything else (the next tile's products wait for it)
+        uint32_t w[2][16];
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+          uint32_t y[32];
+          tmem_ld32(o_addr + 32 * blk, y);
+          tmem_wait_ld32(y);
+          if (blk == 1) {
+            tc_fence_before();
+            warp_arrive(&sm.o_free, lane);
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            float y0, y1;
+            f2_unpack(f2_mul(f2_pack(__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])), ff), y0, y1);
+            w[blk][e] = pack_bf16(y0, y1);
+          }
+        }
+        if (r >= nv) {  // tokens behind the sequence's end: zeros
+#pragma unroll
+          for (int e = 0; e < 32; ++e) w[e >> 4][e & 15] = 0u;
+        }
+        // lane: row 16 i + lane / 2 of the warp's 32, 16 bytes lane mod 2 of each 32
+        const int tok = (c0 + ci) * kChunk + 32 * (warp & 3) + (lane >> 1);
+        __nv_bfloat16* const o = p.out.at(b, kvh * p.group + h0 + h, tok) + 64 * half + 8 * (lane & 1);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t* x = &w[q >> 1][8 * (q & 1)];
+          __syncwarp();
+          turn[2 * lane + ((lane >> 2) & 1)] = make_uint4(x[0], x[1], x[2], x[3]);
+          turn[2 * lane + (((lane >> 2) & 1) ^ 1)] = make_uint4(x[4], x[5], x[6], x[7]);
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = 16 * i + (lane >> 1);
+            if (tok + 16 * i < p.n_tok)
+              *reinterpret_cast<uint4*>(o + 16 * i * p.out.st + 16 * q) = turn[2 * row + ((lane & 1) ^ ((row >> 2) & 1))];
+          }
+        }
+      }
+    }
+    tc_fence_before();
+  } else {
+    rebalance<kLRegP>();
+    // -------------------------------------------------------------------- P
+    const int x = warp >> 2;          // half of the columns (keys)
+    const int r = threadIdx.x & 127;  // TMEM lane: token of the tile
+    const int wr = 32 * (warp & 3);   // the warp's first row
+    const uint32_t slot0 = tmem + ((uint32_t)wr << 16) + 64 * x;
+    // (strong decay only) 1 / a_i
+    const float inv_a = strong ? 1.f / fmaxf(sm.pw[r + 1], kLeastScale) : 0.f;
+    for (int t = 0; t < tiles; ++t) {
+      if (!dwait_warp(&sm.s_full[t & 1], (t >> 1) & 1, st, 64, aborted, lim)) break;
+      tc_fence_after();
+      const uint32_t slot = slot0 + 128 * (t & 1);
+      // 16 keys at a time, the next ones' loads in flight (P overwrites only
+      // columns that are read); keys behind the warp's last row need no load
+      uint32_t sr[2][16];
+      if (64 * x < wr + 32) tmem_ld16(slot, sr[0]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int j0 = 64 * x + 16 * q;
+        uint32_t(&y)[16] = sr[q & 1];
+        tmem_wait_ld16(y);
+        if (q < 3 && j0 + 16 < wr + 32) tmem_ld16(slot + 16 * (q + 1), sr[(q + 1) & 1]);
+        uint32_t pk[8];
+        if (j0 >= wr + 32) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pk[e] = 0u;
+        } else if (!strong) {
+          const ulonglong2* cj = reinterpret_cast<const ulonglong2*>(sm.cj + j0);  // pairs of fp32
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const ulonglong2 w = cj[e];
+            float z[4];
+            f2_unpack(f2_mul(f2_pack(__uint_as_float(y[4 * e]), __uint_as_float(y[4 * e + 1])), w.x), z[0], z[1]);
+            f2_unpack(f2_mul(f2_pack(__uint_as_float(y[4 * e + 2]), __uint_as_float(y[4 * e + 3])), w.y), z[2], z[3]);
+            pk[2 * e] = pack_bf16(z[0], z[1]);
+            pk[2 * e + 1] = pack_bf16(z[2], z[3]);
+          }
+          if (j0 >= wr) {  // keys up to the token (later ones may hold anything)
+            const int last = r - j0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              pk[e] &= (2 * e <= last ? 0xffffu : 0u) | (2 * e + 1 <= last ? 0xffff0000u : 0u);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float z[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int back = r - j0 - 2 * e - u;  // tokens since the key
+              z[u] = back >= 0 ? __uint_as_float(y[2 * e + u]) * (sm.pw[max(back, 0)] * inv_a) : 0.f;
+            }
+            pk[e] = pack_bf16(z[0], z[1]);
+          }
+        }
+        tmem_st8(slot + 8 * q, pk);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      warp_arrive(&sm.p_full[t & 1], lane);
     }
     // tokens of this run in chunks behind the sequence's end: zeros
     const int z0 = (c0 + nc) * kChunk, z1 = min(p.n_tok, (c0 + c.plan.chunks_per_run) * kChunk);
-    for (int64_t i = tid; i < (int64_t)(z1 - z0) * nh * (kHeadDim / 8); i += 256) {
+    for (int64_t i = threadIdx.x; i < (int64_t)(z1 - z0) * nh * (kHeadDim / 8); i += 256) {
       const int e = (int)(i % (kHeadDim / 8)), row = (int)(i / (kHeadDim / 8));
       *reinterpret_cast<uint4*>(p.out.at(b, kvh * p.group + h0 + row % nh, z0 + row / nh) + 8 * e) =
           make_uint4(0, 0, 0, 0);
@@ -557,7 +710,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     tc_fence_before();
   }
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kWarpMma) {
     __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, kTmemLinear);
@@ -566,11 +719,15 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
 
 // A run's own sum: sum_j k_j (gamma^{e-1-j} v_j)^T over its tokens, e its end.
 // The weights fall towards the run's start, so the chunks accumulate in tensor
-// memory without a rescale.
+// memory without a rescale. 16 warps form the decayed values slice by slice.
+constexpr int kLocalRing = 3;  // chunks in flight
+constexpr int kLocalBufs = 2;  // slices per warpgroup
 struct LinearLocalSmem {
-  uint8_t k[2][kTileBytes], v[2][kTileBytes], lo[2][kTileBytes];
+  uint8_t k[kLocalRing][kTileBytes], v[kLocalRing][kTileBytes];
+  uint8_t part[kLocalBufs][3][kSliceBytes];
   float pw[kChunk];  // gamma^n
-  uint64_t k_full[2], v_full[2], empty[2], vt_full[2], done, last_issued, fixed;
+  uint64_t k_full[kLocalRing], v_full[kLocalRing], empty[kLocalRing];
+  uint64_t part_full[kLocalBufs], part_free[kLocalBufs], done;
   uint32_t tmem_base;
 };
 static_assert(sizeof(LinearLocalSmem) + 1024 <= 232448, "linear attention shared memory");
@@ -589,19 +746,21 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
   const int nc = max(0, min(c.plan.chunks_per_run, (len + kChunk - 1) / kChunk - c0));
   auto valid = [&](int ci) { return min(kChunk, len - (c0 + ci) * kChunk); };
   if (threadIdx.x == 0) {
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < kLocalRing; ++s) {
       mbar_init(&sm.k_full[s], 1);
       mbar_init(&sm.v_full[s], 1);
       mbar_init(&sm.empty[s], 1);
-      mbar_init(&sm.vt_full[s], 256);
+    }
+    for (int s = 0; s < kLocalBufs; ++s) {
+      mbar_init(&sm.part_full[s], 8);
+      mbar_init(&sm.part_free[s], 1);
     }
     mbar_init(&sm.done, 1);
-    mbar_init(&sm.last_issued, 1);
-    mbar_init(&sm.fixed, 32);
     fence_barrier_init();
   }
-  if (threadIdx.x < kChunk) sm.pw[threadIdx.x] = decay_pow(p.log2_decay[kvh], threadIdx.x);
-  if (warp == 9) tmem_alloc(&sm.tmem_base, 128);
+  const float2 l2 = p.log2_decay[kvh];
+  if (threadIdx.x < kChunk) sm.pw[threadIdx.x] = decay_pow(l2, threadIdx.x);
+  if (warp == kWarpMma) tmem_alloc(&sm.tmem_base, 128);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -609,90 +768,86 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
   bool aborted = false;
   DevStatus* const st = c.status;
   const uint64_t lim = c.wait_ns;
-  if (warp == 8 && lane == 0) {
+  if (warp == kWarpTma && lane == 0) {
     prefetch_tmap(&c.tk);
     prefetch_tmap(&c.tv);
     int loaded = 0;
     for (int ci = 0; ci < nc; ++ci) {
-      const int s = ci & 1;
-      if (ci >= 2 && !dwait(&sm.empty[s], ((ci >> 1) - 1) & 1, st, 70, aborted, lim)) break;
-      load_tile(sm.k[s], &c.tk, (c0 + ci) * kChunk, kvh, b, &sm.k_full[s]);
+      const int s = ci % kLocalRing;
+      if (ci >= kLocalRing && !dwait(&sm.empty[s], (ci / kLocalRing - 1) & 1, st, 70, aborted, lim)) break;
       load_tile(sm.v[s], &c.tv, (c0 + ci) * kChunk, kvh, b, &sm.v_full[s]);
+      load_tile(sm.k[s], &c.tk, (c0 + ci) * kChunk, kvh, b, &sm.k_full[s]);
       loaded = ci + 1;
-      if (loaded == nc) mbar_arrive(&sm.last_issued);
     }
     if (aborted) {
       bool gone = false;
-      for (int i = max(0, loaded - 2); i < loaded; ++i) {
-        dwait(&sm.k_full[i & 1], (i >> 1) & 1, st, 71, gone, lim);
-        dwait(&sm.v_full[i & 1], (i >> 1) & 1, st, 71, gone, lim);
+      for (int i = max(0, loaded - kLocalRing); i < loaded; ++i) {
+        dwait(&sm.k_full[i % kLocalRing], (i / kLocalRing) & 1, st, 71, gone, lim);
+        dwait(&sm.v_full[i % kLocalRing], (i / kLocalRing) & 1, st, 71, gone, lim);
       }
     }
-  } else if (warp == 10) {
-    if (nc > 0 && valid(nc - 1) < kChunk) {
-      const int s = (nc - 1) & 1;
-      if (dwait_warp(&sm.last_issued, 0, st, 72, aborted, lim) &&
-          dwait_warp(&sm.k_full[s], ((nc - 1) >> 1) & 1, st, 72, aborted, lim)) {
-        zero_rows(sm.k[s], valid(nc - 1), lane);
-        fence_proxy_async_smem();
-        mbar_arrive(&sm.fixed);
-      }
-    }
-  } else if (warp == 9) {
+  } else if (warp == kWarpMma) {
     const uint32_t lead = elect_one();
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     constexpr uint32_t id_ab = idesc_bf16(128, 128, 1, 1);
     const uint32_t dhi = (uint32_t)(smem_desc_sw128(0, 16) >> 32);
-    constexpr uint32_t kStep = kTileBytes >> 4;
     const uint32_t k_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.k[0]), kTileBytes / 2);
-    const uint32_t v_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.v[0]), kTileBytes / 2);
-    const uint32_t l_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.lo[0]), kTileBytes / 2);
-    for (int ci = 0; ci < nc; ++ci) {
-      const int s = ci & 1;
-      if (!dwait_warp(&sm.k_full[s], (ci >> 1) & 1, st, 73, aborted, lim)) break;
-      if (ci == nc - 1 && valid(ci) < kChunk && !dwait_warp(&sm.fixed, 0, st, 74, aborted, lim)) break;
-      if (!dwait_warp(&sm.vt_full[s], (ci >> 1) & 1, st, 75, aborted, lim)) break;
-      tc_fence_after();
-      if (ci == 0)
-        issue_k_v<0>(lead, tm, k_lo + s * kStep, v_lo + s * kStep, dhi, id_ab);
-      else
-        issue_k_v<1>(lead, tm, k_lo + s * kStep, v_lo + s * kStep, dhi, id_ab);
-      issue_k_v<1>(lead, tm, k_lo + s * kStep, l_lo + s * kStep, dhi, id_ab);
+    const uint32_t part_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.part[0][0]), kSliceBytes / 2);
+    int n = 0;
+    for (int ci = 0; ci < nc && !aborted; ++ci) {
+      const int s = ci % kLocalRing;
+      if (!dwait_warp(&sm.k_full[s], (ci / kLocalRing) & 1, st, 73, aborted, lim)) break;
+      if (valid(ci) < kChunk) zero_rows(sm.k[s], valid(ci), lane);
+      for (int sl = 0; sl < kSlices; ++sl, ++n) {
+        const int buf = n % kLocalBufs;
+        if (!dwait_warp(&sm.part_full[buf], (n / kLocalBufs) & 1, st, 75, aborted, lim)) break;
+        tc_fence_after();
+        issue_slice(lead, tm, k_lo + s * (kTileBytes >> 4) + 128 * sl, part_lo + buf * (3 * kSliceBytes >> 4), dhi, id_ab,
+                    n == 0);
+        umma_commit_lead(lead, &sm.part_free[buf]);
+      }
       umma_commit_lead(lead, &sm.empty[s]);
     }
     umma_commit_lead(lead, &sm.done);
-  } else if (warp < 8) {
-    const int x = warp >> 2, r = threadIdx.x & 127;
+  } else if (warp < 16) {
+    // two groups of eight warps take the slices in turn
+    const int grp = warp >> 3;
     const int end = min(len, (c0 + c.plan.chunks_per_run) * kChunk);  // the run's last token + 1
-    for (int ci = 0; ci < nc; ++ci) {
-      const int s = ci & 1, nv = valid(ci);
+    int n = grp;
+    for (int ci = 0; ci < nc && !aborted; ++ci) {
+      const int s = ci % kLocalRing, nv = valid(ci);
       // gamma^{end - 1 - t} = gamma^{tokens of the run behind this chunk} gamma^{nv - 1 - j}
-      const float behind = decay_pow(p.log2_decay[kvh], end - ((c0 + ci) * kChunk + nv));
-      // (the slot's copy is complete only after the products of chunk ci - 2)
-      if (!dwait_warp(&sm.v_full[s], (ci >> 1) & 1, st, 76, aborted, lim)) break;
-      decay_values(sm.v[s], sm.lo[s], nv, threadIdx.x, 256, [&](int j) { return behind * sm.pw[nv - 1 - j]; });
-      fence_proxy_async_smem();
-      mbar_arrive(&sm.vt_full[s]);
-    }
-    float* dst = c.local + (((size_t)run * p.batch * p.n_kv_heads + bh) * kHeadDim + r) * kHeadDim + 64 * x;
-    if (nc > 0 && dwait_warp(&sm.done, 0, st, 77, aborted, 2 * lim)) {
-      tc_fence_after();
-#pragma unroll
-      for (int blk = 0; blk < 2; ++blk) {
-        uint32_t kv[32];
-        tmem_ld32(tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 64 * x + 32 * blk, kv);
-        tmem_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 32; e += 4)
-          *reinterpret_cast<uint4*>(dst + 32 * blk + e) = make_uint4(kv[e], kv[e + 1], kv[e + 2], kv[e + 3]);
+      const float behind = decay_pow(l2, end - ((c0 + ci) * kChunk + nv));
+      if (!dwait_warp(&sm.v_full[s], (ci / kLocalRing) & 1, st, 76, aborted, lim)) break;
+      for (int sl = grp; sl < kSlices; sl += 2, n += 2) {
+        if (n >= kLocalBufs && !dwait_warp(&sm.part_free[grp], (n / kLocalBufs - 1) & 1, st, 76, aborted, lim)) break;
+        decay_slice<256>(sm.v[s], sm.part[grp], sl, nv, threadIdx.x & 255,
+                         [&](int j) { return behind * sm.pw[nv - 1 - j]; });
+        fence_proxy_async_smem();
+        warp_arrive(&sm.part_full[grp], lane);
       }
-    } else if (nc == 0) {
-      for (int e = 0; e < 64; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    if (warp < 4) {
+      float* dst = c.local + (((size_t)run * p.batch * p.n_kv_heads + bh) * kHeadDim + threadIdx.x) * kHeadDim;
+      if (nc > 0 && dwait_warp(&sm.done, 0, st, 77, aborted, lim)) {
+        tc_fence_after();
+#pragma unroll 1
+        for (int blk = 0; blk < 4; ++blk) {
+          uint32_t kv[32];
+          tmem_ld32(tmem + ((uint32_t)(32 * warp) << 16) + 32 * blk, kv);
+          tmem_wait_ld32(kv);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<uint4*>(dst + 32 * blk + e) = make_uint4(kv[e], kv[e + 1], kv[e + 2], kv[e + 3]);
+        }
+      } else if (nc == 0) {
+        for (int e = 0; e < kHeadDim; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
     }
     tc_fence_before();
   }
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kWarpMma) {
     __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, 128);
@@ -714,14 +869,22 @@ __global__ void __launch_bounds__(kJoinThreads) linear_join_kernel(const __grid_
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (p.state_in) s = *reinterpret_cast<const float4*>(p.state_in + at);
   const int run_tok = c.plan.chunks_per_run * kChunk;
-  const float whole = decay_pow(p.log2_decay[bh % p.n_kv_heads], run_tok);
-  for (int run = 0; run < c.plan.runs; ++run) {
-    const int n = min(run_tok, max(0, len - run * run_tok));
-    *reinterpret_cast<float4*>(c.start + run * step + at) = s;
-    if (n == 0) continue;
-    const float g = n == run_tok ? whole : decay_pow(p.log2_decay[bh % p.n_kv_heads], n);
-    const float4 l = *reinterpret_cast<const float4*>(c.local + run * step + at);
-    s = make_float4(fmaf(s.x, g, l.x), fmaf(s.y, g, l.y), fmaf(s.z, g, l.z), fmaf(s.w, g, l.w));
+  const float2 l2 = p.log2_decay[bh % p.n_kv_heads];
+  const float whole = decay_pow(l2, run_tok);
+  constexpr int kAhead = 8;  // sums in flight
+  for (int run0 = 0; run0 < c.plan.runs; run0 += kAhead) {
+    float4 l[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (run0 + u < c.plan.runs) l[u] = *reinterpret_cast<const float4*>(c.local + (run0 + u) * step + at);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (run0 + u >= c.plan.runs) break;
+      const int n = min(run_tok, max(0, len - (run0 + u) * run_tok));
+      *reinterpret_cast<float4*>(c.start + (run0 + u) * step + at) = s;
+      const float g = n == run_tok ? whole : decay_pow(l2, n);  // (no token: gamma^0 = 1, and the sum is 0)
+      s = make_float4(fmaf(s.x, g, l[u].x), fmaf(s.y, g, l[u].y), fmaf(s.z, g, l[u].z), fmaf(s.w, g, l[u].w));
+    }
   }
   *reinterpret_cast<float4*>(p.state_out + at) = s;
 }
