@@ -637,11 +637,14 @@ def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: 
             raise ValueError("linear_attend: states are contiguous fp32 [B, Hkv, 128, 128]")
     ws = ws or default_workspace(q.device)
     L = lib()
-    wp, wn = ws.get(L.uc_linear_workspace_size(B, hq, hkv, T))
-    check("uc_linear_attend", L.uc_linear_attend(
-        C.byref(_rows(q)), C.byref(_rows(k)), C.byref(_rows(v)), B, hq, hkv, T,
-        None if lengths is None else (C.c_int32 * B)(*lengths), (C.c_float * hkv)(*log_decay), _ptr(state),
-        out_state.data_ptr(), C.byref(_rows(out)), wp, wn, _stream(stream)))
+    args = (C.byref(_rows(q)), C.byref(_rows(k)), C.byref(_rows(v)), B, hq, hkv, T,
+            None if lengths is None else (C.c_int32 * B)(*lengths), (C.c_float * hkv)(*log_decay), _ptr(state),
+            out_state.data_ptr(), C.byref(_rows(out)))
+    st = _stream(stream)
+    code = L.uc_linear_attend(*args, *ws.get(256), st)
+    if code == _lib.UC_ERR_OOM:   # nothing is launched then: only now is the size asked for
+        code = L.uc_linear_attend(*args, *ws.get(L.uc_linear_workspace_size(B, hq, hkv, T)), st)
+    check("uc_linear_attend", code)
     return out, out_state
 
 

@@ -69,48 +69,96 @@ using namespace uc;
 extern "C" {
 
 // ------------------------------------------------------- linear attention
+// States of runs that a plan may ask for (64 KB each, twice): the workspace's bound.
+constexpr int64_t kMaxLinearSums = 640;
+
 // Decode-shaped calls take the recurrence token by token.
 static bool linear_steps(int n_q_heads, int n_kv_heads, int n_tok) {
   return n_tok <= UC_MAX_QTOKENS;
 }
 
-// How a prompt is cut: over query heads and over tokens where the (sequence,
-// KV head) pairs alone leave SMs idle. Either costs a pass over k and v before
-// (the states that the runs start from) and two launches. Costs in clocks of a
-// CTA.
-static LinearPlan plan_linear(int batch, int n_q_heads, int n_kv_heads, int n_tok) {
-  constexpr double kTile = 3200, kChunkCost = 1500, kCta = 6000, kFirstChunk = 3000, kFirstPass = 12000;
-  const int pairs = batch * n_kv_heads, g = n_q_heads / n_kv_heads, sms = num_sms();
-  const int chunks = (n_tok + kChunk - 1) / kChunk;
+// How prompts are cut: over query heads (each part forms the state on its own)
+// and over tokens (a pass over k and v before, for the states that the runs
+// start from). Costs in clocks of a CTA, from measured launches: a tile of one
+// head and chunk, a chunk's update, a CTA's start and end; the same for the
+// pass before.
+static LinearPlan plan_linear(int batch, int n_q_heads, int n_kv_heads, const int32_t* lengths) {
+  constexpr double kTile = 3400, kUpdate = 2500, kCta = 9000, kSumChunk = 3500, kSumCta = 12000;
+  const int g = n_q_heads / n_kv_heads, sms = num_sms();
+  int64_t chunks = 0;
+  int longest = 1;
+  auto chunks_of = [](int n) { return (n + kChunk - 1) / kChunk; };
+  for (int b = 0; b < batch; ++b) {
+    chunks += chunks_of(lengths[b]);
+    longest = std::max(longest, chunks_of(lengths[b]));
+  }
   LinearPlan best;
   memset(&best, 0, sizeof(best));
   double least = 0;
   for (int per = 1; per <= g; ++per) {
     const int parts = (g + per - 1) / per;
-    for (int waves = 0; waves <= 4; ++waves) {
-      // one run, or as many as fill so many rounds of CTAs
-      const int64_t want = waves == 0 ? 1 : (int64_t)waves * sms / ((int64_t)pairs * parts);
-      if (want < 1 || (waves > 0 && want == 1)) continue;
-      const int cpr = (int)((chunks + want - 1) / want), runs = (chunks + cpr - 1) / cpr;
-      const bool two = runs > 1 || parts > 1;
-      double cost = std::ceil((double)pairs * runs * parts / sms) * (kCta + cpr * (kChunkCost + per * kTile));
-      if (two) cost += kFirstPass + std::ceil((double)pairs * runs / sms) * cpr * kFirstChunk + runs * 200.0;
+    if (per > 1 && parts == (g + per - 2) / (per - 1)) continue;  // as many parts as before, less even
+    int last_cpr = 0;
+    for (int rounds = 0; rounds <= 4; ++rounds) {
+      // whole sequences, or runs that fill so many rounds of CTAs
+      int cpr = longest;
+      if (rounds > 0) {
+        const int64_t want = (int64_t)rounds * sms / ((int64_t)n_kv_heads * parts);
+        if (want <= batch) continue;
+        cpr = (int)std::max<int64_t>(1, (chunks + want - 1) / want);
+        // (sequences' ends leave runs short: raise it until the rounds hold them)
+        for (;; ++cpr) {
+          int64_t n = 0;
+          for (int b = 0; b < batch; ++b) n += std::max(1, (chunks_of(lengths[b]) + cpr - 1) / cpr);
+          if (n <= want || cpr >= longest) break;
+        }
+      }
+      if (cpr == last_cpr) continue;
+      last_cpr = cpr;
+      int64_t n = 0;
+      bool several = false;
+      double total = 0, most = 0;
+      for (int b = 0; b < batch; ++b) {
+        const int nb = chunks_of(lengths[b]), r = std::max(1, (nb + cpr - 1) / cpr);
+        n += r;
+        several |= r > 1;
+        total += (double)n_kv_heads * parts * (r * kCta + nb * (kUpdate + per * kTile));
+        most = std::max(most, kCta + std::min(cpr, nb) * (kUpdate + per * kTile));
+      }
+      if (n * n_kv_heads * parts > INT32_MAX) continue;
+      if (several && n * n_kv_heads > kMaxLinearSums) continue;
+      const double ctas = (double)n * n_kv_heads * parts;
+      double cost = std::min(std::ceil(ctas / sms) * most, (total - most) / sms + most);
+      if (several) {
+        const double sums = (double)(n - batch) * n_kv_heads;
+        cost += std::ceil(sums / sms) * (kSumCta + cpr * kSumChunk);
+      }
       if (least == 0 || cost < least) {
         least = cost;
-        best = LinearPlan{chunks, runs, cpr, parts, per, two};
+        best.chunks_per_run = cpr;
+        best.head_parts = parts;
+        best.heads_per_part = per;
+        best.several = several;
       }
     }
   }
+  for (int b = 0; b < batch; ++b)
+    best.run_begin[b + 1] =
+        best.run_begin[b] + std::max(1, (chunks_of(lengths[b]) + best.chunks_per_run - 1) / best.chunks_per_run);
+  best.runs = best.run_begin[batch];
   return best;
 }
+
+// Bytes of `states` pairs of run states (own sum, start) behind the header.
+static size_t linear_bytes(uint64_t states) { return 256 + 2 * states * UC_HEAD_DIM * UC_HEAD_DIM * sizeof(float); }
 
 size_t uc_linear_workspace_size(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_tok) {
   UC_TRACE();
   if (batch < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || n_tok < 1) return 0;
   if (linear_steps(n_q_heads, n_kv_heads, n_tok)) return 256;
-  const LinearPlan plan = plan_linear(batch, n_q_heads, n_kv_heads, n_tok);
-  if (!plan.two_pass) return 256;
-  return 256 + 2ull * plan.runs * batch * n_kv_heads * UC_HEAD_DIM * UC_HEAD_DIM * sizeof(float);
+  // whatever the lengths: every chunk a run of its own, as far as plans go
+  const uint64_t pairs = (uint64_t)batch * n_kv_heads, chunks = (n_tok + kChunk - 1) / kChunk;
+  return linear_bytes(std::max(pairs, std::min(pairs * chunks, (uint64_t)kMaxLinearSums)));
 }
 
 uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v, int32_t batch, int32_t n_q_heads,
@@ -160,9 +208,6 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
       return UC_ERR_SHAPE;
     }
   }
-  st = check_workspace(workspace, workspace_bytes, uc_linear_workspace_size(batch, n_q_heads, n_kv_heads, n_tok),
-                       "uc_linear_attend");
-  if (st != UC_OK) return st;
   p.state_in = state_in;
   p.state_out = state_out;
   p.batch = batch;
@@ -173,19 +218,26 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
   p.scale = (float)(1.0 / std::sqrt((double)UC_HEAD_DIM));
   const cudaStream_t cs = reinterpret_cast<cudaStream_t>(stream);
   if (linear_steps(n_q_heads, n_kv_heads, n_tok)) {
+    st = check_workspace(workspace, workspace_bytes, 256, "uc_linear_attend");
+    if (st != UC_OK) return st;
     launch_linear_step(p, cs);
     return cuda_check("uc_linear_attend");
   }
   LinearChunkParams c;
   memset(&c, 0, sizeof(c));
+  c.plan = plan_linear(batch, n_q_heads, n_kv_heads, p.lengths);
+  // (in place, a CTA may write a state that others have yet to start from)
+  c.from_start = c.plan.several || (c.plan.head_parts > 1 && state_in == state_out);
+  const uint64_t states = c.from_start ? (uint64_t)c.plan.runs * n_kv_heads : 0;
+  st = check_workspace(workspace, workspace_bytes, linear_bytes(states), "uc_linear_attend");
+  if (st != UC_OK) return st;
   c.p = p;
   st = encode_rows_4d(&c.tq, p.q, n_tok, n_q_heads, batch, kChunk);
   if (st == UC_OK) st = encode_rows_4d(&c.tk, p.k, n_tok, n_kv_heads, batch, kChunk);
   if (st == UC_OK) st = encode_rows_4d(&c.tv, p.v, n_tok, n_kv_heads, batch, kChunk);
   if (st != UC_OK) return st;
-  c.plan = plan_linear(batch, n_q_heads, n_kv_heads, n_tok);
   c.local = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 256);
-  c.start = c.local + (size_t)c.plan.runs * batch * n_kv_heads * UC_HEAD_DIM * UC_HEAD_DIM;
+  c.start = c.local + states * UC_HEAD_DIM * UC_HEAD_DIM;
   c.status = static_cast<DevStatus*>(workspace);
   c.wait_ns = wait_limit_ns();
   launch_linear_chunks(c, cs);

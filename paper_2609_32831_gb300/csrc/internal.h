@@ -307,20 +307,22 @@ struct LinearParams {
 void launch_linear_step(const LinearParams& p, cudaStream_t st);
 
 // Prompts in chunks of kChunk tokens. The chunks of a sequence are cut into
-// `runs` runs of chunks_per_run, the query heads of a KV head into
-// `head_parts` parts; one CTA takes (sequence, KV head, run, part). With more
-// than one of either, the states that the runs start from are formed first
-// (`runs` > 1: sums of the runs' own tokens, then joined).
+// runs of chunks_per_run, the query heads of a KV head into head_parts parts;
+// one CTA takes (run, KV head, part). Where a sequence has several runs, the
+// states that they start from are formed first: the runs' own sums, then joined.
 constexpr int kChunk = 128;
 struct LinearPlan {
-  int chunks, runs, chunks_per_run, head_parts, heads_per_part;
-  bool two_pass;
+  int chunks_per_run, head_parts, heads_per_part;
+  int runs;                 // of all sequences
+  bool several;             // some sequence has more than one run
+  int32_t run_begin[UC_MAX_BATCH + 1];
 };
 struct LinearChunkParams {
   LinearParams p;
   CUtensorMap tq, tk, tv;  // bf16 [128, T, H, B], box 64 x kChunk, 128B swizzle
   LinearPlan plan;
-  float* local;            // [runs][B * Hkv][128][128]: a run's own sum, fp32
+  bool from_start;         // runs start from `start`, else from state_in
+  float* local;            // [runs][Hkv][128][128]: a run's own sum, fp32
   float* start;            // the same: the state a run starts from
   DevStatus* status;
   uint64_t wait_ns;

@@ -121,9 +121,9 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 constexpr int kLThreads = 768;
 constexpr int kLRegLaunch = 80;  // registers per thread at launch, and after the warpgroups rebalance
 constexpr int kLRegP = 88;
-constexpr int kLRegEpilogue = 80;
-constexpr int kLRegState = 72;
-constexpr int kLRegOther = 72;
+constexpr int kLRegEpilogue = 88;
+constexpr int kLRegState = 64;
+constexpr int kLRegOther = 56;
 static_assert(256 * (kLRegP + kLRegEpilogue) + 128 * (kLRegState + kLRegOther) <= kLThreads * kLRegLaunch, "register split");
 constexpr int kWarpEpilogue = 8, kWarpState = 16, kWarpTma = 20, kWarpQk = 21, kWarpMma = 22, kWarpSlice = 23;
 constexpr uint32_t kTmemLinear = 512;
@@ -247,19 +247,19 @@ __device__ __forceinline__ void issue_p_v(uint32_t lead, uint32_t d, uint32_t a,
   for (uint32_t k = 0; k < 8; ++k) issue_ts(lead, d, a + 8 * k + 32 * (k >> 2), b + 128 * k, hi, id);
 }
 
-// The decayed values of tokens 16 sl .. 16 sl + 15 of a chunk as three bf16
-// parts, by `threads` threads (a divisor of 256). Token j's weight w(j), 0 from
-// nv on (whatever the row holds).
-template <int THREADS, typename W>
-__device__ __forceinline__ void decay_slice(const uint8_t* v, uint8_t (*parts)[kSliceBytes], int sl, int nv, int thread,
-                                            const W& weight) {
-#pragma unroll
-  for (int i = thread; i < 2 * kSlice * 8; i += THREADS) {
-    const int half = i / (8 * kSlice), in = i % (8 * kSlice), j = kSlice * sl + (in >> 3);
+// The decayed values of tokens ROWS sl .. ROWS sl + ROWS - 1 of a chunk as
+// three bf16 parts ([2 x 64 channels][ROWS][128 B] each), by THREADS threads.
+// Token j's weight w(j), 0 from nv on (whatever the row holds).
+template <int ROWS, int THREADS, typename W>
+__device__ __forceinline__ void decay_slice(const uint8_t* v, uint8_t (*parts)[ROWS * kHeadDim * 2], int sl, int nv,
+                                            int thread, const W& weight) {
+#pragma unroll 2
+  for (int i = thread; i < 2 * ROWS * 8; i += THREADS) {
+    const int half = i / (8 * ROWS), in = i % (8 * ROWS), j = ROWS * sl + (in >> 3);
     uint32_t part[3][4] = {};
     if (j < nv) {
       const float w = weight(j);
-      const uint4 x = *(reinterpret_cast<const uint4*>(v + half * (kTileBytes / 2) + kSlice * sl * 128) + in);
+      const uint4 x = *(reinterpret_cast<const uint4*>(v + half * (kTileBytes / 2) + ROWS * sl * 128) + in);
       const uint32_t bits[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -280,10 +280,9 @@ __device__ __forceinline__ void decay_slice(const uint8_t* v, uint8_t (*parts)[k
 }
 
 // D += K^T V over one slice: A the slice's rows of k, B its three parts.
-__device__ __forceinline__ void issue_slice(uint32_t lead, uint32_t d, uint32_t k, uint32_t parts, uint32_t hi, uint32_t id,
-                                            bool first) {
+__device__ __forceinline__ void issue_slice(uint32_t lead, uint32_t d, uint32_t k, uint32_t parts, uint32_t hi, uint32_t id) {
 #pragma unroll 1
-  for (uint32_t u = 0; u < 3; ++u) issue_ss(lead, d, k, parts + u * (kSliceBytes >> 4), hi, id, !first || u > 0);
+  for (uint32_t u = 0; u < 3; ++u) issue_ss(lead, d, k, parts + u * (kSliceBytes >> 4), hi, id, 1u);
 }
 
 // Zeroes rows nv .. 127 of a tile, by one warp.
@@ -295,6 +294,16 @@ __device__ __forceinline__ void zero_rows(uint8_t* tile, int nv, int lane) {
   __syncwarp();
 }
 
+// The sequence of run `grun`.
+__device__ __forceinline__ int sequence_of(const LinearPlan& plan, int batch, int grun) {
+  int lo = 0, hi = batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (plan.run_begin[mid] <= grun) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
 __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid_constant__ LinearChunkParams c) {
   extern __shared__ uint8_t dyn_smem[];
   LinearSmem& sm = *reinterpret_cast<LinearSmem*>(
@@ -302,18 +311,19 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
   const LinearParams& p = c.p;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int part = blockIdx.x % c.plan.head_parts;
-  const int run = blockIdx.x / c.plan.head_parts % c.plan.runs;
-  const int bh = blockIdx.x / (c.plan.head_parts * c.plan.runs);
-  const int b = bh / p.n_kv_heads, kvh = bh % p.n_kv_heads;
+  const int kvh = blockIdx.x / c.plan.head_parts % p.n_kv_heads;
+  const int grun = blockIdx.x / (c.plan.head_parts * p.n_kv_heads);
+  const int b = sequence_of(c.plan, p.batch, grun);
+  const int run = grun - c.plan.run_begin[b];
   const int h0 = part * c.plan.heads_per_part;
   const int nh = min(c.plan.heads_per_part, p.group - h0);
   const int len = p.lengths[b];
   const int c0 = run * c.plan.chunks_per_run;
   const int n_all = (len + kChunk - 1) / kChunk;  // chunks with a valid token
-  const int nc = max(0, min(c.plan.chunks_per_run, n_all - c0));
+  const int nc = min(c.plan.chunks_per_run, n_all - c0);
   const int tiles = nc * nh;
-  // the state behind the last chunk is needed where this launch writes it
-  const bool last_state = !c.plan.two_pass;
+  // a sequence's last run ends with the state behind its last token
+  const bool last_state = part == 0 && grun + 1 == c.plan.run_begin[b + 1];
   auto valid = [&](int ci) { return min(kChunk, len - (c0 + ci) * kChunk); };
   // loads in order, nh + 2 per chunk: k, the first head's q, v, the other heads' q
   auto load_k = [&](int ci) { return ci * (nh + 2); };
@@ -487,7 +497,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
           if (!dwait_warp(&sm.part_full[buf], (n >> 1) & 1, st, 62, aborted, lim)) break;
           tc_fence_after();
           issue_slice(lead, tm + kColState, col_lo + ks * (kTileBytes >> 4) + 128 * sl,
-                      part_lo + buf * (3 * kSliceBytes >> 4), dhi, id_ab, false);
+                      part_lo + buf * (3 * kSliceBytes >> 4), dhi, id_ab);
           umma_commit_lead(lead, &sm.part_free[buf]);
         }
         umma_commit_lead(lead, &sm.kv_done);
@@ -504,10 +514,10 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     // ---------------------------------------------------------------- state
     const int r = threadIdx.x & 127;  // key channel = TMEM lane
     const uint32_t s_addr = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColState;
-    if (c.plan.two_pass) griddep_wait();
-    const size_t row = ((size_t)bh * kHeadDim + r) * kHeadDim;
-    const float* src = c.plan.two_pass ? c.start + (size_t)run * p.batch * p.n_kv_heads * kHeadDim * kHeadDim + row
-                                       : (p.state_in ? p.state_in + row : nullptr);
+    if (c.from_start) griddep_wait();
+    const size_t row = ((size_t)(b * p.n_kv_heads + kvh) * kHeadDim + r) * kHeadDim;
+    const float* src = c.from_start ? c.start + ((size_t)(grun * p.n_kv_heads + kvh) * kHeadDim + r) * kHeadDim
+                                    : (p.state_in ? p.state_in + row : nullptr);
 #pragma unroll 1
     for (int blk = 0; blk < 4; ++blk) {
       uint32_t w[32];
@@ -563,7 +573,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       for (int sl = 0; sl < kSlices; ++sl, ++n_slice) {
         const int buf = n_slice & 1;
         if (n_slice >= 2 && !dwait_warp(&sm.part_free[buf], ((n_slice >> 1) - 1) & 1, st, 68, aborted, lim)) break;
-        decay_slice<128>(v, sm.part[buf], sl, nv, r, [&](int j) { return sm.pw[nv - 1 - j]; });
+        decay_slice<kSlice, 128>(v, sm.part[buf], sl, nv, r, [&](int j) { return sm.pw[nv - 1 - j]; });
         fence_proxy_async_smem();
         warp_arrive(&sm.part_full[buf], lane);
       }
@@ -700,13 +710,6 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       tc_fence_before();
       warp_arrive(&sm.p_full[t & 1], lane);
     }
-    // tokens of this run in chunks behind the sequence's end: zeros
-    const int z0 = (c0 + nc) * kChunk, z1 = min(p.n_tok, (c0 + c.plan.chunks_per_run) * kChunk);
-    for (int64_t i = threadIdx.x; i < (int64_t)(z1 - z0) * nh * (kHeadDim / 8); i += 256) {
-      const int e = (int)(i % (kHeadDim / 8)), row = (int)(i / (kHeadDim / 8));
-      *reinterpret_cast<uint4*>(p.out.at(b, kvh * p.group + h0 + row % nh, z0 + row / nh) + 8 * e) =
-          make_uint4(0, 0, 0, 0);
-    }
     tc_fence_before();
   }
   __syncthreads();
@@ -717,17 +720,19 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
   }
 }
 
-// A run's own sum: sum_j k_j (gamma^{e-1-j} v_j)^T over its tokens, e its end.
-// The weights fall towards the run's start, so the chunks accumulate in tensor
-// memory without a rescale. 16 warps form the decayed values slice by slice.
-constexpr int kLocalRing = 3;  // chunks in flight
-constexpr int kLocalBufs = 2;  // slices per warpgroup
+// A run's own sum: sum_j k_j (gamma^{e-1-j} v_j)^T over its tokens, e its end
+// (a sequence's last run needs none). The weights fall towards the run's
+// start, so the chunks accumulate in tensor memory without a rescale. Four
+// groups of four warps form the decayed values, a quarter chunk each.
+constexpr int kLocalRing = 2;  // chunks in flight
+constexpr int kQuarter = kChunk / 4;
+constexpr uint32_t kQuarterBytes = kQuarter * kHeadDim * 2;
 struct LinearLocalSmem {
   uint8_t k[kLocalRing][kTileBytes], v[kLocalRing][kTileBytes];
-  uint8_t part[kLocalBufs][3][kSliceBytes];
-  float pw[kChunk];  // gamma^n
+  uint8_t part[4][3][kQuarterBytes];  // [2 x 64 channels][32 tokens][128 B]
+  float pw[kChunk];                   // gamma^n
   uint64_t k_full[kLocalRing], v_full[kLocalRing], empty[kLocalRing];
-  uint64_t part_full[kLocalBufs], part_free[kLocalBufs], done;
+  uint64_t part_full[4], part_free[4], done;
   uint32_t tmem_base;
 };
 static_assert(sizeof(LinearLocalSmem) + 1024 <= 232448, "linear attention shared memory");
@@ -739,20 +744,19 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
   griddep_launch_dependents();
   const LinearParams& p = c.p;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-  const int run = blockIdx.x % c.plan.runs, bh = blockIdx.x / c.plan.runs;
-  const int b = bh / p.n_kv_heads, kvh = bh % p.n_kv_heads;
-  const int len = p.lengths[b];
-  const int c0 = run * c.plan.chunks_per_run;
-  const int nc = max(0, min(c.plan.chunks_per_run, (len + kChunk - 1) / kChunk - c0));
-  auto valid = [&](int ci) { return min(kChunk, len - (c0 + ci) * kChunk); };
+  const int kvh = blockIdx.x % p.n_kv_heads, grun = blockIdx.x / p.n_kv_heads;
+  const int b = sequence_of(c.plan, p.batch, grun);
+  if (grun + 1 == c.plan.run_begin[b + 1]) return;
+  const int c0 = (grun - c.plan.run_begin[b]) * c.plan.chunks_per_run;
+  const int nc = c.plan.chunks_per_run;  // every chunk of a run before the last is whole
   if (threadIdx.x == 0) {
     for (int s = 0; s < kLocalRing; ++s) {
       mbar_init(&sm.k_full[s], 1);
       mbar_init(&sm.v_full[s], 1);
       mbar_init(&sm.empty[s], 1);
     }
-    for (int s = 0; s < kLocalBufs; ++s) {
-      mbar_init(&sm.part_full[s], 8);
+    for (int s = 0; s < 4; ++s) {
+      mbar_init(&sm.part_full[s], 4);
       mbar_init(&sm.part_free[s], 1);
     }
     mbar_init(&sm.done, 1);
@@ -789,59 +793,53 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
   } else if (warp == kWarpMma) {
     const uint32_t lead = elect_one();
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-    constexpr uint32_t id_ab = idesc_bf16(128, 128, 1, 1);
+    constexpr uint32_t id_ab = idesc_bf16(128, 128, 1, 1);  // A and B along their rows
     const uint32_t dhi = (uint32_t)(smem_desc_sw128(0, 16) >> 32);
     const uint32_t k_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.k[0]), kTileBytes / 2);
-    const uint32_t part_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.part[0][0]), kSliceBytes / 2);
-    int n = 0;
+    const uint32_t part_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.part[0][0]), kQuarterBytes / 2);
+    uint32_t first = 0;
     for (int ci = 0; ci < nc && !aborted; ++ci) {
       const int s = ci % kLocalRing;
       if (!dwait_warp(&sm.k_full[s], (ci / kLocalRing) & 1, st, 73, aborted, lim)) break;
-      if (valid(ci) < kChunk) zero_rows(sm.k[s], valid(ci), lane);
-      for (int sl = 0; sl < kSlices; ++sl, ++n) {
-        const int buf = n % kLocalBufs;
-        if (!dwait_warp(&sm.part_full[buf], (n / kLocalBufs) & 1, st, 75, aborted, lim)) break;
+      for (int g = 0; g < 4; ++g) {
+        if (!dwait_warp(&sm.part_full[g], ci & 1, st, 75, aborted, lim)) break;
         tc_fence_after();
-        issue_slice(lead, tm, k_lo + s * (kTileBytes >> 4) + 128 * sl, part_lo + buf * (3 * kSliceBytes >> 4), dhi, id_ab,
-                    n == 0);
-        umma_commit_lead(lead, &sm.part_free[buf]);
+#pragma unroll 1
+        for (uint32_t u = 0; u < 6; ++u) {  // three parts of two 16-token steps
+          const uint32_t step = u & 1;
+          issue_ss(lead, tm, k_lo + s * (kTileBytes >> 4) + (kQuarter * 128 >> 4) * g + 128 * step,
+                   part_lo + (3 * g + (u >> 1)) * (kQuarterBytes >> 4) + 128 * step, dhi, id_ab, first);
+          first = 1;
+        }
+        umma_commit_lead(lead, &sm.part_free[g]);
       }
       umma_commit_lead(lead, &sm.empty[s]);
     }
     umma_commit_lead(lead, &sm.done);
   } else if (warp < 16) {
-    // two groups of eight warps take the slices in turn
-    const int grp = warp >> 3;
-    const int end = min(len, (c0 + c.plan.chunks_per_run) * kChunk);  // the run's last token + 1
-    int n = grp;
-    for (int ci = 0; ci < nc && !aborted; ++ci) {
-      const int s = ci % kLocalRing, nv = valid(ci);
-      // gamma^{end - 1 - t} = gamma^{tokens of the run behind this chunk} gamma^{nv - 1 - j}
-      const float behind = decay_pow(l2, end - ((c0 + ci) * kChunk + nv));
+    const int g = warp >> 2;
+    for (int ci = 0; ci < nc; ++ci) {
+      const int s = ci % kLocalRing;
+      // gamma^{e - 1 - t} = gamma^{tokens of the run behind this chunk} gamma^{127 - j}
+      const float behind = decay_pow(l2, (nc - 1 - ci) * kChunk);
       if (!dwait_warp(&sm.v_full[s], (ci / kLocalRing) & 1, st, 76, aborted, lim)) break;
-      for (int sl = grp; sl < kSlices; sl += 2, n += 2) {
-        if (n >= kLocalBufs && !dwait_warp(&sm.part_free[grp], (n / kLocalBufs - 1) & 1, st, 76, aborted, lim)) break;
-        decay_slice<256>(sm.v[s], sm.part[grp], sl, nv, threadIdx.x & 255,
-                         [&](int j) { return behind * sm.pw[nv - 1 - j]; });
-        fence_proxy_async_smem();
-        warp_arrive(&sm.part_full[grp], lane);
-      }
+      if (ci > 0 && !dwait_warp(&sm.part_free[g], (ci - 1) & 1, st, 76, aborted, lim)) break;
+      decay_slice<kQuarter, 128>(sm.v[s], sm.part[g], g, kChunk, threadIdx.x & 127,
+                                 [&](int j) { return behind * sm.pw[kChunk - 1 - j]; });
+      fence_proxy_async_smem();
+      warp_arrive(&sm.part_full[g], lane);
     }
-    if (warp < 4) {
-      float* dst = c.local + (((size_t)run * p.batch * p.n_kv_heads + bh) * kHeadDim + threadIdx.x) * kHeadDim;
-      if (nc > 0 && dwait_warp(&sm.done, 0, st, 77, aborted, lim)) {
-        tc_fence_after();
+    if (warp < 4 && dwait_warp(&sm.done, 0, st, 77, aborted, lim)) {
+      tc_fence_after();
+      float* dst = c.local + ((size_t)(grun * p.n_kv_heads + kvh) * kHeadDim + threadIdx.x) * kHeadDim;
 #pragma unroll 1
-        for (int blk = 0; blk < 4; ++blk) {
-          uint32_t kv[32];
-          tmem_ld32(tmem + ((uint32_t)(32 * warp) << 16) + 32 * blk, kv);
-          tmem_wait_ld32(kv);
+      for (int blk = 0; blk < 4; ++blk) {
+        uint32_t kv[32];
+        tmem_ld32(tmem + ((uint32_t)(32 * warp) << 16) + 32 * blk, kv);
+        tmem_wait_ld32(kv);
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<uint4*>(dst + 32 * blk + e) = make_uint4(kv[e], kv[e + 1], kv[e + 2], kv[e + 3]);
-        }
-      } else if (nc == 0) {
-        for (int e = 0; e < kHeadDim; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int e = 0; e < 32; e += 4)
+          *reinterpret_cast<uint4*>(dst + 32 * blk + e) = make_uint4(kv[e], kv[e + 1], kv[e + 2], kv[e + 3]);
       }
     }
     tc_fence_before();
@@ -854,39 +852,50 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
   }
 }
 
-// start[run] and the final state from the runs' own sums, four elements per
-// thread: S <- gamma^{tokens of the run} S + local[run].
+// start of every run from the sums of the runs before it, four elements per
+// thread: S <- gamma^{tokens of the run} S + local. (A sequence of one run
+// starts from its state_in; this copies it where state_out is the same array
+// and several CTAs read it.)
 constexpr int kJoinThreads = 128;
 __global__ void __launch_bounds__(kJoinThreads) linear_join_kernel(const __grid_constant__ LinearChunkParams c) {
-  griddep_wait();
   griddep_launch_dependents();
+  griddep_wait();
   const LinearParams& p = c.p;
   constexpr int kBlocks = kHeadDim * kHeadDim / 4 / kJoinThreads;
-  const int bh = blockIdx.x / kBlocks;
-  const size_t at = (size_t)bh * kHeadDim * kHeadDim + 4 * ((blockIdx.x % kBlocks) * kJoinThreads + threadIdx.x);
-  const size_t step = (size_t)p.batch * p.n_kv_heads * kHeadDim * kHeadDim;
-  const int len = p.lengths[bh / p.n_kv_heads];
+  const int bh = blockIdx.x / kBlocks, b = bh / p.n_kv_heads, kvh = bh % p.n_kv_heads;
+  const int first = c.plan.run_begin[b], runs = c.plan.run_begin[b + 1] - first;
+  const size_t in = 4 * ((blockIdx.x % kBlocks) * kJoinThreads + threadIdx.x);
+  const size_t step = (size_t)p.n_kv_heads * kHeadDim * kHeadDim;
+  const size_t at = (size_t)first * step + (size_t)kvh * kHeadDim * kHeadDim + in;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (p.state_in) s = *reinterpret_cast<const float4*>(p.state_in + at);
-  const int run_tok = c.plan.chunks_per_run * kChunk;
-  const float2 l2 = p.log2_decay[bh % p.n_kv_heads];
-  const float whole = decay_pow(l2, run_tok);
+  if (p.state_in) s = *reinterpret_cast<const float4*>(p.state_in + (size_t)bh * kHeadDim * kHeadDim + in);
+  const float g = decay_pow(p.log2_decay[kvh], c.plan.chunks_per_run * kChunk);
   constexpr int kAhead = 8;  // sums in flight
-  for (int run0 = 0; run0 < c.plan.runs; run0 += kAhead) {
+  for (int run0 = 0; run0 < runs; run0 += kAhead) {
     float4 l[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      if (run0 + u < c.plan.runs) l[u] = *reinterpret_cast<const float4*>(c.local + (run0 + u) * step + at);
+      if (run0 + u + 1 < runs) l[u] = *reinterpret_cast<const float4*>(c.local + (run0 + u) * step + at);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      if (run0 + u >= c.plan.runs) break;
-      const int n = min(run_tok, max(0, len - (run0 + u) * run_tok));
+      if (run0 + u >= runs) break;
       *reinterpret_cast<float4*>(c.start + (run0 + u) * step + at) = s;
-      const float g = n == run_tok ? whole : decay_pow(l2, n);  // (no token: gamma^0 = 1, and the sum is 0)
-      s = make_float4(fmaf(s.x, g, l[u].x), fmaf(s.y, g, l[u].y), fmaf(s.z, g, l[u].z), fmaf(s.w, g, l[u].w));
+      if (run0 + u + 1 < runs)
+        s = make_float4(fmaf(s.x, g, l[u].x), fmaf(s.y, g, l[u].y), fmaf(s.z, g, l[u].z), fmaf(s.w, g, l[u].w));
     }
   }
-  *reinterpret_cast<float4*>(p.state_out + at) = s;
+}
+
+// Zeros for the tokens behind a sequence's last chunk with a valid one (the
+// chunk kernel writes those inside it). One CTA per (sequence, query head,
+// kZeroRows tokens).
+constexpr int kZeroRows = 512;
+__global__ void __launch_bounds__(256) linear_zero_kernel(const __grid_constant__ LinearParams p) {
+  const int b = blockIdx.z, h = blockIdx.y;
+  const int begin = max((int)blockIdx.x * kZeroRows, (p.lengths[b] + kChunk - 1) / kChunk * kChunk);
+  const int end = min(p.n_tok, ((int)blockIdx.x + 1) * kZeroRows);
+  for (int64_t i = 16ll * begin + threadIdx.x; i < 16ll * end; i += 256)
+    *reinterpret_cast<uint4*>(p.out.at(b, h, (int)(i >> 4)) + 8 * (int)(i & 15)) = make_uint4(0, 0, 0, 0);
 }
 
 void launch_linear_chunks(const LinearChunkParams& c, cudaStream_t st) {
@@ -896,14 +905,23 @@ void launch_linear_chunks(const LinearChunkParams& c, cudaStream_t st) {
     cudaFuncSetAttribute(linear_chunk_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
     cudaFuncSetAttribute(linear_local_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLocalSmem);
   });
-  const int pairs = c.p.batch * c.p.n_kv_heads;
-  if (c.plan.two_pass) {
-    linear_local_kernel<<<pairs * c.plan.runs, kLThreads, kLocalSmem, st>>>(c);
-    count_launch();
-    launch_maybe_pdl(true, linear_join_kernel, pairs * (kHeadDim * kHeadDim / 4 / kJoinThreads), kJoinThreads, 0, st, c);
+  const LinearParams& p = c.p;
+  bool behind = false;
+  for (int b = 0; b < p.batch; ++b) behind |= (p.lengths[b] + kChunk - 1) / kChunk * kChunk < p.n_tok;
+  if (behind) {
+    linear_zero_kernel<<<dim3((p.n_tok + kZeroRows - 1) / kZeroRows, p.n_q_heads, p.batch), 256, 0, st>>>(p);
     count_launch();
   }
-  launch_maybe_pdl(c.plan.two_pass, linear_chunk_kernel, pairs * c.plan.runs * c.plan.head_parts, kLThreads, kSmem, st, c);
+  if (c.plan.several) {
+    linear_local_kernel<<<c.plan.runs * p.n_kv_heads, kLThreads, kLocalSmem, st>>>(c);
+    count_launch();
+  }
+  if (c.from_start) {
+    launch_maybe_pdl(c.plan.several, linear_join_kernel, p.batch * p.n_kv_heads * (kHeadDim * kHeadDim / 4 / kJoinThreads),
+                     kJoinThreads, 0, st, c);
+    count_launch();
+  }
+  launch_maybe_pdl(c.from_start, linear_chunk_kernel, c.plan.runs * p.n_kv_heads * c.plan.head_parts, kLThreads, kSmem, st, c);
   count_launch();
 }
 
