@@ -69,100 +69,96 @@ using namespace uc;
 extern "C" {
 
 // ------------------------------------------------------- linear attention
+// States of runs that a plan may ask for (64 KB each, twice): the workspace's bound.
+constexpr int64_t kMaxLinearSums = 640;
+
 // Decode-shaped calls take the recurrence token by token.
 static bool linear_steps(int n_q_heads, int n_kv_heads, int n_tok) {
   return n_tok <= UC_MAX_QTOKENS;
 }
 
 // How prompts are cut: over query heads (each part forms the state on its own)
-// and over tokens (equal ranges of chunks, one per SM, with a pass over k and v
-// before for the states that they start from). Costs in clocks of a CTA, from
-// measured launches: a tile of one head and chunk, a chunk's update of the
-// state, a CTA's start and end; the same for the pass before.
-static uc_status plan_linear(int batch, int n_q_heads, int n_kv_heads, const int32_t* lengths, LinearPlan* plan) {
-  constexpr double kTile = 3400, kUpdate = 2500, kCta = 9000, kSumChunk = 3500, kSumCta = 14000;
+// and over tokens (a pass over k and v before, for the states that the runs
+// start from). Costs in clocks of a CTA, from measured launches: a tile of one
+// head and chunk, a chunk's update, a CTA's start and end; the same for the
+// pass before.
+static LinearPlan plan_linear(int batch, int n_q_heads, int n_kv_heads, const int32_t* lengths) {
+  constexpr double kTile = 3400, kUpdate = 2500, kCta = 9000, kSumChunk = 3500, kSumCta = 12000;
   const int g = n_q_heads / n_kv_heads, sms = num_sms();
-  // sequences with a token: chunks of each, and of those before them
-  int n_seq = 0, n_of[UC_MAX_BATCH];
-  int64_t before[UC_MAX_BATCH + 1] = {0};
-  int longest = 0, shortest = INT_MAX;
+  int64_t chunks = 0;
+  int longest = 1;
+  auto chunks_of = [](int n) { return (n + kChunk - 1) / kChunk; };
   for (int b = 0; b < batch; ++b) {
-    if (lengths[b] == 0) continue;
-    const int n = (lengths[b] + kChunk - 1) / kChunk;
-    n_of[n_seq] = n;
-    before[n_seq + 1] = before[n_seq] + (int64_t)n * n_kv_heads;
-    ++n_seq;
-    longest = std::max(longest, n);
-    shortest = std::min(shortest, n);
+    chunks += chunks_of(lengths[b]);
+    longest = std::max(longest, chunks_of(lengths[b]));
   }
-  memset(plan, 0, sizeof(*plan));
-  plan->head_parts = 1;
-  plan->heads_per_part = g;
-  if (n_seq == 0) return UC_OK;
+  LinearPlan best;
+  memset(&best, 0, sizeof(best));
   double least = 0;
-  for (int per = std::min(g, 255); per >= 1; --per) {
+  for (int per = 1; per <= g; ++per) {
     const int parts = (g + per - 1) / per;
-    if (per > 1 && parts == (g + per - 2) / (per - 1)) continue;  // as many parts with fewer heads each: more even
-    const int64_t total = before[n_seq] * parts;
-    if (total > INT32_MAX) continue;
-    // the pair (sequence, KV head, part) of chunk x, and its first chunk
-    auto pair_of = [&](int64_t x, int64_t* first) {
-      int s = 0;
-      while (before[s + 1] * parts <= x) ++s;
-      const int64_t in = (x - before[s] * parts) / n_of[s];
-      *first = before[s] * parts + in * n_of[s];
-      return (int64_t)s * n_kv_heads * parts + in;
-    };
-    for (int whole = 0; whole < 2; ++whole) {
-      // one range per SM, or one per pair where all are equally long
-      if (whole && shortest != longest) continue;
-      int64_t ctas = whole ? total / longest : std::min<int64_t>(total, sms);
-      // (a CTA takes kMaxRuns pairs at most: more ranges where pairs are many and short)
-      bool cut = false;
-      for (bool fits = whole != 0; !fits; ctas = fits ? ctas : std::min(total, 2 * ctas)) {
-        fits = true;
-        cut = false;
-        for (int64_t i = 0; i < ctas && fits; ++i) {
-          int64_t first, unused;
-          const int64_t a = pair_of(i * total / ctas, &first), z = pair_of((i + 1) * total / ctas - 1, &unused);
-          cut |= first != i * total / ctas;
-          fits = z - a < kMaxRuns;
+    if (per > 1 && parts == (g + per - 2) / (per - 1)) continue;  // as many parts as before, less even
+    int last_cpr = 0;
+    for (int rounds = 0; rounds <= 4; ++rounds) {
+      // whole sequences, or runs that fill so many rounds of CTAs
+      int cpr = longest;
+      if (rounds > 0) {
+        const int64_t want = (int64_t)rounds * sms / ((int64_t)n_kv_heads * parts);
+        if (want <= batch) continue;
+        cpr = (int)std::max<int64_t>(1, (chunks + want - 1) / want);
+        // (sequences' ends leave runs short: raise it until the rounds hold them)
+        for (;; ++cpr) {
+          int64_t n = 0;
+          for (int b = 0; b < batch; ++b) n += std::max(1, (chunks_of(lengths[b]) + cpr - 1) / cpr);
+          if (n <= want || cpr >= longest) break;
         }
       }
-      const double each = std::ceil((double)total / ctas), rounds = std::ceil((double)ctas / sms);
-      const double cost = rounds * (kCta + each * (kUpdate + per * kTile)) + (cut ? kSumCta + each * kSumChunk : 0.0);
+      if (cpr == last_cpr) continue;
+      last_cpr = cpr;
+      int64_t n = 0;
+      bool several = false;
+      double total = 0, most = 0;
+      for (int b = 0; b < batch; ++b) {
+        const int nb = chunks_of(lengths[b]), r = std::max(1, (nb + cpr - 1) / cpr);
+        n += r;
+        several |= r > 1;
+        total += (double)n_kv_heads * parts * (r * kCta + nb * (kUpdate + per * kTile));
+        most = std::max(most, kCta + std::min(cpr, nb) * (kUpdate + per * kTile));
+      }
+      if (n * n_kv_heads * parts > INT32_MAX) continue;
+      if (several && n * n_kv_heads > kMaxLinearSums) continue;
+      const double ctas = (double)n * n_kv_heads * parts;
+      double cost = std::min(std::ceil(ctas / sms) * most, (total - most) / sms + most);
+      if (several) {
+        const double sums = (double)(n - batch) * n_kv_heads;
+        cost += std::ceil(sums / sms) * (kSumCta + cpr * kSumChunk);
+      }
       if (least == 0 || cost < least) {
         least = cost;
-        plan->ctas = (int)ctas;
-        plan->head_parts = parts;
-        plan->heads_per_part = per;
-        plan->cut = cut;
-        plan->total = (int32_t)total;
+        best.chunks_per_run = cpr;
+        best.head_parts = parts;
+        best.heads_per_part = per;
+        best.several = several;
       }
     }
   }
-  if (least == 0) {
-    set_error("uc_linear_attend: too many chunks");
-    return UC_ERR_SHAPE;
-  }
   for (int b = 0; b < batch; ++b)
-    plan->begin[b + 1] = plan->begin[b] + (lengths[b] + kChunk - 1) / kChunk * n_kv_heads * plan->head_parts;
-  return UC_OK;
+    best.run_begin[b + 1] =
+        best.run_begin[b] + std::max(1, (chunks_of(lengths[b]) + best.chunks_per_run - 1) / best.chunks_per_run);
+  best.runs = best.run_begin[batch];
+  return best;
 }
 
-// Behind the header: a sum and a start per CTA of a cut plan, and a copy of the
-// states that are updated in place.
-static size_t linear_bytes(uint64_t ctas, uint64_t pairs) {
-  return 256 + (2 * ctas + pairs) * UC_HEAD_DIM * UC_HEAD_DIM * sizeof(float);
-}
+// Bytes of `states` pairs of run states (own sum, start) behind the header.
+static size_t linear_bytes(uint64_t states) { return 256 + 2 * states * UC_HEAD_DIM * UC_HEAD_DIM * sizeof(float); }
 
 size_t uc_linear_workspace_size(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_tok) {
   UC_TRACE();
   if (batch < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || n_tok < 1) return 0;
   if (linear_steps(n_q_heads, n_kv_heads, n_tok)) return 256;
-  // whatever the lengths: a range per SM, or (short sequences) at most one per pair and part
-  const uint64_t pairs = (uint64_t)batch * n_kv_heads;
-  return linear_bytes(std::max<uint64_t>(num_sms(), 2 * ((uint64_t)batch * n_q_heads / (kMaxRuns / 2) + 1)), pairs);
+  // whatever the lengths: every chunk a run of its own, as far as plans go
+  const uint64_t pairs = (uint64_t)batch * n_kv_heads, chunks = (n_tok + kChunk - 1) / kChunk;
+  return linear_bytes(std::max(pairs, std::min(pairs * chunks, (uint64_t)kMaxLinearSums)));
 }
 
 uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v, int32_t batch, int32_t n_q_heads,
@@ -171,7 +167,7 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
                            size_t workspace_bytes, void* stream) {
   UC_TRACE();
   if (batch < 1 || batch > UC_MAX_BATCH || n_kv_heads < 1 || n_kv_heads > UC_MAX_LINEAR_HEADS ||
-      n_q_heads < n_kv_heads || n_q_heads % n_kv_heads != 0 || n_q_heads > 16384 || n_tok < 1 || n_tok > (1 << 28)) {
+      n_q_heads < n_kv_heads || n_q_heads % n_kv_heads != 0 || n_q_heads > 65535 || n_tok < 1 || n_tok > (1 << 28)) {
     set_error("uc_linear_attend: unsupported shape (batch %d, query heads %d, kv heads %d, tokens %d)", batch,
               n_q_heads, n_kv_heads, n_tok);
     return UC_ERR_SHAPE;
@@ -229,12 +225,11 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
   }
   LinearChunkParams c;
   memset(&c, 0, sizeof(c));
-  st = plan_linear(batch, n_q_heads, n_kv_heads, p.lengths, &c.plan);
-  if (st != UC_OK) return st;
-  // in place, a CTA may write a state that another has yet to start from
-  const uint64_t pairs = (uint64_t)batch * n_kv_heads, ctas = c.plan.cut ? c.plan.ctas : 0;
-  const bool copy = state_in == state_out && (c.plan.cut || c.plan.head_parts > 1);
-  st = check_workspace(workspace, workspace_bytes, linear_bytes(ctas, copy ? pairs : 0), "uc_linear_attend");
+  c.plan = plan_linear(batch, n_q_heads, n_kv_heads, p.lengths);
+  // (in place, a CTA may write a state that others have yet to start from)
+  c.from_start = c.plan.several || (c.plan.head_parts > 1 && state_in == state_out);
+  const uint64_t states = c.from_start ? (uint64_t)c.plan.runs * n_kv_heads : 0;
+  st = check_workspace(workspace, workspace_bytes, linear_bytes(states), "uc_linear_attend");
   if (st != UC_OK) return st;
   c.p = p;
   st = encode_rows_4d(&c.tq, p.q, n_tok, n_q_heads, batch, kChunk);
@@ -242,15 +237,9 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
   if (st == UC_OK) st = encode_rows_4d(&c.tv, p.v, n_tok, n_kv_heads, batch, kChunk);
   if (st != UC_OK) return st;
   c.local = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 256);
-  c.start = c.local + ctas * UC_HEAD_DIM * UC_HEAD_DIM;
+  c.start = c.local + states * UC_HEAD_DIM * UC_HEAD_DIM;
   c.status = static_cast<DevStatus*>(workspace);
   c.wait_ns = wait_limit_ns();
-  if (copy) {
-    float* const before = c.start + ctas * UC_HEAD_DIM * UC_HEAD_DIM;
-    if (cudaMemcpyAsync(before, state_in, ns, cudaMemcpyDeviceToDevice, cs) != cudaSuccess)
-      return cuda_check("uc_linear_attend");
-    c.p.state_in = before;
-  }
   launch_linear_chunks(c, cs);
   return cuda_check("uc_linear_attend");
 }

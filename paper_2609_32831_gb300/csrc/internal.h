@@ -306,25 +306,24 @@ struct LinearParams {
 };
 void launch_linear_step(const LinearParams& p, cudaStream_t st);
 
-// Prompts in chunks of kChunk tokens. The query heads of a KV head are cut into
-// head_parts parts; the chunks of all (sequence, KV head, part) in a row are cut
-// into `ctas` equal ranges, one per CTA, wherever that falls. Where a cut falls
-// inside a sequence, the state that the next CTA starts from is formed first:
-// the CTAs' own sums, then joined.
+// Prompts in chunks of kChunk tokens. The chunks of a sequence are cut into
+// runs of chunks_per_run, the query heads of a KV head into head_parts parts;
+// one CTA takes (run, KV head, part). Where a sequence has several runs, the
+// states that they start from are formed first: the runs' own sums, then joined.
 constexpr int kChunk = 128;
-constexpr int kMaxRuns = 32;  // runs of one CTA
 struct LinearPlan {
-  int ctas, head_parts, heads_per_part;
-  bool cut;                           // some range ends inside a sequence
-  int32_t total;                      // chunks
-  int32_t begin[UC_MAX_BATCH + 1];    // of the sequences before
+  int chunks_per_run, head_parts, heads_per_part;
+  int runs;                 // of all sequences
+  bool several;             // some sequence has more than one run
+  int32_t run_begin[UC_MAX_BATCH + 1];
 };
 struct LinearChunkParams {
   LinearParams p;
   CUtensorMap tq, tk, tv;  // bf16 [128, T, H, B], box 64 x kChunk, 128B swizzle
   LinearPlan plan;
-  float* local;            // [ctas][128][128]: what a CTA's last, cut run adds up, fp32
-  float* start;            // [ctas][128][128]: the state a CTA's first run starts from, where it is cut
+  bool from_start;         // runs start from `start`, else from state_in
+  float* local;            // [runs][Hkv][128][128]: a run's own sum, fp32
+  float* start;            // the same: the state a run starts from
   DevStatus* status;
   uint64_t wait_ns;
 };

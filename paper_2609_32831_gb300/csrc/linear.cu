@@ -86,8 +86,7 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 // HBM: 64 KB of q and o per head and chunk, 1.5 us of an SM's share, against
 // 3 x 512 cycles of the tensor pipe.
 //
-// One CTA per SM takes an equal share of all chunks (LinearPlan): runs of chunks
-// of one (sequence, KV head, part of its query heads) after another.
+// One CTA per (sequence, KV head, run of chunks, part of its query heads):
 //   WG0, WG1 (warps 0-7) halves of the columns of Q K^T: P = mask and weights,
 //            bf16, back to tensor memory
 //   WG2, WG3 (8-15) the epilogue, halves of the channels: o scaled, rounded and
@@ -96,8 +95,7 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 //   WG4      (16-19) the state. It stays in tensor memory in fp32; per chunk
 //            its bf16 copy goes to shared memory for Q S, it is scaled by
 //            gamma^nv in place, and the chunk's decayed values are formed in
-//            slices of 16 tokens that accumulate on it while the chunk's tiles
-//            run (the first two slices before the chunk's turn)
+//            slices of 16 tokens that accumulate on it while the chunk's tiles run
 //   warp 20  TMA producer: k and v tiles per chunk and a q tile per head, in the
 //            order they are needed, each into whichever slot is free
 //   warp 21  issues Q K^T, one tile ahead
@@ -113,7 +111,7 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 //
 // Roundings to bf16: P and the copy of S that Q multiplies (each about as
 // large as the output's own rounding), and none on the state's path: the
-// decayed values enter as three bf16 parts (all 24 bits of v gamma^n; two parts left
+// decayed values enter as three bf16 parts (v gamma^n to 2^-25; two parts left
 // the state 2.7e-6 off), the update accumulates in fp32.
 //
 // a_i and gamma^{-(j+1)} take the row's common factor out of both products.
@@ -122,10 +120,10 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 // it should be less still.
 constexpr int kLThreads = 768;
 constexpr int kLRegLaunch = 80;  // registers per thread at launch, and after the warpgroups rebalance
-constexpr int kLRegP = 80;
-constexpr int kLRegEpilogue = 80;
-constexpr int kLRegState = 88;
-constexpr int kLRegOther = 72;
+constexpr int kLRegP = 88;
+constexpr int kLRegEpilogue = 88;
+constexpr int kLRegState = 64;
+constexpr int kLRegOther = 56;
 static_assert(256 * (kLRegP + kLRegEpilogue) + 128 * (kLRegState + kLRegOther) <= kLThreads * kLRegLaunch, "register split");
 constexpr int kWarpEpilogue = 8, kWarpState = 16, kWarpTma = 20, kWarpQk = 21, kWarpMma = 22, kWarpSlice = 23;
 constexpr uint32_t kTmemLinear = 512;
@@ -145,28 +143,18 @@ __device__ __forceinline__ void rebalance() {
   if constexpr (N > kLRegLaunch) setmaxnreg_inc<N>();
 }
 
-// A run: chunks c0 .. c0 + n - 1 of nh query heads of a (sequence, KV head).
-struct LinearRun {
-  uint8_t b, kvh, nh, last_state;  // last_state: the state behind it is the sequence's, and this run writes it
-  uint16_t head0, last;            // first query head; valid tokens of the last chunk
-  int32_t c0, n;
-};
-static_assert(UC_MAX_BATCH <= 256 && UC_MAX_LINEAR_HEADS <= 256, "one byte each");
-
 struct LinearSmem {
   uint8_t slot[kLSlots][kTileBytes];   // [2 x 64 channels][128 tokens][128 B], 128B swizzle
   uint8_t s[kTileBytes];               // the chunk's state, bf16 [2 x 64 value channels][128 key channels][128 B]
   uint8_t part[2][3][kSliceBytes];     // decayed values, three parts: [2 x 64 channels][16 tokens][128 B]
   uint4 turn[8][32 * 2];               // per epilogue warp: 32 rows of 32 B
-  float pw[kChunk + 4];                // gamma^n of the state's run
-  float wt[kChunk];                    // gamma^{-(n + 1)} of P's run (strong decay: gamma^n)
+  float pw[kChunk + 4];                // gamma^n
+  float cj[kChunk];                    // gamma^{-(n + 1)}
   uint64_t full[kLFull], empty[kLSlots];
   uint64_t s_full[2], p_full[2], o_full, o_free;
-  uint64_t st_ready, s_free, chunk_go[2], k_done[2], v_done[2], kv_done, part_full[2], part_free[2];
+  uint64_t st_ready, s_free, chunk_go, k_done[2], v_done[2], kv_done, part_full[2], part_free[2];
   uint32_t tmem_base;
-  uint32_t ks[2], vs[2];               // slots of a chunk's k and v, by the chunk's parity
-  int32_t n_runs;
-  LinearRun runs[kMaxRuns];
+  uint32_t ks[2], vs;                  // slots of a chunk's k (by parity) and v
   uint8_t slot_of[16];                 // slot of load L at L mod 16
 };
 static_assert(sizeof(LinearSmem) + 1024 <= 232448, "linear attention shared memory");
@@ -275,14 +263,12 @@ __device__ __forceinline__ void decay_slice(const uint8_t* v, uint8_t (*parts)[R
       const uint32_t bits[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        // eight bits of the fp32 value per part, by cutting: nothing is left
         float a = bf16_lo(bits[e]) * w, b = bf16_hi(bits[e]) * w;
 #pragma unroll
         for (int u = 0; u < 3; ++u) {
-          const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
-          part[u][e] = __byte_perm(x, y, 0x7632);
-          a -= __uint_as_float(x & 0xffff0000u);
-          b -= __uint_as_float(y & 0xffff0000u);
+          part[u][e] = pack_bf16(a, b);
+          a -= bf16_lo(part[u][e]);
+          b -= bf16_hi(part[u][e]);
         }
       }
     }
@@ -308,54 +294,15 @@ __device__ __forceinline__ void zero_rows(uint8_t* tile, int nv, int lane) {
   __syncwarp();
 }
 
-// First chunk of a CTA; the CTA of a chunk.
-__device__ __forceinline__ int range_begin(const LinearPlan& plan, int cta) {
-  return (int)((int64_t)cta * plan.total / plan.ctas);
-}
-__device__ __forceinline__ int range_of(const LinearPlan& plan, int x) {
-  return (int)((((int64_t)x + 1) * plan.ctas - 1) / plan.total);
-}
-// The runs of chunks x .. x_end - 1 (at most kMaxRuns); returns their number.
-__device__ __forceinline__ int find_runs(const LinearChunkParams& c, int x, int x_end, LinearRun* out) {
-  const LinearParams& p = c.p;
-  int b = 0, hi = p.batch - 1;
-  while (b < hi) {
-    const int mid = (b + hi + 1) >> 1;
-    if (c.plan.begin[mid] <= x) b = mid; else hi = mid - 1;
+// The sequence of run `grun`.
+__device__ __forceinline__ int sequence_of(const LinearPlan& plan, int batch, int grun) {
+  int lo = 0, hi = batch - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (plan.run_begin[mid] <= grun) lo = mid; else hi = mid - 1;
   }
-  int chunks = (p.lengths[b] + kChunk - 1) / kChunk;
-  int pair = (x - c.plan.begin[b]) / chunks, c0 = (x - c.plan.begin[b]) % chunks, n_runs = 0;
-  while (x < x_end && n_runs < kMaxRuns) {
-    const int kvh = pair / c.plan.head_parts, part = pair % c.plan.head_parts, h0 = part * c.plan.heads_per_part;
-    const int n = min(chunks - c0, x_end - x);
-    const bool whole = c0 + n == chunks;
-    LinearRun& r = out[n_runs++];
-    r.b = (uint8_t)b;
-    r.kvh = (uint8_t)kvh;
-    r.nh = (uint8_t)min(c.plan.heads_per_part, p.group - h0);
-    r.last_state = whole && part == 0;
-    r.head0 = (uint16_t)(kvh * p.group + h0);
-    r.last = (uint16_t)(whole ? p.lengths[b] - (chunks - 1) * kChunk : kChunk);
-    r.c0 = c0;
-    r.n = n;
-    x += n;
-    c0 = 0;
-    if (++pair == p.n_kv_heads * c.plan.head_parts) {
-      pair = 0;
-      do ++b; while (b < p.batch && p.lengths[b] == 0);
-      chunks = b < p.batch ? (p.lengths[b] + kChunk - 1) / kChunk : 1;
-    }
-  }
-  return n_runs;
+  return lo;
 }
-
-template <int ID, int THREADS>
-__device__ __forceinline__ void group_bar() {
-  asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory");
-}
-
-// gamma^kChunk below 2^-64: a memory of under two tokens
-__device__ __forceinline__ bool strong_decay(float2 log2_gamma) { return log2_gamma.x * kChunk < -64.f; }
 
 __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid_constant__ LinearChunkParams c) {
   extern __shared__ uint8_t dyn_smem[];
@@ -363,15 +310,33 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       (reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~static_cast<uintptr_t>(1023));
   const LinearParams& p = c.p;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const int part = blockIdx.x % c.plan.head_parts;
+  const int kvh = blockIdx.x / c.plan.head_parts % p.n_kv_heads;
+  const int grun = blockIdx.x / (c.plan.head_parts * p.n_kv_heads);
+  const int b = sequence_of(c.plan, p.batch, grun);
+  const int run = grun - c.plan.run_begin[b];
+  const int h0 = part * c.plan.heads_per_part;
+  const int nh = min(c.plan.heads_per_part, p.group - h0);
+  const int len = p.lengths[b];
+  const int c0 = run * c.plan.chunks_per_run;
+  const int n_all = (len + kChunk - 1) / kChunk;  // chunks with a valid token
+  const int nc = min(c.plan.chunks_per_run, n_all - c0);
+  const int tiles = nc * nh;
+  // a sequence's last run ends with the state behind its last token
+  const bool last_state = part == 0 && grun + 1 == c.plan.run_begin[b + 1];
+  auto valid = [&](int ci) { return min(kChunk, len - (c0 + ci) * kChunk); };
+  // loads in order, nh + 2 per chunk: k, the first head's q, v, the other heads' q
+  auto load_k = [&](int ci) { return ci * (nh + 2); };
+  auto load_v = [&](int ci) { return ci * (nh + 2) + 2; };
+  auto load_q = [&](int ci, int h) { return ci * (nh + 2) + (h == 0 ? 1 : h + 2); };
   if (threadIdx.x == 0) {
     for (int s = 0; s < kLFull; ++s) mbar_init(&sm.full[s], 1);
     for (int s = 0; s < kLSlots; ++s) mbar_init(&sm.empty[s], 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&sm.s_full[s], 1);
-      mbar_init(&sm.p_full[s], 8);  // (arrivals: one per warp)
+      mbar_init(&sm.p_full[s], 8);     // (arrivals: one per warp)
       mbar_init(&sm.part_full[s], 4);
       mbar_init(&sm.part_free[s], 1);
-      mbar_init(&sm.chunk_go[s], 2);
       mbar_init(&sm.k_done[s], 1);
       mbar_init(&sm.v_done[s], 1);
     }
@@ -380,8 +345,15 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     mbar_init(&sm.st_ready, 4);
     mbar_init(&sm.s_free, 1);
     mbar_init(&sm.kv_done, 1);
+    mbar_init(&sm.chunk_go, 1);
     fence_barrier_init();
-    sm.n_runs = find_runs(c, range_begin(c.plan, blockIdx.x), range_begin(c.plan, blockIdx.x + 1), sm.runs);
+  }
+  const float2 l2 = p.log2_decay[kvh];
+  const bool strong = l2.x * kChunk < -64.f;
+  if (threadIdx.x <= kChunk) {
+    const float w = decay_pow(l2, threadIdx.x);
+    sm.pw[threadIdx.x] = w;
+    if (threadIdx.x < kChunk) sm.cj[threadIdx.x] = strong ? 0.f : decay_pow(l2, -1 - (int)threadIdx.x);
   }
   if (warp == kWarpMma) tmem_alloc(&sm.tmem_base, kTmemLinear);
   tc_fence_before();
@@ -391,10 +363,6 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
   bool aborted = false;
   DevStatus* const st = c.status;
   const uint64_t lim = c.wait_ns;
-  // Counters over all of the CTA's runs, the same in every role: cc chunks, t
-  // tiles, L loads. Loads of a chunk in order: k, the first head's q, v, the
-  // other heads' q.
-  int cc = 0, t = 0, L = 0;
 
   if (warp >= kWarpTma) {
     rebalance<kLRegOther>();
@@ -404,31 +372,35 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       prefetch_tmap(&c.tk);
       prefetch_tmap(&c.tv);
       uint32_t used = 0, phase = 0;  // by slot: taken before; parity of the release waited for
-      for (int i_run = 0; i_run < sm.n_runs && !aborted; ++i_run) {
-        const LinearRun& run = sm.runs[i_run];
-        const int nh = run.nh, n = run.n;
-        for (int ci = 0, in = 0; ci < n; ++L) {
-          int s = -1;
-          const uint64_t t0 = global_ns();
-          for (uint32_t it = 0; s < 0; ++it) {
-            for (int i = 0; i < kLSlots && s < 0; ++i)
-              if (!((used >> i) & 1u) || mbar_test(&sm.empty[i], (phase >> i) & 1u)) s = i;
-            if (s < 0 && (it & 15u) == 15u && global_ns() - t0 > lim) {
-              set_status(st, UC_ERR_TIMEOUT, 50);
-              aborted = true;
-              break;
-            }
+      int L = 0;
+      const int n_loads = nc * (nh + 2);
+      for (int ci = 0, in = 0; L < n_loads; ++L) {
+        int s = -1;
+        const uint64_t t0 = global_ns();
+        for (uint32_t it = 0; s < 0; ++it) {
+          for (int i = 0; i < kLSlots && s < 0; ++i)
+            if (!((used >> i) & 1u) || mbar_test(&sm.empty[i], (phase >> i) & 1u)) s = i;
+          if (s < 0 && (it & 15u) == 15u && global_ns() - t0 > lim) {
+            set_status(st, UC_ERR_TIMEOUT, 50);
+            aborted = true;
+            break;
           }
-          if (aborted) break;
-          if ((used >> s) & 1u) phase ^= 1u << s;
-          used |= 1u << s;
-          sm.slot_of[L & 15] = (uint8_t)s;
-          load_tile(sm.slot[s], in == 0 ? &c.tk : in == 2 ? &c.tv : &c.tq, (run.c0 + ci) * kChunk,
-                    in == 0 || in == 2 ? run.kvh : run.head0 + max(0, in - 2), run.b, &sm.full[L % kLFull]);
-          if (++in == nh + 2) {
-            in = 0;
-            ++ci;
-          }
+        }
+        if (aborted) break;
+        if ((used >> s) & 1u) phase ^= 1u << s;
+        used |= 1u << s;
+        sm.slot_of[L & 15] = (uint8_t)s;
+        uint64_t* bar = &sm.full[L % kLFull];
+        const int t = (c0 + ci) * kChunk;
+        if (in == 0)
+          load_tile(sm.slot[s], &c.tk, t, kvh, b, bar);
+        else if (in == 2)
+          load_tile(sm.slot[s], &c.tv, t, kvh, b, bar);
+        else
+          load_tile(sm.slot[s], &c.tq, t, kvh * p.group + h0 + (in == 1 ? 0 : in - 2), b, bar);
+        if (++in == nh + 2) {
+          in = 0;
+          ++ci;
         }
       }
       if (aborted) {
@@ -443,32 +415,26 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
       const uint32_t dhi = (uint32_t)(smem_desc_sw128(0, 16) >> 32);
       const uint32_t row_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.slot[0]), 16);
-      for (int i_run = 0; i_run < sm.n_runs && !aborted; ++i_run) {
-        const LinearRun& run = sm.runs[i_run];
-        const int nh = run.nh, n = run.n;
-        for (int ci = 0; ci < n && !aborted; ++ci, ++cc, L += nh + 2) {
-          uint32_t ks = 0;
-          for (int h = 0; h < nh; ++h, ++t) {
-            // P of the tile before the last has been read: its slot is free
-            if (t > 1 && !dwait_warp(&sm.o_full, t & 1, st, 58, aborted, lim)) break;
-            if (h == 0) {
-              if (!dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, 54, aborted, lim)) break;
-              ks = __shfl_sync(0xffffffffu, (uint32_t)sm.slot_of[L & 15], 0);
-              if (ci == n - 1 && run.last < kChunk) zero_rows(sm.slot[ks], run.last, lane);
-              if (lane == 0) {
-                sm.ks[cc & 1] = ks;
-                mbar_arrive(&sm.chunk_go[cc & 1]);
-              }
-            }
-            const int lq = L + (h == 0 ? 1 : h + 2);
-            if (!dwait_warp(&sm.full[lq % kLFull], (lq / kLFull) & 1, st, 56, aborted, lim)) break;
-            const uint32_t qs = __shfl_sync(0xffffffffu, (uint32_t)sm.slot_of[lq & 15], 0);
-            tc_fence_after();
-            issue_q_k(lead, tm + 128 * (t & 1), row_lo + qs * (kTileBytes >> 4), row_lo + ks * (kTileBytes >> 4), dhi,
-                      idesc_bf16(128, 128, 0, 0));
-            umma_commit_lead(lead, &sm.s_full[t & 1]);
-            if (h == nh - 1) umma_commit_lead(lead, &sm.k_done[cc & 1]);
+      for (int ci = 0, t = 0; ci < nc && !aborted; ++ci) {
+        uint32_t ks = 0;
+        for (int h = 0; h < nh; ++h, ++t) {
+          // P of the tile before the last has been read: its slot is free
+          if (t > 1 && !dwait_warp(&sm.o_full, t & 1, st, 58, aborted, lim)) break;
+          if (h == 0) {
+            const int L = load_k(ci);
+            if (!dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, 54, aborted, lim)) break;
+            ks = __shfl_sync(0xffffffffu, (uint32_t)sm.slot_of[L & 15], 0);
+            if (valid(ci) < kChunk) zero_rows(sm.slot[ks], valid(ci), lane);
+            if (lane == 0) sm.ks[ci & 1] = ks;
           }
+          const int L = load_q(ci, h);
+          if (!dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, 56, aborted, lim)) break;
+          const uint32_t qs = __shfl_sync(0xffffffffu, (uint32_t)sm.slot_of[L & 15], 0);
+          tc_fence_after();
+          issue_q_k(lead, tm + 128 * (t & 1), row_lo + qs * (kTileBytes >> 4), row_lo + ks * (kTileBytes >> 4), dhi,
+                    idesc_bf16(128, 128, 0, 0));
+          umma_commit_lead(lead, &sm.s_full[t & 1]);
+          if (h == nh - 1) umma_commit_lead(lead, &sm.k_done[ci & 1]);
         }
       }
     } else if (warp == kWarpMma) {
@@ -482,39 +448,34 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       const uint32_t row_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.slot[0]), 16);
       const uint32_t col_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.slot[0]), kTileBytes / 2);
       const uint32_t s_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.s), kTileBytes / 2);
-      auto take = [&](int l, int where) -> uint32_t {  // waits for load l; its slot
-        dwait_warp(&sm.full[l % kLFull], (l / kLFull) & 1, st, where, aborted, lim);
-        return __shfl_sync(0xffffffffu, (uint32_t)sm.slot_of[l & 15], 0);
+      auto take = [&](int L, int where) -> uint32_t {  // waits for load L; its slot
+        dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, where, aborted, lim);
+        return __shfl_sync(0xffffffffu, (uint32_t)sm.slot_of[L & 15], 0);
       };
-      for (int i_run = 0; i_run < sm.n_runs && !aborted; ++i_run) {
-        const LinearRun& run = sm.runs[i_run];
-        const int nh = run.nh, n = run.n;
-        for (int ci = 0; ci < n && !aborted; ++ci, ++cc, L += nh + 2) {
-          uint32_t vs = 0;
-          for (int h = 0; h < nh; ++h, ++t) {
-            const bool last = h == nh - 1;
-            const uint32_t qs = take(L + (h == 0 ? 1 : h + 2), 56);
-            if (h == 0) {
-              vs = take(L + 2, 60);
-              if (aborted) break;
-              if (ci == n - 1 && run.last < kChunk) zero_rows(sm.slot[vs], run.last, lane);
-              if (lane == 0) {
-                sm.vs[cc & 1] = vs;
-                mbar_arrive(&sm.chunk_go[cc & 1]);
-              }
-              // the chunk's state is in shared memory, the next scaled in place
-              if (!dwait_warp(&sm.st_ready, cc & 1, st, 57, aborted, lim)) break;
-            }
-            if (t > 0 && !dwait_warp(&sm.o_free, (t - 1) & 1, st, 59, aborted, lim)) break;
-            tc_fence_after();
-            issue_q_s(lead, tm + kColOut, row_lo + qs * kStep, s_lo, dhi, id_b);
-            if (last) umma_commit_lead(lead, &sm.s_free);
-            if (!dwait_warp(&sm.p_full[t & 1], (t >> 1) & 1, st, 61, aborted, lim)) break;
-            tc_fence_after();
-            umma_commit_lead(lead, &sm.empty[qs]);  // Q S is issued, and Q K^T was done before P
-            issue_p_v(lead, tm + kColOut, tm + 128 * (t & 1), col_lo + vs * kStep, dhi, id_b);
-            umma_commit_lead(lead, &sm.o_full);
-            if (last) umma_commit_lead(lead, &sm.v_done[cc & 1]);
+      for (int ci = 0, t = 0; ci < nc && !aborted; ++ci) {
+        uint32_t vs = 0;
+        for (int h = 0; h < nh; ++h, ++t) {
+          const bool last = h == nh - 1;
+          const uint32_t qs = take(load_q(ci, h), 56);
+          if (h == 0) {
+            vs = take(load_v(ci), 60);
+            if (!aborted && valid(ci) < kChunk) zero_rows(sm.slot[vs], valid(ci), lane);
+            // the chunk's state is in shared memory, the next scaled in place
+            if (!dwait_warp(&sm.st_ready, ci & 1, st, 57, aborted, lim)) break;
+          }
+          if (t > 0 && !dwait_warp(&sm.o_free, (t - 1) & 1, st, 59, aborted, lim)) break;
+          tc_fence_after();
+          issue_q_s(lead, tm + kColOut, row_lo + qs * kStep, s_lo, dhi, id_b);
+          if (last) umma_commit_lead(lead, &sm.s_free);
+          if (!dwait_warp(&sm.p_full[t & 1], (t >> 1) & 1, st, 61, aborted, lim)) break;
+          tc_fence_after();
+          umma_commit_lead(lead, &sm.empty[qs]);  // Q S is issued, and Q K^T was done before P
+          issue_p_v(lead, tm + kColOut, tm + 128 * (t & 1), col_lo + vs * kStep, dhi, id_b);
+          umma_commit_lead(lead, &sm.o_full);
+          if (last) umma_commit_lead(lead, &sm.v_done[ci & 1]);
+          if (h == 0 && lane == 0) {
+            sm.vs = vs;
+            mbar_arrive(&sm.chunk_go);  // the chunk's k and v are there
           }
         }
       }
@@ -526,33 +487,26 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       const uint32_t dhi = (uint32_t)(smem_desc_sw128(0, 16) >> 32);
       const uint32_t col_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.slot[0]), kTileBytes / 2);
       const uint32_t part_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.part[0][0]), kSliceBytes / 2);
-      int n_slice = 0, updates = 0;
-      for (int i_run = 0; i_run < sm.n_runs && !aborted; ++i_run) {
-        const LinearRun& run = sm.runs[i_run];
-        const int n = run.n;
-        for (int ci = 0; ci < n; ++ci, ++cc) {
-          if (!dwait_warp(&sm.chunk_go[cc & 1], (cc >> 1) & 1, st, 62, aborted, lim)) break;
-          const uint32_t ks = __shfl_sync(0xffffffffu, sm.ks[cc & 1], 0), vs = __shfl_sync(0xffffffffu, sm.vs[cc & 1], 0);
-          if (!dwait_warp(&sm.st_ready, cc & 1, st, 62, aborted, lim)) break;  // the state is scaled
-          if (ci + 1 < n || run.last_state) {
-            for (int sl = 0; sl < kSlices; ++sl, ++n_slice) {
-              const int buf = n_slice & 1;
-              if (!dwait_warp(&sm.part_full[buf], (n_slice >> 1) & 1, st, 62, aborted, lim)) break;
-              tc_fence_after();
-              issue_slice(lead, tm + kColState, col_lo + ks * (kTileBytes >> 4) + 128 * sl,
-                          part_lo + buf * (3 * kSliceBytes >> 4), dhi, id_ab);
-              umma_commit_lead(lead, &sm.part_free[buf]);
-            }
-            umma_commit_lead(lead, &sm.kv_done);
-            if (!dwait_warp(&sm.kv_done, updates & 1, st, 62, aborted, lim)) break;
-            ++updates;
-          }
-          // (two barriers each: the tiles of the next chunk may be done before this is looked at)
-          if (!dwait_warp(&sm.k_done[cc & 1], (cc >> 1) & 1, st, 62, aborted, lim)) break;
-          if (lane == 0) mbar_arrive(&sm.empty[ks]);
-          if (!dwait_warp(&sm.v_done[cc & 1], (cc >> 1) & 1, st, 62, aborted, lim)) break;
-          if (lane == 0) mbar_arrive(&sm.empty[vs]);
+      int n = 0;
+      for (int ci = 0; ci < (last_state ? nc : nc - 1) && !aborted; ++ci) {
+        // (the state is scaled for this chunk before the chunk's first tile goes)
+        if (!dwait_warp(&sm.chunk_go, ci & 1, st, 62, aborted, lim)) break;
+        const uint32_t ks = __shfl_sync(0xffffffffu, sm.ks[ci & 1], 0), vs = __shfl_sync(0xffffffffu, sm.vs, 0);
+        for (int sl = 0; sl < kSlices; ++sl, ++n) {
+          const int buf = n & 1;
+          if (!dwait_warp(&sm.part_full[buf], (n >> 1) & 1, st, 62, aborted, lim)) break;
+          tc_fence_after();
+          issue_slice(lead, tm + kColState, col_lo + ks * (kTileBytes >> 4) + 128 * sl,
+                      part_lo + buf * (3 * kSliceBytes >> 4), dhi, id_ab);
+          umma_commit_lead(lead, &sm.part_free[buf]);
         }
+        umma_commit_lead(lead, &sm.kv_done);
+        if (!dwait_warp(&sm.kv_done, ci & 1, st, 62, aborted, lim)) break;
+        // (two barriers each: the tiles of the next chunk may be done before this is looked at)
+        if (!dwait_warp(&sm.k_done[ci & 1], (ci >> 1) & 1, st, 62, aborted, lim)) break;
+        if (lane == 0) mbar_arrive(&sm.empty[ks]);
+        if (!dwait_warp(&sm.v_done[ci & 1], (ci >> 1) & 1, st, 62, aborted, lim)) break;
+        if (lane == 0) mbar_arrive(&sm.empty[vs]);
       }
     }
   } else if (warp >= kWarpState) {
@@ -560,100 +514,81 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     // ---------------------------------------------------------------- state
     const int r = threadIdx.x & 127;  // key channel = TMEM lane
     const uint32_t s_addr = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColState;
-    if (c.plan.cut) griddep_wait();  // (the starts of cut runs)
-    int n_slice = 0, updates = 0;
-    for (int i_run = 0; i_run < sm.n_runs && !aborted; ++i_run) {
-      const LinearRun& run = sm.runs[i_run];
-      const size_t row = ((size_t)(run.b * p.n_kv_heads + run.kvh) * kHeadDim + r) * kHeadDim;
-      const int n = run.n;
-      group_bar<2, 128>();
-      sm.pw[r] = decay_pow(p.log2_decay[run.kvh], r);
-      if (r == 0) sm.pw[kChunk] = decay_pow(p.log2_decay[run.kvh], kChunk);
-      group_bar<2, 128>();
-      const float* src = run.c0 > 0 ? c.start + ((size_t)blockIdx.x * kHeadDim + r) * kHeadDim
+    if (c.from_start) griddep_wait();
+    const size_t row = ((size_t)(b * p.n_kv_heads + kvh) * kHeadDim + r) * kHeadDim;
+    const float* src = c.from_start ? c.start + ((size_t)(grun * p.n_kv_heads + kvh) * kHeadDim + r) * kHeadDim
                                     : (p.state_in ? p.state_in + row : nullptr);
 #pragma unroll 1
-      for (int blk = 0; blk < 4; ++blk) {
-        uint32_t w[32];
+    for (int blk = 0; blk < 4; ++blk) {
+      uint32_t w[32];
 #pragma unroll
-        for (int e = 0; e < 32; e += 4) {
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (src) x = *reinterpret_cast<const uint4*>(src + 32 * blk + e);
-          w[e] = x.x;
-          w[e + 1] = x.y;
-          w[e + 2] = x.z;
-          w[e + 3] = x.w;
+      for (int e = 0; e < 32; e += 4) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (src) x = *reinterpret_cast<const uint4*>(src + 32 * blk + e);
+        w[e] = x.x;
+        w[e + 1] = x.y;
+        w[e + 2] = x.z;
+        w[e + 3] = x.w;
+      }
+      tmem_st32(s_addr + 32 * blk, w);
+    }
+    tmem_wait_st();
+    int n_slice = 0;
+    for (int ci = 0; ci < nc && !aborted; ++ci) {
+      const bool update = ci + 1 < nc || last_state;
+      const int nv = valid(ci);
+      if (ci > 0 && !(dwait_warp(&sm.kv_done, (ci - 1) & 1, st, 66, aborted, lim) &&
+                      dwait_warp(&sm.s_free, (ci - 1) & 1, st, 66, aborted, lim)))
+        break;
+      tc_fence_after();
+      const float g = sm.pw[nv];
+#pragma unroll
+      for (int blk = 0; blk < 4; ++blk) {
+        uint32_t x[32];
+        tmem_ld32(s_addr + 32 * blk, x);
+        tmem_wait_ld32(x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          uint32_t w[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            w[u] = pack_bf16(__uint_as_float(x[8 * e + 2 * u]), __uint_as_float(x[8 * e + 2 * u + 1]));
+          const int chunk16 = 4 * (blk & 1) + e;  // 16 bytes of the row's half
+          *reinterpret_cast<uint4*>(sm.s + (blk >> 1) * (kTileBytes / 2) + r * 128 + ((chunk16 ^ (r & 7)) << 4)) =
+              make_uint4(w[0], w[1], w[2], w[3]);
         }
-        tmem_st32(s_addr + 32 * blk, w);
+        if (update) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * g);
+          tmem_st32(s_addr + 32 * blk, x);
+        }
       }
       tmem_wait_st();
-      for (int ci = 0; ci < n; ++ci, ++cc) {
-        const bool update = ci + 1 < n || run.last_state;
-        const int nv = ci + 1 < n ? kChunk : run.last;
-        if (!dwait_warp(&sm.chunk_go[cc & 1], (cc >> 1) & 1, st, 67, aborted, lim)) break;  // V is there
-        const uint8_t* const v = sm.slot[sm.vs[cc & 1]];
-        auto slice = [&](int sl) -> bool {
-          const int buf = n_slice & 1;
-          if (n_slice >= 2 && !dwait_warp(&sm.part_free[buf], ((n_slice >> 1) - 1) & 1, st, 68, aborted, lim)) return false;
-          decay_slice<kSlice, 128>(v, sm.part[buf], sl, nv, r, [&](int j) { return sm.pw[nv - 1 - j]; });
-          fence_proxy_async_smem();
-          warp_arrive(&sm.part_full[buf], lane);
-          ++n_slice;
-          return true;
-        };
-        int sl = 0;
-        if (update)
-          for (; sl < 2; ++sl)
-            if (!slice(sl)) break;
-        if (aborted) break;
-        // the sums of the chunk before are complete, its copy of the state is read
-        if (ci > 0 && !dwait_warp(&sm.kv_done, (updates - 1) & 1, st, 66, aborted, lim)) break;
-        if (cc > 0 && !dwait_warp(&sm.s_free, (cc - 1) & 1, st, 66, aborted, lim)) break;
-        tc_fence_after();
-        const float g = sm.pw[nv];
-#pragma unroll
-        for (int blk = 0; blk < 4; ++blk) {
-          uint32_t x[32];
-          tmem_ld32(s_addr + 32 * blk, x);
-          tmem_wait_ld32(x);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint32_t w[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-              w[u] = pack_bf16(__uint_as_float(x[8 * e + 2 * u]), __uint_as_float(x[8 * e + 2 * u + 1]));
-            const int chunk16 = 4 * (blk & 1) + e;  // 16 bytes of the row's half
-            *reinterpret_cast<uint4*>(sm.s + (blk >> 1) * (kTileBytes / 2) + r * 128 + ((chunk16 ^ (r & 7)) << 4)) =
-                make_uint4(w[0], w[1], w[2], w[3]);
-          }
-          if (update) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * g);
-            tmem_st32(s_addr + 32 * blk, x);
-          }
-        }
-        tmem_wait_st();
-        tc_fence_before();
+      tc_fence_before();
+      fence_proxy_async_smem();
+      warp_arrive(&sm.st_ready, lane);
+      if (!update) break;
+      if (!dwait_warp(&sm.chunk_go, ci & 1, st, 67, aborted, lim)) break;  // V is there
+      const uint8_t* v = sm.slot[sm.vs];
+      for (int sl = 0; sl < kSlices; ++sl, ++n_slice) {
+        const int buf = n_slice & 1;
+        if (n_slice >= 2 && !dwait_warp(&sm.part_free[buf], ((n_slice >> 1) - 1) & 1, st, 68, aborted, lim)) break;
+        decay_slice<kSlice, 128>(v, sm.part[buf], sl, nv, r, [&](int j) { return sm.pw[nv - 1 - j]; });
         fence_proxy_async_smem();
-        warp_arrive(&sm.st_ready, lane);
-        if (!update) continue;
-        for (; sl < kSlices; ++sl)
-          if (!slice(sl)) break;
-        if (aborted) break;
-        ++updates;
+        warp_arrive(&sm.part_full[buf], lane);
       }
-      if (run.last_state && dwait_warp(&sm.kv_done, (updates - 1) & 1, st, 66, aborted, lim)) {
-        tc_fence_after();
-        float* dst = p.state_out + row;
+    }
+    if (last_state && !aborted && (nc == 0 || dwait_warp(&sm.kv_done, (nc - 1) & 1, st, 66, aborted, lim))) {
+      tc_fence_after();
+      float* dst = p.state_out + row;
 #pragma unroll 1
-        for (int blk = 0; blk < 4; ++blk) {
-          uint32_t x[32];
-          tmem_ld32(s_addr + 32 * blk, x);
-          tmem_wait_ld32(x);
+      for (int blk = 0; blk < 4; ++blk) {
+        uint32_t x[32];
+        tmem_ld32(s_addr + 32 * blk, x);
+        tmem_wait_ld32(x);
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<uint4*>(dst + 32 * blk + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-        }
+        for (int e = 0; e < 32; e += 4)
+          *reinterpret_cast<uint4*>(dst + 32 * blk + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
       }
     }
     tc_fence_before();
@@ -663,57 +598,51 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     const int r = threadIdx.x & 127;  // TMEM lane: token of the tile
     const int half = (warp - kWarpEpilogue) >> 2;  // of the channels
     const uint32_t o_addr = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColOut + 64 * half;
+    const float f = fmaxf(sm.pw[r + 1], strong ? kLeastScale : 0.f) * p.scale;
+    const uint64_t ff = f2_pack(f, f);
     uint4* const turn = sm.turn[warp - kWarpEpilogue];
-    for (int i_run = 0; i_run < sm.n_runs && !aborted; ++i_run) {
-      const LinearRun& run = sm.runs[i_run];
-      const float2 l2 = p.log2_decay[run.kvh];
-      const float f = fmaxf(decay_pow(l2, r + 1), strong_decay(l2) ? kLeastScale : 0.f) * p.scale;
-      const uint64_t ff = f2_pack(f, f);
-      const int nh = run.nh, n = run.n;
-      for (int ci = 0; ci < n && !aborted; ++ci) {
-        const int nv = ci + 1 < n ? kChunk : run.last;
+    for (int ci = 0, t = 0; ci < nc && !aborted; ++ci) {
+      const int nv = valid(ci);
+      for (int h = 0; h < nh; ++h, ++t) {
+        if (!dwait_warp(&sm.o_full, t & 1, st, 65, aborted, lim)) break;
+        tc_fence_after();
+        // o leaves tensor memory before anything else (the next tile's products wait for it)
+        uint32_t w[2][16];
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+          uint32_t y[32];
+          tmem_ld32(o_addr + 32 * blk, y);
+          tmem_wait_ld32(y);
+          if (blk == 1) {
+            tc_fence_before();
+            warp_arrive(&sm.o_free, lane);
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            float y0, y1;
+            f2_unpack(f2_mul(f2_pack(__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])), ff), y0, y1);
+            w[blk][e] = pack_bf16(y0, y1);
+          }
+        }
+        if (r >= nv) {  // tokens behind the sequence's end: zeros
+#pragma unroll
+          for (int e = 0; e < 32; ++e) w[e >> 4][e & 15] = 0u;
+        }
         // lane: row 16 i + lane / 2 of the warp's 32, 16 bytes lane mod 2 of each 32
-        const int tok = (run.c0 + ci) * kChunk + 32 * (warp & 3) + (lane >> 1);
-        __nv_bfloat16* o = p.out.at(run.b, run.head0, tok) + 64 * half + 8 * (lane & 1);
-        for (int h = 0; h < nh; ++h, ++t, o += p.out.sh) {
-          if (!dwait_warp(&sm.o_full, t & 1, st, 65, aborted, lim)) break;
-          tc_fence_after();
-          // o leaves tensor memory before anything else (the next tile's products wait for it)
-          uint32_t w[2][16];
+        const int tok = (c0 + ci) * kChunk + 32 * (warp & 3) + (lane >> 1);
+        __nv_bfloat16* const o = p.out.at(b, kvh * p.group + h0 + h, tok) + 64 * half + 8 * (lane & 1);
 #pragma unroll
-          for (int blk = 0; blk < 2; ++blk) {
-            uint32_t y[32];
-            tmem_ld32(o_addr + 32 * blk, y);
-            tmem_wait_ld32(y);
-            if (blk == 1) {
-              tc_fence_before();
-              warp_arrive(&sm.o_free, lane);
-            }
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t* x = &w[q >> 1][8 * (q & 1)];
+          __syncwarp();
+          turn[2 * lane + ((lane >> 2) & 1)] = make_uint4(x[0], x[1], x[2], x[3]);
+          turn[2 * lane + (((lane >> 2) & 1) ^ 1)] = make_uint4(x[4], x[5], x[6], x[7]);
+          __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              float y0, y1;
-              f2_unpack(f2_mul(f2_pack(__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])), ff), y0, y1);
-              w[blk][e] = pack_bf16(y0, y1);
-            }
-          }
-          if (r >= nv) {  // tokens behind the sequence's end: zeros
-#pragma unroll
-            for (int e = 0; e < 32; ++e) w[e >> 4][e & 15] = 0u;
-          }
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const uint32_t* x = &w[q >> 1][8 * (q & 1)];
-            __syncwarp();
-            turn[2 * lane + ((lane >> 2) & 1)] = make_uint4(x[0], x[1], x[2], x[3]);
-            turn[2 * lane + (((lane >> 2) & 1) ^ 1)] = make_uint4(x[4], x[5], x[6], x[7]);
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int row = 16 * i + (lane >> 1);
-              if (tok + 16 * i < p.n_tok)
-                *reinterpret_cast<uint4*>(o + 16 * i * p.out.st + 16 * q) =
-                    turn[2 * row + ((lane & 1) ^ ((row >> 2) & 1))];
-            }
+          for (int i = 0; i < 2; ++i) {
+            const int row = 16 * i + (lane >> 1);
+            if (tok + 16 * i < p.n_tok)
+              *reinterpret_cast<uint4*>(o + 16 * i * p.out.st + 16 * q) = turn[2 * row + ((lane & 1) ^ ((row >> 2) & 1))];
           }
         }
       }
@@ -726,69 +655,60 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     const int r = threadIdx.x & 127;  // TMEM lane: token of the tile
     const int wr = 32 * (warp & 3);   // the warp's first row
     const uint32_t slot0 = tmem + ((uint32_t)wr << 16) + 64 * x;
-    for (int i_run = 0; i_run < sm.n_runs && !aborted; ++i_run) {
-      const LinearRun& run = sm.runs[i_run];
-      const float2 l2 = p.log2_decay[run.kvh];
-      const bool strong = strong_decay(l2);
-      // (strong decay only) 1 / a_i
-      const float inv_a = strong ? 1.f / fmaxf(decay_pow(l2, r + 1), kLeastScale) : 0.f;
-      group_bar<1, 256>();
-      if (x == 0) sm.wt[r] = decay_pow(l2, strong ? r : -1 - r);
-      group_bar<1, 256>();
-      const int last_tile = t + run.n * run.nh;
-      for (; t < last_tile; ++t) {
-        if (!dwait_warp(&sm.s_full[t & 1], (t >> 1) & 1, st, 64, aborted, lim)) break;
-        tc_fence_after();
-        const uint32_t slot = slot0 + 128 * (t & 1);
-        // 16 keys at a time, the next ones' loads in flight (P overwrites only
-        // columns that are read); keys behind the warp's last row need no load
-        uint32_t sr[2][16];
-        if (64 * x < wr + 32) tmem_ld16(slot, sr[0]);
+    // (strong decay only) 1 / a_i
+    const float inv_a = strong ? 1.f / fmaxf(sm.pw[r + 1], kLeastScale) : 0.f;
+    for (int t = 0; t < tiles; ++t) {
+      if (!dwait_warp(&sm.s_full[t & 1], (t >> 1) & 1, st, 64, aborted, lim)) break;
+      tc_fence_after();
+      const uint32_t slot = slot0 + 128 * (t & 1);
+      // 16 keys at a time, the next ones' loads in flight (P overwrites only
+      // columns that are read); keys behind the warp's last row need no load
+      uint32_t sr[2][16];
+      if (64 * x < wr + 32) tmem_ld16(slot, sr[0]);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int j0 = 64 * x + 16 * q;
-          uint32_t(&y)[16] = sr[q & 1];
-          tmem_wait_ld16(y);
-          if (q < 3 && j0 + 16 < wr + 32) tmem_ld16(slot + 16 * (q + 1), sr[(q + 1) & 1]);
-          uint32_t pk[8];
-          if (j0 >= wr + 32) {
+      for (int q = 0; q < 4; ++q) {
+        const int j0 = 64 * x + 16 * q;
+        uint32_t(&y)[16] = sr[q & 1];
+        tmem_wait_ld16(y);
+        if (q < 3 && j0 + 16 < wr + 32) tmem_ld16(slot + 16 * (q + 1), sr[(q + 1) & 1]);
+        uint32_t pk[8];
+        if (j0 >= wr + 32) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pk[e] = 0u;
-          } else if (!strong) {
-            const ulonglong2* cj = reinterpret_cast<const ulonglong2*>(sm.wt + j0);  // pairs of fp32
+          for (int e = 0; e < 8; ++e) pk[e] = 0u;
+        } else if (!strong) {
+          const ulonglong2* cj = reinterpret_cast<const ulonglong2*>(sm.cj + j0);  // pairs of fp32
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const ulonglong2 w = cj[e];
-              float z[4];
-              f2_unpack(f2_mul(f2_pack(__uint_as_float(y[4 * e]), __uint_as_float(y[4 * e + 1])), w.x), z[0], z[1]);
-              f2_unpack(f2_mul(f2_pack(__uint_as_float(y[4 * e + 2]), __uint_as_float(y[4 * e + 3])), w.y), z[2], z[3]);
-              pk[2 * e] = pack_bf16(z[0], z[1]);
-              pk[2 * e + 1] = pack_bf16(z[2], z[3]);
-            }
-            if (j0 >= wr) {  // keys up to the token (later ones may hold anything)
-              const int last = r - j0;
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                pk[e] &= (2 * e <= last ? 0xffffu : 0u) | (2 * e + 1 <= last ? 0xffff0000u : 0u);
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float z[2];
-#pragma unroll
-              for (int u = 0; u < 2; ++u) {
-                const int back = r - j0 - 2 * e - u;  // tokens since the key
-                z[u] = back >= 0 ? __uint_as_float(y[2 * e + u]) * (sm.wt[max(back, 0)] * inv_a) : 0.f;
-              }
-              pk[e] = pack_bf16(z[0], z[1]);
-            }
+          for (int e = 0; e < 4; ++e) {
+            const ulonglong2 w = cj[e];
+            float z[4];
+            f2_unpack(f2_mul(f2_pack(__uint_as_float(y[4 * e]), __uint_as_float(y[4 * e + 1])), w.x), z[0], z[1]);
+            f2_unpack(f2_mul(f2_pack(__uint_as_float(y[4 * e + 2]), __uint_as_float(y[4 * e + 3])), w.y), z[2], z[3]);
+            pk[2 * e] = pack_bf16(z[0], z[1]);
+            pk[2 * e + 1] = pack_bf16(z[2], z[3]);
           }
-          tmem_st8(slot + 8 * q, pk);
+          if (j0 >= wr) {  // keys up to the token (later ones may hold anything)
+            const int last = r - j0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              pk[e] &= (2 * e <= last ? 0xffffu : 0u) | (2 * e + 1 <= last ? 0xffff0000u : 0u);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float z[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int back = r - j0 - 2 * e - u;  // tokens since the key
+              z[u] = back >= 0 ? __uint_as_float(y[2 * e + u]) * (sm.pw[max(back, 0)] * inv_a) : 0.f;
+            }
+            pk[e] = pack_bf16(z[0], z[1]);
+          }
         }
-        tmem_wait_st();
-        tc_fence_before();
-        warp_arrive(&sm.p_full[t & 1], lane);
+        tmem_st8(slot + 8 * q, pk);
       }
+      tmem_wait_st();
+      tc_fence_before();
+      warp_arrive(&sm.p_full[t & 1], lane);
     }
     tc_fence_before();
   }
@@ -800,8 +720,8 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
   }
 }
 
-// What a CTA's cut run adds up: sum_j k_j (gamma^{e-1-j} v_j)^T over its tokens,
-// e its end (only a CTA's last run can end inside a sequence). The weights fall towards the run's
+// A run's own sum: sum_j k_j (gamma^{e-1-j} v_j)^T over its tokens, e its end
+// (a sequence's last run needs none). The weights fall towards the run's
 // start, so the chunks accumulate in tensor memory without a rescale. Four
 // groups of four warps form the decayed values, a quarter chunk each.
 constexpr int kLocalRing = 2;  // chunks in flight
@@ -814,7 +734,6 @@ struct LinearLocalSmem {
   uint64_t k_full[kLocalRing], v_full[kLocalRing], empty[kLocalRing];
   uint64_t part_full[4], part_free[4], done;
   uint32_t tmem_base;
-  LinearRun run;
 };
 static_assert(sizeof(LinearLocalSmem) + 1024 <= 232448, "linear attention shared memory");
 
@@ -825,13 +744,11 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
   griddep_launch_dependents();
   const LinearParams& p = c.p;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-  const int x_end = range_begin(c.plan, blockIdx.x + 1);
-  if (threadIdx.x == 0) find_runs(c, x_end - 1, x_end, &sm.run);
-  __syncthreads();
-  // its chunks up to the last of the CTA's; every chunk before a sequence's last is whole
-  const int b = sm.run.b, kvh = sm.run.kvh, c1 = sm.run.c0 + 1;
-  const int nc = min(c1, x_end - range_begin(c.plan, blockIdx.x)), c0 = c1 - nc;
-  if (c1 == (p.lengths[b] + kChunk - 1) / kChunk) return;
+  const int kvh = blockIdx.x % p.n_kv_heads, grun = blockIdx.x / p.n_kv_heads;
+  const int b = sequence_of(c.plan, p.batch, grun);
+  if (grun + 1 == c.plan.run_begin[b + 1]) return;
+  const int c0 = (grun - c.plan.run_begin[b]) * c.plan.chunks_per_run;
+  const int nc = c.plan.chunks_per_run;  // every chunk of a run before the last is whole
   if (threadIdx.x == 0) {
     for (int s = 0; s < kLocalRing; ++s) {
       mbar_init(&sm.k_full[s], 1);
@@ -914,7 +831,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
     }
     if (warp < 4 && dwait_warp(&sm.done, 0, st, 77, aborted, lim)) {
       tc_fence_after();
-      float* dst = c.local + ((size_t)blockIdx.x * kHeadDim + threadIdx.x) * kHeadDim;
+      float* dst = c.local + ((size_t)(grun * p.n_kv_heads + kvh) * kHeadDim + threadIdx.x) * kHeadDim;
 #pragma unroll 1
       for (int blk = 0; blk < 4; ++blk) {
         uint32_t kv[32];
@@ -935,58 +852,50 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
   }
 }
 
-// Where CTAs start inside a sequence, from the sums of the CTAs before, four
-// elements per thread: S <- gamma^{tokens of the run} S + local.
+// start of every run from the sums of the runs before it, four elements per
+// thread: S <- gamma^{tokens of the run} S + local. (A sequence of one run
+// starts from its state_in; this copies it where state_out is the same array
+// and several CTAs read it.)
 constexpr int kJoinThreads = 128;
 __global__ void __launch_bounds__(kJoinThreads) linear_join_kernel(const __grid_constant__ LinearChunkParams c) {
   griddep_launch_dependents();
+  griddep_wait();
   const LinearParams& p = c.p;
   constexpr int kBlocks = kHeadDim * kHeadDim / 4 / kJoinThreads;
-  const int parts = c.plan.head_parts, pair = blockIdx.x / kBlocks;  // (b, kvh, part)
-  const int b = pair / (p.n_kv_heads * parts), kvh = pair / parts % p.n_kv_heads;
-  const int n = (p.lengths[b] + kChunk - 1) / kChunk;
-  const int x0 = c.plan.begin[b] + pair % (p.n_kv_heads * parts) * n;
-  const int first = n == 0 ? 0 : range_of(c.plan, x0), last = n == 0 ? 0 : range_of(c.plan, x0 + n - 1);
-  if (first == last) return;
+  const int bh = blockIdx.x / kBlocks, b = bh / p.n_kv_heads, kvh = bh % p.n_kv_heads;
+  const int first = c.plan.run_begin[b], runs = c.plan.run_begin[b + 1] - first;
   const size_t in = 4 * ((blockIdx.x % kBlocks) * kJoinThreads + threadIdx.x);
-  constexpr size_t kState = kHeadDim * kHeadDim;
-  const float2 l2 = p.log2_decay[kvh];
+  const size_t step = (size_t)p.n_kv_heads * kHeadDim * kHeadDim;
+  const size_t at = (size_t)first * step + (size_t)kvh * kHeadDim * kHeadDim + in;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (p.state_in) s = *reinterpret_cast<const float4*>(p.state_in + (size_t)(b * p.n_kv_heads + kvh) * kState + in);
-  griddep_wait();
+  if (p.state_in) s = *reinterpret_cast<const float4*>(p.state_in + (size_t)bh * kHeadDim * kHeadDim + in);
+  const float g = decay_pow(p.log2_decay[kvh], c.plan.chunks_per_run * kChunk);
   constexpr int kAhead = 8;  // sums in flight
-  for (int i0 = first; i0 < last; i0 += kAhead) {
+  for (int run0 = 0; run0 < runs; run0 += kAhead) {
     float4 l[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      if (i0 + u < last) l[u] = *reinterpret_cast<const float4*>(c.local + (i0 + u) * kState + in);
+      if (run0 + u + 1 < runs) l[u] = *reinterpret_cast<const float4*>(c.local + (run0 + u) * step + at);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int i = i0 + u;
-      if (i >= last) break;
-      const float g = decay_pow(l2, (range_begin(c.plan, i + 1) - max(range_begin(c.plan, i), x0)) * kChunk);
-      s = make_float4(fmaf(s.x, g, l[u].x), fmaf(s.y, g, l[u].y), fmaf(s.z, g, l[u].z), fmaf(s.w, g, l[u].w));
-      *reinterpret_cast<float4*>(c.start + (i + 1) * kState + in) = s;
+      if (run0 + u >= runs) break;
+      *reinterpret_cast<float4*>(c.start + (run0 + u) * step + at) = s;
+      if (run0 + u + 1 < runs)
+        s = make_float4(fmaf(s.x, g, l[u].x), fmaf(s.y, g, l[u].y), fmaf(s.z, g, l[u].z), fmaf(s.w, g, l[u].w));
     }
   }
 }
 
-// What no chunk covers: zeros for the tokens behind a sequence's last chunk with
-// a valid one (the chunk kernel writes those inside it), and the state of a
-// sequence without a token. One CTA per (sequence, query head, kZeroRows tokens).
+// Zeros for the tokens behind a sequence's last chunk with a valid one (the
+// chunk kernel writes those inside it). One CTA per (sequence, query head,
+// kZeroRows tokens).
 constexpr int kZeroRows = 512;
-__global__ void __launch_bounds__(256) linear_rest_kernel(const __grid_constant__ LinearParams p) {
+__global__ void __launch_bounds__(256) linear_zero_kernel(const __grid_constant__ LinearParams p) {
   const int b = blockIdx.z, h = blockIdx.y;
   const int begin = max((int)blockIdx.x * kZeroRows, (p.lengths[b] + kChunk - 1) / kChunk * kChunk);
   const int end = min(p.n_tok, ((int)blockIdx.x + 1) * kZeroRows);
   for (int64_t i = 16ll * begin + threadIdx.x; i < 16ll * end; i += 256)
     *reinterpret_cast<uint4*>(p.out.at(b, h, (int)(i >> 4)) + 8 * (int)(i & 15)) = make_uint4(0, 0, 0, 0);
-  if (p.lengths[b] == 0 && blockIdx.x == 0 && h % p.group == 0) {
-    const size_t at = (size_t)(b * p.n_kv_heads + h / p.group) * kHeadDim * kHeadDim;
-    for (int i = 4 * threadIdx.x; i < kHeadDim * kHeadDim; i += 4 * 256)
-      *reinterpret_cast<float4*>(p.state_out + at + i) =
-          p.state_in ? *reinterpret_cast<const float4*>(p.state_in + at + i) : make_float4(0.f, 0.f, 0.f, 0.f);
-  }
 }
 
 void launch_linear_chunks(const LinearChunkParams& c, cudaStream_t st) {
@@ -997,23 +906,22 @@ void launch_linear_chunks(const LinearChunkParams& c, cudaStream_t st) {
     cudaFuncSetAttribute(linear_local_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLocalSmem);
   });
   const LinearParams& p = c.p;
-  bool rest = false;
-  for (int b = 0; b < p.batch; ++b)
-    rest |= p.lengths[b] == 0 || (p.lengths[b] + kChunk - 1) / kChunk * kChunk < p.n_tok;
-  if (rest) {
-    linear_rest_kernel<<<dim3((p.n_tok + kZeroRows - 1) / kZeroRows, p.n_q_heads, p.batch), 256, 0, st>>>(p);
+  bool behind = false;
+  for (int b = 0; b < p.batch; ++b) behind |= (p.lengths[b] + kChunk - 1) / kChunk * kChunk < p.n_tok;
+  if (behind) {
+    linear_zero_kernel<<<dim3((p.n_tok + kZeroRows - 1) / kZeroRows, p.n_q_heads, p.batch), 256, 0, st>>>(p);
     count_launch();
   }
-  if (c.plan.total == 0) return;
-  if (c.plan.cut) {
-    linear_local_kernel<<<c.plan.ctas, kLThreads, kLocalSmem, st>>>(c);
-    count_launch();
-    launch_maybe_pdl(true, linear_join_kernel,
-                     p.batch * p.n_kv_heads * c.plan.head_parts * (kHeadDim * kHeadDim / 4 / kJoinThreads), kJoinThreads, 0,
-                     st, c);
+  if (c.plan.several) {
+    linear_local_kernel<<<c.plan.runs * p.n_kv_heads, kLThreads, kLocalSmem, st>>>(c);
     count_launch();
   }
-  launch_maybe_pdl(c.plan.cut, linear_chunk_kernel, c.plan.ctas, kLThreads, kSmem, st, c);
+  if (c.from_start) {
+    launch_maybe_pdl(c.plan.several, linear_join_kernel, p.batch * p.n_kv_heads * (kHeadDim * kHeadDim / 4 / kJoinThreads),
+                     kJoinThreads, 0, st, c);
+    count_launch();
+  }
+  launch_maybe_pdl(c.from_start, linear_chunk_kernel, c.plan.runs * p.n_kv_heads * c.plan.head_parts, kLThreads, kSmem, st, c);
   count_launch();
 }
 
