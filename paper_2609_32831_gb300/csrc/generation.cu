@@ -80,10 +80,10 @@ static bool linear_steps(int n_q_heads, int n_kv_heads, int n_tok) {
 // How prompts are cut: over query heads (each part forms the state on its own)
 // and over tokens (a pass over k and v before, for the states that the runs
 // start from). Costs in clocks of a CTA, from measured launches: a tile of one
-// head and chunk, a chunk's update, a CTA's start and end; the same for the
-// pass before.
+// head and chunk, a chunk's update of the state (beside its tiles, a chain that
+// takes kChain), a CTA's start and end; the same for the pass before.
 static LinearPlan plan_linear(int batch, int n_q_heads, int n_kv_heads, const int32_t* lengths) {
-  constexpr double kTile = 3400, kUpdate = 2500, kCta = 9000, kSumChunk = 3500, kSumCta = 12000;
+  constexpr double kTile = 3400, kUpdate = 2500, kChain = 10500, kCta = 9000, kSumChunk = 4000, kSumCta = 14000;
   const int g = n_q_heads / n_kv_heads, sms = num_sms();
   int64_t chunks = 0;
   int longest = 1;
@@ -98,6 +98,7 @@ static LinearPlan plan_linear(int batch, int n_q_heads, int n_kv_heads, const in
   for (int per = 1; per <= g; ++per) {
     const int parts = (g + per - 1) / per;
     if (per > 1 && parts == (g + per - 2) / (per - 1)) continue;  // as many parts as before, less even
+    const double chunk = std::max(kChain, kUpdate + per * kTile);
     int last_cpr = 0;
     for (int rounds = 0; rounds <= 4; ++rounds) {
       // whole sequences, or runs that fill so many rounds of CTAs
@@ -122,13 +123,14 @@ static LinearPlan plan_linear(int batch, int n_q_heads, int n_kv_heads, const in
         const int nb = chunks_of(lengths[b]), r = std::max(1, (nb + cpr - 1) / cpr);
         n += r;
         several |= r > 1;
-        total += (double)n_kv_heads * parts * (r * kCta + nb * (kUpdate + per * kTile));
-        most = std::max(most, kCta + std::min(cpr, nb) * (kUpdate + per * kTile));
+        total += (double)n_kv_heads * parts * (r * kCta + nb * chunk);
+        most = std::max(most, kCta + std::min(cpr, nb) * chunk);
       }
       if (n * n_kv_heads * parts > INT32_MAX) continue;
       if (several && n * n_kv_heads > kMaxLinearSums) continue;
       const double ctas = (double)n * n_kv_heads * parts;
-      double cost = std::min(std::ceil(ctas / sms) * most, (total - most) / sms + most);
+      // (unequal ones fill in behind each other)
+      double cost = std::min(std::ceil(ctas / sms) * most, std::max(1.15 * total / sms, most));
       if (several) {
         const double sums = (double)(n - batch) * n_kv_heads;
         cost += std::ceil(sums / sms) * (kSumCta + cpr * kSumChunk);

@@ -111,7 +111,7 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 //
 // Roundings to bf16: P and the copy of S that Q multiplies (each about as
 // large as the output's own rounding), and none on the state's path: the
-// decayed values enter as three bf16 parts (v gamma^n to 2^-25; two parts left
+// decayed values enter as three bf16 parts (all 24 bits of v gamma^n; two parts left
 // the state 2.7e-6 off), the update accumulates in fp32.
 //
 // a_i and gamma^{-(j+1)} take the row's common factor out of both products.
@@ -263,12 +263,14 @@ __device__ __forceinline__ void decay_slice(const uint8_t* v, uint8_t (*parts)[R
       const uint32_t bits[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
+        // eight bits of the fp32 value per part, by cutting: nothing is left
         float a = bf16_lo(bits[e]) * w, b = bf16_hi(bits[e]) * w;
 #pragma unroll
         for (int u = 0; u < 3; ++u) {
-          part[u][e] = pack_bf16(a, b);
-          a -= bf16_lo(part[u][e]);
-          b -= bf16_hi(part[u][e]);
+          const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+          part[u][e] = __byte_perm(x, y, 0x7632);
+          a -= __uint_as_float(x & 0xffff0000u);
+          b -= __uint_as_float(y & 0xffff0000u);
         }
       }
     }
