@@ -8,12 +8,16 @@
 // higher logit, lower token (a total order, so the result does not depend on
 // how the work is split). Within a beam the score grows with the logit, so a
 // row's best n logits are all that can be chosen.
-// 1. beam_tile_kernel: one CTA per tile of kBeamTile logits of a row, which
-//    stay in registers: their maximum, the sum of exp(x - max) and the tile's
-//    best n logits. The logits are read once.
+// 1. beam_tile_kernel: one CTA per tile of a row, 2048 16-byte vectors at a
+//    time in registers: their maximum, the sum of exp(x - max) and the tile's
+//    best n logits. The logits are read once, the next vectors while these are
+//    worked on.
+//    Bound by HBM where rows are many: an SM's share is 11 two-byte logits per
+//    cycle, the exponentials alone take 16 of the SM's per cycle at most.
 // 2. beam_merge_kernel: one CTA per request joins its tiles.
 #include "common.cuh"
 #include "internal.h"
+#include "tcgen05.cuh"
 
 namespace uc {
 
@@ -21,15 +25,17 @@ namespace {
 
 constexpr int kSelThreads = 256;
 constexpr int kSelWarps = kSelThreads / 32;
-constexpr int kPer = kBeamTile / kSelThreads;  // logits per thread
-constexpr int kSelGroups = 64;                 // thread groups whose maxima bound the n-th best
-constexpr int kGroupLanes = kSelThreads / kSelGroups;
-static_assert(kSelGroups >= UC_MAX_BEAM_OUT, "n groups have to exist");
-// The n-th largest of the groups' maxima is at most the tile's n-th largest
-// logit, and only n groups reach it: no more candidates than their logits.
-constexpr int kSelCap = UC_MAX_BEAM_OUT * kGroupLanes * kPer;
+constexpr int kVecs = 8;  // 16-byte vectors per thread and round
+constexpr int kRound = kSelThreads * kVecs;
+constexpr int kSelGroups = 64;  // groups of four threads
+constexpr int kSelMany = 512;  // candidates from which they are cut to the best n after a round
+// Candidates: the n-th largest of a round's thread maxima is at most its n-th
+// largest logit, and fewer than n threads hold larger ones; n equal ones; and
+// what the rounds before left.
+constexpr int kSelCap = kSelMany + UC_MAX_BEAM_OUT * kVecs * 8;
 constexpr float kNegInf = -INFINITY;
 constexpr float kLog2e = 1.4426950408889634f;
+static_assert(kSelGroups >= UC_MAX_BEAM_OUT, "n groups have to exist");
 
 // Order-preserving map of floats (no NaN) to unsigned integers; -0 and +0 map
 // to one value.
@@ -37,39 +43,88 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
+__device__ __forceinline__ float unordered(uint32_t k) {
+  return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
+}
 // (logit, position) as one key: the higher logit, then the lower position.
 __device__ __forceinline__ uint64_t logit_key(float x, uint32_t pos) {
   return ((uint64_t)ordered(x) << 32) | (0xffffffffu - pos);
 }
 
+// A 16-byte vector of logits by type: its elements as fp32, its largest element
+// (NaN if there is one).
 template <typename T>
-__device__ __forceinline__ float to_float(T x);
+struct Logits;
 template <>
-__device__ __forceinline__ float to_float<float>(float x) { return x; }
+struct Logits<float> {
+  static constexpr int kE = 4;
+  static __device__ __forceinline__ float get(const uint4& v, int e) {
+    return __uint_as_float(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w);
+  }
+  static __device__ __forceinline__ uint32_t raw(float x) { return __float_as_uint(x); }
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(get(v, 0)), "f"(get(v, 1)));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(get(v, 2)));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(get(v, 3)));
+    return m;
+  }
+};
+template <typename H, typename H2>
+struct Logits16 {
+  static constexpr int kE = 8;
+  static __device__ __forceinline__ H2 pair(uint32_t w) { return *reinterpret_cast<H2*>(&w); }
+  static __device__ __forceinline__ H2 largest2(const uint4& v) {
+    return __hmax2_nan(__hmax2_nan(pair(v.x), pair(v.y)), __hmax2_nan(pair(v.z), pair(v.w)));
+  }
+};
 template <>
-__device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+struct Logits<__nv_bfloat16> : Logits16<__nv_bfloat16, __nv_bfloat162> {
+  static __device__ __forceinline__ float get(const uint4& v, int e) {
+    const uint32_t w = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
+    return e & 1 ? bf16_hi(w) : bf16_lo(w);
+  }
+  static __device__ __forceinline__ uint32_t raw(float x) { return __float_as_uint(x) >> 16; }  // (exact)
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    const __nv_bfloat162 m = largest2(v);
+    return __bfloat162float(__hmax_nan(m.x, m.y));
+  }
+};
 template <>
-__device__ __forceinline__ float to_float<__half>(__half x) { return __half2float(x); }
-// A logit as the selection sees it: NaN and +inf (reported as UC_ERR_RANGE)
-// count as -inf, so that every bound below holds for them too.
-template <typename T>
-__device__ __forceinline__ float logit(T x) {
-  const float f = to_float(x);
-  return f < INFINITY ? f : kNegInf;
+struct Logits<__half> : Logits16<__half, __half2> {
+  static __device__ __forceinline__ float get(const uint4& v, int e) {
+    const __half2 h = pair(e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w);
+    return e & 1 ? __high2float(h) : __low2float(h);
+  }
+  static __device__ __forceinline__ uint32_t raw(float x) { return __half_as_ushort(__float2half_rn(x)); }
+  static __device__ __forceinline__ float largest(const uint4& v) {
+    const __half2 m = largest2(v);
+    return __half2float(__hmax_nan(m.x, m.y));
+  }
+};
+// A vector from its elements (rows' ends, values that are no logits).
+template <typename T, typename F>
+__device__ __forceinline__ uint4 make_vector(const F& element) {
+  constexpr int kE = Logits<T>::kE;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (kE == 4)
+      w[i] = Logits<T>::raw(element(i));
+    else
+      w[i] = Logits<T>::raw(element(2 * i)) | (Logits<T>::raw(element(2 * i + 1)) << 16);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
-
-__device__ __forceinline__ uint64_t shfl_xor_u64(uint64_t x, int m) {
-  const uint32_t lo = __shfl_xor_sync(0xffffffffu, (uint32_t)x, m);
-  const uint32_t hi = __shfl_xor_sync(0xffffffffu, (uint32_t)(x >> 32), m);
-  return ((uint64_t)hi << 32) | lo;
-}
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 
 // A finished beam goes on with the end token alone, at no cost: as if its
-// logits were 0 there and -inf elsewhere. Writes the tile's part of that.
-__device__ void finished_tile(const BeamParams& p, int row, int tile, int len) {
-  const int lo = tile * kBeamTile;
+// logits were 0 there and -inf elsewhere. Writes the part of that of tokens lo
+// .. lo + len - 1.
+__device__ void finished_tile(const BeamParams& p, size_t at, int lo, int len) {
   const bool here = p.eos >= lo && p.eos < lo + len;
-  const size_t at = (size_t)row * p.tiles + tile;
   if (threadIdx.x == 0) p.part_ms[at] = here ? make_float2(0.f, 1.f) : make_float2(kNegInf, 0.f);
   const int i = threadIdx.x;
   if (i < p.n) {
@@ -89,105 +144,257 @@ __device__ void finished_tile(const BeamParams& p, int row, int tile, int len) {
   }
 }
 
+// The k-th largest (from 1) of COUNT values, ties by place; one value per
+// thread below COUNT.
+template <int COUNT>
+__device__ __forceinline__ void kth_largest(const uint32_t* vals, int k, float* out) {
+  if (threadIdx.x < COUNT) {
+    const uint32_t mine = vals[threadIdx.x];
+    int rank = 0;
+    for (int g = 0; g < COUNT; g += 4) {
+      const uint4 o = *reinterpret_cast<const uint4*>(vals + g);
+      rank += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+      if (g <= (int)threadIdx.x) {
+        rank += (o.x == mine && g < (int)threadIdx.x) + (o.y == mine && g + 1 < (int)threadIdx.x) +
+                (o.z == mine && g + 2 < (int)threadIdx.x) + (o.w == mine && g + 3 < (int)threadIdx.x);
+      }
+    }
+    if (rank == k - 1) *out = unordered(mine);
+  }
+}
+
+// The best n of c candidates, in order, to out(rank, key); every thread calls it.
+template <typename F>
+__device__ __forceinline__ void best_of(const uint64_t* keys, int c, int n, F&& out) {
+  for (int i = threadIdx.x; i < c; i += kSelThreads) {
+    const uint64_t mine = keys[i];
+    int rank = 0;
+    for (int j = 0; j < c && rank < n; ++j) rank += keys[j] > mine;
+    if (rank < n) out(rank, mine);
+  }
+}
+
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads) beam_tile_kernel(const __grid_constant__ BeamParams p) {
-  __shared__ uint64_t s_group[kSelGroups];
-  __shared__ float s_red[kSelWarps];
-  __shared__ uint16_t s_cand[kSelCap];
-  __shared__ int s_count, s_bad;
-  __shared__ uint64_t s_tau;
+__global__ void __launch_bounds__(kSelThreads, 2) beam_tile_kernel(const __grid_constant__ BeamParams p) {
+  using L = Logits<T>;
+  constexpr int kE = L::kE;
+  __shared__ __align__(16) uint32_t s_max[kSelThreads];
+  __shared__ float s_red[2][kSelWarps];
+  __shared__ int s_scan[kSelWarps];
+  __shared__ uint64_t s_key[kSelCap], s_best[UC_MAX_BEAM_OUT];
+  __shared__ float s_tau;
+  __shared__ int s_count;
   griddep_launch_dependents();
   const int tile = blockIdx.x, row = blockIdx.y;
   const int b = row / p.beams, kb = row % p.beams;
-  const int lo = tile * kBeamTile, len = min(kBeamTile, p.vocab - lo);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const T* const x = static_cast<const T*>(p.logits) + b * p.stride_b + kb * p.stride_k;
+  // vectors lie on 16-byte boundaries: the row's first may start before it
+  const int lead = (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
+  const int vec0 = min(tile * p.span, (int)(((int64_t)p.vocab + lead + kE - 1) / kE));
+  const int vec1 = (int)min((int64_t)vec0 + p.span, ((int64_t)p.vocab + lead + kE - 1) / kE);
+  const int lo = max(0, (int)((int64_t)vec0 * kE - lead));
+  const int len = max(0, (int)(min((int64_t)p.vocab, (int64_t)vec1 * kE - lead) - lo));
+  const size_t at = (size_t)row * p.tiles + tile;
   if (p.finished != nullptr && p.finished[row]) {
-    finished_tile(p, row, tile, len);
+    finished_tile(p, at, lo, len);
     return;
   }
-  if (threadIdx.x == 0) {
-    s_count = 0;
-    s_bad = 0;
-  }
-  const T* x = static_cast<const T*>(p.logits) + b * p.stride_b + kb * p.stride_k + lo;
-  // thread t holds logits t, t + 256, ...
-  float v[kPer];
-  float best = kNegInf;
-  int best_at = threadIdx.x;
+  if (tid == 0) s_count = 0;
   bool bad = false;
+  const uint32_t vocab = (uint32_t)p.vocab;
+  const uint4* const xv = reinterpret_cast<const uint4*>(x - lead);
+  const int tail = (int)(((int64_t)p.vocab + lead) % kE);  // elements of the row's last vector, 0: all
+  // round vectors from `from`: thread t holds vectors t, t + 256, ...
+  auto token = [&](int vec, int e) { return (uint32_t)vec * kE + e - lead; };  // (not below vocab: no token)
+  auto load = [&](uint4(&v)[kVecs], int from) {
+    const uint32_t none = L::raw(kNegInf), fill = kE == 4 ? none : none | none << 16;
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    const int i = e * kSelThreads + threadIdx.x;
-    v[e] = kNegInf;
-    if (i < len) {
-      v[e] = logit(x[i]);
-      bad |= !(to_float(x[i]) < INFINITY);
+    for (int k = 0; k < kVecs; ++k) {
+      const int i = from + k * kSelThreads + tid;
+      v[k] = make_uint4(fill, fill, fill, fill);
+      if (i < vec1 && (i > 0 || lead == 0) && (tail == 0 || token(i, kE - 1) < vocab)) v[k] = xv[i];
     }
-    if (v[e] > best) {
-      best = v[e];
-      best_at = i;
+  };
+  uint4 v[kVecs], next[kVecs];
+  float best_of_all = kNegInf, sum = 0.f, tau = kNegInf;
+  const int n = min(p.n, len);
+  load(next, vec0);
+  for (int from = vec0; from < vec1; from += kRound) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) v[k] = next[k];
+    if (from + kRound < vec1) load(next, from + kRound);
+    // a row's ends: only what the row has
+    if ((lead != 0 && from == 0 && tid == 0) || (tail != 0 && from + kRound >= vec1 && token(vec1, 0) >= vocab)) {
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        const int i = from + k * kSelThreads + tid;
+        if (i < vec1 && ((i == 0 && lead != 0) || token(i, kE - 1) >= vocab))
+          v[k] = make_vector<T>([&](int e) {
+            const uint32_t t = token(i, e);
+            return t < vocab ? to_float(x[t]) : kNegInf;
+          });
+      }
+    }
+    float best = kNegInf;
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      const float m = L::largest(v[k]);
+      asm("max.NaN.f32 %0, %0, %1;" : "+f"(best) : "f"(m));
+    }
+    if (!(best < INFINITY)) {
+      // NaN or +inf, reported as UC_ERR_RANGE: they count as -inf
+      bad = true;
+      best = kNegInf;
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        v[k] = make_vector<T>([&](int e) {
+          const float f = L::get(v[k], e);
+          return f < INFINITY ? f : kNegInf;
+        });
+        best = fmaxf(best, L::largest(v[k]));
+      }
+    }
+    if (from == vec0) {  // a bound on the tile's n-th largest: that of the first round's groups
+      float m = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+      if ((lane & 3) == 0) s_max[tid >> 2] = ordered(m);
+      __syncthreads();
+      kth_largest<kSelGroups>(s_max, n, &s_tau);
+    }
+    // sum of exp(x - m) with m the thread's maximum so far: the exponent
+    // x log2(e) - m log2(e) in one rounding, and what rounding m log2(e) leaves
+    // (common to all terms) put right on the sum
+    const float top = fmaxf(best_of_all, best), base = top == kNegInf ? 0.f : top;
+    const float shift = base * kLog2e, left = fmaf(-base, kLog2e, shift);
+    const uint64_t l2 = f2_pack(kLog2e, kLog2e), ns = f2_pack(-shift, -shift);
+    uint64_t acc[2] = {0ull, 0ull};
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k)
+#pragma unroll
+      for (int e = 0; e < kE; e += 2) {
+        float a, c;
+        f2_unpack(f2_fma(f2_pack(L::get(v[k], e), L::get(v[k], e + 1)), l2, ns), a, c);
+        acc[(e >> 1) & 1] = f2_add(acc[(e >> 1) & 1], f2_pack(ex2_approx(a), ex2_approx(c)));
+      }
+    float part[4];
+    f2_unpack(acc[0], part[0], part[1]);
+    f2_unpack(acc[1], part[2], part[3]);
+    sum = fmaf(sum, ex2_approx((best_of_all - base) * kLog2e), ((part[0] + part[1]) + (part[2] + part[3])) * ex2_approx(left));
+    best_of_all = top;
+    // the candidates: everything from tau up in the first round, which has n
+    // of them; above tau after it, where equal ones come too late
+    bool more = best > tau;
+    if (from == vec0) {
+      __syncthreads();
+      tau = s_tau;
+      more = best >= tau;
+    }
+    const int before = s_count;  // (equal in every thread: nothing is added before the barrier below)
+    auto take = [&](bool equal) {  // its logits above tau or equal to it, as far as there is room
+      uint32_t mask = 0;
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        const float m = L::largest(v[k]);
+        mask |= (uint32_t)(m > tau || (equal && m == tau)) << k;
+      }
+      for (; mask; mask &= mask - 1) {
+        const int k = __ffs(mask) - 1, i = from + k * kSelThreads + tid;
+        uint4 w = v[0];
+#pragma unroll
+        for (int j = 1; j < kVecs; ++j)
+          if (j == k) w = v[j];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          const float f = L::get(w, e);
+          if ((f > tau || (equal && f == tau)) && token(i, e) < vocab) {
+            const int c = atomicAdd(&s_count, 1);
+            if (c < kSelCap) s_key[c] = logit_key(f, token(i, e));
+          }
+        }
+      }
+    };
+    __syncthreads();
+    if (more) take(from == vec0);
+    __syncthreads();
+    int count = s_count;
+    if (count > kSelCap) {
+      // many large or many equal ones: bounded closer by this round's threads'
+      // maxima, with equal ones by place until the round has n
+      s_max[tid] = ordered(best);
+      __syncthreads();
+      kth_largest<kSelThreads>(s_max, min(n, kSelThreads), &s_tau);
+      if (tid == 0) s_count = before;
+      __syncthreads();
+      tau = fmaxf(tau, s_tau);
+      take(false);
+      __syncthreads();
+      int want = n - (s_count - before);
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        if (want <= 0) break;
+        const int i = from + k * kSelThreads + tid;
+        uint32_t mask = 0;
+#pragma unroll
+        for (int e = 0; e < kE; ++e)
+          mask |= (uint32_t)(i < vec1 && token(i, e) < vocab && L::get(v[k], e) == tau) << e;
+        int ahead = __popc(mask);
+        const int mine = ahead;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, ahead, o);
+          if (lane >= o) ahead += y;
+        }
+        __syncthreads();
+        if (lane == 31) s_scan[warp] = ahead;
+        __syncthreads();
+        ahead -= mine;
+        int total = 0;
+        for (int w = 0; w < kSelWarps; ++w) {
+          if (w < warp) ahead += s_scan[w];
+          total += s_scan[w];
+        }
+        for (; mask && ahead < want; mask &= mask - 1, ++ahead)
+          s_key[atomicAdd(&s_count, 1)] = logit_key(tau, token(i, __ffs(mask) - 1));
+        want -= total;
+      }
+      __syncthreads();
+      count = s_count;
+    }
+    if (count > kSelMany && from + kRound < vec1) {
+      best_of(s_key, count, n, [&](int rank, uint64_t key) { s_best[rank] = key; });
+      __syncthreads();
+      if (tid < n) s_key[tid] = s_best[tid];
+      if (tid == 0) s_count = n;
+      tau = unordered((uint32_t)(s_best[n - 1] >> 32));
+      __syncthreads();
     }
   }
-  float m = best;
+  // the tile's maximum and sum
+  float m = best_of_all;
 #pragma unroll
   for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (lane == 0) s_red[warp] = m;
-  uint64_t key = logit_key(best, best_at);
-#pragma unroll
-  for (int o = 1; o < kGroupLanes; o <<= 1) {
-    const uint64_t other = shfl_xor_u64(key, o);
-    key = key > other ? key : other;
-  }
-  if (threadIdx.x % kGroupLanes == 0) s_group[threadIdx.x / kGroupLanes] = key;
+  if (lane == 0) s_red[0][warp] = m;
   __syncthreads();
-  if (bad) s_bad = 1;
 #pragma unroll
-  for (int w = 0; w < kSelWarps; ++w) m = fmaxf(m, s_red[w]);
-  // the n-th largest group maximum (positions differ, so keys do)
-  const int n = min(p.n, len);
-  if (threadIdx.x < kSelGroups) {
-    const uint64_t mine = s_group[threadIdx.x];
-    int rank = 0;
-    for (int g = 0; g < kSelGroups; ++g) rank += s_group[g] > mine;
-    if (rank == n - 1) s_tau = mine;
-  }
-  const float base = m == kNegInf ? 0.f : m;
-  float sum = 0.f;
-#pragma unroll
-  for (int e = 0; e < kPer; ++e) sum += ex2_approx((v[e] - base) * kLog2e);
+  for (int w = 0; w < kSelWarps; ++w) m = fmaxf(m, s_red[0][w]);
+  if (m != kNegInf) sum *= ex2_approx((best_of_all - m) * kLog2e);
 #pragma unroll
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  __syncthreads();
-  if (lane == 0) s_red[warp] = sum;
-  const uint64_t tau = s_tau;
-#pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    const int i = e * kSelThreads + threadIdx.x;
-    if (i < len && logit_key(v[e], i) >= tau) s_cand[atomicAdd(&s_count, 1)] = (uint16_t)i;
-  }
-  __syncthreads();
-  const size_t at = (size_t)row * p.tiles + tile;
-  if (threadIdx.x == 0) {
+  if (lane == 0) s_red[1][warp] = sum;
+  bad = __syncthreads_or(bad);
+  if (tid == 0) {
     float total = 0.f;
 #pragma unroll
-    for (int w = 0; w < kSelWarps; ++w) total += s_red[w];
+    for (int w = 0; w < kSelWarps; ++w) total += s_red[1][w];
     p.part_ms[at] = make_float2(m, total);
-    if (s_bad) set_status(p.status, UC_ERR_RANGE, row);
+    if (bad) set_status(p.status, UC_ERR_RANGE, row);
   }
-  // the candidates' ranks; the first n are the tile's best
-  const int c = s_count;
-  for (int i = threadIdx.x; i < c; i += kSelThreads) {
-    const int pos = s_cand[i];
-    const float xi = logit(x[pos]);
-    const uint64_t mine = logit_key(xi, pos);
-    int rank = 0;
-    for (int j = 0; j < c && rank < n; ++j) rank += logit_key(logit(x[s_cand[j]]), s_cand[j]) > mine;
-    if (rank < n) {
-      p.part_x[at * p.n + rank] = xi;
-      p.part_tok[at * p.n + rank] = lo + pos;
-    }
-  }
-  for (int i = n + threadIdx.x; i < p.n; i += kSelThreads) {
+  best_of(s_key, s_count, n, [&](int rank, uint64_t key) {
+    p.part_x[at * p.n + rank] = unordered((uint32_t)(key >> 32));
+    p.part_tok[at * p.n + rank] = (int32_t)(0xffffffffu - (uint32_t)key);
+  });
+  for (int i = n + tid; i < p.n; i += kSelThreads) {
     p.part_x[at * p.n + i] = kNegInf;
     p.part_tok[at * p.n + i] = -1;  // no such candidate
   }
@@ -200,89 +407,107 @@ struct CandKey {
 };
 
 constexpr int kMergeThreads = 256;
+constexpr int kMergeHeads = 512;  // lists whose heads fit shared memory
 constexpr int kMaxMerge = UC_MAX_BEAM_OUT * UC_MAX_BEAM_OUT;  // n lists of n candidates
 
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_constant__ BeamParams p) {
   __shared__ float s_base[UC_MAX_BEAMS], s_log[UC_MAX_BEAMS], s_score[UC_MAX_BEAMS];
-  __shared__ CandKey s_tau, s_key[kMaxMerge];
-  __shared__ int s_id[kMaxMerge];
-  __shared__ int s_count;
-  griddep_wait();
-  const int b = blockIdx.x;
-  const int lists = p.beams * p.tiles;
-  if (threadIdx.x == 0) {
+  __shared__ CandKey s_tau, s_key[kMaxMerge], s_head[kMergeHeads];
+  __shared__ int s_id[kMaxMerge], s_list[UC_MAX_BEAM_OUT];
+  __shared__ int s_count, s_lists;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
+  const int lists = p.beams * p.tiles, n = p.n;
+  if (tid == 0) {
     s_count = 0;
+    s_lists = 0;
     s_tau = CandKey{0, 0};
   }
+  griddep_wait();
+  const size_t row0 = (size_t)b * p.beams, first = (size_t)b * lists * n;
   // each beam's log sum exp over its tiles, one warp per beam
-  for (int kb = threadIdx.x >> 5; kb < p.beams; kb += kMergeThreads / 32) {
-    const int lane = threadIdx.x & 31;
-    const float2* ms = p.part_ms + ((size_t)b * p.beams + kb) * p.tiles;
-    float m = kNegInf;
-    for (int t = lane; t < p.tiles; t += 32) m = fmaxf(m, ms[t].x);
+  for (int kb = tid >> 5; kb < p.beams; kb += kMergeThreads / 32) {
+    const float2* ms = p.part_ms + (row0 + kb) * p.tiles;
+    float m = kNegInf, sum = 0.f;
+    for (int t = lane; t < p.tiles; t += 32) {
+      const float2 x = ms[t];
+      if (x.x > m) {
+        sum = fmaf(sum, expf(m - x.x), x.y);
+        m = x.x;
+      } else if (x.x != kNegInf) {
+        sum = fmaf(x.y, expf(x.x - m), sum);
+      }
+    }
+    float top = m;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float base = m == kNegInf ? 0.f : m;
-    float sum = 0.f;
-    for (int t = lane; t < p.tiles; t += 32)
-      if (ms[t].x != kNegInf) sum += ms[t].y * expf(ms[t].x - base);
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float base = top == kNegInf ? 0.f : top;
+    if (m != kNegInf) sum *= expf(m - base);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) {
-      const float sc = p.scores[(size_t)b * p.beams + kb];
+      const float sc = p.scores[row0 + kb];
       s_base[kb] = base;
       s_log[kb] = logf(sum);
       s_score[kb] = sc;
-      if (!(sc < INFINITY)) set_status(p.status, UC_ERR_RANGE, b * p.beams + kb);
+      if (!(sc < INFINITY)) set_status(p.status, UC_ERR_RANGE, (int)(row0 + kb));
     }
   }
   __syncthreads();
   auto score_of = [&](int kb, float x) {
     return x == kNegInf ? kNegInf : s_score[kb] + ((x - s_base[kb]) - s_log[kb]);
   };
-  const size_t first = (size_t)b * lists * p.n;
-  auto key_of = [&](int id) {  // id: list * n + rank; a, b = 0 where there is no such candidate
-    const int tok = p.part_tok[first + id];
+  auto key_of = [&](int list, int r) {  // a, b = 0 where there is no such candidate
+    const size_t id = first + (size_t)list * n + r;
+    const int tok = p.part_tok[id];
+    const float x = p.part_x[id];
     if (tok < 0) return CandKey{0, 0};
-    const int kb = id / p.n / p.tiles;
-    const float x = p.part_x[first + id];
+    const int kb = list / p.tiles;
     return CandKey{((uint64_t)ordered(score_of(kb, x)) << 32) | (0xffffffffu - kb), logit_key(x, tok)};
   };
   // the n-th best list head bounds the result from below, and only n lists
   // reach it
-  const int n = p.n;
-  if (lists > n)
-    for (int l = threadIdx.x; l < lists; l += kMergeThreads) {
-      const CandKey mine = key_of(l * n);
-      int rank = 0;
-      for (int o = 0; o < lists && rank < n; ++o) rank += key_of(o * n).before(mine);
-      if (rank == n - 1) s_tau = mine;
-    }
+  for (int l = tid; l < min(lists, kMergeHeads); l += kMergeThreads) s_head[l] = key_of(l, 0);
   __syncthreads();
-  const CandKey tau = s_tau;
-  for (int l = threadIdx.x; l < lists; l += kMergeThreads)
-    for (int r = 0; r < n; ++r) {
-      const CandKey k = key_of(l * n + r);
-      if ((k.a | k.b) == 0 || tau.before(k)) break;
-      const int at = atomicAdd(&s_count, 1);
-      s_key[at] = k;
-      s_id[at] = l * n + r;
+  if (lists > n) {
+    for (int l = tid; l < lists; l += kMergeThreads) {
+      const CandKey mine = l < kMergeHeads ? s_head[l] : key_of(l, 0);
+      int rank = 0;
+#pragma unroll 8
+      for (int o = 0; o < min(lists, kMergeHeads); ++o) rank += s_head[o].before(mine);
+      for (int o = kMergeHeads; o < lists && rank < n; ++o) rank += key_of(o, 0).before(mine);
+      if (rank == n - 1) s_tau = mine;  // (no two candidates are equal; where fewer exist, none is the n-th)
     }
+    __syncthreads();
+  }
+  const CandKey tau = s_tau;
+  for (int l = tid; l < lists; l += kMergeThreads) {
+    const CandKey head = l < kMergeHeads ? s_head[l] : key_of(l, 0);
+    if ((head.a | head.b) != 0 && !tau.before(head)) s_list[atomicAdd(&s_lists, 1)] = l;
+  }
+  __syncthreads();
+  for (int i = tid; i < s_lists * n; i += kMergeThreads) {
+    const int l = s_list[i / n], r = i % n;
+    const CandKey k = key_of(l, r);
+    if ((k.a | k.b) == 0 || tau.before(k)) continue;
+    const int at = atomicAdd(&s_count, 1);
+    s_key[at] = k;
+    s_id[at] = l;
+  }
   __syncthreads();
   const int c = s_count;
-  for (int i = threadIdx.x; i < c; i += kMergeThreads) {
+  for (int i = tid; i < c; i += kMergeThreads) {
     const CandKey mine = s_key[i];
     int rank = 0;
-    for (int j = 0; j < c && rank < n; ++j) rank += s_key[j].before(mine);
+#pragma unroll 4
+    for (int j = 0; j < c; ++j) rank += s_key[j].before(mine);
     if (rank < n) {
-      const int kb = s_id[i] / n / p.tiles;
-      const int tok = p.part_tok[first + s_id[i]];
+      const int kb = s_id[i] / p.tiles;
+      const int tok = (int)(0xffffffffu - (uint32_t)mine.b);
       const size_t o = (size_t)b * n + rank;
-      p.out_scores[o] = score_of(kb, p.part_x[first + s_id[i]]);
+      p.out_scores[o] = score_of(kb, unordered((uint32_t)(mine.b >> 32)));
       p.out_parent[o] = kb;
       p.out_token[o] = tok;
-      if (p.out_finished)
-        p.out_finished[o] = tok == p.eos || (p.finished != nullptr && p.finished[(size_t)b * p.beams + kb]);
+      if (p.out_finished) p.out_finished[o] = tok == p.eos || (p.finished != nullptr && p.finished[row0 + kb]);
     }
   }
 }

@@ -247,12 +247,33 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
 }
 
 // --------------------------------------------------------- beam selection
-static int64_t beam_tiles(int32_t vocab) { return ((int64_t)vocab + kBeamTile - 1) / kBeamTile; }
+// Vectors of 16 bytes of a row, the first of which may start before it.
+static int64_t row_vecs(int32_t vocab, int element) {
+  const int per = 16 / element;
+  return ((int64_t)vocab + (per - 1) + (per - 1)) / per;
+}
+static int64_t most_tiles(int64_t vecs) { return vecs < 64 * kBeamMinSpan ? (vecs + kBeamMinSpan - 1) / kBeamMinSpan : 64; }
+// Vectors per tile: the split of the rows that the SMs, two CTAs each, are
+// through with first. A CTA takes kStart as long as its start, its first bound
+// and its ranking take, in units of a vector's time.
+static int beam_span(int64_t rows, int64_t vecs, int sms) {
+  constexpr int64_t kStart = 4096;
+  int64_t best = vecs, cost = INT64_MAX;
+  for (int64_t t = 1; t <= most_tiles(vecs); ++t) {
+    const int64_t span = ((vecs + t - 1) / t + 31) / 32 * 32;
+    const int64_t c = (rows * t + 2 * sms - 1) / (2 * sms) * (kStart + span);
+    if (c < cost) {
+      cost = c;
+      best = span;
+    }
+  }
+  return (int)best;
+}
 
 size_t uc_beam_workspace_size(int32_t batch, int32_t n_beams, int32_t vocab, int32_t n) {
   UC_TRACE();
   if (batch < 1 || n_beams < 1 || vocab < 1 || n < 1) return 0;
-  const uint64_t lists = (uint64_t)batch * n_beams * beam_tiles(vocab);
+  const uint64_t lists = (uint64_t)batch * n_beams * most_tiles(row_vecs(vocab, 4));  // (the most of any type)
   return 256 + lists * (sizeof(float2) + (uint64_t)n * 8);
 }
 
@@ -302,7 +323,9 @@ uc_status uc_beam_select(const void* logits, int32_t dtype, int64_t stride_b, in
   p.beams = n_beams;
   p.vocab = vocab;
   p.n = n;
-  p.tiles = (int)beam_tiles(vocab);
+  const int64_t vecs = row_vecs(vocab, dtype == UC_FP32 ? 4 : 2);
+  p.span = beam_span((int64_t)batch * n_beams, vecs, num_sms());
+  p.tiles = (int)((vecs + p.span - 1) / p.span);
   p.eos = eos;
   p.status = static_cast<DevStatus*>(workspace);
   const size_t lists = (size_t)batch * n_beams * p.tiles;

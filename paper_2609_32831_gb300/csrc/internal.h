@@ -330,7 +330,7 @@ struct LinearChunkParams {
 void launch_linear_chunks(const LinearChunkParams& p, cudaStream_t st);
 
 // ------------------------------------------------- beam selection, reorder
-constexpr int kBeamTile = 8192;  // logits of a row that one CTA selects from
+constexpr int kBeamMinSpan = 512;  // least 16-byte vectors of a row that one CTA selects from, where the row has them
 
 struct BeamParams {
   const void* logits;
@@ -345,7 +345,8 @@ struct BeamParams {
   float* part_x;               // [B * K][tiles][n]: the tile's best logits
   int32_t* part_tok;           // and their tokens
   DevStatus* status;
-  int batch, beams, vocab, n, tiles, eos;
+  int batch, beams, vocab, n, eos;
+  int tiles, span;  // tiles of a row, 16-byte vectors in each
 };
 void launch_beam(const BeamParams& p, int dtype, cudaStream_t st);
 
