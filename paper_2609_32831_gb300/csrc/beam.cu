@@ -28,11 +28,11 @@ constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kVecs = 8;  // 16-byte vectors per thread and round
 constexpr int kRound = kSelThreads * kVecs;
 constexpr int kSelGroups = 64;  // groups of four threads
-constexpr int kSelMany = 512;  // candidates from which they are cut to the best n after a round
 // Candidates: the n-th largest of a round's thread maxima is at most its n-th
 // largest logit, and fewer than n threads hold larger ones; n equal ones; and
-// what the rounds before left.
-constexpr int kSelCap = kSelMany + UC_MAX_BEAM_OUT * kVecs * 8;
+// what the rounds before left, fewer than many(n).
+constexpr __host__ __device__ int many(int n) { return 2 * n + 16; }
+constexpr int kSelCap = many(UC_MAX_BEAM_OUT) + UC_MAX_BEAM_OUT * kVecs * 8;
 constexpr float kNegInf = -INFINITY;
 constexpr float kLog2e = 1.4426950408889634f;
 static_assert(kSelGroups >= UC_MAX_BEAM_OUT, "n groups have to exist");
@@ -144,23 +144,23 @@ __device__ void finished_tile(const BeamParams& p, size_t at, int lo, int len) {
   }
 }
 
-// The k-th largest (from 1) of COUNT values, ties by place; one value per
-// thread below COUNT.
+// The k-th largest (from 1) of COUNT values, ties by place: the CTA's threads
+// share each value's ranking out.
 template <int COUNT>
 __device__ __forceinline__ void kth_largest(const uint32_t* vals, int k, float* out) {
-  if (threadIdx.x < COUNT) {
-    const uint32_t mine = vals[threadIdx.x];
-    int rank = 0;
-    for (int g = 0; g < COUNT; g += 4) {
-      const uint4 o = *reinterpret_cast<const uint4*>(vals + g);
-      rank += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
-      if (g <= (int)threadIdx.x) {
-        rank += (o.x == mine && g < (int)threadIdx.x) + (o.y == mine && g + 1 < (int)threadIdx.x) +
-                (o.z == mine && g + 2 < (int)threadIdx.x) + (o.w == mine && g + 3 < (int)threadIdx.x);
-      }
-    }
-    if (rank == k - 1) *out = unordered(mine);
+  constexpr int kPer = kSelThreads / COUNT;  // threads per value
+  const int g = threadIdx.x / kPer, part = threadIdx.x % kPer * (COUNT / kPer);
+  const uint32_t mine = vals[g];
+  int rank = 0;
+#pragma unroll 4
+  for (int o = part; o < part + COUNT / kPer; o += 4) {
+    const uint4 w = *reinterpret_cast<const uint4*>(vals + o);
+    rank += (w.x > mine || (w.x == mine && o < g)) + (w.y > mine || (w.y == mine && o + 1 < g)) +
+            (w.z > mine || (w.z == mine && o + 2 < g)) + (w.w > mine || (w.w == mine && o + 3 < g));
   }
+#pragma unroll
+  for (int o = 1; o < kPer; o <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+  if (threadIdx.x % kPer == 0 && rank == k - 1) *out = unordered(mine);
 }
 
 // The best n of c candidates, in order, to out(rank, key); every thread calls it.
@@ -169,13 +169,17 @@ __device__ __forceinline__ void best_of(const uint64_t* keys, int c, int n, F&& 
   for (int i = threadIdx.x; i < c; i += kSelThreads) {
     const uint64_t mine = keys[i];
     int rank = 0;
-    for (int j = 0; j < c && rank < n; ++j) rank += keys[j] > mine;
+    int j = 0;
+    for (; j + 8 <= c && rank < n; j += 8)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) rank += keys[j + u] > mine;
+    for (; j < c && rank < n; ++j) rank += keys[j] > mine;
     if (rank < n) out(rank, mine);
   }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads, 2) beam_tile_kernel(const __grid_constant__ BeamParams p) {
+__global__ void __launch_bounds__(kSelThreads, kBeamPerSm) beam_tile_kernel(const __grid_constant__ BeamParams p) {
   using L = Logits<T>;
   constexpr int kE = L::kE;
   __shared__ __align__(16) uint32_t s_max[kSelThreads];
@@ -183,7 +187,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_tile_kernel(const __grid_
   __shared__ int s_scan[kSelWarps];
   __shared__ uint64_t s_key[kSelCap], s_best[UC_MAX_BEAM_OUT];
   __shared__ float s_tau;
-  __shared__ int s_count;
+  __shared__ int s_new[3];  // candidates of a round, of rounds in turn: zeroed a barrier before their round
   griddep_launch_dependents();
   const int tile = blockIdx.x, row = blockIdx.y;
   const int b = row / p.beams, kb = row % p.beams;
@@ -200,39 +204,51 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_tile_kernel(const __grid_
     finished_tile(p, at, lo, len);
     return;
   }
-  if (tid == 0) s_count = 0;
+  if (tid == 0) s_new[0] = 0;
   bool bad = false;
   const uint32_t vocab = (uint32_t)p.vocab;
   const uint4* const xv = reinterpret_cast<const uint4*>(x - lead);
-  const int tail = (int)(((int64_t)p.vocab + lead) % kE);  // elements of the row's last vector, 0: all
+  // vectors that the row has wholly
+  const int whole0 = lead != 0, whole1 = min(vec1, (int)(((int64_t)p.vocab + lead) / kE));
   // round vectors from `from`: thread t holds vectors t, t + 256, ...
   auto token = [&](int vec, int e) { return (uint32_t)vec * kE + e - lead; };  // (not below vocab: no token)
   auto load = [&](uint4(&v)[kVecs], int from) {
+    const uint4* const at = xv + from + tid;
+    if (from >= whole0 && from + kRound <= whole1) {
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) v[k] = at[k * kSelThreads];
+      return;
+    }
     const uint32_t none = L::raw(kNegInf), fill = kE == 4 ? none : none | none << 16;
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       const int i = from + k * kSelThreads + tid;
       v[k] = make_uint4(fill, fill, fill, fill);
-      if (i < vec1 && (i > 0 || lead == 0) && (tail == 0 || token(i, kE - 1) < vocab)) v[k] = xv[i];
+      if (i >= whole0 && i < whole1) v[k] = at[k * kSelThreads];
     }
   };
   uint4 v[kVecs], next[kVecs];
   float best_of_all = kNegInf, sum = 0.f, tau = kNegInf;
   const int n = min(p.n, len);
+  int count = 0, turn = 0;  // candidates so far (equal in every thread)
   load(next, vec0);
   for (int from = vec0; from < vec1; from += kRound) {
+    int* const fresh = s_new + turn;
+    turn = turn == 2 ? 0 : turn + 1;
+    if (tid == 0) s_new[turn] = 0;
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) v[k] = next[k];
     if (from + kRound < vec1) load(next, from + kRound);
     // a row's ends: only what the row has
-    if ((lead != 0 && from == 0 && tid == 0) || (tail != 0 && from + kRound >= vec1 && token(vec1, 0) >= vocab)) {
+    if (from < whole0 || (whole1 < vec1 && from + kRound > whole1)) {
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
         const int i = from + k * kSelThreads + tid;
-        if (i < vec1 && ((i == 0 && lead != 0) || token(i, kE - 1) >= vocab))
+        if (i < vec1 && (i < whole0 || i >= whole1))
           v[k] = make_vector<T>([&](int e) {
             const uint32_t t = token(i, e);
-            return t < vocab ? to_float(x[t]) : kNegInf;
+            const float f = to_float(x[min(t, vocab - 1)]);  // (loads that wait for nothing)
+            return t < vocab ? f : kNegInf;
           });
       }
     }
@@ -262,26 +278,6 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_tile_kernel(const __grid_
       __syncthreads();
       kth_largest<kSelGroups>(s_max, n, &s_tau);
     }
-    // sum of exp(x - m) with m the thread's maximum so far: the exponent
-    // x log2(e) - m log2(e) in one rounding, and what rounding m log2(e) leaves
-    // (common to all terms) put right on the sum
-    const float top = fmaxf(best_of_all, best), base = top == kNegInf ? 0.f : top;
-    const float shift = base * kLog2e, left = fmaf(-base, kLog2e, shift);
-    const uint64_t l2 = f2_pack(kLog2e, kLog2e), ns = f2_pack(-shift, -shift);
-    uint64_t acc[2] = {0ull, 0ull};
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k)
-#pragma unroll
-      for (int e = 0; e < kE; e += 2) {
-        float a, c;
-        f2_unpack(f2_fma(f2_pack(L::get(v[k], e), L::get(v[k], e + 1)), l2, ns), a, c);
-        acc[(e >> 1) & 1] = f2_add(acc[(e >> 1) & 1], f2_pack(ex2_approx(a), ex2_approx(c)));
-      }
-    float part[4];
-    f2_unpack(acc[0], part[0], part[1]);
-    f2_unpack(acc[1], part[2], part[3]);
-    sum = fmaf(sum, ex2_approx((best_of_all - base) * kLog2e), ((part[0] + part[1]) + (part[2] + part[3])) * ex2_approx(left));
-    best_of_all = top;
     // the candidates: everything from tau up in the first round, which has n
     // of them; above tau after it, where equal ones come too late
     bool more = best > tau;
@@ -290,7 +286,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_tile_kernel(const __grid_
       tau = s_tau;
       more = best >= tau;
     }
-    const int before = s_count;  // (equal in every thread: nothing is added before the barrier below)
+    const int before = count;
     auto take = [&](bool equal) {  // its logits above tau or equal to it, as far as there is room
       uint32_t mask = 0;
 #pragma unroll
@@ -304,32 +300,57 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_tile_kernel(const __grid_
 #pragma unroll
         for (int j = 1; j < kVecs; ++j)
           if (j == k) w = v[j];
+        uint32_t hits = 0;
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
           const float f = L::get(w, e);
-          if ((f > tau || (equal && f == tau)) && token(i, e) < vocab) {
-            const int c = atomicAdd(&s_count, 1);
-            if (c < kSelCap) s_key[c] = logit_key(f, token(i, e));
-          }
+          hits |= (uint32_t)(f > tau || (equal && f == tau)) << e;
+        }
+        for (; hits; hits &= hits - 1) {
+          const int e = __ffs(hits) - 1;
+          if (i >= vec1 || token(i, e) >= vocab) continue;  // what fills the last vectors up
+          const int c = before + atomicAdd(fresh, 1);
+          if (c < kSelCap) s_key[c] = logit_key(L::get(w, e), token(i, e));
         }
       }
     };
-    __syncthreads();
     if (more) take(from == vec0);
+    // sum of exp(x - m) with m the thread's maximum so far: the exponent
+    // x log2(e) - m log2(e) in one rounding, and what rounding m log2(e) leaves
+    // (common to all terms) put right on the sum
+    const float top = fmaxf(best_of_all, best), base = top == kNegInf ? 0.f : top;
+    const float shift = base * kLog2e, left = fmaf(-base, kLog2e, shift);
+    const uint64_t l2 = f2_pack(kLog2e, kLog2e), ns = f2_pack(-shift, -shift);
+    uint64_t acc[2] = {0ull, 0ull};
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      if (from + k * kSelThreads >= vec1) break;
+#pragma unroll
+      for (int e = 0; e < kE; e += 2) {
+        float a, c;
+        f2_unpack(f2_fma(f2_pack(L::get(v[k], e), L::get(v[k], e + 1)), l2, ns), a, c);
+        acc[(e >> 1) & 1] = f2_add(acc[(e >> 1) & 1], f2_pack(ex2_approx(a), ex2_approx(c)));
+      }
+    }
+    float part[4];
+    f2_unpack(acc[0], part[0], part[1]);
+    f2_unpack(acc[1], part[2], part[3]);
+    sum = fmaf(sum, ex2_approx((best_of_all - base) * kLog2e), ((part[0] + part[1]) + (part[2] + part[3])) * ex2_approx(left));
+    best_of_all = top;
     __syncthreads();
-    int count = s_count;
+    count = before + *fresh;
     if (count > kSelCap) {
       // many large or many equal ones: bounded closer by this round's threads'
       // maxima, with equal ones by place until the round has n
       s_max[tid] = ordered(best);
       __syncthreads();
       kth_largest<kSelThreads>(s_max, min(n, kSelThreads), &s_tau);
-      if (tid == 0) s_count = before;
+      if (tid == 0) *fresh = 0;
       __syncthreads();
       tau = fmaxf(tau, s_tau);
       take(false);
       __syncthreads();
-      int want = n - (s_count - before);
+      int want = n - *fresh;
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
         if (want <= 0) break;
@@ -355,17 +376,17 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_tile_kernel(const __grid_
           total += s_scan[w];
         }
         for (; mask && ahead < want; mask &= mask - 1, ++ahead)
-          s_key[atomicAdd(&s_count, 1)] = logit_key(tau, token(i, __ffs(mask) - 1));
+          s_key[before + atomicAdd(fresh, 1)] = logit_key(tau, token(i, __ffs(mask) - 1));
         want -= total;
       }
       __syncthreads();
-      count = s_count;
+      count = before + *fresh;
     }
-    if (count > kSelMany && from + kRound < vec1) {
+    if (count > many(n) && from + kRound < vec1) {
       best_of(s_key, count, n, [&](int rank, uint64_t key) { s_best[rank] = key; });
       __syncthreads();
       if (tid < n) s_key[tid] = s_best[tid];
-      if (tid == 0) s_count = n;
+      count = n;
       tau = unordered((uint32_t)(s_best[n - 1] >> 32));
       __syncthreads();
     }
@@ -390,7 +411,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) beam_tile_kernel(const __grid_
     p.part_ms[at] = make_float2(m, total);
     if (bad) set_status(p.status, UC_ERR_RANGE, row);
   }
-  best_of(s_key, s_count, n, [&](int rank, uint64_t key) {
+  best_of(s_key, count, n, [&](int rank, uint64_t key) {
     p.part_x[at * p.n + rank] = unordered((uint32_t)(key >> 32));
     p.part_tok[at * p.n + rank] = (int32_t)(0xffffffffu - (uint32_t)key);
   });

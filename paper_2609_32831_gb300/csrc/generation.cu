@@ -253,15 +253,15 @@ static int64_t row_vecs(int32_t vocab, int element) {
   return ((int64_t)vocab + (per - 1) + (per - 1)) / per;
 }
 static int64_t most_tiles(int64_t vecs) { return vecs < 64 * kBeamMinSpan ? (vecs + kBeamMinSpan - 1) / kBeamMinSpan : 64; }
-// Vectors per tile: the split of the rows that the SMs, two CTAs each, are
-// through with first. A CTA takes kStart as long as its start, its first bound
+// Vectors per tile: the split of the rows that the SMs are through with
+// first. A CTA takes kStart as long as its start, its first bound
 // and its ranking take, in units of a vector's time.
-static int beam_span(int64_t rows, int64_t vecs, int sms) {
-  constexpr int64_t kStart = 4096;
+static int beam_span(int64_t rows, int64_t vecs, int64_t slots) {
+  constexpr int64_t kStart = 2048;
   int64_t best = vecs, cost = INT64_MAX;
   for (int64_t t = 1; t <= most_tiles(vecs); ++t) {
     const int64_t span = ((vecs + t - 1) / t + 31) / 32 * 32;
-    const int64_t c = (rows * t + 2 * sms - 1) / (2 * sms) * (kStart + span);
+    const int64_t c = (rows * t + slots - 1) / slots * (kStart + span);
     if (c < cost) {
       cost = c;
       best = span;
@@ -324,7 +324,7 @@ uc_status uc_beam_select(const void* logits, int32_t dtype, int64_t stride_b, in
   p.vocab = vocab;
   p.n = n;
   const int64_t vecs = row_vecs(vocab, dtype == UC_FP32 ? 4 : 2);
-  p.span = beam_span((int64_t)batch * n_beams, vecs, num_sms());
+  p.span = beam_span((int64_t)batch * n_beams, vecs, kBeamPerSm * num_sms());
   p.tiles = (int)((vecs + p.span - 1) / p.span);
   p.eos = eos;
   p.status = static_cast<DevStatus*>(workspace);
