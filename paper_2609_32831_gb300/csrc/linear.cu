@@ -93,9 +93,14 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 //            stored, turned around in shared memory so that two lanes write a
 //            32-byte sector of a row
 //   WG4      (16-19) the state. It stays in tensor memory in fp32; per chunk
-//            its bf16 copy goes to shared memory for Q S, it is scaled by
-//            gamma^nv in place, and the chunk's decayed values are formed in
-//            slices of 16 tokens that accumulate on it while the chunk's tiles run
+//            its bf16 copy goes to shared memory for Q S, what that rounding
+//            left stays behind, scaled by gamma^nv, and the chunk's decayed
+//            values are formed in slices of 16 tokens that accumulate on the
+//            rest while the chunk's tiles run; the copy joins them, scaled,
+//            in fp32. (The tensor cores' sums are cut, not rounded: 24 of them
+//            per chunk on the whole state pulled it towards zero by up to 1.2e-5
+//            of its size where gamma is near 1; on the rest they cost 1e-7 of the
+//            chunk's own sum.)
 //   warp 20  TMA producer: k and v tiles per chunk and a q tile per head, in the
 //            order they are needed, each into whichever slot is free
 //   warp 21  issues Q K^T, one tile ahead
@@ -122,7 +127,7 @@ constexpr int kLThreads = 768;
 constexpr int kLRegLaunch = 80;  // registers per thread at launch, and after the warpgroups rebalance
 constexpr int kLRegP = 88;
 constexpr int kLRegEpilogue = 88;
-constexpr int kLRegState = 64;
+constexpr int kLRegState = 72;
 constexpr int kLRegOther = 56;
 static_assert(256 * (kLRegP + kLRegEpilogue) + 128 * (kLRegState + kLRegOther) <= kLThreads * kLRegLaunch, "register split");
 constexpr int kWarpEpilogue = 8, kWarpState = 16, kWarpTma = 20, kWarpQk = 21, kWarpMma = 22, kWarpSlice = 23;
@@ -535,6 +540,32 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       tmem_st32(s_addr + 32 * blk, w);
     }
     tmem_wait_st();
+    auto copy = [&](int blk, int e) {  // eight channels of the row's bf16 copy
+      const int chunk16 = 4 * (blk & 1) + e;  // 16 bytes of the row's half
+      return reinterpret_cast<uint4*>(sm.s + (blk >> 1) * (kTileBytes / 2) + r * 128 + ((chunk16 ^ (r & 7)) << 4));
+    };
+    // what rounding leaves; nothing where the state has overflowed
+    auto rest = [](float x, float rounded) {
+      const float d = x - rounded;
+      return d == d ? d : 0.f;
+    };
+    // 32 channels of the state: tensor memory's part and the copy's, scaled by g
+    // since it was made (g = 0: there is none yet)
+    auto whole_state = [&](int blk, uint32_t(&x)[32], float g) {
+      tmem_ld32(s_addr + 32 * blk, x);
+      tmem_wait_ld32(x);
+      if (g == 0.f) return;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint4 c = *copy(blk, e);
+        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          x[8 * e + 2 * u] = __float_as_uint(fmaf(bf16_lo(w[u]), g, __uint_as_float(x[8 * e + 2 * u])));
+          x[8 * e + 2 * u + 1] = __float_as_uint(fmaf(bf16_hi(w[u]), g, __uint_as_float(x[8 * e + 2 * u + 1])));
+        }
+      }
+    };
     int n_slice = 0;
     for (int ci = 0; ci < nc && !aborted; ++ci) {
       const bool update = ci + 1 < nc || last_state;
@@ -547,23 +578,20 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
 #pragma unroll
       for (int blk = 0; blk < 4; ++blk) {
         uint32_t x[32];
-        tmem_ld32(s_addr + 32 * blk, x);
-        tmem_wait_ld32(x);
+        whole_state(blk, x, ci > 0 ? sm.pw[kChunk] : 0.f);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           uint32_t w[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u)
-            w[u] = pack_bf16(__uint_as_float(x[8 * e + 2 * u]), __uint_as_float(x[8 * e + 2 * u + 1]));
-          const int chunk16 = 4 * (blk & 1) + e;  // 16 bytes of the row's half
-          *reinterpret_cast<uint4*>(sm.s + (blk >> 1) * (kTileBytes / 2) + r * 128 + ((chunk16 ^ (r & 7)) << 4)) =
-              make_uint4(w[0], w[1], w[2], w[3]);
+          for (int u = 0; u < 4; ++u) {
+            uint32_t &a = x[8 * e + 2 * u], &c = x[8 * e + 2 * u + 1];
+            w[u] = pack_bf16(__uint_as_float(a), __uint_as_float(c));
+            a = __float_as_uint(rest(__uint_as_float(a), bf16_lo(w[u])) * g);
+            c = __float_as_uint(rest(__uint_as_float(c), bf16_hi(w[u])) * g);
+          }
+          *copy(blk, e) = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        if (update) {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * g);
-          tmem_st32(s_addr + 32 * blk, x);
-        }
+        if (update) tmem_st32(s_addr + 32 * blk, x);
       }
       tmem_wait_st();
       tc_fence_before();
@@ -586,8 +614,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
 #pragma unroll 1
       for (int blk = 0; blk < 4; ++blk) {
         uint32_t x[32];
-        tmem_ld32(s_addr + 32 * blk, x);
-        tmem_wait_ld32(x);
+        whole_state(blk, x, nc > 0 ? sm.pw[valid(nc - 1)] : 0.f);
 #pragma unroll
         for (int e = 0; e < 32; e += 4)
           *reinterpret_cast<uint4*>(dst + 32 * blk + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
@@ -724,8 +751,10 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
 
 // A run's own sum: sum_j k_j (gamma^{e-1-j} v_j)^T over its tokens, e its end
 // (a sequence's last run needs none). The weights fall towards the run's
-// start, so the chunks accumulate in tensor memory without a rescale. Four
-// groups of four warps form the decayed values, a quarter chunk each.
+// start, so the chunks add up without a rescale: each one's sum in tensor
+// memory from zero, in turns of two, and all of them in registers (rounded,
+// where the tensor cores cut). Four groups of four warps form the decayed
+// values, a quarter chunk each, and hold a quarter of the channels.
 constexpr int kLocalRing = 2;  // chunks in flight
 constexpr int kQuarter = kChunk / 4;
 constexpr uint32_t kQuarterBytes = kQuarter * kHeadDim * 2;
@@ -734,7 +763,7 @@ struct LinearLocalSmem {
   uint8_t part[4][3][kQuarterBytes];  // [2 x 64 channels][32 tokens][128 B]
   float pw[kChunk];                   // gamma^n
   uint64_t k_full[kLocalRing], v_full[kLocalRing], empty[kLocalRing];
-  uint64_t part_full[4], part_free[4], done;
+  uint64_t part_full[4], part_free[4], sum_full[2], sum_free[2];
   uint32_t tmem_base;
 };
 static_assert(sizeof(LinearLocalSmem) + 1024 <= 232448, "linear attention shared memory");
@@ -761,12 +790,15 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
       mbar_init(&sm.part_full[s], 4);
       mbar_init(&sm.part_free[s], 1);
     }
-    mbar_init(&sm.done, 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&sm.sum_full[s], 1);
+      mbar_init(&sm.sum_free[s], 16);
+    }
     fence_barrier_init();
   }
   const float2 l2 = p.log2_decay[kvh];
   if (threadIdx.x < kChunk) sm.pw[threadIdx.x] = decay_pow(l2, threadIdx.x);
-  if (warp == kWarpMma) tmem_alloc(&sm.tmem_base, 128);
+  if (warp == kWarpMma) tmem_alloc(&sm.tmem_base, 256);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -799,9 +831,10 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
     const uint32_t dhi = (uint32_t)(smem_desc_sw128(0, 16) >> 32);
     const uint32_t k_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.k[0]), kTileBytes / 2);
     const uint32_t part_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.part[0][0]), kQuarterBytes / 2);
-    uint32_t first = 0;
     for (int ci = 0; ci < nc && !aborted; ++ci) {
       const int s = ci % kLocalRing;
+      uint32_t first = 0;
+      if (ci > 1 && !dwait_warp(&sm.sum_free[ci & 1], ((ci >> 1) - 1) & 1, st, 77, aborted, lim)) break;
       if (!dwait_warp(&sm.k_full[s], (ci / kLocalRing) & 1, st, 73, aborted, lim)) break;
       for (int g = 0; g < 4; ++g) {
         if (!dwait_warp(&sm.part_full[g], ci & 1, st, 75, aborted, lim)) break;
@@ -809,17 +842,31 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
 #pragma unroll 1
         for (uint32_t u = 0; u < 6; ++u) {  // three parts of two 16-token steps
           const uint32_t step = u & 1;
-          issue_ss(lead, tm, k_lo + s * (kTileBytes >> 4) + (kQuarter * 128 >> 4) * g + 128 * step,
+          issue_ss(lead, tm + 128 * (ci & 1), k_lo + s * (kTileBytes >> 4) + (kQuarter * 128 >> 4) * g + 128 * step,
                    part_lo + (3 * g + (u >> 1)) * (kQuarterBytes >> 4) + 128 * step, dhi, id_ab, first);
           first = 1;
         }
         umma_commit_lead(lead, &sm.part_free[g]);
       }
       umma_commit_lead(lead, &sm.empty[s]);
+      umma_commit_lead(lead, &sm.sum_full[ci & 1]);
     }
-    umma_commit_lead(lead, &sm.done);
   } else if (warp < 16) {
     const int g = warp >> 2;
+    // a chunk's own sum (32 rows, 32 channels per warp) joins the others in registers
+    float sum[32] = {};
+    auto fold = [&](int ci) {
+      if (!dwait_warp(&sm.sum_full[ci & 1], (ci >> 1) & 1, st, 77, aborted, lim)) return false;
+      tc_fence_after();
+      uint32_t x[32];
+      tmem_ld32(tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 128 * (ci & 1) + 32 * g, x);
+      tmem_wait_ld32(x);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) sum[e] += __uint_as_float(x[e]);
+      tc_fence_before();
+      warp_arrive(&sm.sum_free[ci & 1], lane);
+      return true;
+    };
     for (int ci = 0; ci < nc; ++ci) {
       const int s = ci % kLocalRing;
       // gamma^{e - 1 - t} = gamma^{tokens of the run behind this chunk} gamma^{127 - j}
@@ -830,19 +877,13 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
                                  [&](int j) { return behind * sm.pw[kChunk - 1 - j]; });
       fence_proxy_async_smem();
       warp_arrive(&sm.part_full[g], lane);
+      if (ci > 0 && !fold(ci - 1)) break;
     }
-    if (warp < 4 && dwait_warp(&sm.done, 0, st, 77, aborted, lim)) {
-      tc_fence_after();
-      float* dst = c.local + ((size_t)(grun * p.n_kv_heads + kvh) * kHeadDim + threadIdx.x) * kHeadDim;
-#pragma unroll 1
-      for (int blk = 0; blk < 4; ++blk) {
-        uint32_t kv[32];
-        tmem_ld32(tmem + ((uint32_t)(32 * warp) << 16) + 32 * blk, kv);
-        tmem_wait_ld32(kv);
+    if (!aborted && fold(nc - 1)) {
+      float* dst = c.local + ((size_t)(grun * p.n_kv_heads + kvh) * kHeadDim + (threadIdx.x & 127)) * kHeadDim + 32 * g;
 #pragma unroll
-        for (int e = 0; e < 32; e += 4)
-          *reinterpret_cast<uint4*>(dst + 32 * blk + e) = make_uint4(kv[e], kv[e + 1], kv[e + 2], kv[e + 3]);
-      }
+      for (int e = 0; e < 32; e += 4)
+        *reinterpret_cast<float4*>(dst + e) = make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]);
     }
     tc_fence_before();
   }
@@ -850,7 +891,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
   if (warp == kWarpMma) {
     __syncwarp();
     tc_fence_after();
-    tmem_dealloc(tmem, 128);
+    tmem_dealloc(tmem, 256);
   }
 }
 
