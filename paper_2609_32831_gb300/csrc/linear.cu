@@ -157,9 +157,9 @@ struct LinearSmem {
   float cj[kChunk];                    // gamma^{-(n + 1)}
   uint64_t full[kLFull], empty[kLSlots];
   uint64_t s_full[2], p_full[2], o_full, o_free;
-  uint64_t st_ready, s_free, chunk_go, k_done[2], v_done[2], kv_done, part_full[2], part_free[2];
+  uint64_t st_ready, s_free, chunk_go[2], k_done[2], v_done[2], kv_done, part_full[2], part_free[2];
   uint32_t tmem_base;
-  uint32_t ks[2], vs;                  // slots of a chunk's k (by parity) and v
+  uint32_t ks[2], vs[2];               // slots of a chunk's k and v, by parity
   uint8_t slot_of[16];                 // slot of load L at L mod 16
 };
 static_assert(sizeof(LinearSmem) + 1024 <= 232448, "linear attention shared memory");
@@ -344,6 +344,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       mbar_init(&sm.p_full[s], 8);     // (arrivals: one per warp)
       mbar_init(&sm.part_full[s], 4);
       mbar_init(&sm.part_free[s], 1);
+      mbar_init(&sm.chunk_go[s], 1);
       mbar_init(&sm.k_done[s], 1);
       mbar_init(&sm.v_done[s], 1);
     }
@@ -352,7 +353,6 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     mbar_init(&sm.st_ready, 4);
     mbar_init(&sm.s_free, 1);
     mbar_init(&sm.kv_done, 1);
-    mbar_init(&sm.chunk_go, 1);
     fence_barrier_init();
   }
   const float2 l2 = p.log2_decay[kvh];
@@ -432,7 +432,6 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
             if (!dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, 54, aborted, lim)) break;
             ks = __shfl_sync(0xffffffffu, (uint32_t)sm.slot_of[L & 15], 0);
             if (valid(ci) < kChunk) zero_rows(sm.slot[ks], valid(ci), lane);
-            if (lane == 0) sm.ks[ci & 1] = ks;
           }
           const int L = load_q(ci, h);
           if (!dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, 56, aborted, lim)) break;
@@ -465,8 +464,15 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
           const bool last = h == nh - 1;
           const uint32_t qs = take(load_q(ci, h), 56);
           if (h == 0) {
+            const uint32_t ks = take(load_k(ci), 60);
             vs = take(load_v(ci), 60);
-            if (!aborted && valid(ci) < kChunk) zero_rows(sm.slot[vs], valid(ci), lane);
+            if (aborted) break;
+            if (valid(ci) < kChunk) zero_rows(sm.slot[vs], valid(ci), lane);
+            if (lane == 0) {
+              sm.ks[ci & 1] = ks;
+              sm.vs[ci & 1] = vs;
+              if (valid(ci) == kChunk) mbar_arrive(&sm.chunk_go[ci & 1]);  // the chunk's k and v are there
+            }
             // the chunk's state is in shared memory, the next scaled in place
             if (!dwait_warp(&sm.st_ready, ci & 1, st, 57, aborted, lim)) break;
           }
@@ -480,10 +486,8 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
           issue_p_v(lead, tm + kColOut, tm + 128 * (t & 1), col_lo + vs * kStep, dhi, id_b);
           umma_commit_lead(lead, &sm.o_full);
           if (last) umma_commit_lead(lead, &sm.v_done[ci & 1]);
-          if (h == 0 && lane == 0) {
-            sm.vs = vs;
-            mbar_arrive(&sm.chunk_go);  // the chunk's k and v are there
-          }
+          // (a last chunk's k rows behind the end were zeroed before its Q K^T)
+          if (h == 0 && lane == 0 && valid(ci) < kChunk) mbar_arrive(&sm.chunk_go[ci & 1]);
         }
       }
     } else if (warp == kWarpSlice) {
@@ -496,9 +500,9 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       const uint32_t part_lo = (uint32_t)smem_desc_sw128(smem_u32(sm.part[0][0]), kSliceBytes / 2);
       int n = 0;
       for (int ci = 0; ci < (last_state ? nc : nc - 1) && !aborted; ++ci) {
-        // (the state is scaled for this chunk before the chunk's first tile goes)
-        if (!dwait_warp(&sm.chunk_go, ci & 1, st, 62, aborted, lim)) break;
-        const uint32_t ks = __shfl_sync(0xffffffffu, sm.ks[ci & 1], 0), vs = __shfl_sync(0xffffffffu, sm.vs, 0);
+        // (the state is scaled for this chunk before its first slice is formed)
+        if (!dwait_warp(&sm.chunk_go[ci & 1], (ci >> 1) & 1, st, 62, aborted, lim)) break;
+        const uint32_t ks = __shfl_sync(0xffffffffu, sm.ks[ci & 1], 0), vs = __shfl_sync(0xffffffffu, sm.vs[ci & 1], 0);
         for (int sl = 0; sl < kSlices; ++sl, ++n) {
           const int buf = n & 1;
           if (!dwait_warp(&sm.part_full[buf], (n >> 1) & 1, st, 62, aborted, lim)) break;
@@ -598,8 +602,8 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       fence_proxy_async_smem();
       warp_arrive(&sm.st_ready, lane);
       if (!update) break;
-      if (!dwait_warp(&sm.chunk_go, ci & 1, st, 67, aborted, lim)) break;  // V is there
-      const uint8_t* v = sm.slot[sm.vs];
+      if (!dwait_warp(&sm.chunk_go[ci & 1], (ci >> 1) & 1, st, 67, aborted, lim)) break;  // V is there
+      const uint8_t* v = sm.slot[sm.vs[ci & 1]];
       for (int sl = 0; sl < kSlices; ++sl, ++n_slice) {
         const int buf = n_slice & 1;
         if (n_slice >= 2 && !dwait_warp(&sm.part_free[buf], ((n_slice >> 1) - 1) & 1, st, 68, aborted, lim)) break;
