@@ -156,7 +156,7 @@ struct LinearSmem {
   float pw[kChunk + 4];                // gamma^n
   float cj[kChunk];                    // gamma^{-(n + 1)}
   uint64_t full[kLFull], empty[kLSlots];
-  uint64_t s_full[2], p_full[2], o_full, o_free;
+  uint64_t s_full[2], p_full[2], o_full[2], o_free;
   uint64_t st_ready, s_free, chunk_go[2], k_done[2], v_done[2], kv_done, part_full[2], part_free[2];
   uint32_t tmem_base;
   uint32_t ks[2], vs[2];               // slots of a chunk's k and v, by parity
@@ -341,6 +341,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     for (int s = 0; s < kLSlots; ++s) mbar_init(&sm.empty[s], 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&sm.s_full[s], 1);
+      mbar_init(&sm.o_full[s], 1);
       mbar_init(&sm.p_full[s], 8);     // (arrivals: one per warp)
       mbar_init(&sm.part_full[s], 4);
       mbar_init(&sm.part_free[s], 1);
@@ -348,7 +349,6 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       mbar_init(&sm.k_done[s], 1);
       mbar_init(&sm.v_done[s], 1);
     }
-    mbar_init(&sm.o_full, 1);
     mbar_init(&sm.o_free, 8);
     mbar_init(&sm.st_ready, 4);
     mbar_init(&sm.s_free, 1);
@@ -425,8 +425,9 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       for (int ci = 0, t = 0; ci < nc && !aborted; ++ci) {
         uint32_t ks = 0;
         for (int h = 0; h < nh; ++h, ++t) {
-          // P of the tile before the last has been read: its slot is free
-          if (t > 1 && !dwait_warp(&sm.o_full, t & 1, st, 58, aborted, lim)) break;
+          // P of the tile before the last has been read: its slot is free. (Two
+          // barriers by tile: the last tile's may complete before this is looked at.)
+          if (t > 1 && !dwait_warp(&sm.o_full[t & 1], ((t >> 1) - 1) & 1, st, 58, aborted, lim)) break;
           if (h == 0) {
             const int L = load_k(ci);
             if (!dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, 54, aborted, lim)) break;
@@ -484,7 +485,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
           tc_fence_after();
           umma_commit_lead(lead, &sm.empty[qs]);  // Q S is issued, and Q K^T was done before P
           issue_p_v(lead, tm + kColOut, tm + 128 * (t & 1), col_lo + vs * kStep, dhi, id_b);
-          umma_commit_lead(lead, &sm.o_full);
+          umma_commit_lead(lead, &sm.o_full[t & 1]);
           if (last) umma_commit_lead(lead, &sm.v_done[ci & 1]);
           // (a last chunk's k rows behind the end were zeroed before its Q K^T)
           if (h == 0 && lane == 0 && valid(ci) < kChunk) mbar_arrive(&sm.chunk_go[ci & 1]);
@@ -637,7 +638,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     for (int ci = 0, t = 0; ci < nc && !aborted; ++ci) {
       const int nv = valid(ci);
       for (int h = 0; h < nh; ++h, ++t) {
-        if (!dwait_warp(&sm.o_full, t & 1, st, 65, aborted, lim)) break;
+        if (!dwait_warp(&sm.o_full[t & 1], (t >> 1) & 1, st, 65, aborted, lim)) break;
         tc_fence_after();
         // o leaves tensor memory before anything else (the next tile's products wait for it)
         uint32_t w[2][16];
