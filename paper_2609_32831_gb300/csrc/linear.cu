@@ -126,9 +126,9 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 constexpr int kLThreads = 768;
 constexpr int kLRegLaunch = 80;  // registers per thread at launch, and after the warpgroups rebalance
 constexpr int kLRegP = 88;
-constexpr int kLRegEpilogue = 88;
-constexpr int kLRegState = 72;
-constexpr int kLRegOther = 56;
+constexpr int kLRegEpilogue = 80;
+constexpr int kLRegState = 80;
+constexpr int kLRegOther = 64;
 static_assert(256 * (kLRegP + kLRegEpilogue) + 128 * (kLRegState + kLRegOther) <= kLThreads * kLRegLaunch, "register split");
 constexpr int kWarpEpilogue = 8, kWarpState = 16, kWarpTma = 20, kWarpQk = 21, kWarpMma = 22, kWarpSlice = 23;
 constexpr uint32_t kTmemLinear = 512;
@@ -139,6 +139,7 @@ constexpr int kSlice = 16;  // tokens of one slice of decayed values
 constexpr int kSlices = kChunk / kSlice;
 constexpr uint32_t kSliceBytes = kSlice * kHeadDim * 2;
 constexpr float kLeastScale = 5.421010862427522e-20f;  // 2^-64
+constexpr int kHelpHeads = 2;  // query heads up to which WG0 and WG1 form the odd slices
 constexpr int kLSlots = 5;
 constexpr int kLFull = 8;  // "arrived" barriers, by load number: more than loads in flight
 
@@ -329,6 +330,10 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
   const int n_all = (len + kChunk - 1) / kChunk;  // chunks with a valid token
   const int nc = min(c.plan.chunks_per_run, n_all - c0);
   const int tiles = nc * nh;
+  // with few heads the update's chain of steps is longer than the tiles': WG0 and
+  // WG1 take a part of it (one head, 16 x up to 4097 tokens: 239 -> 233 us; with
+  // seven heads their tiles would wait for it: 267 -> 289 us for 8 x 8192)
+  const bool help = nh <= kHelpHeads;
   // a sequence's last run ends with the state behind its last token
   const bool last_state = part == 0 && grun + 1 == c.plan.run_begin[b + 1];
   auto valid = [&](int ci) { return min(kChunk, len - (c0 + ci) * kChunk); };
@@ -343,7 +348,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       mbar_init(&sm.s_full[s], 1);
       mbar_init(&sm.o_full[s], 1);
       mbar_init(&sm.p_full[s], 8);     // (arrivals: one per warp)
-      mbar_init(&sm.part_full[s], 4);
+      mbar_init(&sm.part_full[s], help && s == 1 ? 8 : 4);
       mbar_init(&sm.part_free[s], 1);
       mbar_init(&sm.chunk_go[s], 1);
       mbar_init(&sm.k_done[s], 1);
@@ -605,7 +610,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       if (!update) break;
       if (!dwait_warp(&sm.chunk_go[ci & 1], (ci >> 1) & 1, st, 67, aborted, lim)) break;  // V is there
       const uint8_t* v = sm.slot[sm.vs[ci & 1]];
-      for (int sl = 0; sl < kSlices; ++sl, ++n_slice) {
+      for (int sl = 0; sl < kSlices; sl += help ? 2 : 1, n_slice += help ? 2 : 1) {
         const int buf = n_slice & 1;
         if (n_slice >= 2 && !dwait_warp(&sm.part_free[buf], ((n_slice >> 1) - 1) & 1, st, 68, aborted, lim)) break;
         decay_slice<kSlice, 128>(v, sm.part[buf], sl, nv, r, [&](int j) { return sm.pw[nv - 1 - j]; });
@@ -691,7 +696,8 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     const uint32_t slot0 = tmem + ((uint32_t)wr << 16) + 64 * x;
     // (strong decay only) 1 / a_i
     const float inv_a = strong ? 1.f / fmaxf(sm.pw[r + 1], kLeastScale) : 0.f;
-    for (int t = 0; t < tiles; ++t) {
+    int n_odd = 0;
+    for (int t = 0, ci = 0, h = 0; t < tiles; ++t) {
       if (!dwait_warp(&sm.s_full[t & 1], (t >> 1) & 1, st, 64, aborted, lim)) break;
       tc_fence_after();
       const uint32_t slot = slot0 + 128 * (t & 1);
@@ -743,6 +749,21 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       tmem_wait_st();
       tc_fence_before();
       warp_arrive(&sm.p_full[t & 1], lane);
+      if (++h < nh) continue;
+      if (help && (ci + 1 < nc || last_state)) {  // the chunk's odd slices
+        if (!dwait_warp(&sm.chunk_go[ci & 1], (ci >> 1) & 1, st, 67, aborted, lim)) break;
+        const uint8_t* v = sm.slot[sm.vs[ci & 1]];
+        const int nv = valid(ci);
+        for (int sl = 1; sl < kSlices; sl += 2, ++n_odd) {
+          if (n_odd > 0 && !dwait_warp(&sm.part_free[1], (n_odd - 1) & 1, st, 68, aborted, lim)) break;
+          decay_slice<kSlice, 256>(v, sm.part[1], sl, nv, threadIdx.x, [&](int j) { return sm.pw[nv - 1 - j]; });
+          fence_proxy_async_smem();
+          warp_arrive(&sm.part_full[1], lane);
+        }
+        if (aborted) break;
+      }
+      h = 0;
+      ++ci;
     }
     tc_fence_before();
   }
