@@ -7,6 +7,7 @@ entry point; nothing here computes any part of the method.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import List, Optional, Sequence, Tuple
 
 import torch
@@ -595,9 +596,13 @@ def append_next(seg: Segment, k_new: torch.Tensor, v_new: torch.Tensor, base_pos
 
 # -------------------------------------- layers with a state of constant size
 
-def _rows(t: torch.Tensor) -> "_lib.UcRows":
+_pack_rows = struct.Struct("=Qqqq").pack   # uc_rows (bytes are built faster than a Structure)
+_pack_item = struct.Struct("=QQQQQ").pack  # uc_reorder_item
+
+
+def _rows(t: torch.Tensor) -> bytes:
     sb, sh, st, _ = t.stride()
-    return _lib.UcRows(t.data_ptr(), sb, sh, st)
+    return _pack_rows(t.data_ptr(), sb, sh, st)
 
 
 def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: Sequence[float],
@@ -629,7 +634,8 @@ def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: 
     elif out.shape != q.shape or out.dtype != q.dtype or out.stride(3) != 1:
         raise ValueError("linear_attend: out has q's shape and type, every row contiguous")
     if out_state is None:
-        out_state = torch.empty((B, hkv, d, d), dtype=torch.float32, device=q.device)
+        out_state = torch.empty((B, hkv, d, d), dtype=torch.float32, device=q.device) if state is None else \
+            torch.empty_like(state)
         if stream is not None:
             out_state.record_stream(stream)
     for s in (state, out_state):
@@ -637,9 +643,9 @@ def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: 
             raise ValueError("linear_attend: states are contiguous fp32 [B, Hkv, 128, 128]")
     ws = ws or default_workspace(q.device)
     L = lib()
-    args = (C.byref(_rows(q)), C.byref(_rows(k)), C.byref(_rows(v)), B, hq, hkv, T,
+    args = (_rows(q), _rows(k), _rows(v), B, hq, hkv, T,
             None if lengths is None else (C.c_int32 * B)(*lengths), (C.c_float * hkv)(*log_decay), _ptr(state),
-            out_state.data_ptr(), C.byref(_rows(out)))
+            out_state.data_ptr(), _rows(out))
     st = _stream(stream)
     code = L.uc_linear_attend(*args, *ws.get(256), st)
     if code == _lib.UC_ERR_OOM:   # nothing is launched then: only now is the size asked for
@@ -669,19 +675,22 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int, finished: Op
         raise ValueError("beam_select: finished is contiguous bool [B, K]")
     dev = logits.device
     best = torch.empty((B, n), dtype=torch.float32, device=dev)
-    at = torch.empty((2, B, n), dtype=torch.int32, device=dev)
+    parent = torch.empty((B, n), dtype=torch.int32, device=dev)
+    token = torch.empty_like(parent)
     done = torch.empty((B, n), dtype=torch.bool, device=dev)
     if stream is not None:
-        for t in (best, at, done):
+        for t in (best, parent, token, done):
             t.record_stream(stream)
-    parent, token = at.unbind(0)
     ws = ws or default_workspace(dev)
     L = lib()
-    wp, wn = ws.get(L.uc_beam_workspace_size(B, K, V, n))
-    check("uc_beam_select", L.uc_beam_select(
-        logits.data_ptr(), _LOGIT_TYPES[logits.dtype], logits.stride(0), logits.stride(1), B, K, V, scores.data_ptr(),
-        _ptr(finished), eos, n, best.data_ptr(), parent.data_ptr(), token.data_ptr(), done.data_ptr(), wp, wn,
-        _stream(stream)))
+    sb, sk, _ = logits.stride()
+    args = (logits.data_ptr(), _LOGIT_TYPES[logits.dtype], sb, sk, B, K, V, scores.data_ptr(), _ptr(finished), eos, n,
+            best.data_ptr(), parent.data_ptr(), token.data_ptr(), done.data_ptr())
+    st = _stream(stream)
+    code = L.uc_beam_select(*args, *ws.get(256), st)
+    if code == _lib.UC_ERR_OOM:   # nothing is launched then: only now is the size asked for
+        code = L.uc_beam_select(*args, *ws.get(L.uc_beam_workspace_size(B, K, V, n)), st)
+    check("uc_beam_select", code)
     return best, parent, token, done
 
 
@@ -699,14 +708,14 @@ def reorder(pairs, parent: torch.Tensor, ws: Optional[Workspace] = None, stream=
     for src, dst in pairs:
         if isinstance(src, Segment):
             have = src.batch
-            items.append(_lib.UcReorderItem(C.addressof(src.c), C.addressof(dst.c), None, None, 0))
+            items.append(_pack_item(C.addressof(src.c), C.addressof(dst.c), 0, 0, 0))
         else:
             have = src.shape[0]
             if not (src.is_contiguous() and dst.is_contiguous()) or src.dtype != dst.dtype \
                     or src.shape[1:] != dst.shape[1:] or dst.shape[0] != groups * n_to:
                 raise ValueError("reorder: tensors are contiguous [sequences, ...] of one type and shape per sequence")
-            items.append(_lib.UcReorderItem(None, None, src.data_ptr(), dst.data_ptr(),
-                                            src.element_size() * (src.numel() // have if have else 0)))
+            items.append(_pack_item(0, 0, src.data_ptr(), dst.data_ptr(),
+                                    src.element_size() * (src.numel() // have if have else 0)))
         if n_seq not in (None, have):
             raise ValueError("reorder: the sources hold different numbers of sequences")
         n_seq = have
@@ -714,7 +723,7 @@ def reorder(pairs, parent: torch.Tensor, ws: Optional[Workspace] = None, stream=
         raise ValueError("reorder: the sources' sequences are a multiple of the groups")
     ws = ws or default_workspace(parent.device)
     wp, wn = ws.get(256)
-    check("uc_reorder", lib().uc_reorder((_lib.UcReorderItem * len(items))(*items), len(items), parent.data_ptr(),
+    check("uc_reorder", lib().uc_reorder(b"".join(items), len(items), parent.data_ptr(),
                                          groups, n_seq // groups, n_to, wp, wn, _stream(stream)))
 
 

@@ -15,6 +15,8 @@
 //    Bound by HBM where rows are many: an SM's share is 11 two-byte logits per
 //    cycle, the exponentials alone take 16 of the SM's per cycle at most.
 // 2. beam_merge_kernel: one CTA per request joins its tiles.
+#include <algorithm>
+
 #include "common.cuh"
 #include "internal.h"
 #include "tcgen05.cuh"
@@ -538,7 +540,8 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_
 // wide where both blocks allow it, four bytes otherwise and at the end.
 constexpr int kCopyThreads = 256;
 
-__global__ void __launch_bounds__(kCopyThreads) reorder_kernel(const __grid_constant__ ReorderParams p) {
+template <int N>
+__global__ void __launch_bounds__(kCopyThreads) reorder_kernel(const __grid_constant__ ReorderParamsOf<N> p) {
   for (int u = blockIdx.x; u < p.n_units; u += gridDim.x) {
     int lo = 0, hi = p.n_arrays - 1;  // the array of this unit
     while (lo < hi) {
@@ -598,7 +601,21 @@ void launch_beam(const BeamParams& p, int dtype, cudaStream_t st) {
 }
 
 void launch_reorder(const ReorderParams& p, cudaStream_t st) {
-  reorder_kernel<<<p.n_units < 8 * num_sms() ? p.n_units : 8 * num_sms(), kCopyThreads, 0, st>>>(p);
+  const int grid = p.n_units < 8 * num_sms() ? p.n_units : 8 * num_sms();
+  if (p.n_arrays <= kReorderFew) {  // (18 KB of parameters are a good part of a small call's launch)
+    ReorderParamsOf<kReorderFew> few;
+    std::copy(p.a, p.a + p.n_arrays, few.a);
+    few.parent = p.parent;
+    few.status = p.status;
+    few.n_arrays = p.n_arrays;
+    few.n_seq = p.n_seq;
+    few.n_from = p.n_from;
+    few.n_to = p.n_to;
+    few.n_units = p.n_units;
+    reorder_kernel<kReorderFew><<<grid, kCopyThreads, 0, st>>>(few);
+  } else {
+    reorder_kernel<kReorderArrays><<<grid, kCopyThreads, 0, st>>>(p);
+  }
   count_launch();
 }
 

@@ -369,12 +369,15 @@ struct ReorderArray {
 };
 constexpr int kReorderArrays = 256;  // arrays of one launch
 constexpr int kReorderBytes = 16384;  // bytes of a work unit
-struct ReorderParams {
-  ReorderArray a[kReorderArrays];
+constexpr int kReorderFew = 32;       // arrays of a launch whose parameters are a tenth of the full size
+template <int N>
+struct ReorderParamsOf {
+  ReorderArray a[N];
   const int32_t* parent;
   DevStatus* status;
   int32_t n_arrays, n_seq, n_from, n_to, n_units;
 };
+using ReorderParams = ReorderParamsOf<kReorderArrays>;
 void launch_reorder(const ReorderParams& p, cudaStream_t st);
 
 // Shared by the files with C-ABI entry points (defined in api.cu).
