@@ -126,9 +126,9 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 constexpr int kLThreads = 768;
 constexpr int kLRegLaunch = 80;  // registers per thread at launch, and after the warpgroups rebalance
 constexpr int kLRegP = 88;
-constexpr int kLRegEpilogue = 80;
+constexpr int kLRegEpilogue = 72;
 constexpr int kLRegState = 80;
-constexpr int kLRegOther = 64;
+constexpr int kLRegOther = 72;
 static_assert(256 * (kLRegP + kLRegEpilogue) + 128 * (kLRegState + kLRegOther) <= kLThreads * kLRegLaunch, "register split");
 constexpr int kWarpEpilogue = 8, kWarpState = 16, kWarpTma = 20, kWarpQk = 21, kWarpMma = 22, kWarpSlice = 23;
 constexpr uint32_t kTmemLinear = 512;
@@ -217,17 +217,18 @@ __device__ __forceinline__ void issue_ss(uint32_t lead, uint32_t d, uint32_t a, 
       "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc), "r"(lead)
       : "memory");
 }
-__device__ __forceinline__ void issue_ts(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id) {
+__device__ __forceinline__ void issue_ts(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id,
+                                         uint32_t acc) {
   asm volatile(
       "{\n"
       ".reg .pred p, q;\n"
       ".reg .b64 db;\n"
       "setp.ne.b32 q, %5, 0;\n"
-      "setp.eq.b32 p, 0, 0;\n"
+      "setp.ne.b32 p, %6, 0;\n"
       "mov.b64 db, {%2, %3};\n"
       "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n"
       "}\n" ::"r"(d),
-      "r"(a), "r"(b), "r"(hi), "r"(id), "r"(lead)
+      "r"(a), "r"(b), "r"(hi), "r"(id), "r"(lead), "r"(acc)
       : "memory");
 }
 // The three products of a tile, in loops of one step each: 24 warps share the
@@ -240,17 +241,19 @@ __device__ __forceinline__ void issue_q_k(uint32_t lead, uint32_t d, uint32_t a,
     issue_ss(lead, d, a + off, b + off, hi, id, k);
   }
 }
-// O = Q S: the state's key channels along its rows (16 rows of 128 B per step).
-__device__ __forceinline__ void issue_q_s(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id) {
+// O (+)= Q S: the state's key channels along its rows (16 rows of 128 B per step).
+__device__ __forceinline__ void issue_q_s(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id,
+                                          uint32_t acc) {
 #pragma unroll 1
   for (uint32_t k = 0; k < 8; ++k)
-    issue_ss(lead, d, a + (k & 3) * 2 + (k >> 2) * (kTileBytes >> 5), b + 128 * k, hi, id, k);
+    issue_ss(lead, d, a + (k & 3) * 2 + (k >> 2) * (kTileBytes >> 5), b + 128 * k, hi, id, acc | k);
 }
-// O += P V: P of keys 0-63 in the slot's columns 0-31, of keys 64-127 in 64-95
+// O (+)= P V: P of keys 0-63 in the slot's columns 0-31, of keys 64-127 in 64-95
 // (each warpgroup's P lies in the columns that it alone read).
-__device__ __forceinline__ void issue_p_v(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id) {
+__device__ __forceinline__ void issue_p_v(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id,
+                                          uint32_t acc) {
 #pragma unroll 1
-  for (uint32_t k = 0; k < 8; ++k) issue_ts(lead, d, a + 8 * k + 32 * (k >> 2), b + 128 * k, hi, id);
+  for (uint32_t k = 0; k < 8; ++k) issue_ts(lead, d, a + 8 * k + 32 * (k >> 2), b + 128 * k, hi, id, acc | k);
 }
 
 // The decayed values of tokens ROWS sl .. ROWS sl + ROWS - 1 of a chunk as
@@ -331,7 +334,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
   const int nc = min(c.plan.chunks_per_run, n_all - c0);
   const int tiles = nc * nh;
   // with few heads the update's chain of steps is longer than the tiles': WG0 and
-  // WG1 take a part of it (one head, 16 x up to 4097 tokens: 239 -> 233 us; with
+  // WG1 take a part of it (one head, 16 x up to 4097 tokens: 239 -> 233 us when it was added; with
   // seven heads their tiles would wait for it: 267 -> 289 us for 8 x 8192)
   const bool help = nh <= kHelpHeads;
   // a sequence's last run ends with the state behind its last token
@@ -479,17 +482,27 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
               sm.vs[ci & 1] = vs;
               if (valid(ci) == kChunk) mbar_arrive(&sm.chunk_go[ci & 1]);  // the chunk's k and v are there
             }
-            // the chunk's state is in shared memory, the next scaled in place
-            if (!dwait_warp(&sm.st_ready, ci & 1, st, 57, aborted, lim)) break;
           }
           if (t > 0 && !dwait_warp(&sm.o_free, (t - 1) & 1, st, 59, aborted, lim)) break;
-          tc_fence_after();
-          issue_q_s(lead, tm + kColOut, row_lo + qs * kStep, s_lo, dhi, id_b);
-          if (last) umma_commit_lead(lead, &sm.s_free);
+          // Q S, then P V; a chunk's first tile the other way round, since the
+          // state is the last to come
+          if (h > 0) {
+            tc_fence_after();
+            issue_q_s(lead, tm + kColOut, row_lo + qs * kStep, s_lo, dhi, id_b, 0u);
+            if (last) umma_commit_lead(lead, &sm.s_free);
+          }
           if (!dwait_warp(&sm.p_full[t & 1], (t >> 1) & 1, st, 61, aborted, lim)) break;
           tc_fence_after();
-          umma_commit_lead(lead, &sm.empty[qs]);  // Q S is issued, and Q K^T was done before P
-          issue_p_v(lead, tm + kColOut, tm + 128 * (t & 1), col_lo + vs * kStep, dhi, id_b);
+          if (h > 0) umma_commit_lead(lead, &sm.empty[qs]);  // Q S is issued, and Q K^T was done before P
+          issue_p_v(lead, tm + kColOut, tm + 128 * (t & 1), col_lo + vs * kStep, dhi, id_b, h > 0);
+          if (h == 0) {
+            // the chunk's state is in shared memory, the next scaled in place
+            if (!dwait_warp(&sm.st_ready, ci & 1, st, 57, aborted, lim)) break;
+            tc_fence_after();
+            issue_q_s(lead, tm + kColOut, row_lo + qs * kStep, s_lo, dhi, id_b, 1u);
+            if (last) umma_commit_lead(lead, &sm.s_free);
+            umma_commit_lead(lead, &sm.empty[qs]);
+          }
           umma_commit_lead(lead, &sm.o_full[t & 1]);
           if (last) umma_commit_lead(lead, &sm.v_done[ci & 1]);
           // (a last chunk's k rows behind the end were zeroed before its Q K^T)
@@ -554,11 +567,6 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       const int chunk16 = 4 * (blk & 1) + e;  // 16 bytes of the row's half
       return reinterpret_cast<uint4*>(sm.s + (blk >> 1) * (kTileBytes / 2) + r * 128 + ((chunk16 ^ (r & 7)) << 4));
     };
-    // what rounding leaves; nothing where the state has overflowed
-    auto rest = [](float x, float rounded) {
-      const float d = x - rounded;
-      return d == d ? d : 0.f;
-    };
     // 32 channels of the state: tensor memory's part and the copy's, scaled by g
     // since it was made (g = 0: there is none yet)
     auto whole_state = [&](int blk, uint32_t(&x)[32], float g) {
@@ -571,8 +579,11 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
         const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          x[8 * e + 2 * u] = __float_as_uint(fmaf(bf16_lo(w[u]), g, __uint_as_float(x[8 * e + 2 * u])));
-          x[8 * e + 2 * u + 1] = __float_as_uint(fmaf(bf16_hi(w[u]), g, __uint_as_float(x[8 * e + 2 * u + 1])));
+          float a, b;
+          f2_unpack(f2_fma(f2_pack(bf16_lo(w[u]), bf16_hi(w[u])), f2_pack(g, g),
+                           f2_pack(__uint_as_float(x[8 * e + 2 * u]), __uint_as_float(x[8 * e + 2 * u + 1]))), a, b);
+          x[8 * e + 2 * u] = __float_as_uint(a);
+          x[8 * e + 2 * u + 1] = __float_as_uint(b);
         }
       }
     };
@@ -594,10 +605,13 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
           uint32_t w[4];
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            uint32_t &a = x[8 * e + 2 * u], &c = x[8 * e + 2 * u + 1];
-            w[u] = pack_bf16(__uint_as_float(a), __uint_as_float(c));
-            a = __float_as_uint(rest(__uint_as_float(a), bf16_lo(w[u])) * g);
-            c = __float_as_uint(rest(__uint_as_float(c), bf16_hi(w[u])) * g);
+            float a = __uint_as_float(x[8 * e + 2 * u]), c = __uint_as_float(x[8 * e + 2 * u + 1]);
+            w[u] = pack_bf16(a, c);
+            // what rounding leaves (anything finite where the state has overflowed)
+            f2_unpack(f2_fma(f2_pack(bf16_lo(w[u]), bf16_hi(w[u])), f2_pack(-1.f, -1.f), f2_pack(a, c)), a, c);
+            f2_unpack(f2_mul(f2_pack(fminf(a, 3e38f), fminf(c, 3e38f)), f2_pack(g, g)), a, c);
+            x[8 * e + 2 * u] = __float_as_uint(a);
+            x[8 * e + 2 * u + 1] = __float_as_uint(c);
           }
           *copy(blk, e) = make_uint4(w[0], w[1], w[2], w[3]);
         }
