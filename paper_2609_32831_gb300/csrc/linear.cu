@@ -14,56 +14,93 @@ namespace uc {
 // One CTA per (sequence, KV head, 32 value channels): a state column needs
 // its own value channel only, so column slices are independent. Warp w holds
 // rows (key channels) 16 w .. 16 w + 15, lane l the column 32 slice + l; the
-// partial sums over a warp's rows meet in shared memory.
+// partial sums over a warp's rows meet in shared memory. Everything is loaded
+// before the first token is taken: the state into registers, k, v and (where
+// they fit) q of all tokens into shared memory.
 constexpr int kStepCols = 32;
 constexpr int kStepWarps = 8;
 constexpr int kStepRows = kHeadDim / kStepWarps;
-constexpr int kStepHeads = 8;  // query heads reduced at a time
+constexpr int kStepHeads = 8;   // query heads reduced at a time
+constexpr int kStepQRows = 64;  // rows of q in shared memory
 
 __global__ void __launch_bounds__(32 * kStepWarps) linear_step_kernel(const __grid_constant__ LinearParams p) {
-  __shared__ float qs[kStepHeads][kHeadDim];
-  __shared__ float part[kStepHeads][kStepWarps][kStepCols];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __shared__ __align__(16) __nv_bfloat16 qs[kStepQRows][kHeadDim];
+  __shared__ __align__(16) __nv_bfloat16 ks[UC_MAX_QTOKENS][kHeadDim];
+  __shared__ __nv_bfloat16 vs[UC_MAX_QTOKENS][kStepCols];
+  __shared__ float part[2][kStepHeads][kStepWarps][kStepCols];  // in turns
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   constexpr int kSlices = kHeadDim / kStepCols;
   const int bh = blockIdx.x / kSlices, slice = blockIdx.x % kSlices;
   const int b = bh / p.n_kv_heads, kvh = bh % p.n_kv_heads;
-  const int col = slice * kStepCols + lane;
-  const int n = p.lengths[b];
+  const int n = min(p.lengths[b], p.n_tok);
   // gamma as two fp32 parts: rounded to one, a decay that remembers thousands
   // of tokens would drift by their number times 2^-25
   const float g_hi = p.decay[kvh].x, g_lo = p.decay[kvh].y;
   float s[kStepRows];
-  const size_t at = ((size_t)bh * kHeadDim + warp * kStepRows) * kHeadDim + col;
+  const size_t at = ((size_t)bh * kHeadDim + warp * kStepRows) * kHeadDim + slice * kStepCols + lane;
 #pragma unroll
   for (int r = 0; r < kStepRows; ++r) s[r] = p.state_in ? p.state_in[at + (size_t)r * kHeadDim] : 0.f;
+  constexpr int kRow16 = kHeadDim / 8;  // 16-byte pieces of a row
+  for (int i = tid; i < n * kRow16; i += 32 * kStepWarps)
+    reinterpret_cast<uint4*>(ks[i / kRow16])[i % kRow16] =
+        reinterpret_cast<const uint4*>(p.k.at(b, kvh, i / kRow16))[i % kRow16];
+  for (int i = tid; i < n * kStepCols; i += 32 * kStepWarps)
+    vs[i / kStepCols][i % kStepCols] = p.v.at(b, kvh, i / kStepCols)[slice * kStepCols + i % kStepCols];
+  auto load_q = [&](int rows, auto&& from) {  // rows of q, the t and head of each by from()
+    for (int i = tid; i < rows * kRow16; i += 32 * kStepWarps) {
+      const int2 th = from(i / kRow16);
+      reinterpret_cast<uint4*>(qs[i / kRow16])[i % kRow16] =
+          reinterpret_cast<const uint4*>(p.q.at(b, kvh * p.group + th.y, th.x))[i % kRow16];
+    }
+  };
+  const bool all = p.n_tok * p.group <= kStepQRows;
+  if (all) load_q(n * p.group, [&](int i) { return make_int2(i / p.group, i % p.group); });
+  __syncthreads();
+  int turn = 0;
   for (int t = 0; t < p.n_tok; ++t) {
     if (t < n) {
-      const __nv_bfloat16* kr = p.k.at(b, kvh, t);
-      const float v = __bfloat162float(p.v.at(b, kvh, t)[col]);
+      const float v = __bfloat162float(vs[t][lane]);
 #pragma unroll
-      for (int r = 0; r < kStepRows; ++r) s[r] = fmaf(s[r], g_hi, fmaf(s[r], g_lo, __bfloat162float(kr[warp * kStepRows + r]) * v));
+      for (int r = 0; r < kStepRows; r += 8) {
+        const uint4 k8 = *reinterpret_cast<const uint4*>(&ks[t][warp * kStepRows + r]);
+        const uint32_t w[4] = {k8.x, k8.y, k8.z, k8.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          s[r + 2 * u] = fmaf(s[r + 2 * u], g_hi, fmaf(s[r + 2 * u], g_lo, bf16_lo(w[u]) * v));
+          s[r + 2 * u + 1] = fmaf(s[r + 2 * u + 1], g_hi, fmaf(s[r + 2 * u + 1], g_lo, bf16_hi(w[u]) * v));
+        }
+      }
     }
-    for (int h0 = 0; h0 < p.group; h0 += kStepHeads) {
+    for (int h0 = 0; h0 < p.group; h0 += kStepHeads, turn ^= 1) {
       const int nh = min(kStepHeads, p.group - h0);
-      __syncthreads();
-      for (int i = threadIdx.x; i < nh * kHeadDim; i += blockDim.x)
-        qs[i / kHeadDim][i % kHeadDim] =
-            t < n ? __bfloat162float(p.q.at(b, kvh * p.group + h0 + i / kHeadDim, t)[i % kHeadDim]) : 0.f;
-      __syncthreads();
-      for (int h = 0; h < nh; ++h) {
-        float o = 0.f;
+      if (!all && t < n) {
+        __syncthreads();  // (the last heads' q has been read)
+        load_q(nh, [&](int i) { return make_int2(t, h0 + i); });
+        __syncthreads();
+      }
+      if (t < n) {
+        const int row = all ? t * p.group + h0 : 0;
+        for (int h = 0; h < nh; ++h) {
+          float o = 0.f;
 #pragma unroll
-        for (int r = 0; r < kStepRows; ++r) o = fmaf(qs[h][warp * kStepRows + r], s[r], o);
-        part[h][warp][lane] = o;
+          for (int r = 0; r < kStepRows; r += 8) {
+            const uint4 q8 = *reinterpret_cast<const uint4*>(&qs[row + h][warp * kStepRows + r]);
+            const uint32_t w[4] = {q8.x, q8.y, q8.z, q8.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) o = fmaf(bf16_hi(w[u]), s[r + 2 * u + 1], fmaf(bf16_lo(w[u]), s[r + 2 * u], o));
+          }
+          part[turn][h][warp][lane] = o;
+        }
       }
       __syncthreads();
-      for (int i = threadIdx.x; i < nh * kStepCols; i += blockDim.x) {
+      for (int i = tid; i < nh * kStepCols; i += 32 * kStepWarps) {
         float o = 0.f;
+        if (t < n)
 #pragma unroll
-        for (int w = 0; w < kStepWarps; ++w) o += part[i / kStepCols][w][i % kStepCols];
+          for (int w = 0; w < kStepWarps; ++w) o += part[turn][i / kStepCols][w][i % kStepCols];
         // a token behind the sequence's end has no output: zero
         p.out.at(b, kvh * p.group + h0 + i / kStepCols, t)[slice * kStepCols + i % kStepCols] =
-            __float2bfloat16_rn(t < n ? o * p.scale : 0.f);
+            __float2bfloat16_rn(o * p.scale);
       }
     }
   }
