@@ -16,7 +16,11 @@ namespace uc {
 // rows (key channels) 16 w .. 16 w + 15, lane l the column 32 slice + l; the
 // partial sums over a warp's rows meet in shared memory. Everything is loaded
 // before the first token is taken: the state into registers, k, v and (where
-// they fit) q of all tokens into shared memory.
+// they fit) q of all tokens into shared memory. Bound by HBM in large batches:
+// 64 sequences of 4 heads, 34.6 MB: 8.5 us, 4.1 TB/s; by the latency of its
+// loads and one reduction per token in small ones (one sequence: 3.7 us).
+// (Loads token by token: 9.1 and 4.1 us, five tokens of 8 x 16 heads 10.1
+// instead of 8.0.)
 constexpr int kStepCols = 32;
 constexpr int kStepWarps = 8;
 constexpr int kStepRows = kHeadDim / kStepWarps;
@@ -119,9 +123,14 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 //   o_i  = a_i (q_i S + sum_{j <= i} (q_i . k_j) gamma^{-(j+1)} v_j) / sqrt(128),  a_i = gamma^{i+1}
 //   S'   = gamma^nv S + sum_j k_j (gamma^{nv-1-j} v_j)^T
 // so a chunk costs three 128^3 products per query head (Q K^T, Q S and P V, the
-// last two into one accumulator) and one per KV head for the state. Bound by
+// last two into one accumulator) and one per KV head for the state. The floor is
 // HBM: 64 KB of q and o per head and chunk, 1.5 us of an SM's share, against
-// 3 x 512 cycles of the tensor pipe.
+// 3 x 512 cycles of the tensor pipe. What bounds it are hand-overs between
+// warps: with seven heads a tile's (o read, Q S, P V: 3600 cycles), with one
+// head those of the state's update (9 to 10 thousand cycles a chunk).
+// 8 x 8192 tokens, 28 query and 4 KV heads: 267 us, 4.0 TB/s of q, k, v and o;
+// 16 x up to 4097 tokens of 16 heads: 217 us, 2.9 TB/s; 131072 tokens: 455 to
+// 483 us, 4.6 TB/s.
 //
 // One CTA per (sequence, KV head, run of chunks, part of its query heads):
 //   WG0, WG1 (warps 0-7) halves of the columns of Q K^T: P = mask and weights,
@@ -141,7 +150,7 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 //   warp 20  TMA producer: k and v tiles per chunk and a q tile per head, in the
 //            order they are needed, each into whichever slot is free
 //   warp 21  issues Q K^T, one tile ahead
-//   warp 22  issues Q S and P V
+//   warp 22  issues Q S and P V (a chunk's first tile: P V and Q S)
 //   warp 23  issues the slices' products and releases the chunk's k and v slots
 //            (one warp for all of it: its own waits and issues took 3500 cycles a tile)
 // In a sequence's last chunk, warps 21 and 22 first zero the k and v rows behind
@@ -831,7 +840,8 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
 // start, so the chunks add up without a rescale: each one's sum in tensor
 // memory from zero, in turns of two, and all of them in registers (rounded,
 // where the tensor cores cut). Four groups of four warps form the decayed
-// values, a quarter chunk each, and hold a quarter of the channels.
+// values, a quarter chunk each, and hold a quarter of the channels. A pass over
+// k and v: about 4000 cycles a chunk, bound by forming the three parts.
 constexpr int kLocalRing = 2;  // chunks in flight
 constexpr int kQuarter = kChunk / 4;
 constexpr uint32_t kQuarterBytes = kQuarter * kHeadDim * 2;
