@@ -642,7 +642,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
         break;
       tc_fence_after();
       const float g = sm.pw[nv];
-#pragma unroll
+#pragma unroll 1
       for (int blk = 0; blk < 4; ++blk) {
         uint32_t x[32];
         whole_state(blk, x, ci > 0 ? sm.pw[kChunk] : 0.f);
