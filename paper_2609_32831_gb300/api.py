@@ -710,9 +710,10 @@ def reorder(pairs, parent: torch.Tensor, ws: Optional[Workspace] = None, stream=
             have = src.batch
             items.append(_pack_item(C.addressof(src.c), C.addressof(dst.c), 0, 0, 0))
         else:
-            have = src.shape[0]
-            if not (src.is_contiguous() and dst.is_contiguous()) or src.dtype != dst.dtype \
-                    or src.shape[1:] != dst.shape[1:] or dst.shape[0] != groups * n_to:
+            have, *rest = src.shape
+            to, *same = dst.shape
+            if rest != same or to != groups * n_to or src.dtype != dst.dtype \
+                    or not (src.is_contiguous() and dst.is_contiguous()):
                 raise ValueError("reorder: tensors are contiguous [sequences, ...] of one type and shape per sequence")
             items.append(_pack_item(0, 0, src.data_ptr(), dst.data_ptr(),
                                     src.element_size() * (src.numel() // have if have else 0)))

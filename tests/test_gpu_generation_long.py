@@ -119,3 +119,44 @@ def test_an_overflowed_state_stays_infinite():
     assert new[0, 0, 3, 5].item() == float("inf") and new[0, 0, 4, 6].item() == float("-inf")
     new[0, 0, 3, 5] = new[0, 0, 4, 6] = new[0, 0, 0, 0]
     assert torch.isfinite(new).all()
+
+
+def test_a_step_replays_from_a_graph():
+    """One decoding step (a linear layer, the selection, the reorder) and a
+    prompt, captured once and replayed over new inputs, equal the calls."""
+    B, K, V, hq, hkv = 2, 3, 5000, 6, 2
+    S = B * K
+    g = torch.Generator(device=DEV).manual_seed(3)
+    rand = lambda *s: torch.randn(s, generator=g, device=DEV)
+    decay = [-0.01, -0.4]
+    qkv = [rand(S, h, 1, 128).bfloat16() for h in (hq, hkv, hkv)]
+    prompt = [rand(B, h, 400, 128).bfloat16() for h in (hq, hkv, hkv)]
+    state, moved, new = (torch.empty((n, hkv, 128, 128), device=DEV) for n in (S, S, B))
+    logits, scores = rand(B, K, V), rand(B, K)
+    ws = uc.Workspace(DEV)
+
+    def step():
+        o = uc.linear_attend(*qkv, decay, state=state, out_state=state, ws=ws)[0]
+        sel = uc.beam_select(logits, scores, K, eos=1, ws=ws)
+        uc.reorder([(state, moved)], sel[1], ws=ws)
+        p = uc.linear_attend(*prompt, decay, out_state=new, ws=ws)[0]
+        return (o, *sel, p)
+
+    start = rand(S, hkv, 128, 128)
+    state.copy_(start)
+    step()  # (the workspace has its size before the capture)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for i in range(3):
+        for t in qkv + prompt:
+            t.copy_(torch.randn(t.shape, generator=g, device=DEV))
+        logits.normal_(generator=g)
+        state.copy_(start)
+        graph.replay()
+        got_now = [t.clone() for t in got] + [moved.clone(), new.clone(), state.clone()]
+        state.copy_(start)
+        want = [*step(), moved, new, state]
+        for a, b in zip(got_now, want):
+            assert torch.equal(a, b)
+    assert ws.status() == 0
