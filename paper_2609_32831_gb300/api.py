@@ -600,11 +600,6 @@ _pack_rows = struct.Struct("=Qqqq").pack   # uc_rows (bytes are built faster tha
 _pack_item = struct.Struct("=QQQQQ").pack  # uc_reorder_item
 
 
-def _rows(t: torch.Tensor) -> bytes:
-    sb, sh, st, _ = t.stride()
-    return _pack_rows(t.data_ptr(), sb, sh, st)
-
-
 def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: Sequence[float],
                   state: Optional[torch.Tensor] = None, out_state: Optional[torch.Tensor] = None,
                   lengths: Optional[Sequence[int]] = None, out: Optional[torch.Tensor] = None,
@@ -620,10 +615,12 @@ def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: 
     sequence (None: T); outputs behind them are zero. Returns (out, out_state),
     out with q's shape and strides."""
     B, hq, T, d = q.shape
-    hkv = k.shape[1]
-    if q.dtype != torch.bfloat16 or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16 or d != HEAD_DIM:
+    kv = k.shape
+    hkv = kv[1]
+    sq, sk, sv = q.stride(), k.stride(), v.stride()
+    if not q.dtype is k.dtype is v.dtype is torch.bfloat16 or d != HEAD_DIM:
         raise ValueError("linear_attend: q, k and v are bf16 with 128 channels")
-    if k.shape != (B, hkv, T, d) or v.shape != k.shape or q.stride(3) != 1 or k.stride(3) != 1 or v.stride(3) != 1:
+    if kv != (B, hkv, T, d) or v.shape != kv or not sq[3] == sk[3] == sv[3] == 1:
         raise ValueError("linear_attend: k and v are [B, Hkv, T, 128], every row contiguous")
     if len(log_decay) != hkv or (lengths is not None and len(lengths) != B):
         raise ValueError("linear_attend: one log_decay per KV head, one length per sequence")
@@ -633,19 +630,21 @@ def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: 
             out.record_stream(stream)
     elif out.shape != q.shape or out.dtype != q.dtype or out.stride(3) != 1:
         raise ValueError("linear_attend: out has q's shape and type, every row contiguous")
+    for s in (state,) if out_state is None or out_state is state else (state, out_state):
+        if s is not None and (s.shape != (B, hkv, d, d) or s.dtype is not torch.float32 or not s.is_contiguous()):
+            raise ValueError("linear_attend: states are contiguous fp32 [B, Hkv, 128, 128]")
     if out_state is None:
         out_state = torch.empty((B, hkv, d, d), dtype=torch.float32, device=q.device) if state is None else \
             torch.empty_like(state)
         if stream is not None:
             out_state.record_stream(stream)
-    for s in (state, out_state):
-        if s is not None and (s.shape != (B, hkv, d, d) or s.dtype != torch.float32 or not s.is_contiguous()):
-            raise ValueError("linear_attend: states are contiguous fp32 [B, Hkv, 128, 128]")
     ws = ws or default_workspace(q.device)
     L = lib()
-    args = (_rows(q), _rows(k), _rows(v), B, hq, hkv, T,
+    so = out.stride()
+    args = (_pack_rows(q.data_ptr(), sq[0], sq[1], sq[2]), _pack_rows(k.data_ptr(), sk[0], sk[1], sk[2]),
+            _pack_rows(v.data_ptr(), sv[0], sv[1], sv[2]), B, hq, hkv, T,
             None if lengths is None else (C.c_int32 * B)(*lengths), (C.c_float * hkv)(*log_decay), _ptr(state),
-            out_state.data_ptr(), _rows(out))
+            out_state.data_ptr(), _pack_rows(out.data_ptr(), so[0], so[1], so[2]))
     st = _stream(stream)
     code = L.uc_linear_attend(*args, *ws.get(256), st)
     if code == _lib.UC_ERR_OOM:   # nothing is launched then: only now is the size asked for
@@ -666,7 +665,9 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int, finished: Op
     [B, K] bool or None -> (scores fp32, parent int32, token int32, finished
     bool), each [B, n], best first."""
     B, K, V = logits.shape
-    if logits.dtype not in _LOGIT_TYPES or logits.stride(2) != 1:
+    sb, sk, sv = logits.stride()
+    kind = _LOGIT_TYPES.get(logits.dtype)
+    if kind is None or sv != 1:
         raise ValueError("beam_select: logits are fp32, bf16 or fp16 with contiguous rows")
     if scores.shape != (B, K) or scores.dtype != torch.float32 or not scores.is_contiguous():
         raise ValueError("beam_select: scores are contiguous fp32 [B, K]")
@@ -683,8 +684,7 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int, finished: Op
             t.record_stream(stream)
     ws = ws or default_workspace(dev)
     L = lib()
-    sb, sk, _ = logits.stride()
-    args = (logits.data_ptr(), _LOGIT_TYPES[logits.dtype], sb, sk, B, K, V, scores.data_ptr(), _ptr(finished), eos, n,
+    args = (logits.data_ptr(), kind, sb, sk, B, K, V, scores.data_ptr(), _ptr(finished), eos, n,
             best.data_ptr(), parent.data_ptr(), token.data_ptr(), done.data_ptr())
     st = _stream(stream)
     code = L.uc_beam_select(*args, *ws.get(256), st)
