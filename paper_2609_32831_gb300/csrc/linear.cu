@@ -127,10 +127,10 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 // HBM: 64 KB of q and o per head and chunk, 1.5 us of an SM's share, against
 // 3 x 512 cycles of the tensor pipe. What bounds it are hand-overs between
 // warps: with seven heads a tile's (o read, Q S, P V: 3600 cycles), with one
-// head those of the state's update (9 to 10 thousand cycles a chunk).
-// 8 x 8192 tokens, 28 query and 4 KV heads: 267 us, 4.0 TB/s of q, k, v and o;
-// 16 x up to 4097 tokens of 16 heads: 217 us, 2.9 TB/s; 131072 tokens: 455 to
-// 483 us, 4.6 TB/s.
+// head those of the state's update (10 to 11 thousand cycles a chunk).
+// 8 x 8192 tokens, 28 query and 4 KV heads: 263 us, 4.1 TB/s of q, k, v and o;
+// 16 x up to 4097 tokens of 16 heads: 214 us, 3.0 TB/s; 131072 tokens: 456 to
+// 475 us, 4.6 TB/s.
 //
 // One CTA per (sequence, KV head, run of chunks, part of its query heads):
 //   WG0, WG1 (warps 0-7) halves of the columns of Q K^T: P = mask and weights,
@@ -141,7 +141,8 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 //   WG4      (16-19) the state. It stays in tensor memory in fp32; per chunk
 //            its bf16 copy goes to shared memory for Q S, what that rounding
 //            left stays behind, scaled by gamma^nv, and the chunk's decayed
-//            values are formed in slices of 16 tokens that accumulate on the
+//            values are formed in slices of 16 tokens (with one or two heads
+//            the odd ones by WG0 and WG1) that accumulate on the
 //            rest while the chunk's tiles run; the copy joins them, scaled,
 //            in fp32. (The tensor cores' sums are cut, not rounded: 24 of them
 //            per chunk on the whole state pulled it towards zero by up to 1.2e-5
