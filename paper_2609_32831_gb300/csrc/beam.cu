@@ -436,12 +436,11 @@ struct CandKey {
 };
 
 constexpr int kMergeThreads = 256;
-constexpr int kMergeHeads = 512;  // lists whose heads fit shared memory
 constexpr int kMaxMerge = UC_MAX_BEAM_OUT * UC_MAX_BEAM_OUT;  // n lists of n candidates
 
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_constant__ BeamParams p) {
   __shared__ float s_base[UC_MAX_BEAMS], s_log[UC_MAX_BEAMS], s_score[UC_MAX_BEAMS];
-  __shared__ CandKey s_tau, s_key[kMaxMerge], s_head[kMergeHeads];
+  __shared__ CandKey s_tau, s_key[kMaxMerge], s_head[kBeamLists];
   __shared__ int s_id[kMaxMerge], s_list[UC_MAX_BEAM_OUT];
   __shared__ int s_count, s_lists;
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
@@ -495,22 +494,21 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(const __grid_
   };
   // the n-th best list head bounds the result from below, and only n lists
   // reach it
-  for (int l = tid; l < min(lists, kMergeHeads); l += kMergeThreads) s_head[l] = key_of(l, 0);
+  for (int l = tid; l < lists; l += kMergeThreads) s_head[l] = key_of(l, 0);
   __syncthreads();
   if (lists > n) {
     for (int l = tid; l < lists; l += kMergeThreads) {
-      const CandKey mine = l < kMergeHeads ? s_head[l] : key_of(l, 0);
+      const CandKey mine = s_head[l];
       int rank = 0;
 #pragma unroll 8
-      for (int o = 0; o < min(lists, kMergeHeads); ++o) rank += s_head[o].before(mine);
-      for (int o = kMergeHeads; o < lists && rank < n; ++o) rank += key_of(o, 0).before(mine);
+      for (int o = 0; o < lists; ++o) rank += s_head[o].before(mine);
       if (rank == n - 1) s_tau = mine;  // (no two candidates are equal; where fewer exist, none is the n-th)
     }
     __syncthreads();
   }
   const CandKey tau = s_tau;
   for (int l = tid; l < lists; l += kMergeThreads) {
-    const CandKey head = l < kMergeHeads ? s_head[l] : key_of(l, 0);
+    const CandKey head = s_head[l];
     if ((head.a | head.b) != 0 && !tau.before(head)) s_list[atomicAdd(&s_lists, 1)] = l;
   }
   __syncthreads();

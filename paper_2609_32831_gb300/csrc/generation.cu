@@ -257,10 +257,10 @@ static int64_t most_tiles(int64_t vecs) { return vecs < 64 * kBeamMinSpan ? (vec
 // kStart is a CTA's start, first bound and ranking, in vectors' time: from 1024
 // on 256 rows of 18751 vectors stay whole (36 us), below they become seven
 // tiles each (47 us); few rows are cut as far as kBeamMinSpan either way.
-static int beam_span(int64_t rows, int64_t vecs, int64_t slots) {
+static int beam_span(int64_t rows, int n_beams, int64_t vecs, int64_t slots) {
   constexpr int64_t kStart = 2048;
   int64_t best = vecs, cost = INT64_MAX;
-  for (int64_t t = 1; t <= most_tiles(vecs); ++t) {
+  for (int64_t t = 1; t <= most_tiles(vecs) && t * n_beams <= kBeamLists; ++t) {
     const int64_t span = ((vecs + t - 1) / t + 31) / 32 * 32;
     const int64_t c = (rows * t + slots - 1) / slots * (kStart + span);
     if (c < cost) {
@@ -325,7 +325,7 @@ uc_status uc_beam_select(const void* logits, int32_t dtype, int64_t stride_b, in
   p.vocab = vocab;
   p.n = n;
   const int64_t vecs = row_vecs(vocab, dtype == UC_FP32 ? 4 : 2);
-  p.span = beam_span((int64_t)batch * n_beams, vecs, kBeamPerSm * num_sms());
+  p.span = beam_span((int64_t)batch * n_beams, n_beams, vecs, kBeamPerSm * num_sms());
   p.tiles = (int)((vecs + p.span - 1) / p.span);
   p.eos = eos;
   p.status = static_cast<DevStatus*>(workspace);

@@ -330,6 +330,7 @@ struct LinearChunkParams {
 void launch_linear_chunks(const LinearChunkParams& p, cudaStream_t st);
 
 // ------------------------------------------------- beam selection, reorder
+constexpr int kBeamLists = 512;    // tiles of a request at most, over its beams (each gives a list of candidates)
 constexpr int kBeamPerSm = 2;      // CTAs that an SM holds at a time
 constexpr int kBeamMinSpan = 512;  // least 16-byte vectors of a row that one CTA selects from, where the row has them
 
