@@ -842,7 +842,10 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
 // memory from zero, in turns of two, and all of them in registers (rounded,
 // where the tensor cores cut). Four groups of four warps form the decayed
 // values, a quarter chunk each, and hold a quarter of the channels. A pass over
-// k and v: about 4000 cycles a chunk, bound by forming the three parts.
+// k and v: about 4000 cycles a chunk (131072 tokens of 4 heads: 57 us, 4.7 TB/s),
+// bound by shared memory: at 128 B a cycle the products' operands take 1500, the
+// parts' 96 KB 800, the tiles 800. (Barriers per half of a group's quarter, or v
+// freed before k: the same.)
 constexpr int kLocalRing = 2;  // chunks in flight
 constexpr int kQuarter = kChunk / 4;
 constexpr uint32_t kQuarterBytes = kQuarter * kHeadDim * 2;
