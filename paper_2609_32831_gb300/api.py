@@ -613,7 +613,7 @@ def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: 
     128, 128] fp32: what earlier tokens left (None: zeros). out_state: where
     the new state goes (may be ``state``: in place). lengths: host tokens per
     sequence (None: T); outputs behind them are zero. Returns (out, out_state),
-    out with q's shape and strides."""
+    out with q's shape (and its strides where q has no gaps)."""
     B, hq, T, d = q.shape
     kv = k.shape
     hkv = kv[1]
