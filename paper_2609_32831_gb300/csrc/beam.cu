@@ -323,12 +323,12 @@ __global__ void __launch_bounds__(kSelThreads, kBeamPerSm) beam_tile_kernel(cons
       }
     };
     if (more) take(from == vec0);
-    // sum of exp(x - m) with m the thread's maximum so far: the exponent
-    // x log2(e) - m log2(e) in one rounding, and what rounding m log2(e) leaves
-    // (common to all terms) put right on the sum
+    // sum of exp(x - m) with m the thread's maximum so far. The difference is
+    // taken before it is scaled: it is at most 0, so no finite logits overflow
+    // (a mask of the type's lowest value, a thread that holds nothing else), and
+    // its rounding is 2^-24 of itself
     const float top = fmaxf(best_of_all, best), base = top == kNegInf ? 0.f : top;
-    const float shift = base * kLog2e, left = fmaf(-base, kLog2e, shift);
-    const uint64_t l2 = f2_pack(kLog2e, kLog2e), ns = f2_pack(-shift, -shift);
+    const uint64_t l2 = f2_pack(kLog2e, kLog2e), nb = f2_pack(-base, -base);
     uint64_t acc[2] = {0ull, 0ull};
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
@@ -336,14 +336,14 @@ __global__ void __launch_bounds__(kSelThreads, kBeamPerSm) beam_tile_kernel(cons
 #pragma unroll
       for (int e = 0; e < kE; e += 2) {
         float a, c;
-        f2_unpack(f2_fma(f2_pack(L::get(v[k], e), L::get(v[k], e + 1)), l2, ns), a, c);
+        f2_unpack(f2_mul(f2_add(f2_pack(L::get(v[k], e), L::get(v[k], e + 1)), nb), l2), a, c);
         acc[(e >> 1) & 1] = f2_add(acc[(e >> 1) & 1], f2_pack(ex2_approx(a), ex2_approx(c)));
       }
     }
     float part[4];
     f2_unpack(acc[0], part[0], part[1]);
     f2_unpack(acc[1], part[2], part[3]);
-    sum = fmaf(sum, ex2_approx((best_of_all - base) * kLog2e), ((part[0] + part[1]) + (part[2] + part[3])) * ex2_approx(left));
+    sum = fmaf(sum, ex2_approx((best_of_all - base) * kLog2e), (part[0] + part[1]) + (part[2] + part[3]));
     best_of_all = top;
     __syncthreads();
     count = before + *fresh;
