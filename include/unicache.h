@@ -643,6 +643,9 @@ typedef struct uc_rows {
  *   log_decay  host float [n_kv_heads], finite, <= 0
  *   state_in, state_out  fp32 [B, Hkv, 128, 128]; they may be the same array
  *              (the state is then updated in place) but not overlap otherwise
+ * A NaN or infinity in k or v of a valid token reaches that token and later
+ * ones, never an earlier one (v: its own channel alone); which of NaN and
+ * infinity its outputs and states then hold is left open.
  * Query head h reads KV head h / (Hq / Hkv). n_tok <= UC_MAX_QTOKENS (decode)
  * takes the recurrence token by token in fp32; more take chunks of 128 tokens
  * on the tensor cores, with the decayed q.k and the state that q multiplies

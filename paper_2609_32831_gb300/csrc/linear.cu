@@ -155,7 +155,14 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 //   warp 23  issues the slices' products and releases the chunk's k and v slots
 //            (one warp for all of it: its own waits and issues took 3500 cycles a tile)
 // In a sequence's last chunk, warps 21 and 22 first zero the k and v rows behind
-// its end: they may hold NaN, and 0 x NaN is not 0.
+// its end: they may hold NaN, and 0 x NaN is not 0. For the same reason a NaN or
+// infinity in v would reach earlier tokens through P V, where their P is 0. So
+// WG0 and WG1 look a chunk's v through beside its first P (on the issuing warp,
+// between two products, 8 x 8192 tokens took 281 us). Where they find any, the
+// chunk's slices are formed first (the state takes them as they are), warp 22
+// puts zeros in their place before P V, and behind its last tile the CTA makes NaN
+// of a channel's outputs from the token on that held one (8 x 8192 tokens 265 us in
+// all, 262 without any of it; code for it in the epilogue's loop: 275 to 300).
 // Order of the products: Q K^T of the next tile while the epilogue reads the
 // last one's o, then Q S and P V. (With the epilogue and the update on the
 // warps that form P, and rows stored from registers, 32 lines per instruction,
@@ -208,6 +215,8 @@ struct LinearSmem {
   uint64_t st_ready, s_free, chunk_go[2], k_done[2], v_done[2], kv_done, part_full[2], part_free[2];
   uint32_t tmem_base;
   uint32_t ks[2], vs[2];               // slots of a chunk's k and v, by parity
+  uint64_t v_hit[2];                   // a byte per warp that found NaN or infinities in its part of the chunk's v
+  uint32_t v_odd;                      // some did, in any chunk
   uint8_t slot_of[16];                 // slot of load L at L mod 16
 };
 static_assert(sizeof(LinearSmem) + 1024 <= 232448, "linear attention shared memory");
@@ -352,6 +361,45 @@ __device__ __forceinline__ void zero_rows(uint8_t* tile, int nv, int lane) {
   __syncwarp();
 }
 
+// Do rows 0 .. nv - 1 of a tile hold NaN or infinities? 0 times them is NaN, and
+// so is what it is added to. A warp's share of eight, by all of its lanes.
+__device__ __forceinline__ bool holds_not_finite(const uint8_t* tile, int nv, int thread) {
+  const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+  __nv_bfloat162 sum[4] = {zero, zero, zero, zero};
+#pragma unroll
+  for (int k = 0; k < (int)(kTileBytes / 16 / 256); ++k) {
+    const int i = 256 * k + thread;  // 16 bytes: half, row, piece of the row's half
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if ((i >> 3) % kChunk < nv) x = reinterpret_cast<const uint4*>(tile)[i];
+    sum[0] = __hfma2(reinterpret_cast<__nv_bfloat162&>(x.x), zero, sum[0]);
+    sum[1] = __hfma2(reinterpret_cast<__nv_bfloat162&>(x.y), zero, sum[1]);
+    sum[2] = __hfma2(reinterpret_cast<__nv_bfloat162&>(x.z), zero, sum[2]);
+    sum[3] = __hfma2(reinterpret_cast<__nv_bfloat162&>(x.w), zero, sum[3]);
+  }
+  const __nv_bfloat162 all = __hadd2(__hadd2(sum[0], sum[1]), __hadd2(sum[2], sum[3]));
+  return __any_sync(0xffffffffu, __hisnan(all.x) || __hisnan(all.y));
+}
+
+// The elements of eight that are NaN or infinite, as a mask.
+__device__ __forceinline__ uint32_t not_finite(const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t mask = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) mask |= (uint32_t)((~(w[e >> 1] >> (16 * (e & 1))) & 0x7f80u) == 0u) << e;
+  return mask;
+}
+
+// Zeroes those of a tile, by one warp.
+__device__ __forceinline__ void clear_not_finite(uint8_t* tile, int lane) {
+#pragma unroll 1
+  for (int i = lane; i < (int)(kTileBytes / 16); i += 32)
+    if (const uint32_t odd = not_finite(reinterpret_cast<const uint4*>(tile)[i]))
+      for (int e = 0; e < 8; ++e)
+        if ((odd >> e) & 1u) reinterpret_cast<uint16_t*>(tile)[8 * i + e] = 0;
+  fence_proxy_async_smem();
+  __syncwarp();
+}
+
 // The sequence of run `grun`.
 __device__ __forceinline__ int sequence_of(const LinearPlan& plan, int batch, int grun) {
   int lo = 0, hi = batch - 1;
@@ -362,23 +410,58 @@ __device__ __forceinline__ int sequence_of(const LinearPlan& plan, int batch, in
   return lo;
 }
 
+// What a CTA takes: a run of chunks of a KV head, and a part of its query heads.
+struct LinearTask {
+  int b, kvh, grun, h0, nh, len, c0, nc, part;
+};
+__device__ __forceinline__ LinearTask linear_task(const LinearChunkParams& c, int cta) {
+  const LinearParams& p = c.p;
+  LinearTask k;
+  k.part = cta % c.plan.head_parts;
+  k.kvh = cta / c.plan.head_parts % p.n_kv_heads;
+  k.grun = cta / (c.plan.head_parts * p.n_kv_heads);
+  k.b = sequence_of(c.plan, p.batch, k.grun);
+  k.h0 = k.part * c.plan.heads_per_part;
+  k.nh = min(c.plan.heads_per_part, p.group - k.h0);
+  k.len = p.lengths[k.b];
+  k.c0 = (k.grun - c.plan.run_begin[k.b]) * c.plan.chunks_per_run;
+  k.nc = min(c.plan.chunks_per_run, (k.len + kChunk - 1) / kChunk - k.c0);  // chunks with a valid token
+  return k;
+}
+
+// Makes NaN of a CTA's outputs in the channels, and from the token on, where v is
+// not finite (what comes behind its run has it from the state). `first` is shared.
+// The CTA's task is worked out anew: nothing has to be kept for it.
+__device__ __noinline__ void spoil_outputs(const LinearChunkParams& c, int cta, int* first) {
+  const LinearParams& p = c.p;
+  const LinearTask k = linear_task(c, cta);
+  const int t0 = k.c0 * kChunk, t1 = min(k.len, (k.c0 + k.nc) * kChunk);
+  for (int i = threadIdx.x; i < kHeadDim; i += kLThreads) first[i] = t1;
+  __syncthreads();
+  constexpr int kPieces = kHeadDim / 8;
+  const int piece = threadIdx.x % kPieces;
+  for (int t = t0 + threadIdx.x / kPieces; t < t1; t += kLThreads / kPieces) {
+    const uint32_t odd = not_finite(reinterpret_cast<const uint4*>(p.v.at(k.b, k.kvh, t))[piece]);
+    for (int e = 0; e < 8; ++e)
+      if ((odd >> e) & 1u) atomicMin(first + 8 * piece + e, t);
+  }
+  __syncthreads();
+  for (int t = t0 + threadIdx.x / kPieces; t < t1; t += kLThreads / kPieces)
+    for (int e = 0; e < 8; ++e)
+      if (t >= first[8 * piece + e])
+        for (int h = 0; h < k.nh; ++h)
+          p.out.at(k.b, k.kvh * p.group + k.h0 + h, t)[8 * piece + e] = __ushort_as_bfloat16(0x7fff);
+}
+
 __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid_constant__ LinearChunkParams c) {
   extern __shared__ uint8_t dyn_smem[];
   LinearSmem& sm = *reinterpret_cast<LinearSmem*>(
       (reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~static_cast<uintptr_t>(1023));
   const LinearParams& p = c.p;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-  const int part = blockIdx.x % c.plan.head_parts;
-  const int kvh = blockIdx.x / c.plan.head_parts % p.n_kv_heads;
-  const int grun = blockIdx.x / (c.plan.head_parts * p.n_kv_heads);
-  const int b = sequence_of(c.plan, p.batch, grun);
-  const int run = grun - c.plan.run_begin[b];
-  const int h0 = part * c.plan.heads_per_part;
-  const int nh = min(c.plan.heads_per_part, p.group - h0);
-  const int len = p.lengths[b];
-  const int c0 = run * c.plan.chunks_per_run;
-  const int n_all = (len + kChunk - 1) / kChunk;  // chunks with a valid token
-  const int nc = min(c.plan.chunks_per_run, n_all - c0);
+  const LinearTask task = linear_task(c, blockIdx.x);
+  const int part = task.part, kvh = task.kvh, grun = task.grun, b = task.b, h0 = task.h0, nh = task.nh, len = task.len;
+  const int c0 = task.c0, nc = task.nc;
   const int tiles = nc * nh;
   // with few heads the update's chain of steps is longer than the tiles': WG0 and
   // WG1 take a part of it (one head, 16 x up to 4097 tokens: 239 -> 233 us when it was added; with
@@ -409,6 +492,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     mbar_init(&sm.s_free, 1);
     mbar_init(&sm.kv_done, 1);
     fence_barrier_init();
+    sm.v_odd = 0;
   }
   const float2 l2 = p.log2_decay[kvh];
   const bool strong = l2.x * kChunk < -64.f;
@@ -516,6 +600,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       };
       for (int ci = 0, t = 0; ci < nc && !aborted; ++ci) {
         uint32_t vs = 0;
+        bool gone = valid(ci) == kChunk;  // chunk_go has been given
         for (int h = 0; h < nh; ++h, ++t) {
           const bool last = h == nh - 1;
           const uint32_t qs = take(load_q(ci, h), 56);
@@ -527,7 +612,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
             if (lane == 0) {
               sm.ks[ci & 1] = ks;
               sm.vs[ci & 1] = vs;
-              if (valid(ci) == kChunk) mbar_arrive(&sm.chunk_go[ci & 1]);  // the chunk's k and v are there
+              if (gone) mbar_arrive(&sm.chunk_go[ci & 1]);  // the chunk's k and v are there
             }
           }
           if (t > 0 && !dwait_warp(&sm.o_free, (t - 1) & 1, st, 59, aborted, lim)) break;
@@ -539,6 +624,16 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
             if (last) umma_commit_lead(lead, &sm.s_free);
           }
           if (!dwait_warp(&sm.p_full[t & 1], (t >> 1) & 1, st, 61, aborted, lim)) break;
+          if (h == 0 && sm.v_hit[ci & 1] != 0) {
+            // (k's zeroed rows are there behind Q K^T, and the update before this one
+            // is done where the state's copy is there)
+            if (!dwait_warp(&sm.st_ready, ci & 1, st, 57, aborted, lim)) break;
+            if (!gone && lane == 0) mbar_arrive(&sm.chunk_go[ci & 1]);
+            gone = true;
+            if ((ci + 1 < nc || last_state) && !dwait_warp(&sm.kv_done, ci & 1, st, 63, aborted, lim)) break;
+            clear_not_finite(sm.slot[vs], lane);
+            if (lane == 0) sm.v_odd = 1;
+          }
           tc_fence_after();
           if (h > 0) umma_commit_lead(lead, &sm.empty[qs]);  // Q S is issued, and Q K^T was done before P
           issue_p_v(lead, tm + kColOut, tm + 128 * (t & 1), col_lo + vs * kStep, dhi, id_b, h > 0);
@@ -553,7 +648,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
           umma_commit_lead(lead, &sm.o_full[t & 1]);
           if (last) umma_commit_lead(lead, &sm.v_done[ci & 1]);
           // (a last chunk's k rows behind the end were zeroed before its Q K^T)
-          if (h == 0 && lane == 0 && valid(ci) < kChunk) mbar_arrive(&sm.chunk_go[ci & 1]);
+          if (h == 0 && lane == 0 && !gone) mbar_arrive(&sm.chunk_go[ci & 1]);
         }
       }
     } else if (warp == kWarpSlice) {
@@ -614,12 +709,13 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       const int chunk16 = 4 * (blk & 1) + e;  // 16 bytes of the row's half
       return reinterpret_cast<uint4*>(sm.s + (blk >> 1) * (kTileBytes / 2) + r * 128 + ((chunk16 ^ (r & 7)) << 4));
     };
-    // 32 channels of the state: tensor memory's part and the copy's, scaled by g
-    // since it was made (g = 0: there is none yet)
-    auto whole_state = [&](int blk, uint32_t(&x)[32], float g) {
+    // 32 channels of the state: tensor memory's part and, where there is one, the
+    // copy's, scaled by g since it was made (also by 0: an infinity stays one or
+    // becomes NaN, as in the recurrence)
+    auto whole_state = [&](int blk, uint32_t(&x)[32], bool copied, float g) {
       tmem_ld32(s_addr + 32 * blk, x);
       tmem_wait_ld32(x);
-      if (g == 0.f) return;
+      if (!copied) return;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint4 c = *copy(blk, e);
@@ -646,7 +742,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
 #pragma unroll 1
       for (int blk = 0; blk < 4; ++blk) {
         uint32_t x[32];
-        whole_state(blk, x, ci > 0 ? sm.pw[kChunk] : 0.f);
+        whole_state(blk, x, ci > 0, sm.pw[kChunk]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           uint32_t w[4];
@@ -685,7 +781,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
 #pragma unroll 1
       for (int blk = 0; blk < 4; ++blk) {
         uint32_t x[32];
-        whole_state(blk, x, nc > 0 ? sm.pw[valid(nc - 1)] : 0.f);
+        whole_state(blk, x, nc > 0, nc > 0 ? sm.pw[valid(nc - 1)] : 0.f);
 #pragma unroll
         for (int e = 0; e < 32; e += 4)
           *reinterpret_cast<uint4*>(dst + 32 * blk + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
@@ -807,6 +903,12 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
         }
         tmem_st8(slot + 8 * q, pk);
       }
+      if (h == 0) {
+        const int L = load_v(ci);
+        if (!dwait_warp(&sm.full[L % kLFull], (L / kLFull) & 1, st, 60, aborted, lim)) break;
+        const bool odd = holds_not_finite(sm.slot[sm.slot_of[L & 15]], valid(ci), threadIdx.x);
+        if (lane == 0) reinterpret_cast<uint8_t*>(&sm.v_hit[ci & 1])[warp] = odd;
+      }
       tmem_wait_st();
       tc_fence_before();
       warp_arrive(&sm.p_full[t & 1], lane);
@@ -833,6 +935,11 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, kTmemLinear);
+  }
+  if (sm.v_odd) {
+    int cta = blockIdx.x;
+    asm volatile("" : "+r"(cta));
+    spoil_outputs(c, cta, reinterpret_cast<int*>(sm.turn));
   }
 }
 
