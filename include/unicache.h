@@ -650,7 +650,9 @@ typedef struct uc_rows {
  * takes the recurrence token by token in fp32; more take chunks of 128 tokens
  * on the tensor cores, with the decayed q.k and the state that q multiplies
  * rounded to bf16 and sums and states in fp32. 1 <= B <= UC_MAX_BATCH, Hkv <= UC_MAX_LINEAR_HEADS,
- * 1 <= n_tok <= 2^28. out must not overlap q, k or v.
+ * 1 <= n_tok <= 2^28. Rows of out share no memory with one another, with rows of
+ * q, k and v, or with the states (rows may interleave in one buffer); nor does
+ * state_out with any of them.
  * workspace: uc_linear_workspace_size() bytes, 16-byte aligned.
  */
 uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v, int32_t batch, int32_t n_q_heads,

@@ -37,6 +37,73 @@ float2 two_floats(double x) {
   return make_float2(hi, std::isfinite(hi) ? (float)(x - (double)hi) : 0.f);
 }
 
+constexpr int64_t kMostElements = int64_t(1) << 44;  // between two rows of one tensor
+
+// stride * x, lo <= x <= hi.
+struct Term {
+  int64_t stride, lo, hi;
+};
+
+// Is there a sum d + stride_0 x_0 + ... strictly between -before and after (all x
+// zero: only if `zero`)? Terms by falling stride: what the later ones reach
+// leaves few x to look at, one or two each where strides nest. A search that
+// grows past `steps` counts as found.
+bool reaches(const Term* t, int n, int64_t d, int64_t before, int64_t after, bool zero, int* steps) {
+  if (n == 0) return zero && d > -before && d < after;
+  int64_t lo = 0, hi = 0;
+  for (int i = 1; i < n; ++i) {
+    lo += t[i].stride * t[i].lo;
+    hi += t[i].stride * t[i].hi;
+  }
+  auto floor_div = [](int64_t a, int64_t b) { return a / b - (a % b < 0); };
+  const int64_t first = std::max(t->lo, floor_div(-before - d - hi, t->stride) + 1);
+  const int64_t last = std::min(t->hi, -floor_div(-(after - d - lo), t->stride) - 1);
+  for (int64_t x = first; x <= last; ++x)
+    if (--*steps < 0 || reaches(t + 1, n - 1, d + t->stride * x, before, after, zero || x != 0, steps)) return true;
+  return false;
+}
+
+// Rows of a tensor: [batch, heads, tokens] of UC_HEAD_DIM elements.
+struct RowSet {
+  const RowsDev* r;
+  int size[3];
+  uint64_t bytes;  // from the first row to the last's end
+  int64_t stride(int i) const { return i == 0 ? r->sb : i == 1 ? r->sh : r->st; }
+};
+
+// Does a row of a share an element with a row of b (with another row, where both are one)?
+bool rows_meet(const RowSet& a, const RowSet& b) {
+  const bool same = &a == &b;
+  if (!same && !overlap(a.r->base, a.bytes, b.r->base, b.bytes)) return false;
+  Term t[6];
+  int n = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (a.size[i] > 1 && b.size[i] > 1 && a.stride(i) == b.stride(i)) {
+      t[n++] = {a.stride(i), 1 - b.size[i], a.size[i] - 1};
+    } else {
+      if (a.size[i] > 1) t[n++] = {a.stride(i), 0, a.size[i] - 1};
+      if (b.size[i] > 1) t[n++] = {b.stride(i), 1 - b.size[i], 0};
+    }
+  }
+  std::sort(t, t + n, [](const Term& x, const Term& y) { return x.stride > y.stride; });
+  int steps = 1 << 16;
+  const int64_t d = ((int64_t)reinterpret_cast<uintptr_t>(a.r->base) - (int64_t)reinterpret_cast<uintptr_t>(b.r->base)) / 2;
+  return reaches(t, n, d, UC_HEAD_DIM, UC_HEAD_DIM, !same, &steps);
+}
+
+// Does a row of a share a byte with the `bytes` bytes at x?
+bool rows_meet(const RowSet& a, const void* x, uint64_t bytes) {
+  if (!overlap(a.r->base, a.bytes, x, bytes)) return false;
+  Term t[3];
+  int n = 0;
+  for (int i = 0; i < 3; ++i)
+    if (a.size[i] > 1) t[n++] = {a.stride(i), 0, a.size[i] - 1};
+  std::sort(t, t + n, [](const Term& x, const Term& y) { return x.stride > y.stride; });
+  int steps = 1 << 16;
+  const int64_t d = ((int64_t)reinterpret_cast<uintptr_t>(a.r->base) - (int64_t)reinterpret_cast<uintptr_t>(x)) / 2;
+  return reaches(t, n, d, UC_HEAD_DIM, (int64_t)(bytes / 2), true, &steps);
+}
+
 // Rows of `heads` heads of `n_tok` tokens: strides in the kernels' form (0
 // where the extent is 1) and the bytes from the first row to the last's end.
 uc_status check_rows(const uc_rows* r, const char* what, int batch, int heads, int n_tok, RowsDev* out,
@@ -52,6 +119,10 @@ uc_status check_rows(const uc_rows* r, const char* what, int batch, int heads, i
     if (size[i] > 1 && (stride[i] < UC_HEAD_DIM || stride[i] % 8 != 0 || stride[i] > (int64_t(1) << 37))) {
       set_error("uc_linear_attend: strides of %s must be multiples of 8 elements, at least %d and below 2^37", what,
                 UC_HEAD_DIM);
+      return UC_ERR_SHAPE;
+    }
+    if (size[i] > 1 && stride[i] > kMostElements / (size[i] - 1)) {
+      set_error("uc_linear_attend: rows of %s lie more than 2^44 elements apart", what);
       return UC_ERR_SHAPE;
     }
     last += stride[i] * (size[i] - 1);
@@ -187,8 +258,6 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
     return UC_ERR_ARG;
   }
   const uint64_t ns = 4ull * batch * n_kv_heads * UC_HEAD_DIM * UC_HEAD_DIM;
-  // (rows of different tensors may interleave in one buffer, so only equal
-  // bases and the dense state arrays are compared)
   if (out->ptr == q->ptr || out->ptr == k->ptr || out->ptr == v->ptr ||
       (state_in != state_out && overlap(state_in, state_in ? ns : 0, state_out, ns))) {
     set_error("uc_linear_attend: outputs overlap inputs");
@@ -219,8 +288,27 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
   p.n_tok = n_tok;
   p.scale = (float)(1.0 / std::sqrt((double)UC_HEAD_DIM));
   const cudaStream_t cs = reinterpret_cast<cudaStream_t>(stream);
+  // (rows of different tensors may interleave in one buffer)
+  auto check_shared = [&]() -> uc_status {
+    const RowSet rows[4] = {{&p.out, {batch, n_q_heads, n_tok}, no},
+                            {&p.q, {batch, n_q_heads, n_tok}, nq},
+                            {&p.k, {batch, n_kv_heads, n_tok}, nk},
+                            {&p.v, {batch, n_kv_heads, n_tok}, nv}};
+    if (rows_meet(rows[0], rows[0])) {
+      set_error("uc_linear_attend: rows of out overlap one another");
+      return UC_ERR_SHAPE;
+    }
+    bool shared = state_in != nullptr && rows_meet(rows[0], state_in, ns);
+    for (int i = 0; i < 4; ++i) shared |= (i > 0 && rows_meet(rows[0], rows[i])) || rows_meet(rows[i], state_out, ns);
+    if (shared) {
+      set_error("uc_linear_attend: outputs overlap inputs or each other");
+      return UC_ERR_ARG;
+    }
+    return UC_OK;
+  };
   if (linear_steps(n_q_heads, n_kv_heads, n_tok)) {
     st = check_workspace(workspace, workspace_bytes, 256, "uc_linear_attend");
+    if (st == UC_OK) st = check_shared();
     if (st != UC_OK) return st;
     launch_linear_step(p, cs);
     return cuda_check("uc_linear_attend");
@@ -232,6 +320,7 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
   c.from_start = c.plan.several || (c.plan.head_parts > 1 && state_in == state_out);
   const uint64_t states = c.from_start ? (uint64_t)c.plan.runs * n_kv_heads : 0;
   st = check_workspace(workspace, workspace_bytes, linear_bytes(states), "uc_linear_attend");
+  if (st == UC_OK) st = check_shared();
   if (st != UC_OK) return st;
   c.p = p;
   st = encode_rows_4d(&c.tq, p.q, n_tok, n_q_heads, batch, kChunk);
