@@ -412,7 +412,7 @@ __device__ __forceinline__ int sequence_of(const LinearPlan& plan, int batch, in
 
 // What a CTA takes: a run of chunks of a KV head, and a part of its query heads.
 struct LinearTask {
-  int b, kvh, grun, h0, nh, len, c0, nc, part;
+  int b, kvh, grun, h0, nh, len, c0, chunks, part;
 };
 __device__ __forceinline__ LinearTask linear_task(const LinearChunkParams& c, int cta) {
   const LinearParams& p = c.p;
@@ -425,7 +425,7 @@ __device__ __forceinline__ LinearTask linear_task(const LinearChunkParams& c, in
   k.nh = min(c.plan.heads_per_part, p.group - k.h0);
   k.len = p.lengths[k.b];
   k.c0 = (k.grun - c.plan.run_begin[k.b]) * c.plan.chunks_per_run;
-  k.nc = min(c.plan.chunks_per_run, (k.len + kChunk - 1) / kChunk - k.c0);  // chunks with a valid token
+  k.chunks = min(c.plan.chunks_per_run, (k.len + kChunk - 1) / kChunk - k.c0);  // chunks with a valid token
   return k;
 }
 
@@ -435,7 +435,7 @@ __device__ __forceinline__ LinearTask linear_task(const LinearChunkParams& c, in
 __device__ __noinline__ void spoil_outputs(const LinearChunkParams& c, int cta, int* first) {
   const LinearParams& p = c.p;
   const LinearTask k = linear_task(c, cta);
-  const int t0 = k.c0 * kChunk, t1 = min(k.len, (k.c0 + k.nc) * kChunk);
+  const int t0 = k.c0 * kChunk, t1 = min(k.len, (k.c0 + k.chunks) * kChunk);
   for (int i = threadIdx.x; i < kHeadDim; i += kLThreads) first[i] = t1;
   __syncthreads();
   constexpr int kPieces = kHeadDim / 8;
@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const LinearTask task = linear_task(c, blockIdx.x);
   const int part = task.part, kvh = task.kvh, grun = task.grun, b = task.b, h0 = task.h0, nh = task.nh, len = task.len;
-  const int c0 = task.c0, nc = task.nc;
+  const int c0 = task.c0, nc = task.chunks;
   const int tiles = nc * nh;
   // with few heads the update's chain of steps is longer than the tiles': WG0 and
   // WG1 take a part of it (one head, 16 x up to 4097 tokens: 239 -> 233 us when it was added; with
