@@ -39,6 +39,9 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+_STATUS_BYTES = 16   # of a workspace's first bytes (see uc_workspace_status)
+
+
 class Workspace:
     """Zero-filled device scratch, grown on demand and reused across calls.
 
@@ -49,21 +52,59 @@ class Workspace:
     def __init__(self, device=None):
         self.device = torch.device(device or "cuda")
         self.bufs = {}
+        self._at = {}     # (kind, stream handle) -> (address, bytes), for the streams that have worked in the buffer
+        self._kept = []   # buffers replaced during a graph's capture, for their status words
 
-    def get(self, nbytes: int, kind: str = "scratch") -> Tuple[int, int]:
+    def get(self, nbytes: int, kind: str = "scratch", stream=None, handle: Optional[int] = None) -> Tuple[int, int]:
+        """(address, bytes) of a buffer of at least ``nbytes`` for a launch on
+        ``stream`` (the current one if None; its handle, where the caller has it)."""
+        if handle is None and self.device.type == "cuda":
+            handle = _stream(stream)
+        at = self._at.get((kind, handle))
+        if at is not None and at[1] >= nbytes:
+            return at
         nbytes = max(256, int(nbytes))
         buf = self.bufs.get(kind)
         if buf is None or buf.numel() < nbytes:
+            buf = self._grow(buf, nbytes, kind, stream)
+        elif self.device.type == "cuda":
+            self._record(buf, stream)
+        at = self._at[kind, handle] = buf.data_ptr(), buf.numel()
+        return at
+
+    @staticmethod
+    def _record(buf: torch.Tensor, stream) -> None:
+        """The allocator gives ``buf`` to nobody else before ``stream`` is done with it."""
+        buf.record_stream(stream or torch.cuda.current_stream())
+
+    def _grow(self, old: Optional[torch.Tensor], nbytes: int, kind: str, stream) -> torch.Tensor:
+        """A larger buffer, cleared on the launch's own stream (a fill on another
+        one could run beside the launch); it takes the status word over."""
+        if self.device.type != "cuda":
             buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
-            self.bufs[kind] = buf
-        return buf.data_ptr(), buf.numel()
+            if old is not None:
+                buf[:_STATUS_BYTES] = old[:_STATUS_BYTES]
+        else:
+            if old is not None:
+                self._record(old, stream)
+            with torch.cuda.stream(stream):
+                buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+                if old is not None:
+                    if torch.cuda.is_current_stream_capturing():
+                        self._kept.append(old)   # (a captured copy would read it at every replay)
+                    else:
+                        buf[:_STATUS_BYTES].copy_(old[:_STATUS_BYTES])
+        self._at = {key: at for key, at in self._at.items() if key[0] != kind}
+        self.bufs[kind] = buf
+        return buf
 
     def status(self, stream=None) -> int:
         """Synchronise and read (then clear) the device status words."""
         code = 0
-        for buf in self.bufs.values():
+        for buf in [*self.bufs.values(), *self._kept]:
             c = lib().uc_workspace_status(C.c_void_p(buf.data_ptr()), _stream(stream))
             code = code or c
+        self._kept.clear()
         return code
 
 
@@ -304,7 +345,7 @@ def score_accumulate(qwin: torch.Tensor, k: torch.Tensor, n_ctx: Optional[int] =
         out = torch.empty((B, hkv, n_ctx), dtype=torch.float32, device=k.device)
     ws = ws or default_workspace(k.device)
     need = lib().uc_score_workspace_size(B, hq, hkv, W, n_ctx)
-    wp, wn = ws.get(need)
+    wp, wn = ws.get(need, stream=stream)
     check("uc_score_accumulate", lib().uc_score_accumulate(
         _ptr(qwin), _ptr(k), B, hq, hkv, W, n_ctx, N, _ptr(out), wp, wn, _stream(stream)))
     return out
@@ -334,7 +375,7 @@ def compress_segment(k_src: torch.Tensor, v_src: torch.Tensor, seg: Segment, beg
     into ``seg`` (keep counts set with ``seg.set_keep``). scores [B, Hkv, Ns]."""
     B, hkv, N, d = k_src.shape
     ws = ws or default_workspace(k_src.device)
-    wp, wn = ws.get(lib().uc_compress_workspace_size(C.byref(seg.c)))
+    wp, wn = ws.get(lib().uc_compress_workspace_size(C.byref(seg.c)), stream=stream)
     s_stride = scores.shape[-1] if scores is not None else 0
     s_off = (begin if scores_begin is None else scores_begin) if scores is not None else 0
     check("uc_compress_segment", lib().uc_compress_segment(
@@ -433,7 +474,7 @@ def recompress_segment(src: Segment, dst: Segment, scores: Optional[torch.Tensor
     set with ``dst.set_keep``). scores [B, Hkv, Ns] fp32 indexed by logical
     token (position scores_begin + token index), needed when dst evicts."""
     ws = ws or default_workspace(src.device)
-    wp, wn = ws.get(lib().uc_recompress_workspace_size(C.byref(src.c), C.byref(dst.c)))
+    wp, wn = ws.get(lib().uc_recompress_workspace_size(C.byref(src.c), C.byref(dst.c)), stream=stream)
     s_stride = scores.shape[-1] if scores is not None else 0
     check("uc_recompress_segment", lib().uc_recompress_segment(
         C.byref(src.c), _ptr(scores), s_stride, scores_begin, n_recent, C.byref(dst.c), wp, wn,
@@ -448,10 +489,11 @@ def accumulate_scores(q: torch.Tensor, seg: Segment, lse: torch.Tensor, acc: tor
     acc_begin + token (lse: that call's [B, Hq, T] output)."""
     B, hq, T, d = q.shape
     ws = ws or default_workspace(q.device)
-    wp, wn = ws.get(256)
+    st = _stream(stream)
+    wp, wn = ws.get(256, "scratch", stream, st)
     check("uc_accumulate_scores", lib().uc_accumulate_scores(
         _ptr(q), hq, T, C.byref(seg.c), _ptr(lse), _ptr(acc), acc.shape[-1], acc_begin, wp, wn,
-        _stream(stream)))
+        st))
     return acc
 
 
@@ -491,14 +533,12 @@ def attend(q: torch.Tensor, segs: Sequence[Segment], out: Optional[torch.Tensor]
     L = lib()
     # the call plans once and says if the workspace at hand is too small for
     # it (nothing is launched then): only then is the size asked for
-    buf = ws.bufs.get("attend")
-    wp, wn = (buf.data_ptr(), buf.numel()) if buf is not None else \
-        ws.get(L.uc_attend_workspace_size(arr, ns, hq, T), "attend")
-    args = (q.data_ptr(), hq, T, arr, ns, out.data_ptr(), _ptr(lse), _ptr(mass))
     st = _stream(stream)
+    wp, wn = ws.get(0 if "attend" in ws.bufs else L.uc_attend_workspace_size(arr, ns, hq, T), "attend", stream, st)
+    args = (q.data_ptr(), hq, T, arr, ns, out.data_ptr(), _ptr(lse), _ptr(mass))
     code = L.uc_attend(*args, wp, wn, st)
     if code == _lib.UC_ERR_OOM:
-        wp, wn = ws.get(L.uc_attend_workspace_size(arr, ns, hq, T), "attend")
+        wp, wn = ws.get(L.uc_attend_workspace_size(arr, ns, hq, T), "attend", stream, st)
         code = L.uc_attend(*args, wp, wn, st)
     check("uc_attend", code)
     return out, lse, mass
@@ -558,13 +598,13 @@ def attend_batch(calls, ws: Optional[Workspace] = None, stream=None):
     arr = (_lib.UcAttendCall * n)(*structs)
     ws = ws or default_workspace(calls[0][0].device)
     L = lib()
-    buf = ws.bufs.get("attend_batch")   # as in attend(): the size is asked for only when the call needs more
-    wp, wn = (buf.data_ptr(), buf.numel()) if buf is not None else \
-        ws.get(L.uc_attend_batch_workspace_size(arr, n), "attend_batch")
+    # as in attend(): the size is asked for only when the call needs more
     st = _stream(stream)
+    wp, wn = ws.get(0 if "attend_batch" in ws.bufs else L.uc_attend_batch_workspace_size(arr, n), "attend_batch", stream,
+                    st)
     code = L.uc_attend_batch(arr, n, wp, wn, st)
     if code == _lib.UC_ERR_OOM:
-        wp, wn = ws.get(L.uc_attend_batch_workspace_size(arr, n), "attend_batch")
+        wp, wn = ws.get(L.uc_attend_batch_workspace_size(arr, n), "attend_batch", stream, st)
         code = L.uc_attend_batch(arr, n, wp, wn, st)
     check("uc_attend_batch", code)
     return results
@@ -578,9 +618,10 @@ def append(seg: Segment, k_new: torch.Tensor, v_new: torch.Tensor, position: int
            ws: Optional[Workspace] = None, stream=None) -> None:
     """Append one token per sequence: k_new, v_new [B, Hkv, 128] (or [B, Hkv, 1, 128])."""
     ws = ws or default_workspace(k_new.device)
-    wp, wn = ws.get(256)
+    st = _stream(stream)
+    wp, wn = ws.get(256, "scratch", stream, st)
     check("uc_append", lib().uc_append(
-        C.byref(seg.c), _ptr(k_new), _ptr(v_new), int(position), wp, wn, _stream(stream)))
+        C.byref(seg.c), _ptr(k_new), _ptr(v_new), int(position), wp, wn, st))
 
 
 
@@ -589,9 +630,10 @@ def append_next(seg: Segment, k_new: torch.Tensor, v_new: torch.Tensor, base_pos
     """Like ``append`` with the logical index base_position + n_kept[b] taken on
     the device and no host-side state: capturable in a CUDA graph."""
     ws = ws or default_workspace(k_new.device)
-    wp, wn = ws.get(256)
+    st = _stream(stream)
+    wp, wn = ws.get(256, "scratch", stream, st)
     check("uc_append_next", lib().uc_append_next(
-        C.byref(seg.c), _ptr(k_new), _ptr(v_new), int(base_position), wp, wn, _stream(stream)))
+        C.byref(seg.c), _ptr(k_new), _ptr(v_new), int(base_position), wp, wn, st))
 
 
 # -------------------------------------- layers with a state of constant size
@@ -646,9 +688,9 @@ def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: 
             None if lengths is None else (C.c_int32 * B)(*lengths), (C.c_float * hkv)(*log_decay), _ptr(state),
             out_state.data_ptr(), _pack_rows(out.data_ptr(), so[0], so[1], so[2]))
     st = _stream(stream)
-    code = L.uc_linear_attend(*args, *ws.get(256), st)
+    code = L.uc_linear_attend(*args, *ws.get(256, "scratch", stream, st), st)
     if code == _lib.UC_ERR_OOM:   # nothing is launched then: only now is the size asked for
-        code = L.uc_linear_attend(*args, *ws.get(L.uc_linear_workspace_size(B, hq, hkv, T)), st)
+        code = L.uc_linear_attend(*args, *ws.get(L.uc_linear_workspace_size(B, hq, hkv, T), "scratch", stream, st), st)
     check("uc_linear_attend", code)
     return out, out_state
 
@@ -687,9 +729,9 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int, finished: Op
     args = (logits.data_ptr(), kind, sb, sk, B, K, V, scores.data_ptr(), _ptr(finished), eos, n,
             best.data_ptr(), parent.data_ptr(), token.data_ptr(), done.data_ptr())
     st = _stream(stream)
-    code = L.uc_beam_select(*args, *ws.get(256), st)
+    code = L.uc_beam_select(*args, *ws.get(256, "scratch", stream, st), st)
     if code == _lib.UC_ERR_OOM:   # nothing is launched then: only now is the size asked for
-        code = L.uc_beam_select(*args, *ws.get(L.uc_beam_workspace_size(B, K, V, n)), st)
+        code = L.uc_beam_select(*args, *ws.get(L.uc_beam_workspace_size(B, K, V, n), "scratch", stream, st), st)
     check("uc_beam_select", code)
     return best, parent, token, done
 
@@ -723,9 +765,10 @@ def reorder(pairs, parent: torch.Tensor, ws: Optional[Workspace] = None, stream=
     if n_seq is None or groups == 0 or n_seq % groups:
         raise ValueError("reorder: the sources' sequences are a multiple of the groups")
     ws = ws or default_workspace(parent.device)
-    wp, wn = ws.get(256)
+    st = _stream(stream)
+    wp, wn = ws.get(256, "scratch", stream, st)
     check("uc_reorder", lib().uc_reorder(b"".join(items), len(items), parent.data_ptr(),
-                                         groups, n_seq // groups, n_to, wp, wn, _stream(stream)))
+                                         groups, n_seq // groups, n_to, wp, wn, st))
 
 
 def set_dense_serial_pv(serial: bool) -> bool:
