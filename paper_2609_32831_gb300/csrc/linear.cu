@@ -215,8 +215,11 @@ struct LinearSmem {
   uint64_t st_ready, s_free, chunk_go[2], k_done[2], v_done[2], kv_done, part_full[2], part_free[2];
   uint32_t tmem_base;
   uint32_t ks[2], vs[2];               // slots of a chunk's k and v, by parity
+  uint64_t drain[3];                   // the issuing warps' last products
   uint64_t v_hit[2];                   // a byte per warp that found NaN or infinities in its part of the chunk's v
   uint32_t v_odd;                      // some did, in any chunk
+  int loads;                           // loads issued
+  DevStatus status;                    // of this CTA's waits
   uint8_t slot_of[16];                 // slot of load L at L mod 16
 };
 static_assert(sizeof(LinearSmem) + 1024 <= 232448, "linear attention shared memory");
@@ -410,6 +413,28 @@ __device__ __forceinline__ int sequence_of(const LinearPlan& plan, int batch, in
   return lo;
 }
 
+// Where a wait ran out in any warp, the others may have left their loops with copies
+// and products still in flight: neither shared nor tensor memory is given back
+// under them. By all threads behind a barrier (a role's lanes are apart before
+// it), with the ordinary limit (the call's may be too short for it). The CTA's
+// waits record in shared memory, so that its end knows of them without a register
+// in any role; they reach the call's status word here.
+__device__ __forceinline__ void drain_cta(LinearSmem& sm, DevStatus* status, int warp) {
+  if (threadIdx.x == 0) set_status(status, sm.status.code, sm.status.detail);
+  bool gone = false;
+  if (warp == kWarpTma) {
+    const int loads = sm.loads;
+#pragma unroll 1
+    for (int i = max(0, loads - kLSlots); i < loads; ++i)
+      dwait_warp(&sm.full[i % kLFull], (i / kLFull) & 1, status, 52, gone);
+  } else if (warp > kWarpTma) {
+    uint64_t* const bar = &sm.drain[warp - kWarpQk];
+    umma_commit_lead(elect_one(), bar);  // (behind what its elected lane has issued)
+    dwait_warp(bar, 0, status, 53, gone);
+  }
+  __syncthreads();
+}
+
 // What a CTA takes: a run of chunks of a KV head, and a part of its query heads.
 struct LinearTask {
   int b, kvh, grun, h0, nh, len, c0, chunks, part;
@@ -491,8 +516,11 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     mbar_init(&sm.st_ready, 4);
     mbar_init(&sm.s_free, 1);
     mbar_init(&sm.kv_done, 1);
+    for (int s = 0; s < 3; ++s) mbar_init(&sm.drain[s], 1);
     fence_barrier_init();
     sm.v_odd = 0;
+    sm.loads = 0;
+    sm.status.code = 0;
   }
   const float2 l2 = p.log2_decay[kvh];
   const bool strong = l2.x * kChunk < -64.f;
@@ -507,7 +535,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
   tc_fence_after();
   const uint32_t tmem = sm.tmem_base;
   bool aborted = false;
-  DevStatus* const st = c.status;
+  DevStatus* const st = &sm.status;
   const uint64_t lim = c.wait_ns;
 
   if (warp >= kWarpTma) {
@@ -549,12 +577,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
           ++ci;
         }
       }
-      if (aborted) {
-        // no copy may land in shared memory that is no longer this CTA's
-        bool gone = false;
-        for (int i = max(0, L - kLSlots); i < L; ++i)
-          dwait(&sm.full[i % kLFull], (i / kLFull) & 1, st, 52, gone, lim);
-      }
+      sm.loads = L;
     } else if (warp == kWarpQk) {
       // ---------------------------------------------------------- Q K^T
       const uint32_t lead = elect_one();
@@ -928,9 +951,11 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
       h = 0;
       ++ci;
     }
+    tmem_wait_st();
     tc_fence_before();
   }
   __syncthreads();
+  if (sm.status.code != 0) drain_cta(sm, c.status, warp);
   if (warp == kWarpMma) {
     __syncwarp();
     tc_fence_after();
@@ -961,8 +986,10 @@ struct LinearLocalSmem {
   uint8_t part[4][3][kQuarterBytes];  // [2 x 64 channels][32 tokens][128 B]
   float pw[kChunk];                   // gamma^n
   uint64_t k_full[kLocalRing], v_full[kLocalRing], empty[kLocalRing];
-  uint64_t part_full[4], part_free[4], sum_full[2], sum_free[2];
+  uint64_t part_full[4], part_free[4], sum_full[2], sum_free[2], drain;
   uint32_t tmem_base;
+  int loads;         // chunks loaded
+  DevStatus status;  // as in LinearSmem
 };
 static_assert(sizeof(LinearLocalSmem) + 1024 <= 232448, "linear attention shared memory");
 
@@ -992,7 +1019,10 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
       mbar_init(&sm.sum_full[s], 1);
       mbar_init(&sm.sum_free[s], 16);
     }
+    mbar_init(&sm.drain, 1);
     fence_barrier_init();
+    sm.loads = 0;
+    sm.status.code = 0;
   }
   const float2 l2 = p.log2_decay[kvh];
   if (threadIdx.x < kChunk) sm.pw[threadIdx.x] = decay_pow(l2, threadIdx.x);
@@ -1002,7 +1032,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
   tc_fence_after();
   const uint32_t tmem = sm.tmem_base;
   bool aborted = false;
-  DevStatus* const st = c.status;
+  DevStatus* const st = &sm.status;
   const uint64_t lim = c.wait_ns;
   if (warp == kWarpTma && lane == 0) {
     prefetch_tmap(&c.tk);
@@ -1015,13 +1045,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
       load_tile(sm.k[s], &c.tk, (c0 + ci) * kChunk, kvh, b, &sm.k_full[s]);
       loaded = ci + 1;
     }
-    if (aborted) {
-      bool gone = false;
-      for (int i = max(0, loaded - kLocalRing); i < loaded; ++i) {
-        dwait(&sm.k_full[i % kLocalRing], (i / kLocalRing) & 1, st, 71, gone, lim);
-        dwait(&sm.v_full[i % kLocalRing], (i / kLocalRing) & 1, st, 71, gone, lim);
-      }
-    }
+    sm.loads = loaded;
   } else if (warp == kWarpMma) {
     const uint32_t lead = elect_one();
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
@@ -1086,6 +1110,22 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
     tc_fence_before();
   }
   __syncthreads();
+  if (sm.status.code != 0) {  // as drain_cta
+    if (threadIdx.x == 0) set_status(c.status, sm.status.code, sm.status.detail);
+    bool gone = false;
+    if (warp == kWarpTma) {
+      const int loads = sm.loads;
+#pragma unroll 1
+      for (int i = max(0, loads - kLocalRing); i < loads; ++i) {
+        dwait_warp(&sm.k_full[i % kLocalRing], (i / kLocalRing) & 1, c.status, 71, gone);
+        dwait_warp(&sm.v_full[i % kLocalRing], (i / kLocalRing) & 1, c.status, 71, gone);
+      }
+    } else if (warp == kWarpMma) {
+      umma_commit_lead(elect_one(), &sm.drain);
+      dwait_warp(&sm.drain, 0, c.status, 72, gone);
+    }
+    __syncthreads();
+  }
   if (warp == kWarpMma) {
     __syncwarp();
     tc_fence_after();
