@@ -456,24 +456,31 @@ __device__ __forceinline__ LinearTask linear_task(const LinearChunkParams& c, in
 
 // Makes NaN of a CTA's outputs in the channels, and from the token on, where v is
 // not finite (what comes behind its run has it from the state). `first` is shared.
-// The CTA's task is worked out anew: nothing has to be kept for it.
+// The CTA's task is worked out anew: nothing has to be kept for it. Rolled loops:
+// warps call it with the registers that their role left them, 72 at least (as a
+// kernel it takes 26).
 __device__ __noinline__ void spoil_outputs(const LinearChunkParams& c, int cta, int* first) {
   const LinearParams& p = c.p;
   const LinearTask k = linear_task(c, cta);
   const int t0 = k.c0 * kChunk, t1 = min(k.len, (k.c0 + k.chunks) * kChunk);
-  for (int i = threadIdx.x; i < kHeadDim; i += kLThreads) first[i] = t1;
+  if (threadIdx.x < kHeadDim) first[threadIdx.x] = t1;
   __syncthreads();
   constexpr int kPieces = kHeadDim / 8;
   const int piece = threadIdx.x % kPieces;
+#pragma unroll 1
   for (int t = t0 + threadIdx.x / kPieces; t < t1; t += kLThreads / kPieces) {
     const uint32_t odd = not_finite(reinterpret_cast<const uint4*>(p.v.at(k.b, k.kvh, t))[piece]);
+#pragma unroll 1
     for (int e = 0; e < 8; ++e)
       if ((odd >> e) & 1u) atomicMin(first + 8 * piece + e, t);
   }
   __syncthreads();
+#pragma unroll 1
   for (int t = t0 + threadIdx.x / kPieces; t < t1; t += kLThreads / kPieces)
+#pragma unroll 1
     for (int e = 0; e < 8; ++e)
       if (t >= first[8 * piece + e])
+#pragma unroll 1
         for (int h = 0; h < k.nh; ++h)
           p.out.at(k.b, k.kvh * p.group + k.h0 + h, t)[8 * piece + e] = __ushort_as_bfloat16(0x7fff);
 }
