@@ -683,6 +683,8 @@ typedef enum { UC_FP32 = 0, UC_BF16 = 1, UC_FP16 = 2 } uc_dtype;
  *   out_scores fp32, out_parent (the beam), out_token int32 [B, n]
  *   out_finished uint8 [B, n], nullable: 1 where the token is eos or the
  *             parent was finished
+ * Outputs share no memory with one another, with scores or with finished, except
+ * that out_scores may be scores where n = K.
  * Where fewer than n continuations have a finite score the rest follow with
  * -inf in the same order. 1 <= K <= UC_MAX_BEAMS, 1 <= n <= UC_MAX_BEAM_OUT,
  * n <= K * V, B * K <= 65535. workspace: uc_beam_workspace_size() bytes,

@@ -398,6 +398,20 @@ uc_status uc_beam_select(const void* logits, int32_t dtype, int64_t stride_b, in
   const uc_status st = check_workspace(workspace, workspace_bytes, uc_beam_workspace_size(batch, n_beams, vocab, n),
                                        "uc_beam_select");
   if (st != UC_OK) return st;
+  // (a request's scores are read before its results are written, so they may take their place)
+  struct { const void* p; uint64_t bytes; } out[4] = {{out_scores, 4ull * batch * n}, {out_parent, 4ull * batch * n},
+                                                      {out_token, 4ull * batch * n},
+                                                      {out_finished, out_finished ? 1ull * batch * n : 0}};
+  for (int i = 0; i < 4; ++i) {
+    bool shared = overlap(out[i].p, out[i].bytes, finished, finished ? 1ull * batch * n_beams : 0) ||
+                  (!(i == 0 && out_scores == scores && n == n_beams) &&
+                   overlap(out[i].p, out[i].bytes, scores, 4ull * batch * n_beams));
+    for (int j = 0; j < i; ++j) shared |= overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes);
+    if (shared) {
+      set_error("uc_beam_select: outputs overlap inputs or each other");
+      return UC_ERR_ARG;
+    }
+  }
   BeamParams p;
   memset(&p, 0, sizeof(p));
   p.logits = logits;
