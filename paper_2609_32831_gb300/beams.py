@@ -54,6 +54,7 @@ class BeamDecoder:
         self._gen: List[List[api.Segment]] = [[], []]
         self._state: List[List[torch.Tensor]] = [[], []]
         self._at = 0               # which of the two sets holds the beams
+        self._stepped = [0] * len(self.decay)  # tokens that each linear layer has taken behind the prompt
         self._chosen: List[Tuple[torch.Tensor, torch.Tensor]] = []
         self.n_pos = 0
         self.scores: Optional[torch.Tensor] = None
@@ -103,6 +104,7 @@ class BeamDecoder:
         self.scores[:, 0] = 0.0
         self.finished = torch.zeros((self.B, K), dtype=torch.bool, device=dev)
         self._chosen = []
+        self._stepped = [0] * len(self.decay)
         self.n_pos = c.n_pos
 
     def _beam_segment(self, s: api.Segment) -> api.Segment:
@@ -124,6 +126,9 @@ class BeamDecoder:
     def linear(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
         """Linear layer ``layer`` for the beams' newest tokens: q [S, Hq, 1,
         128], k, v [S, Hkv, 1, 128] -> o like q; the states advance in place."""
+        if self._stepped[layer] != len(self._chosen) - 1:
+            raise RuntimeError("BeamDecoder.linear: a layer steps once between two selections, the first behind one")
+        self._stepped[layer] += 1
         state = self._state[self._at][layer]
         return api.linear_attend(q, k, v, self.decay[layer], state=state, out_state=state, ws=self.ws)[0]
 
