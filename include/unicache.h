@@ -214,7 +214,9 @@ int32_t uc_set_programmatic_launch(int32_t on);
  * or uc_recompress_segment into a packed segment, whichever comes first)
  * leaves one K row of its group `pos` uncopied (groups counted block by block,
  * each (sequence, KV head) block holding as many groups as the largest keep
- * count has); the waits for it give up after the wait limit
+ * count has), or the next chunked linear attention never makes load `pos` of
+ * each of its CTAs (of the pass before it, where it has one: chunk `pos`'s k);
+ * the waits for it give up after the wait limit
  * and the call reports UC_ERR_TIMEOUT (its outputs are then meaningless).
  * One-shot; a negative `pos` cancels it. */
 void uc_debug_withhold_tile(int32_t pos);

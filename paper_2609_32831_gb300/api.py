@@ -792,7 +792,8 @@ def set_programmatic_launch(on: bool) -> bool:
 
 def debug_withhold_tile(pos: int) -> None:
     """Test hook: the next decode attention call never copies the first tile
-    of its work item at processing position ``pos`` (see unicache.h)."""
+    of its work item at processing position ``pos``, or the next quantization
+    or chunked linear attention one of its copies (see unicache.h)."""
     lib().uc_debug_withhold_tile(int(pos))
 
 

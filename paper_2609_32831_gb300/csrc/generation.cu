@@ -331,6 +331,9 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
   c.start = c.local + states * UC_HEAD_DIM * UC_HEAD_DIM;
   c.status = static_cast<DevStatus*>(workspace);
   c.wait_ns = wait_limit_ns();
+  const int withhold = take_withhold_pos();
+  c.withhold = c.plan.several ? -1 : withhold;
+  c.withhold_sum = c.plan.several ? withhold : -1;
   launch_linear_chunks(c, cs);
   return cuda_check("uc_linear_attend");
 }

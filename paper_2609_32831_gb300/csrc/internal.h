@@ -326,6 +326,8 @@ struct LinearChunkParams {
   float* start;            // the same: the state a run starts from
   DevStatus* status;
   uint64_t wait_ns;
+  int withhold;      // test hook: the load of a CTA, in its order, that is never made (-1: none)
+  int withhold_sum;  // the same for a run's own sum: the chunk whose k is not loaded
 };
 void launch_linear_chunks(const LinearChunkParams& p, cudaStream_t st);
 

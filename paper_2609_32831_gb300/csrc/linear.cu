@@ -419,14 +419,14 @@ __device__ __forceinline__ int sequence_of(const LinearPlan& plan, int batch, in
 // it), with the ordinary limit (the call's may be too short for it). The CTA's
 // waits record in shared memory, so that its end knows of them without a register
 // in any role; they reach the call's status word here.
-__device__ __forceinline__ void drain_cta(LinearSmem& sm, DevStatus* status, int warp) {
+__device__ __forceinline__ void drain_cta(LinearSmem& sm, DevStatus* status, int withhold, int warp) {
   if (threadIdx.x == 0) set_status(status, sm.status.code, sm.status.detail);
   bool gone = false;
   if (warp == kWarpTma) {
     const int loads = sm.loads;
 #pragma unroll 1
     for (int i = max(0, loads - kLSlots); i < loads; ++i)
-      dwait_warp(&sm.full[i % kLFull], (i / kLFull) & 1, status, 52, gone);
+      if (i != withhold) dwait_warp(&sm.full[i % kLFull], (i / kLFull) & 1, status, 52, gone);
   } else if (warp > kWarpTma) {
     uint64_t* const bar = &sm.drain[warp - kWarpQk];
     umma_commit_lead(elect_one(), bar);  // (behind what its elected lane has issued)
@@ -458,7 +458,7 @@ __device__ __forceinline__ LinearTask linear_task(const LinearChunkParams& c, in
 // not finite (what comes behind its run has it from the state). `first` is shared.
 // The CTA's task is worked out anew: nothing has to be kept for it. Rolled loops:
 // warps call it with the registers that their role left them, 72 at least (as a
-// kernel it takes 26).
+// kernel it takes 25).
 __device__ __noinline__ void spoil_outputs(const LinearChunkParams& c, int cta, int* first) {
   const LinearParams& p = c.p;
   const LinearTask k = linear_task(c, cta);
@@ -573,7 +573,9 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
         sm.slot_of[L & 15] = (uint8_t)s;
         uint64_t* bar = &sm.full[L % kLFull];
         const int t = (c0 + ci) * kChunk;
-        if (in == 0)
+        if (L == c.withhold) {
+          // test hook: this tile is never copied
+        } else if (in == 0)
           load_tile(sm.slot[s], &c.tk, t, kvh, b, bar);
         else if (in == 2)
           load_tile(sm.slot[s], &c.tv, t, kvh, b, bar);
@@ -962,7 +964,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
     tc_fence_before();
   }
   __syncthreads();
-  if (sm.status.code != 0) drain_cta(sm, c.status, warp);
+  if (sm.status.code != 0) drain_cta(sm, c.status, c.withhold, warp);
   if (warp == kWarpMma) {
     __syncwarp();
     tc_fence_after();
@@ -1049,7 +1051,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
       const int s = ci % kLocalRing;
       if (ci >= kLocalRing && !dwait(&sm.empty[s], (ci / kLocalRing - 1) & 1, st, 70, aborted, lim)) break;
       load_tile(sm.v[s], &c.tv, (c0 + ci) * kChunk, kvh, b, &sm.v_full[s]);
-      load_tile(sm.k[s], &c.tk, (c0 + ci) * kChunk, kvh, b, &sm.k_full[s]);
+      if (ci != c.withhold_sum) load_tile(sm.k[s], &c.tk, (c0 + ci) * kChunk, kvh, b, &sm.k_full[s]);  // (test hook)
       loaded = ci + 1;
     }
     sm.loads = loaded;
@@ -1124,7 +1126,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_local_kernel(const __grid
       const int loads = sm.loads;
 #pragma unroll 1
       for (int i = max(0, loads - kLocalRing); i < loads; ++i) {
-        dwait_warp(&sm.k_full[i % kLocalRing], (i / kLocalRing) & 1, c.status, 71, gone);
+        if (i != c.withhold_sum) dwait_warp(&sm.k_full[i % kLocalRing], (i / kLocalRing) & 1, c.status, 71, gone);
         dwait_warp(&sm.v_full[i % kLocalRing], (i / kLocalRing) & 1, c.status, 71, gone);
       }
     } else if (warp == kWarpMma) {
