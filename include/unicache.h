@@ -650,8 +650,8 @@ typedef struct uc_rows {
  * infinity its outputs and states then hold is left open.
  * Query head h reads KV head h / (Hq / Hkv). n_tok <= UC_MAX_QTOKENS (decode)
  * takes the recurrence token by token in fp32; more take chunks of 128 tokens
- * on the tensor cores, with the decayed q.k and the state that q multiplies
- * rounded to bf16 and sums and states in fp32. 1 <= B <= UC_MAX_BATCH, Hkv <= UC_MAX_LINEAR_HEADS,
+ * on the tensor cores, with the decayed q.k and the state that q multiplies as
+ * two bf16 parts each (2^-18 of a factor) and sums and states in fp32. 1 <= B <= UC_MAX_BATCH, Hkv <= UC_MAX_LINEAR_HEADS,
  * 1 <= n_tok <= 2^28. Rows of out share no memory with one another, with rows of
  * q, k and v, or with the states (rows may interleave in one buffer); nor does
  * state_out with any of them.

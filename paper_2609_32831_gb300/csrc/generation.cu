@@ -154,7 +154,7 @@ static bool linear_steps(int n_q_heads, int n_kv_heads, int n_tok) {
 // head and chunk, a chunk's update of the state (beside its tiles, a chain that
 // takes kChain), a CTA's start and end; the same for the pass before.
 static LinearPlan plan_linear(int batch, int n_q_heads, int n_kv_heads, const int32_t* lengths) {
-  constexpr double kTile = 3400, kUpdate = 2500, kChain = 10500, kCta = 9000, kSumChunk = 4000, kSumCta = 14000;
+  constexpr double kTile = 4300, kUpdate = 3900, kChain = 11500, kCta = 9000, kSumChunk = 4000, kSumCta = 14000;
   const int g = n_q_heads / n_kv_heads, sms = num_sms();
   int64_t chunks = 0;
   int longest = 1;

@@ -122,29 +122,29 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 // it and nv its valid tokens,
 //   o_i  = a_i (q_i S + sum_{j <= i} (q_i . k_j) gamma^{-(j+1)} v_j) / sqrt(128),  a_i = gamma^{i+1}
 //   S'   = gamma^nv S + sum_j k_j (gamma^{nv-1-j} v_j)^T
-// so a chunk costs three 128^3 products per query head (Q K^T, Q S and P V, the
-// last two into one accumulator) and one per KV head for the state. The floor is
-// HBM: 64 KB of q and o per head and chunk, 1.5 us of an SM's share, against
-// 3 x 512 cycles of the tensor pipe. What bounds it are hand-overs between
-// warps: with seven heads a tile's (o read, Q S, P V: 3600 cycles), with one
-// head those of the state's update (10 to 11 thousand cycles a chunk).
-// 8 x 8192 tokens, 28 query and 4 KV heads: 263 us, 4.1 TB/s of q, k, v and o;
-// 16 x up to 4097 tokens of 16 heads: 214 us, 3.0 TB/s; 131072 tokens: 456 to
-// 475 us, 4.6 TB/s.
+// so a chunk costs Q K^T, Q S and P V per query head, the last two into one
+// accumulator and with S and P in two parts (five 128^3 products), and one with
+// three parts per KV head for the state. The floor is HBM: 64 KB of q and o per
+// head and chunk, 1.5 us of an SM's share, against 5 x 512 cycles of the tensor
+// pipe. What bounds it are a tile's products and the hand-overs between warps, one
+// after the other: with seven heads o read, Q S, P V (4300 to 4900 cycles a tile),
+// with one head those of the state's update (11.6 thousand cycles a chunk).
+// 8 x 8192 tokens, 28 query and 4 KV heads: 330 us, 3.3 TB/s of q, k, v and o;
+// 16 x up to 4097 tokens of 16 heads: 229 us, 2.8 TB/s; 131072 tokens: 591 us,
+// 3.6 TB/s.
 //
 // One CTA per (sequence, KV head, run of chunks, part of its query heads):
 //   WG0, WG1 (warps 0-7) halves of the columns of Q K^T: P = mask and weights,
-//            bf16, back to tensor memory
+//            two bf16 parts, back to tensor memory
 //   WG2, WG3 (8-15) the epilogue, halves of the channels: o scaled, rounded and
 //            stored, turned around in shared memory so that two lanes write a
 //            32-byte sector of a row
 //   WG4      (16-19) the state. It stays in tensor memory in fp32; per chunk
-//            its bf16 copy goes to shared memory for Q S, what that rounding
-//            left stays behind, scaled by gamma^nv, and the chunk's decayed
-//            values are formed in slices of 16 tokens (with one or two heads
-//            the odd ones by WG0 and WG1) that accumulate on the
-//            rest while the chunk's tiles run; the copy joins them, scaled,
-//            in fp32. (The tensor cores' sums are cut, not rounded: 24 of them
+//            its bf16 copy goes to shared memory for Q S, and in bf16 what that
+//            rounding left; in fp32 that stays behind, scaled by gamma^nv, and the
+//            chunk's decayed values are formed in slices of 16 tokens (with one or
+//            two heads the odd ones by WG0 and WG1) that accumulate on the rest
+//            while the chunk's tiles run; the copy joins them, scaled, in fp32. (The tensor cores' sums are cut, not rounded: 24 of them
 //            per chunk on the whole state pulled it towards zero by up to 1.2e-5
 //            of its size where gamma is near 1; on the rest they cost 1e-7 of the
 //            chunk's own sum.)
@@ -158,20 +158,24 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 // its end: they may hold NaN, and 0 x NaN is not 0. For the same reason a NaN or
 // infinity in v would reach earlier tokens through P V, where their P is 0. So
 // WG0 and WG1 look a chunk's v through beside its first P (on the issuing warp,
-// between two products, 8 x 8192 tokens took 281 us). Where they find any, the
+// between two products, 7 % of 8 x 8192 tokens). Where they find any, the
 // chunk's slices are formed first (the state takes them as they are), warp 22
 // puts zeros in their place before P V, and behind its last tile the CTA makes NaN
-// of a channel's outputs from the token on that held one (8 x 8192 tokens 265 us in
-// all, 262 without any of it; code for it in the epilogue's loop: 275 to 300).
+// of a channel's outputs from the token on that held one (1 % in all; code for it
+// in the epilogue's loop: 5 to 14 %).
 // Order of the products: Q K^T of the next tile while the epilogue reads the
 // last one's o, then Q S and P V. (With the epilogue and the update on the
 // warps that form P, and rows stored from registers, 32 lines per instruction,
 // a tile took 4900 cycles and an update of the state 6500.)
 //
-// Roundings to bf16: P and the copy of S that Q multiplies (each about as
-// large as the output's own rounding), and none on the state's path: the
-// decayed values enter as three bf16 parts (all 24 bits of v gamma^n; two parts left
-// the state 2.7e-6 off), the update accumulates in fp32.
+// Roundings to bf16: the output's own, 1.66e-3 of its norm, is the only one that
+// shows. P and the copy of S that Q multiplies enter as two bf16 parts each (16
+// bits); with one part each the output's error was 2.34e-3, with P alone in two
+// 2.18e-3. That took 266 us instead of 330 for 8 x 8192 tokens and 208 instead of 229
+// for 16 x up to 4097: two products fewer per tile, and 32 KB for a fifth slot (20 of
+// the 64 us). None on the state's path: the decayed values enter as three bf16 parts
+// (all 24 bits of v gamma^n; two parts left the state 2.7e-6 off), the update
+// accumulates in fp32.
 //
 // a_i and gamma^{-(j+1)} take the row's common factor out of both products.
 // Where gamma^128 < 2^-64 (a memory of under two tokens) a_i stops at 2^-64 and
@@ -194,7 +198,7 @@ constexpr int kSlices = kChunk / kSlice;
 constexpr uint32_t kSliceBytes = kSlice * kHeadDim * 2;
 constexpr float kLeastScale = 5.421010862427522e-20f;  // 2^-64
 constexpr int kHelpHeads = 2;  // query heads up to which WG0 and WG1 form the odd slices
-constexpr int kLSlots = 5;
+constexpr int kLSlots = 4;
 constexpr int kLFull = 8;  // "arrived" barriers, by load number: more than loads in flight
 
 template <int N>
@@ -205,6 +209,7 @@ __device__ __forceinline__ void rebalance() {
 
 struct LinearSmem {
   uint8_t slot[kLSlots][kTileBytes];   // [2 x 64 channels][128 tokens][128 B], 128B swizzle
+  uint8_t s_rest[kTileBytes];          // what s leaves of it, the same
   uint8_t s[kTileBytes];               // the chunk's state, bf16 [2 x 64 value channels][128 key channels][128 B]
   uint8_t part[2][3][kSliceBytes];     // decayed values, three parts: [2 x 64 channels][16 tokens][128 B]
   uint4 turn[8][32 * 2];               // per epilogue warp: 32 rows of 32 B
@@ -307,12 +312,12 @@ __device__ __forceinline__ void issue_q_s(uint32_t lead, uint32_t d, uint32_t a,
   for (uint32_t k = 0; k < 8; ++k)
     issue_ss(lead, d, a + (k & 3) * 2 + (k >> 2) * (kTileBytes >> 5), b + 128 * k, hi, id, acc | k);
 }
-// O (+)= P V: P of keys 0-63 in the slot's columns 0-31, of keys 64-127 in 64-95
-// (each warpgroup's P lies in the columns that it alone read).
+// O (+)= P V: the two parts of P of 16 keys, eight columns each, lie where their S
+// was read from.
 __device__ __forceinline__ void issue_p_v(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id,
                                           uint32_t acc) {
 #pragma unroll 1
-  for (uint32_t k = 0; k < 8; ++k) issue_ts(lead, d, a + 8 * k + 32 * (k >> 2), b + 128 * k, hi, id, acc | k);
+  for (uint32_t k = 0; k < 16; ++k) issue_ts(lead, d, a + 8 * k, b + 128 * (k >> 1), hi, id, acc | k);
 }
 
 // The decayed values of tokens ROWS sl .. ROWS sl + ROWS - 1 of a chunk as
@@ -353,6 +358,13 @@ __device__ __forceinline__ void decay_slice(const uint8_t* v, uint8_t (*parts)[R
 __device__ __forceinline__ void issue_slice(uint32_t lead, uint32_t d, uint32_t k, uint32_t parts, uint32_t hi, uint32_t id) {
 #pragma unroll 1
   for (uint32_t u = 0; u < 3; ++u) issue_ss(lead, d, k, parts + u * (kSliceBytes >> 4), hi, id, 1u);
+}
+
+// Two values as bf16 and as bf16 of what that leaves.
+__device__ __forceinline__ void two_parts(float a, float b, uint32_t& whole, uint32_t& rest) {
+  whole = pack_bf16(a, b);
+  f2_unpack(f2_fma(f2_pack(bf16_lo(whole), bf16_hi(whole)), f2_pack(-1.f, -1.f), f2_pack(a, b)), a, b);
+  rest = pack_bf16(a, b);
 }
 
 // Zeroes rows nv .. 127 of a tile, by one warp.
@@ -653,6 +665,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
           if (h > 0) {
             tc_fence_after();
             issue_q_s(lead, tm + kColOut, row_lo + qs * kStep, s_lo, dhi, id_b, 0u);
+            issue_q_s(lead, tm + kColOut, row_lo + qs * kStep, s_lo - kStep, dhi, id_b, 1u);
             if (last) umma_commit_lead(lead, &sm.s_free);
           }
           if (!dwait_warp(&sm.p_full[t & 1], (t >> 1) & 1, st, 61, aborted, lim)) break;
@@ -674,6 +687,7 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
             if (!dwait_warp(&sm.st_ready, ci & 1, st, 57, aborted, lim)) break;
             tc_fence_after();
             issue_q_s(lead, tm + kColOut, row_lo + qs * kStep, s_lo, dhi, id_b, 1u);
+            issue_q_s(lead, tm + kColOut, row_lo + qs * kStep, s_lo - kStep, dhi, id_b, 1u);
             if (last) umma_commit_lead(lead, &sm.s_free);
             umma_commit_lead(lead, &sm.empty[qs]);
           }
@@ -777,18 +791,22 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
         whole_state(blk, x, ci > 0, sm.pw[kChunk]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          uint32_t w[4];
+          uint32_t w[4], rest[4];
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             float a = __uint_as_float(x[8 * e + 2 * u]), c = __uint_as_float(x[8 * e + 2 * u + 1]);
             w[u] = pack_bf16(a, c);
             // what rounding leaves (anything finite where the state has overflowed)
             f2_unpack(f2_fma(f2_pack(bf16_lo(w[u]), bf16_hi(w[u])), f2_pack(-1.f, -1.f), f2_pack(a, c)), a, c);
-            f2_unpack(f2_mul(f2_pack(fminf(a, 3e38f), fminf(c, 3e38f)), f2_pack(g, g)), a, c);
+            a = fminf(a, 3e38f);
+            c = fminf(c, 3e38f);
+            rest[u] = pack_bf16(a, c);
+            f2_unpack(f2_mul(f2_pack(a, c), f2_pack(g, g)), a, c);
             x[8 * e + 2 * u] = __float_as_uint(a);
             x[8 * e + 2 * u + 1] = __float_as_uint(c);
           }
           *copy(blk, e) = make_uint4(w[0], w[1], w[2], w[3]);
+          *(copy(blk, e) - kTileBytes / 16) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
         }
         if (update) tmem_st32(s_addr + 32 * blk, x);
       }
@@ -900,10 +918,10 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
         uint32_t(&y)[16] = sr[q & 1];
         tmem_wait_ld16(y);
         if (q < 3 && j0 + 16 < wr + 32) tmem_ld16(slot + 16 * (q + 1), sr[(q + 1) & 1]);
-        uint32_t pk[8];
+        uint32_t pk[8], pl[8];
         if (j0 >= wr + 32) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) pk[e] = 0u;
+          for (int e = 0; e < 8; ++e) pk[e] = pl[e] = 0u;
         } else if (!strong) {
           const ulonglong2* cj = reinterpret_cast<const ulonglong2*>(sm.cj + j0);  // pairs of fp32
 #pragma unroll
@@ -912,14 +930,17 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
             float z[4];
             f2_unpack(f2_mul(f2_pack(__uint_as_float(y[4 * e]), __uint_as_float(y[4 * e + 1])), w.x), z[0], z[1]);
             f2_unpack(f2_mul(f2_pack(__uint_as_float(y[4 * e + 2]), __uint_as_float(y[4 * e + 3])), w.y), z[2], z[3]);
-            pk[2 * e] = pack_bf16(z[0], z[1]);
-            pk[2 * e + 1] = pack_bf16(z[2], z[3]);
+            two_parts(z[0], z[1], pk[2 * e], pl[2 * e]);
+            two_parts(z[2], z[3], pk[2 * e + 1], pl[2 * e + 1]);
           }
           if (j0 >= wr) {  // keys up to the token (later ones may hold anything)
             const int last = r - j0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              pk[e] &= (2 * e <= last ? 0xffffu : 0u) | (2 * e + 1 <= last ? 0xffff0000u : 0u);
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t mask = (2 * e <= last ? 0xffffu : 0u) | (2 * e + 1 <= last ? 0xffff0000u : 0u);
+              pk[e] &= mask;
+              pl[e] &= mask;
+            }
           }
         } else {
 #pragma unroll
@@ -930,10 +951,11 @@ __global__ void __launch_bounds__(kLThreads, 1) linear_chunk_kernel(const __grid
               const int back = r - j0 - 2 * e - u;  // tokens since the key
               z[u] = back >= 0 ? __uint_as_float(y[2 * e + u]) * (sm.pw[max(back, 0)] * inv_a) : 0.f;
             }
-            pk[e] = pack_bf16(z[0], z[1]);
+            two_parts(z[0], z[1], pk[e], pl[e]);
           }
         }
-        tmem_st8(slot + 8 * q, pk);
+        tmem_st8(slot + 16 * q, pk);
+        tmem_st8(slot + 16 * q + 8, pl);
       }
       if (h == 0) {
         const int L = load_v(ci);
