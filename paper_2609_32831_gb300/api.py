@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+from functools import partial
 from typing import List, Optional, Sequence, Tuple
 
 import torch
@@ -638,6 +639,20 @@ def append_next(seg: Segment, k_new: torch.Tensor, v_new: torch.Tensor, base_pos
 
 # -------------------------------------- layers with a state of constant size
 
+def _new(stream, *makers):
+    """New outputs of a launch on ``stream``: from that stream's memory (the
+    current one's may hold what its queued work still uses), and not given away
+    before the current stream, which called, is done with them."""
+    if stream is None:
+        return [make() for make in makers]
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        made = [make() for make in makers]
+    for t in made:
+        t.record_stream(here)
+    return made
+
+
 _pack_rows = struct.Struct("=Qqqq").pack   # uc_rows (bytes are built faster than a Structure)
 _pack_item = struct.Struct("=QQQQQ").pack  # uc_reorder_item
 
@@ -667,19 +682,15 @@ def linear_attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: 
     if len(log_decay) != hkv or (lengths is not None and len(lengths) != B):
         raise ValueError("linear_attend: one log_decay per KV head, one length per sequence")
     if out is None:
-        out = torch.empty_like(q)
-        if stream is not None:
-            out.record_stream(stream)
+        out = torch.empty_like(q) if stream is None else _new(stream, lambda: torch.empty_like(q))[0]
     elif out.shape != q.shape or out.dtype != q.dtype or out.stride(3) != 1:
         raise ValueError("linear_attend: out has q's shape and type, every row contiguous")
     for s in (state,) if out_state is None or out_state is state else (state, out_state):
         if s is not None and (s.shape != (B, hkv, d, d) or s.dtype is not torch.float32 or not s.is_contiguous()):
             raise ValueError("linear_attend: states are contiguous fp32 [B, Hkv, 128, 128]")
     if out_state is None:
-        out_state = torch.empty((B, hkv, d, d), dtype=torch.float32, device=q.device) if state is None else \
-            torch.empty_like(state)
-        if stream is not None:
-            out_state.record_stream(stream)
+        out_state = _new(stream, lambda: torch.empty((B, hkv, d, d), dtype=torch.float32, device=q.device))[0] \
+            if state is None or stream is not None else torch.empty_like(state)
     ws = ws or default_workspace(q.device)
     L = lib()
     so = out.stride()
@@ -717,13 +728,8 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int, finished: Op
                                  or not finished.is_contiguous()):
         raise ValueError("beam_select: finished is contiguous bool [B, K]")
     dev = logits.device
-    best = torch.empty((B, n), dtype=torch.float32, device=dev)
-    parent = torch.empty((B, n), dtype=torch.int32, device=dev)
-    token = torch.empty_like(parent)
-    done = torch.empty((B, n), dtype=torch.bool, device=dev)
-    if stream is not None:
-        for t in (best, parent, token, done):
-            t.record_stream(stream)
+    best, parent, token, done = _new(stream, *(partial(torch.empty, (B, n), dtype=t, device=dev)
+                                               for t in (torch.float32, torch.int32, torch.int32, torch.bool)))
     ws = ws or default_workspace(dev)
     L = lib()
     args = (logits.data_ptr(), kind, sb, sk, B, K, V, scores.data_ptr(), _ptr(finished), eos, n,
