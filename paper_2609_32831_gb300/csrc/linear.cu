@@ -17,10 +17,10 @@ namespace uc {
 // partial sums over a warp's rows meet in shared memory. Everything is loaded
 // before the first token is taken: the state into registers, k, v and (where
 // they fit) q of all tokens into shared memory. Bound by HBM in large batches:
-// 64 sequences of 4 heads, 34.6 MB: 8.5 us, 4.1 TB/s; by the latency of its
-// loads and one reduction per token in small ones (one sequence: 3.7 us).
-// (Loads token by token: 9.1 and 4.1 us, five tokens of 8 x 16 heads 10.1
-// instead of 8.0.)
+// 64 sequences of 4 heads, 34.6 MB: 8.1 us, 4.3 TB/s; by the latency of its
+// loads and one reduction per token in small ones (one sequence: 3.3 us).
+// (Loads token by token: 0.6 and 0.4 us more, five tokens of 8 x 16 heads 2 us
+// more than their 7.5.)
 constexpr int kStepCols = 32;
 constexpr int kStepWarps = 8;
 constexpr int kStepRows = kHeadDim / kStepWarps;
