@@ -144,10 +144,11 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 //            rounding left; in fp32 that stays behind, scaled by gamma^nv, and the
 //            chunk's decayed values are formed in slices of 16 tokens (with one or
 //            two heads the odd ones by WG0 and WG1) that accumulate on the rest
-//            while the chunk's tiles run; the copy joins them, scaled, in fp32. (The tensor cores' sums are cut, not rounded: 24 of them
-//            per chunk on the whole state pulled it towards zero by up to 1.2e-5
-//            of its size where gamma is near 1; on the rest they cost 1e-7 of the
-//            chunk's own sum.)
+//            while the chunk's tiles run; the copy joins them, scaled, in fp32.
+//            (The tensor cores' sums are cut, not rounded: 24 of them per chunk on
+//            the whole state pulled it towards zero by up to 1.2e-5 of its size
+//            where gamma is near 1; on the rest they cost 1e-7 of the chunk's own
+//            sum.)
 //   warp 20  TMA producer: k and v tiles per chunk and a q tile per head, in the
 //            order they are needed, each into whichever slot is free
 //   warp 21  issues Q K^T, one tile ahead
@@ -166,7 +167,7 @@ void launch_linear_step(const LinearParams& p, cudaStream_t st) {
 // Order of the products: Q K^T of the next tile while the epilogue reads the
 // last one's o, then Q S and P V. (With the epilogue and the update on the
 // warps that form P, and rows stored from registers, 32 lines per instruction,
-// a tile took 4900 cycles and an update of the state 6500.)
+// a tile took a third longer and an update of the state 6500 cycles.)
 //
 // Roundings to bf16: the output's own, 1.66e-3 of its norm, is the only one that
 // shows. P and the copy of S that Q multiplies enter as two bf16 parts each (16
