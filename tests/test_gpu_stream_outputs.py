@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 uc = pytest.importorskip("paper_2609_32831_gb300")
 
 DEV = "cuda"
-LONG = 200_000_000   # cycles, about 0.1 s
+LONG = 1_000_000_000   # cycles, about half a second
 
 
 def _linear(side):

@@ -17,7 +17,7 @@ def test_the_status_word_stays():
 
 
 DEV = "cuda"
-LONG = 200_000_000   # cycles, about 0.1 s
+LONG = 1_000_000_000   # cycles, about half a second
 
 
 def _select(ws, stream=None, bad=False):
