@@ -729,6 +729,141 @@ typedef struct uc_reorder_item {
 uc_status uc_reorder(const uc_reorder_item* items, int32_t n_items, const int32_t* parent, int32_t n_groups,
                      int32_t n_from, int32_t n_to, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------ positions of tokens (rotary) */
+
+#define UC_MAX_ROTARY_PAIRS 64  /* UC_HEAD_DIM / 2 */
+
+/* A rotation by position, host: pair i of a row turns by position * freq[i]
+ * radians and is multiplied by `scale`,
+ *   a' = scale (a cos - b sin),  b' = scale (a sin + b cos).
+ * Pair i is channels (i, i + n_pairs), or (2 i, 2 i + 1) where `interleaved`;
+ * channels from 2 * n_pairs on stay as they are (without `scale`). Long-context
+ * rescalings are a matter of freq and scale. Angles are formed as 64-bit
+ * fractions of a turn, so that every int32 position is as exact as the first
+ * ones: within 2^-32 turns for |freq| <= 64. */
+typedef struct uc_rotary_table {
+  int32_t n_pairs;                     /* 1 .. UC_MAX_ROTARY_PAIRS */
+  int32_t interleaved;                 /* 0 or 1 */
+  double scale;                        /* finite */
+  double freq[UC_MAX_ROTARY_PAIRS];    /* finite, |freq| < 2^31 */
+} uc_rotary_table;
+
+/*
+ * Rotary positions of the rows of q and, where k is not NULL, of k, in one
+ * launch; the compressed cache and uc_attend take keys and queries that are
+ * turned already.
+ *   q, k            [B, n_heads, n_tok] rows of `dtype` elements (UC_FP32,
+ *                   UC_BF16, UC_FP16; uc_rows' strides are in elements)
+ *   q_out, k_out    the same shapes; the same rows as q or k (then in place), or
+ *                   rows that share no memory with q, k or one another
+ *   positions       device int32: [B, n_tok] where per_token, else [B], the
+ *                   position of each sequence's first token
+ * fp32 arithmetic whatever the type, rounded once.
+ */
+uc_status uc_rotary(const uc_rotary_table* table, const int32_t* positions, int32_t per_token, int32_t dtype,
+                    int32_t batch, int32_t n_tok, const uc_rows* q, const uc_rows* q_out, int32_t n_q_heads,
+                    const uc_rows* k, const uc_rows* k_out, int32_t n_kv_heads, void* stream);
+
+/* ------------------------------- layers with a sliding window and first tokens */
+
+/* The cache of a layer whose queries see the last `window` tokens up to
+ * themselves and the first n_sink ones, for `batch` sequences. Token p of a
+ * sequence lies in row p where p < n_sink, else in row
+ * n_sink + (p - n_sink) mod (n_rows - n_sink): the rows behind the first ones
+ * are a ring, or, where n_rows covers every token, all of them in order. */
+typedef struct uc_window_cache {
+  uc_rows k, v;                        /* bf16 [batch, n_kv_heads, n_rows] rows */
+  int32_t batch, n_kv_heads, n_rows;
+  int32_t window;                      /* >= 1 */
+  int32_t n_sink;                      /* 0 .. n_rows - 1 */
+} uc_window_cache;
+
+/*
+ * New tokens into such a cache, and their rotary positions, in one launch:
+ * token t < n_new[b] of sequence b gets position held[b] + t and is stored in
+ * that position's row, k turned by `table` (as it is where that is NULL).
+ * Of tokens that fall into one row of the ring the last one stays.
+ *   k, v       bf16 [B, Hkv, n_tok] rows
+ *   held       device int32 [B], tokens that each sequence holds already
+ *   n_new      device int32 [B], 0 .. n_tok; NULL: n_tok each
+ *   q, q_out   nullable, both or neither: bf16 [B, n_q_heads, n_tok] rows, turned
+ *              by their positions (all n_tok of them); needs `table`
+ *   out_total  device int32 [B]: held + n_new; not the array of held
+ * q_out may be the same rows as q; otherwise what is written shares no memory with
+ * what is read. A negative held, an n_new out of range or a sum beyond 2^31 - 1
+ * sets UC_ERR_RANGE in the status word; that sequence is then not stored, and
+ * its out_total is held. workspace: >= 256 bytes (status word).
+ */
+uc_status uc_window_append(const uc_window_cache* cache, const uc_rows* k, const uc_rows* v, int32_t n_tok,
+                           const int32_t* held, const int32_t* n_new, const uc_rotary_table* table,
+                           const uc_rows* q, const uc_rows* q_out, int32_t n_q_heads, int32_t* out_total,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of a layer with a sliding window: sequence b holds lengths[b]
+ * tokens, the last n_query[b] of which are the queries. Query t (position
+ * p = lengths[b] - n_query[b] + t) of query head h attends with
+ *   o = softmax(q . k / sqrt(128)) v
+ * to the tokens j <= p of KV head h / (Hq / Hkv) with p - j < window or
+ * j < n_sink, as far as the cache holds them: a ring that is shorter than
+ * window + n_query - 1 has lost some to later tokens.
+ *   q, out     bf16 [B, n_q_heads, n_tok] rows
+ *   lengths    device int32 [B], >= 0: tokens held, the queries' own among them
+ *   n_query    device int32 [B], 0 .. n_tok; NULL: n_tok each
+ *   lse        fp32 [B, n_q_heads, n_tok], nullable: log-sum-exp of the scaled
+ *              products (natural logarithm)
+ * Rows from n_query[b] on and queries that see no token are 0, their lse -inf.
+ * Rows of the cache that hold no token are not used: they may be anything. What a
+ * query does not see does not reach it, NaN and infinities included. A length or
+ * n_query out of range sets UC_ERR_RANGE in the status word; it is then taken
+ * as the nearest in range.
+ * out and lse share no memory with one another or with what is read. workspace:
+ * uc_window_workspace_size() bytes, 16-byte aligned.
+ */
+uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32_t n_q_heads, int32_t n_tok,
+                           const int32_t* lengths, const int32_t* n_query, const uc_rows* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
+size_t uc_window_workspace_size(const uc_window_cache* cache, int32_t n_q_heads, int32_t n_tok);
+
+/* ------------------------------------------------- drafted tokens (speculation) */
+
+/*
+ * Drafted tokens against the target's probabilities: which are accepted, and
+ * the token that follows them. Per sequence, with n = n_draft[b] drafts d_t,
+ * p_t = softmax(target[b, t] / temperature) and q_t = softmax(draft[b, t] /
+ * temperature), or q_t = 1 at d_t where draft is NULL:
+ *   draft t is accepted while u[b, t] q_t(d_t) < p_t(d_t); a = the first that is not
+ *   the next token is argmax_v w_v / noise[b, v], the lowest v of equal ones, with
+ *   w = max(p_a - q_a, 0) where a < n and w = p_n where all were accepted
+ * so that with uniform u and noise from the exponential distribution the tokens
+ * are distributed as the target's own. temperature 0: a draft is accepted while it
+ * is the target's best (the lowest of equal ones), and the next token is that;
+ * draft, u and noise are not read and may be NULL, log probabilities are those of
+ * temperature 1.
+ *   target     [B, n_tok + 1, V] of `dtype`, row (b, t) at b*target_b + t*target_t
+ *              elements, V contiguous; -inf bans a token
+ *   draft      [B, n_tok, V] of the same type, nullable, in the same way
+ *   tokens     int32 [B, n_tok]
+ *   n_draft    int32 [B], 0 .. n_tok; NULL: n_tok each. Rows behind are not read
+ *   u          fp32 [B, n_tok] in [0, 1);  noise  fp32 [B, V], > 0
+ *   accepted   int32 [B]: a
+ *   out_tokens int32 [B, n_tok + 1]: the accepted drafts, the next token, then -1
+ *   logprob    fp32 [B, n_tok + 1]: their log p, then 0
+ * NaN and +inf logits, rows without a finite logit, drafts outside the
+ * vocabulary (they are not accepted; one with probability 0 is neither) and an
+ * n_draft out of range (taken as the nearest) set UC_ERR_RANGE in the
+ * status word; NaN and +inf count as -inf. 1 <= n_tok <= UC_MAX_DRAFTS,
+ * B * (n_tok + 1) <= 65535, temperature finite and >= 0. Outputs share no memory with one another or with
+ * inputs. workspace: uc_verify_workspace_size() bytes, 16-byte aligned.
+ */
+#define UC_MAX_DRAFTS 64
+uc_status uc_verify_draft(const void* target, int64_t target_b, int64_t target_t, const void* draft, int64_t draft_b,
+                          int64_t draft_t, int32_t dtype, int32_t batch, int32_t n_tok, int32_t vocab,
+                          const int32_t* tokens, const int32_t* n_draft, const float* u, const float* noise,
+                          double temperature, int32_t* accepted, int32_t* out_tokens, float* logprob, void* workspace,
+                          size_t workspace_bytes, void* stream);
+size_t uc_verify_workspace_size(int32_t batch, int32_t n_tok, int32_t vocab);
+
 #ifdef __cplusplus
 }
 #endif

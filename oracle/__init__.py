@@ -28,10 +28,13 @@ Modules and the passages they follow:
                   per-segment attention mass (App. E, Eq. 1).
 * ``linear``    — linear attention with a decay for each KV head.
 * ``beams``     — beam selection and the reordering of sequences.
+* ``rotary``    — rotary positions.
+* ``window``    — the cache of a layer with a sliding window, attention over it.
+* ``drafts``    — verification of drafted tokens.
 
 Parity status of each function is stated in its module docstring. The only
 unpinned item is whether Gaussian synthetic attention resembles a trained
 model's (no model weights or datasets exist here): "parity unpinned" for
 workload realism, not for any function below.
 """
-from . import scores, policy, select, quant, segment, attention, linear, beams  # noqa: F401
+from . import scores, policy, select, quant, segment, attention, linear, beams, rotary, window, drafts  # noqa: F401

@@ -10,10 +10,10 @@ from .api import (KIND_EVICT, KIND_EVICT_QUANT, KIND_FULL, KIND_QUANT, POLICY_EV
                   accumulate_scores, allocate_budget, append, append_next, attend, attend_batch, attend_plan,
                   attend_workspace_size,
                   attention_mass, beam_select, calibrate_policy, compress_budget, compress_segment, concentration, keep_count,
-                  launch_count, linear_attend, OwnedSegment,
+                  launch_count, linear_attend, OwnedSegment, Rotary, rotary,
                   plan_batch, recompress_segment, reorder, retention_schedule, retention_step, score_accumulate,
                   segment_mass, set_dense_serial_pv, set_programmatic_launch, set_wait_limit,
-                  debug_withhold_tile, version)
+                  debug_withhold_tile, verify_draft, version, window_append, window_attend, WindowCache)
 
 __all__ = [
     "Segment", "SegmentTable", "Workspace", "UniCacheError", "accumulate_scores", "allocate_budget", "append", "append_next",
@@ -22,6 +22,7 @@ __all__ = [
     "concentration", "keep_count", "launch_count", "linear_attend", "plan_batch", "recompress_segment", "reorder",
     "retention_schedule",
     "retention_step", "score_accumulate",
+    "Rotary", "rotary", "verify_draft", "window_append", "window_attend", "WindowCache",
     "segment_mass", "set_dense_serial_pv", "set_programmatic_launch", "set_wait_limit", "debug_withhold_tile", "version", "KIND_FULL", "KIND_EVICT", "KIND_QUANT",
     "KIND_EVICT_QUANT", "POLICY_EVICT", "POLICY_QUANT", "POLICY_PROTECTED",
 ]

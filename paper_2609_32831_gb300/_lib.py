@@ -79,6 +79,20 @@ class UcRows(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("stride_t", C.c_int64)]
 
 
+MAX_ROTARY_PAIRS = 64
+MAX_DRAFTS = 64
+
+
+class UcRotaryTable(C.Structure):
+    _fields_ = [("n_pairs", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_double),
+                ("freq", C.c_double * MAX_ROTARY_PAIRS)]
+
+
+class UcWindowCache(C.Structure):
+    _fields_ = [("k", UcRows), ("v", UcRows), ("batch", C.c_int32), ("n_kv_heads", C.c_int32), ("n_rows", C.c_int32),
+                ("window", C.c_int32), ("n_sink", C.c_int32)]
+
+
 class UcReorderItem(C.Structure):
     _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("state_src", C.c_void_p), ("state_dst", C.c_void_p),
                 ("state_bytes", C.c_uint64)]
@@ -152,6 +166,14 @@ _SIGS = {
                                  C.c_int32, C.c_int32, _P, _P, _P, _P, _P, C.c_size_t, _P]),
     "uc_beam_workspace_size": (C.c_size_t, [C.c_int32] * 4),
     "uc_reorder": (C.c_int, [_P, C.c_int32, _P, C.c_int32, C.c_int32, C.c_int32, _P, C.c_size_t, _P]),
+    "uc_rotary": (C.c_int, [_P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P, C.c_int32, _P, _P, C.c_int32,
+                            _P]),
+    "uc_window_append": (C.c_int, [_P, _P, _P, C.c_int32, _P, _P, _P, _P, _P, C.c_int32, _P, _P, C.c_size_t, _P]),
+    "uc_window_attend": (C.c_int, [_P, _P, C.c_int32, C.c_int32, _P, _P, _P, _P, _P, C.c_size_t, _P]),
+    "uc_window_workspace_size": (C.c_size_t, [_P, C.c_int32, C.c_int32]),
+    "uc_verify_draft": (C.c_int, [_P, C.c_int64, C.c_int64, _P, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
+                                  C.c_int32, _P, _P, _P, _P, C.c_double, _P, _P, _P, _P, C.c_size_t, _P]),
+    "uc_verify_workspace_size": (C.c_size_t, [C.c_int32] * 3),
     "uc_append": (C.c_int, [C.POINTER(UcSegment), _P, _P, C.c_int32, _P, C.c_size_t, _P]),
     "uc_append_next": (C.c_int, [C.POINTER(UcSegment), _P, _P, C.c_int32, _P, C.c_size_t, _P]),
 }

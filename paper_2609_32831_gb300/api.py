@@ -777,6 +777,223 @@ def reorder(pairs, parent: torch.Tensor, ws: Optional[Workspace] = None, stream=
                                          groups, n_seq // groups, n_to, wp, wn, st))
 
 
+# ------------------------------------------------- positions of tokens (rotary)
+
+def _on_device(fn: str, *tensors) -> None:
+    """The library takes plain addresses: what it cannot see of a tensor."""
+    at = -1
+    for t in tensors:
+        if t is None:
+            continue
+        if at < 0 and t.is_cuda:
+            at = torch._C._cuda_getDevice()
+        if t.get_device() != at or at < 0:
+            raise ValueError(f"{fn}: every tensor is on the current CUDA device")
+
+
+def _head_rows(fn: str, name: str, x: torch.Tensor, shape, dtype) -> bytes:
+    """uc_rows of x [batch, heads, tokens, 128]."""
+    s = x.stride()
+    if x.shape != shape or x.dtype is not dtype or s[3] != 1:
+        raise ValueError(f"{fn}: {name} is {dtype} {list(shape)}, every row contiguous")
+    return _pack_rows(x.data_ptr(), s[0], s[1], s[2])
+
+
+def _counts(fn: str, name: str, x: Optional[torch.Tensor], batch: int) -> None:
+    if x is not None and (x.dtype is not torch.int32 or x.shape != (batch,) or not x.is_contiguous()):
+        raise ValueError(f"{fn}: {name} is contiguous int32 [{batch}]")
+
+
+class Rotary:
+    """A rotation by position (uc_rotary_table): ``freqs`` are the pairs'
+    radians per token, 1 to 64 host floats; pair i is channels (i, i + pairs),
+    or (2 i, 2 i + 1) where ``interleaved``; turned channels are multiplied by
+    ``scale``, the others stay as they are. Long-context rescalings are a matter
+    of the frequencies and the scale."""
+
+    def __init__(self, freqs: Sequence[float], interleaved: bool = False, scale: float = 1.0):
+        freqs = [float(f) for f in freqs]
+        if not 1 <= len(freqs) <= _lib.MAX_ROTARY_PAIRS:
+            raise ValueError(f"Rotary: 1 to {_lib.MAX_ROTARY_PAIRS} frequencies")
+        self.c = _lib.UcRotaryTable(len(freqs), int(bool(interleaved)), float(scale))
+        self.c.freq[:len(freqs)] = freqs
+        self._at = C.addressof(self.c)
+
+
+def rotary(table: Rotary, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None,
+           out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None, stream=None):
+    """Rotary positions (uc_rotary) of q [B, Hq, T, 128] and k [B, Hkv, T, 128],
+    fp32, bf16 or fp16 with contiguous rows and strides as ``linear_attend``
+    takes them. positions int32: [B, T], or [B, 1] for the first token's.
+    out_q, out_k: where they go (may be q and k themselves: in place). Returns (out_q, out_k),
+    with the strides of q and k where these have no gaps."""
+    kind = _LOGIT_TYPES.get(q.dtype)
+    if kind is None or q.dim() != 4 or q.shape[3] != HEAD_DIM:
+        raise ValueError("rotary: q is fp32, bf16 or fp16 [B, Hq, T, 128]")
+    B, hq, T, d = q.shape
+    if positions.dtype is not torch.int32 or positions.shape not in ((B, T), (B, 1)) or not positions.is_contiguous():
+        raise ValueError("rotary: positions are contiguous int32 [B, T] or [B, 1]")
+    if k is None and out_k is not None or k is not None and k.dim() != 4:
+        raise ValueError("rotary: k is [B, Hkv, T, 128], and out_k its result")
+    hkv = 0 if k is None else k.shape[1]
+    rq = _head_rows("rotary", "q", q, (B, hq, T, d), q.dtype)
+    rk = None if k is None else _head_rows("rotary", "k", k, (B, hkv, T, d), q.dtype)
+    _on_device("rotary", q, k, positions, out_q, out_k)
+    if out_q is None:
+        out_q = torch.empty_like(q) if stream is None else _new(stream, lambda: torch.empty_like(q))[0]
+    if k is not None and out_k is None:
+        out_k = torch.empty_like(k) if stream is None else _new(stream, lambda: torch.empty_like(k))[0]
+    oq = _head_rows("rotary", "out_q", out_q, (B, hq, T, d), q.dtype)
+    ok = None if k is None else _head_rows("rotary", "out_k", out_k, (B, hkv, T, d), q.dtype)
+    check("uc_rotary", lib().uc_rotary(table._at, positions.data_ptr(), int(positions.shape[1] == T), kind, B, T, rq, oq,
+                                       hq, rk, ok, hkv, _stream(stream)))
+    return out_q, out_k
+
+
+# ----------------------------- layers with a sliding window and first tokens
+
+class WindowCache:
+    """The cache of a layer whose queries see the last ``window`` tokens and the
+    first ``n_sink`` ones (uc_window_cache), over caller tensors k, v [B, Hkv,
+    rows, 128] bf16 with contiguous rows. Token p lies in row p, or, where p >=
+    n_sink, in row n_sink + (p - n_sink) mod (rows - n_sink): a ring, unless the rows
+    hold every token. Queries of T tokens at once need window + T - 1 rows behind the
+    first ones. How many tokens a sequence holds is the caller's, on the device."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, window: int, n_sink: int = 0):
+        if k.dim() != 4 or k.shape[3] != HEAD_DIM:
+            raise ValueError("WindowCache: k and v are bf16 [B, Hkv, rows, 128]")
+        for x, name in ((k, "k"), (v, "v")):
+            _head_rows("WindowCache", name, x, k.shape, torch.bfloat16)
+        if window < 1 or not 0 <= n_sink < k.shape[2]:
+            raise ValueError("WindowCache: window is at least 1, n_sink at least 0 and less than the rows")
+        if k.device != v.device:
+            raise ValueError("WindowCache: k and v are on one device")
+        self.k, self.v, self.window, self.n_sink = k, v, int(window), int(n_sink)
+        self.batch, self.n_kv_heads, self.n_rows, _ = k.shape
+        rows = [_lib.UcRows(x.data_ptr(), *x.stride()[:3]) for x in (k, v)]
+        self.c = _lib.UcWindowCache(*rows, self.batch, self.n_kv_heads, self.n_rows, min(self.window, 1 << 30),
+                                    self.n_sink)
+        self._at = C.addressof(self.c)
+
+
+def window_append(cache: WindowCache, k: torch.Tensor, v: torch.Tensor, held: torch.Tensor,
+                  n_new: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
+                  q: Optional[torch.Tensor] = None, out_q: Optional[torch.Tensor] = None,
+                  total: Optional[torch.Tensor] = None, ws: Optional[Workspace] = None, stream=None):
+    """New tokens into ``cache`` (uc_window_append): k, v bf16 [B, Hkv, T, 128],
+    token t < n_new[b] of sequence b at position held[b] + t, k turned by ``rotary``
+    where that is given. q [B, Hq, T, 128]: turned beside them, into out_q (may
+    be q). held, n_new: device int32 [B] (None: T each). Returns (total, out_q),
+    total = held + n_new (another array than held)."""
+    B, hkv, d = cache.batch, cache.n_kv_heads, HEAD_DIM
+    if k.dim() != 4:
+        raise ValueError("window_append: k and v are bf16 [B, Hkv, T, 128]")
+    T = k.shape[2]
+    rk, rv = (_head_rows("window_append", name, x, (B, hkv, T, d), torch.bfloat16) for x, name in ((k, "k"), (v, "v")))
+    _counts("window_append", "held", held, B)
+    _counts("window_append", "n_new", n_new, B)
+    _counts("window_append", "total", total, B)
+    if held is None or (q is None and out_q is not None) or (q is not None and (rotary is None or q.dim() != 4)):
+        raise ValueError("window_append: held is needed, and a rotary where there is a q [B, Hq, T, 128]")
+    hq = 0 if q is None else q.shape[1]
+    rq = None if q is None else _head_rows("window_append", "q", q, (B, hq, T, d), torch.bfloat16)
+    _on_device("window_append", cache.k, k, v, held, n_new, q, out_q, total)
+    if total is None:
+        total = torch.empty_like(held) if stream is None else _new(stream, lambda: torch.empty_like(held))[0]
+    if q is not None and out_q is None:
+        out_q = torch.empty_like(q) if stream is None else _new(stream, lambda: torch.empty_like(q))[0]
+    oq = None if q is None else _head_rows("window_append", "out_q", out_q, (B, hq, T, d), torch.bfloat16)
+    ws = ws or default_workspace(k.device)
+    st = _stream(stream)
+    wp, wn = ws.get(256, "scratch", stream, st)
+    check("uc_window_append", lib().uc_window_append(
+        cache._at, rk, rv, T, held.data_ptr(), _ptr(n_new), None if rotary is None else rotary._at, rq, oq, hq,
+        total.data_ptr(), wp, wn, st))
+    return total, out_q
+
+
+def window_attend(q: torch.Tensor, cache: WindowCache, lengths: torch.Tensor, n_query: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = True,
+                  ws: Optional[Workspace] = None, stream=None):
+    """Attention with a sliding window and first tokens (uc_window_attend): the
+    queries q bf16 [B, Hq, T, 128] are the last n_query[b] (None: T) of the
+    lengths[b] tokens that sequence b holds in ``cache``, their own among them;
+    device int32 [B]. Returns (out, lse): out with q's shape (and its strides
+    where q has no gaps), 0 behind a sequence's last query; lse fp32 [B, Hq, T] or None."""
+    B, hkv = cache.batch, cache.n_kv_heads
+    if q.dim() != 4 or lengths is None:
+        raise ValueError("window_attend: lengths are needed, and q is bf16 [B, Hq, T, 128]")
+    hq, T = q.shape[1], q.shape[2]
+    rq = _head_rows("window_attend", "q", q, (B, hq, T, HEAD_DIM), torch.bfloat16)
+    _counts("window_attend", "lengths", lengths, B)
+    _counts("window_attend", "n_query", n_query, B)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (B, hq, T) or not lse.is_contiguous()):
+        raise ValueError("window_attend: lse is contiguous fp32 [B, Hq, T]")
+    _on_device("window_attend", cache.k, q, lengths, n_query, out, lse)
+    if out is None:
+        out = torch.empty_like(q) if stream is None else _new(stream, lambda: torch.empty_like(q))[0]
+    ro = _head_rows("window_attend", "out", out, (B, hq, T, HEAD_DIM), torch.bfloat16)
+    if want_lse and lse is None:
+        lse = _new(stream, lambda: torch.empty((B, hq, T), dtype=torch.float32, device=q.device))[0]
+    ws = ws or default_workspace(q.device)
+    L = lib()
+    st = _stream(stream)
+    args = (cache._at, rq, hq, T, lengths.data_ptr(), _ptr(n_query), ro, _ptr(lse))
+    code = L.uc_window_attend(*args, *ws.get(256, "scratch", stream, st), st)
+    if code == _lib.UC_ERR_OOM:   # nothing is launched then: only now is the size asked for
+        code = L.uc_window_attend(*args, *ws.get(L.uc_window_workspace_size(cache._at, hq, T), "scratch", stream, st), st)
+    check("uc_window_attend", code)
+    return out, lse
+
+
+# ------------------------------------------------------------- drafted tokens
+
+def verify_draft(logits: torch.Tensor, tokens: torch.Tensor, u: Optional[torch.Tensor] = None,
+                 noise: Optional[torch.Tensor] = None, draft_logits: Optional[torch.Tensor] = None,
+                 n_draft: Optional[torch.Tensor] = None, temperature: float = 1.0, ws: Optional[Workspace] = None,
+                 stream=None):
+    """Drafted tokens against the target's probabilities (uc_verify_draft):
+    logits [B, T + 1, V] of the target, draft_logits [B, T, V] of the drafter (None:
+    the drafts are taken as certain), fp32, bf16 or fp16 with contiguous rows; tokens
+    int32 [B, T] the drafts, n_draft int32 [B] how many (None: T each). u fp32
+    [B, T] uniform in [0, 1), noise fp32 [B, V] exponential variates; neither is
+    needed at temperature 0. Returns (accepted int32 [B], tokens int32 [B, T + 1]:
+    the accepted drafts, the next token, then -1; log probabilities fp32 [B, T + 1])."""
+    kind = _LOGIT_TYPES.get(logits.dtype)
+    if kind is None or logits.dim() != 3 or logits.stride(2) != 1:
+        raise ValueError("verify_draft: logits are fp32, bf16 or fp16 [B, T + 1, V] with contiguous rows")
+    B, T, V = logits.shape[0], logits.shape[1] - 1, logits.shape[2]
+    if tokens.dtype is not torch.int32 or tokens.shape != (B, T) or not tokens.is_contiguous():
+        raise ValueError("verify_draft: tokens are contiguous int32 [B, T]")
+    if draft_logits is not None and (draft_logits.dtype is not logits.dtype or draft_logits.shape != (B, T, V)
+                                     or draft_logits.stride(2) != 1):
+        raise ValueError("verify_draft: draft_logits are [B, T, V] of the logits' type with contiguous rows")
+    for x, shape, name in ((u, (B, T), "u"), (noise, (B, V), "noise")):
+        if x is None and temperature != 0:
+            raise ValueError(f"verify_draft: {name} is needed unless temperature is 0")
+        if x is not None and (x.dtype is not torch.float32 or x.shape != shape or not x.is_contiguous()):
+            raise ValueError(f"verify_draft: {name} is contiguous fp32 {list(shape)}")
+    _counts("verify_draft", "n_draft", n_draft, B)
+    _on_device("verify_draft", logits, tokens, draft_logits, u, noise, n_draft)
+    dev = logits.device
+    accepted, out, logprob = _new(stream, partial(torch.empty, (B,), dtype=torch.int32, device=dev),
+                                  partial(torch.empty, (B, T + 1), dtype=torch.int32, device=dev),
+                                  partial(torch.empty, (B, T + 1), dtype=torch.float32, device=dev))
+    ws = ws or default_workspace(dev)
+    L = lib()
+    db, dt = (0, 0) if draft_logits is None else draft_logits.stride()[:2]
+    args = (logits.data_ptr(), *logits.stride()[:2], _ptr(draft_logits), db, dt, kind, B, T, V, tokens.data_ptr(),
+            _ptr(n_draft), _ptr(u), _ptr(noise), float(temperature), accepted.data_ptr(), out.data_ptr(),
+            logprob.data_ptr())
+    st = _stream(stream)
+    code = L.uc_verify_draft(*args, *ws.get(256, "scratch", stream, st), st)
+    if code == _lib.UC_ERR_OOM:   # nothing is launched then: only now is the size asked for
+        code = L.uc_verify_draft(*args, *ws.get(L.uc_verify_workspace_size(B, T, V), "scratch", stream, st), st)
+    check("uc_verify_draft", code)
+    return accepted, out, logprob
+
+
 def set_dense_serial_pv(serial: bool) -> bool:
     """A setting of the dense attention kernel kept for its callers, without
     effect any more (see unicache.h); returns the previous one."""

@@ -6,130 +6,16 @@
 #include <cmath>
 #include <cstring>
 
+#include "args.h"
 #include "common.cuh"
 #include "internal.h"
 
 namespace uc {
 namespace {
 
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-// Do [a, a + an) and [b, b + bn) share a byte?
-bool overlap(const void* a, uint64_t an, const void* b, uint64_t bn) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return an != 0 && bn != 0 && x < y + bn && y < x + an;
-}
-
-uc_status check_workspace(const void* workspace, size_t bytes, size_t need, const char* fn) {
-  if (workspace == nullptr || !aligned(workspace, 16)) {
-    set_error("%s: workspace must be non-null and 16-byte aligned", fn);
-    return UC_ERR_ARG;
-  }
-  if (bytes < need) {
-    set_error("%s: workspace of %zu bytes, %zu needed", fn, bytes, need);
-    return UC_ERR_OOM;
-  }
-  return UC_OK;
-}
-
 float2 two_floats(double x) {
   const float hi = (float)x;
   return make_float2(hi, std::isfinite(hi) ? (float)(x - (double)hi) : 0.f);
-}
-
-constexpr int64_t kMostElements = int64_t(1) << 44;  // between two rows of one tensor
-
-// stride * x, lo <= x <= hi.
-struct Term {
-  int64_t stride, lo, hi;
-};
-
-// Is there a sum d + stride_0 x_0 + ... strictly between -before and after (all x
-// zero: only if `zero`)? Terms by falling stride: what the later ones reach
-// leaves few x to look at, one or two each where strides nest. A search that
-// grows past `steps` counts as found.
-bool reaches(const Term* t, int n, int64_t d, int64_t before, int64_t after, bool zero, int* steps) {
-  if (n == 0) return zero && d > -before && d < after;
-  int64_t lo = 0, hi = 0;
-  for (int i = 1; i < n; ++i) {
-    lo += t[i].stride * t[i].lo;
-    hi += t[i].stride * t[i].hi;
-  }
-  auto floor_div = [](int64_t a, int64_t b) { return a / b - (a % b < 0); };
-  const int64_t first = std::max(t->lo, floor_div(-before - d - hi, t->stride) + 1);
-  const int64_t last = std::min(t->hi, -floor_div(-(after - d - lo), t->stride) - 1);
-  for (int64_t x = first; x <= last; ++x)
-    if (--*steps < 0 || reaches(t + 1, n - 1, d + t->stride * x, before, after, zero || x != 0, steps)) return true;
-  return false;
-}
-
-// Rows of a tensor: [batch, heads, tokens] of UC_HEAD_DIM elements.
-struct RowSet {
-  const RowsDev* r;
-  int size[3];
-  uint64_t bytes;  // from the first row to the last's end
-  int64_t stride(int i) const { return i == 0 ? r->sb : i == 1 ? r->sh : r->st; }
-};
-
-// Does a row of a share an element with a row of b (with another row, where both are one)?
-bool rows_meet(const RowSet& a, const RowSet& b) {
-  const bool same = &a == &b;
-  if (!same && !overlap(a.r->base, a.bytes, b.r->base, b.bytes)) return false;
-  Term t[6];
-  int n = 0;
-  for (int i = 0; i < 3; ++i) {
-    if (a.size[i] > 1 && b.size[i] > 1 && a.stride(i) == b.stride(i)) {
-      t[n++] = {a.stride(i), 1 - b.size[i], a.size[i] - 1};
-    } else {
-      if (a.size[i] > 1) t[n++] = {a.stride(i), 0, a.size[i] - 1};
-      if (b.size[i] > 1) t[n++] = {b.stride(i), 1 - b.size[i], 0};
-    }
-  }
-  std::sort(t, t + n, [](const Term& x, const Term& y) { return x.stride > y.stride; });
-  int steps = 1 << 16;
-  const int64_t d = ((int64_t)reinterpret_cast<uintptr_t>(a.r->base) - (int64_t)reinterpret_cast<uintptr_t>(b.r->base)) / 2;
-  return reaches(t, n, d, UC_HEAD_DIM, UC_HEAD_DIM, !same, &steps);
-}
-
-// Does a row of a share a byte with the `bytes` bytes at x?
-bool rows_meet(const RowSet& a, const void* x, uint64_t bytes) {
-  if (!overlap(a.r->base, a.bytes, x, bytes)) return false;
-  Term t[3];
-  int n = 0;
-  for (int i = 0; i < 3; ++i)
-    if (a.size[i] > 1) t[n++] = {a.stride(i), 0, a.size[i] - 1};
-  std::sort(t, t + n, [](const Term& x, const Term& y) { return x.stride > y.stride; });
-  int steps = 1 << 16;
-  const int64_t d = ((int64_t)reinterpret_cast<uintptr_t>(a.r->base) - (int64_t)reinterpret_cast<uintptr_t>(x)) / 2;
-  return reaches(t, n, d, UC_HEAD_DIM, (int64_t)(bytes / 2), true, &steps);
-}
-
-// Rows of `heads` heads of `n_tok` tokens: strides in the kernels' form (0
-// where the extent is 1) and the bytes from the first row to the last's end.
-uc_status check_rows(const uc_rows* r, const char* what, int batch, int heads, int n_tok, RowsDev* out,
-                     uint64_t* extent) {
-  if (r == nullptr || r->ptr == nullptr || !aligned(r->ptr, 16)) {
-    set_error("uc_linear_attend: %s must be non-null and 16-byte aligned", what);
-    return UC_ERR_ARG;
-  }
-  const int64_t stride[3] = {batch > 1 ? r->stride_b : 0, heads > 1 ? r->stride_h : 0, n_tok > 1 ? r->stride_t : 0};
-  const int size[3] = {batch, heads, n_tok};
-  int64_t last = 0;
-  for (int i = 0; i < 3; ++i) {
-    if (size[i] > 1 && (stride[i] < UC_HEAD_DIM || stride[i] % 8 != 0 || stride[i] > (int64_t(1) << 37))) {
-      set_error("uc_linear_attend: strides of %s must be multiples of 8 elements, at least %d and below 2^37", what,
-                UC_HEAD_DIM);
-      return UC_ERR_SHAPE;
-    }
-    if (size[i] > 1 && stride[i] > kMostElements / (size[i] - 1)) {
-      set_error("uc_linear_attend: rows of %s lie more than 2^44 elements apart", what);
-      return UC_ERR_SHAPE;
-    }
-    last += stride[i] * (size[i] - 1);
-  }
-  *out = RowsDev{static_cast<__nv_bfloat16*>(r->ptr), stride[0], stride[1], stride[2]};
-  *extent = 2ull * (uint64_t)(last + UC_HEAD_DIM);
-  return UC_OK;
 }
 
 }  // namespace
@@ -248,10 +134,11 @@ uc_status uc_linear_attend(const uc_rows* q, const uc_rows* k, const uc_rows* v,
   LinearParams p;
   memset(&p, 0, sizeof(p));
   uint64_t nq, nk, nv, no;
-  uc_status st = check_rows(q, "q", batch, n_q_heads, n_tok, &p.q, &nq);
-  if (st == UC_OK) st = check_rows(k, "k", batch, n_kv_heads, n_tok, &p.k, &nk);
-  if (st == UC_OK) st = check_rows(v, "v", batch, n_kv_heads, n_tok, &p.v, &nv);
-  if (st == UC_OK) st = check_rows(out, "out", batch, n_q_heads, n_tok, &p.out, &no);
+  const char* const fn = "uc_linear_attend";
+  uc_status st = check_rows(q, fn, "q", batch, n_q_heads, n_tok, &p.q, &nq);
+  if (st == UC_OK) st = check_rows(k, fn, "k", batch, n_kv_heads, n_tok, &p.k, &nk);
+  if (st == UC_OK) st = check_rows(v, fn, "v", batch, n_kv_heads, n_tok, &p.v, &nv);
+  if (st == UC_OK) st = check_rows(out, fn, "out", batch, n_q_heads, n_tok, &p.out, &no);
   if (st != UC_OK) return st;
   if (log_decay == nullptr || state_out == nullptr || !aligned(state_out, 16) || !aligned(state_in, 16)) {
     set_error("uc_linear_attend: log_decay and state_out must be non-null, states 16-byte aligned");

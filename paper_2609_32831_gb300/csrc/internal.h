@@ -383,6 +383,72 @@ struct ReorderParamsOf {
 using ReorderParams = ReorderParamsOf<kReorderArrays>;
 void launch_reorder(const ReorderParams& p, cudaStream_t st);
 
+// ---------------------------------------------------- positions of tokens
+// Groups of heads that one launch turns, copies or stores: rows of `heads` heads
+// each, taken one behind another.
+enum PositionRole { kTurn = 0, kTurnStore = 1, kStore = 2 };
+struct PositionGroup {
+  RowsDev src, dst;  // (strides in elements of the call's type)
+  int32_t heads, role;
+};
+struct PositionParams {
+  PositionGroup g[3];
+  int n_groups, heads;         // of all groups
+  int batch, n_tok, parts;     // parts: a token's heads go to so many threads, one behind another
+  int n_pairs, interleaved;    // 0 pairs: nothing turns
+  float scale;
+  const int32_t* positions;    // [B, n_tok], or [B]
+  int per_token;
+  // storing: the rows of a window's cache
+  const int32_t* n_new;        // or null
+  int32_t* out_total;          // or null: no storing
+  int n_sink, ring;
+  DevStatus* status;
+  uint64_t turn[UC_MAX_ROTARY_PAIRS];  // of a pair per token, in 2^-64 turns
+};
+void launch_positions(const PositionParams& p, int dtype, cudaStream_t st);
+
+// ------------------------------------------------ attention with a window
+struct WindowParams {
+  RowsDev q, out, k, v;
+  float* lse;
+  const int32_t* lengths;
+  const int32_t* n_query;  // or null
+  DevStatus* status;
+  float* part;             // partial outputs of key ranges, or null
+  int batch, n_q_heads, n_kv_heads, group, n_tok;
+  int n_rows, window, n_sink;
+  float scale_log2;        // log2(e) / sqrt(128)
+  int row_blocks, cluster, splits;
+};
+constexpr int kWindowRows = 64;  // query rows (tokens x heads of a KV head) that a step's CTA takes at most
+void launch_window_step(const WindowParams& p, cudaStream_t st);
+int window_max_cluster();
+
+// ------------------------------------------------------------ drafted tokens
+struct VerifyParams {
+  const void* target;
+  const void* draft;  // or null
+  int64_t target_b, target_t, draft_b, draft_t;
+  const int32_t* tokens;
+  const int32_t* n_draft;  // or null
+  const float* u;
+  const float* noise;
+  int32_t* accepted;
+  int32_t* out_tokens;
+  float* logprob;
+  DevStatus* status;
+  float2* part_ms;     // [rows][tiles]: max, sum of exp((x - max) / temperature)
+  int32_t* part_at;    // [rows][tiles]: the max's lowest index
+  uint64_t* best;      // [B]: the best next token so far
+  int32_t* done;       // [B]: CTAs that have given theirs
+  int batch, n_tok, vocab, tiles, span, pick_tiles, pick_span;
+  bool greedy;
+  float2 scale;        // log2(e) / temperature, and what fp32 leaves of it
+  float inv_temperature;
+};
+void launch_verify(const VerifyParams& p, int dtype, cudaStream_t st);
+
 // Shared by the files with C-ABI entry points (defined in api.cu).
 uc_status cuda_check(const char* where);
 uc_status check_segment(const uc_segment* s, const char* fn);
