@@ -20,7 +20,7 @@ LIB = os.path.join(LIB_DIR, "libunicache.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["api.cu", "attend.cu", "beam.cu", "compress.cu", "dense.cu", "generation.cu", "linear.cu", "positions.cu",
-           "scores.cu", "verify.cu", "window.cu", "policy.cpp", "owned.cpp"]
+           "scores.cu", "verify.cu", "window.cu", "window_prompt.cu", "policy.cpp", "owned.cpp"]
 
 
 def _nvcc() -> str:

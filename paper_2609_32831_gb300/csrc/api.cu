@@ -105,17 +105,17 @@ static uc_status encode_rows_f16(CUtensorMap* map, const void* base, int64_t row
 }
 
 // The same as [128, tokens, heads, sequences] with strides of their own.
-uc_status encode_rows_4d(CUtensorMap* map, const RowsDev& r, int n_tok, int heads, int batch, int rows) {
+static uc_status encode_4d(CUtensorMap* map, const RowsDev& r, const cuuint64_t (&dims)[4], const int64_t (&stride)[3],
+                           int box1, int box2) {
   auto fn = encode_fn();
   if (fn == nullptr) {
     set_error("cuTensorMapEncodeTiled is not available from the driver");
     return UC_ERR_CUDA;
   }
-  cuuint64_t dims[4] = {(cuuint64_t)kHeadDim, (cuuint64_t)n_tok, (cuuint64_t)heads, (cuuint64_t)batch};
   // (an extent of 1 has stride 0 here and needs a valid one)
   auto bytes = [](int64_t elements) { return (cuuint64_t)(elements ? elements : kHeadDim) * 2; };
-  cuuint64_t strides[3] = {bytes(r.st), bytes(r.sh), bytes(r.sb)};
-  cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1};
+  cuuint64_t strides[3] = {bytes(stride[0]), bytes(stride[1]), bytes(stride[2])};
+  cuuint32_t box[4] = {64, (cuuint32_t)box1, (cuuint32_t)box2, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
   const CUresult e = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, r.base, dims, strides, box, estr,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -125,6 +125,17 @@ uc_status encode_rows_4d(CUtensorMap* map, const RowsDev& r, int n_tok, int head
     return UC_ERR_CUDA;
   }
   return UC_OK;
+}
+
+uc_status encode_rows_4d(CUtensorMap* map, const RowsDev& r, int n_tok, int heads, int batch, int rows) {
+  return encode_4d(map, r, {(cuuint64_t)kHeadDim, (cuuint64_t)n_tok, (cuuint64_t)heads, (cuuint64_t)batch},
+                   {r.st, r.sh, r.sb}, rows, 1);
+}
+
+uc_status encode_heads_4d(CUtensorMap* map, const RowsDev& r, int n_tok, int heads, int batch, int box_heads,
+                          int box_tok) {
+  return encode_4d(map, r, {(cuuint64_t)kHeadDim, (cuuint64_t)heads, (cuuint64_t)n_tok, (cuuint64_t)batch},
+                   {r.sh, r.st, r.sb}, box_heads, box_tok);
 }
 
 // Tensor maps of a segment's bf16 rows, cached inside the segment struct.

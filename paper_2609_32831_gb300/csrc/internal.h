@@ -423,7 +423,20 @@ struct WindowParams {
 };
 constexpr int kWindowRows = 64;  // query rows (tokens x heads of a KV head) that a step's CTA takes at most
 void launch_window_step(const WindowParams& p, cudaStream_t st);
-int window_max_cluster();
+void launch_window_join(const WindowParams& p, cudaStream_t st);
+
+// Prompts: tiles of `tokens` tokens x the heads of a KV head, up to 128 rows.
+constexpr int kWindowSeqs = 256;  // sequences of a call at most
+struct WindowPromptParams {
+  WindowParams p;
+  CUtensorMap tq;        // box 64 channels x the group's heads x tokens
+  CUtensorMap tk[3], tv[3];  // box 64 channels x 128 rows; the first tokens' last rows; what they leave of 128
+  int tokens;
+  bool wide_out;         // rows of out start on 32 bytes
+  uint64_t wait_ns;
+  int withhold;          // test hook: the load of a CTA (K and V in turn) that is never made (-1: none)
+};
+void launch_window_prompt(const WindowPromptParams& c, int grid, cudaStream_t st);
 
 // ------------------------------------------------------------ drafted tokens
 struct VerifyParams {
@@ -455,6 +468,9 @@ uc_status check_segment(const uc_segment* s, const char* fn);
 int num_sms();
 // bf16 rows as a 4D tensor map [128, T, H, B], box 64 x `rows`.
 uc_status encode_rows_4d(CUtensorMap* map, const RowsDev& r, int n_tok, int heads, int batch, int rows);
+// The same as [128, H, T, B], box 64 x `box_heads` x `box_tok`.
+uc_status encode_heads_4d(CUtensorMap* map, const RowsDev& r, int n_tok, int heads, int batch, int box_heads,
+                          int box_tok);
 
 int attend_ctas_per_sm(int ntiles);
 constexpr int kMaxClusterItems = 16;  // CTAs of the largest cluster

@@ -76,6 +76,7 @@ __global__ void __launch_bounds__(32 * kStepWarps) window_step_kernel(const __gr
   const int rg = warp % RG, kw = warp / RG;
   const int rows = p.group * p.n_tok, row0 = block * kWindowRows;
   const WindowSeq s = window_seq(p, b);
+  if (threadIdx.x == 0) window_check(p, b);
   // positions of the block's rows that are queries
   const int ta = row0 / p.group, tb = min(min(row0 + kWindowRows, rows) - 1, p.group * s.nq - 1) / p.group;
   WindowKeys keys = {0, 0, 0};
@@ -358,17 +359,20 @@ void launch_window_step(const WindowParams& p, cudaStream_t st) {
     step_launch<2>(p, st);
   else
     step_launch<4>(p, st);
-  if (p.splits > 1) {
-    const int64_t all = (int64_t)p.batch * p.n_q_heads * p.n_tok;
-    window_join_kernel<<<(unsigned)((all + 3) / 4), 128, 0, st>>>(p);
-    count_launch();
-  }
+  if (p.splits > 1) launch_window_join(p, st);
+}
+
+void launch_window_join(const WindowParams& p, cudaStream_t st) {
+  const int64_t all = (int64_t)p.batch * p.n_q_heads * p.n_tok;
+  window_join_kernel<<<(unsigned)((all + 3) / 4), 128, 0, st>>>(p);
+  count_launch();
 }
 
 namespace {
 
 struct WindowPlan {
-  int row_blocks, cluster, splits;
+  bool prompt;
+  int row_blocks, cluster, splits;  // (prompt: row_blocks are pairs of Q tiles)
 };
 
 // Keys that a block of rows may have in reach.
@@ -383,13 +387,24 @@ WindowPlan plan_window(const uc_window_cache& c, int n_q_heads, int n_tok) {
   const int64_t rows = (int64_t)group * n_tok;
   w.row_blocks = (int)((rows + kWindowRows - 1) / kWindowRows);
   const int64_t items = (int64_t)c.batch * c.n_kv_heads * w.row_blocks;
+  w.splits = 1;
+  w.prompt = rows > kWindowRows && group <= 128 && c.batch <= kWindowSeqs;
+  if (w.prompt) {
+    // key ranges of a tile or more where there are too few pairs of Q tiles for the SMs
+    const int tokens = 128 / group;
+    w.row_blocks = (n_tok + 2 * tokens - 1) / (2 * tokens);
+    w.cluster = 1;
+    const int64_t all = (int64_t)c.batch * c.n_kv_heads * w.row_blocks;
+    const int64_t tiles = (std::min<int64_t>(c.n_rows, (int64_t)c.window + c.n_sink + std::min(n_tok, 2 * tokens)) + 127) / 128;
+    w.splits = (int)std::max<int64_t>(1, std::min<int64_t>(num_sms() / all, tiles / 4));
+    return w;
+  }
   const int rg = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   // CTAs with at least one tile a warp, up to what the SMs hold of them
   const int64_t tiles = (most_keys(c, n_tok, group) + kTileKeys * (kStepWarps / rg) - 1) / (kTileKeys * (kStepWarps / rg));
   const int64_t want = std::max<int64_t>(1, std::min(tiles, 2 * (int64_t)num_sms() / items));
   w.cluster = 1;
   while (2 * w.cluster <= std::min<int64_t>(want, 8)) w.cluster *= 2;
-  w.splits = 1;
   return w;
 }
 
@@ -476,7 +491,29 @@ uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32
   p.row_blocks = w.row_blocks;
   p.cluster = w.cluster;
   p.splits = w.splits;
-  launch_window_step(p, reinterpret_cast<cudaStream_t>(stream));
+  if (!w.prompt) {
+    launch_window_step(p, reinterpret_cast<cudaStream_t>(stream));
+    return cuda_check(fn);
+  }
+  WindowPromptParams c;
+  memset(&c, 0, sizeof(c));
+  c.p = p;
+  c.tokens = 128 / p.group;
+  st = encode_heads_4d(&c.tq, p.q, n_tok, n_q_heads, batch, p.group, c.tokens);
+  const int rest = (cache->n_sink + 7) / 8 * 8 % 128;
+  for (int i = 0; i < 2 && st == UC_OK; ++i) {
+    const RowsDev& r = i == 0 ? p.k : p.v;
+    CUtensorMap* const m = i == 0 ? c.tk : c.tv;
+    st = encode_rows_4d(&m[0], r, cache->n_rows, hkv, batch, 128);
+    if (st == UC_OK && rest > 0) st = encode_rows_4d(&m[1], r, cache->n_rows, hkv, batch, rest);
+    if (st == UC_OK && rest > 0) st = encode_rows_4d(&m[2], r, cache->n_rows, hkv, batch, 128 - rest);
+  }
+  if (st != UC_OK) return st;
+  c.wide_out = aligned(p.out.base, 32) && p.out.sb % 16 == 0 && p.out.sh % 16 == 0 && p.out.st % 16 == 0;
+  c.wait_ns = wait_limit_ns();
+  c.withhold = take_withhold_pos();
+  const int64_t items = (int64_t)batch * hkv * w.row_blocks * w.splits;
+  launch_window_prompt(c, (int)std::min<int64_t>(items, num_sms()), reinterpret_cast<cudaStream_t>(stream));
   return cuda_check(fn);
 }
 

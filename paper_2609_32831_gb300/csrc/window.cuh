@@ -22,8 +22,13 @@ __device__ __forceinline__ WindowSeq window_seq(const WindowParams& p, int b) {
   s.nq = min(max(nq, 0), p.n_tok);
   s.first = s.n - s.nq;
   s.kept = s.n > p.n_rows ? s.n - (p.n_rows - p.n_sink) : 0;
-  if ((s.n != n || s.nq != nq) && threadIdx.x == 0) set_status(p.status, UC_ERR_RANGE, b);
   return s;
+}
+
+// Reports counts out of range.
+__device__ __forceinline__ void window_check(const WindowParams& p, int b) {
+  const int nq = p.n_query ? p.n_query[b] : p.n_tok;
+  if (p.lengths[b] < 0 || nq < 0 || nq > p.n_tok) set_status(p.status, UC_ERR_RANGE, b);
 }
 
 // The keys that queries at positions pa .. pb see between them: the first `sinks`

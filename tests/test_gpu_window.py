@@ -79,7 +79,7 @@ def test_steps(B, hq, hkv, T, window, sinks, n_rows, lengths, n_query, layout):
     want = owin.attend(q.float().cpu().numpy(), k.float().cpu().numpy(), v.float().cpu().numpy(), lengths,
                        [T] * B if n_query is None else n_query, window, sinks)
     assert ws.status() == _lib.UC_OK and out.stride() == q.stride()
-    check(out, lse, want, True)
+    check(out, lse, want, hq // hkv * T <= 64)
 
 
 PROMPTS = [
