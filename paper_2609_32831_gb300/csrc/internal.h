@@ -430,7 +430,7 @@ constexpr int kWindowSeqs = 256;  // sequences of a call at most
 struct WindowPromptParams {
   WindowParams p;
   CUtensorMap tq;        // box 64 channels x the group's heads x tokens
-  CUtensorMap tk[3], tv[3];  // box 64 channels x 128 rows; the first tokens' last rows; what they leave of 128
+  CUtensorMap tk[2], tv[2];  // box 64 channels x 128 rows; x the rows of the first tokens' last tile
   int tokens;
   bool wide_out;         // rows of out start on 32 bytes
   uint64_t wait_ns;

@@ -500,13 +500,12 @@ uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32
   c.p = p;
   c.tokens = 128 / p.group;
   st = encode_heads_4d(&c.tq, p.q, n_tok, n_q_heads, batch, p.group, c.tokens);
-  const int rest = (cache->n_sink + 7) / 8 * 8 % 128;
+  const int rest = (cache->n_sink + 15) / 16 * 16 % 128;
   for (int i = 0; i < 2 && st == UC_OK; ++i) {
     const RowsDev& r = i == 0 ? p.k : p.v;
     CUtensorMap* const m = i == 0 ? c.tk : c.tv;
     st = encode_rows_4d(&m[0], r, cache->n_rows, hkv, batch, 128);
     if (st == UC_OK && rest > 0) st = encode_rows_4d(&m[1], r, cache->n_rows, hkv, batch, rest);
-    if (st == UC_OK && rest > 0) st = encode_rows_4d(&m[2], r, cache->n_rows, hkv, batch, 128 - rest);
   }
   if (st != UC_OK) return st;
   c.wide_out = aligned(p.out.base, 32) && p.out.sb % 16 == 0 && p.out.sh % 16 == 0 && p.out.st % 16 == 0;

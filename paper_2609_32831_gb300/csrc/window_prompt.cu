@@ -12,17 +12,19 @@
 //   warp 8          TMA: Q tiles, K tiles (3 slots), V tiles (2 slots)
 //   warp 9          every tcgen05.mma: S_x = Q_x K^T, O_x += P_x V (P from TMEM), the
 //                   two Q tiles in turn, across items too
-//   warps 10, 11    zeros in the rows behind the sequences' last queries
+//   warp 10         what the items are, a few ahead of the others
+//   warp 11         zeros in the rows behind the sequences' last queries
 // P enters its product as one bf16 part, rounded by at most 2^-8 of itself: an output
 // carries that beside its own rounding.
 //
 // Key tiles are 128 rows of the cache. They end where the last query's own key (or
 // the ring) ends, so that the only rows in front of the first key are older ones, or
 // none, which TMA fills with zeros: no row that never held a token is read. First
-// tokens that the window has left lie in the first rows of the first tile(s), by a
-// copy of their own, in place of such rows.
+// tokens that the window has left make tiles of their own, the last of them as wide
+// as they need (in 16s): its products and its softmax take that share of a tile's.
 #include <climits>
 #include <mutex>
+#include <type_traits>
 
 #include "common.cuh"
 #include "internal.h"
@@ -45,12 +47,44 @@ static_assert(2 * 128 * kRegSoftmax + 128 * kRegOther <= kThreads * 168, "regist
 constexpr uint32_t kColP = 128, kColO = 256;
 constexpr float kNone = -INFINITY;
 
+constexpr int kItemSlots = 4;
+
+// What the roles need to know of an item: 2 Q tiles from token t0 on, key tiles j0 ..
+// j1 - 1 of those in reach. Tiles below `firsts` hold first tokens (row i of tile j is token
+// 128 j + i; tile `whole` has `rest` rows, the others 128); row i of another is at
+// position start(j) + i.
+struct Item {
+  int b, kvh, t0, split;
+  int n_query, position;   // of the sequence; of token t0
+  int j0, j1;              // j0 < 0: no more items
+  int first[2], last[2];   // of each Q tile's tiles (last < first: none)
+  int in_first;            // a Q tile takes tiles below this,
+  int in_a[2], in_b[2];    // and from in_a to in_b
+  int n, whole, rest, firsts;
+  int n_a;                 // tiles of the ring's end, before it starts over
+  int end_a, end_b;        // positions behind the two parts' last rows
+  int low_a, low_b;        // positions from which on their rows are what they seem
+  int slot_b;              // the cache's row behind the last
+  int in_order;            // the tiles hold every position from 0 on
+  int plain_lo, plain_hi;  // tiles of 128 that both Q tiles take, neither as its first or last
+  __device__ __forceinline__ bool takes(int x, int j) const {
+    return j >= first[x] && j <= last[x] && (j < in_first || (j >= in_a[x] && j <= in_b[x]));
+  }
+  __device__ __forceinline__ bool part_a(int j) const { return j - firsts < n_a; }
+  __device__ __forceinline__ int start(int j) const {
+    return part_a(j) ? end_a - kKeys * (n_a - (j - firsts)) : end_b - kKeys * (n - j);
+  }
+  __device__ __forceinline__ int width(int j) const { return j == whole && rest > 0 ? rest : kKeys; }
+};
+
 struct PromptSmem {
   uint8_t q[2][2][16384];        // [128 rows][2 x 64 channels], K-major, 128B swizzle
   uint8_t k[kKSlots][2][16384];
   uint8_t v[kVSlots][2][16384];  // (the MN-major B operand)
   uint64_t k_full[kKSlots], k_empty[kKSlots], v_full[kVSlots], v_empty[kVSlots];
   uint64_t q_full[2], q_empty[2], s_full[2], s_free[2], p_full[2], o_full[2], o_empty[2], drain;
+  uint64_t item_full[kItemSlots], item_empty[kItemSlots];
+  Item item[kItemSlots];
   DevStatus status;              // of this CTA's waits
   int loads[4];                  // K, V, Q tile 0 and 1 loads begun
   uint32_t tmem_base;
@@ -58,37 +92,7 @@ struct PromptSmem {
 };
 static_assert(sizeof(PromptSmem) + 1024 <= 232448, "shared memory");
 
-// The key tiles of an item, and where their rows come from. Tile j has rows of
-// first tokens 128 j .. while j < whole (128 of them) and `rest` in tile `whole`;
-// its other rows are row i at position start(j) + i.
-struct KeyTiles {
-  int n;              // tiles
-  int whole, rest;    // tiles of first tokens alone; rows of them in the next
-  int n_a;            // tiles of the ring's end, before it starts over
-  int end_a, end_b;   // positions behind the two parts' last rows
-  int low_a, low_b;   // positions from which on their rows are what they seem
-  int slot_b;         // the cache's row behind the last
-  int sinks;          // keys below this are seen whatever the window
-  bool in_order;      // the tiles hold every position from 0 on
-  __device__ __forceinline__ int start(int j) const {
-    return j - whole < n_a ? end_a - kKeys * (n_a - (j - whole)) : end_b - kKeys * (n - j);
-  }
-  __device__ __forceinline__ int low(int j) const { return j - whole < n_a ? low_a : low_b; }
-};
-
-struct Item {
-  int b, kvh, split, t0;
-  WindowSeq s;
-  int j0, j1;                    // this item's key tiles
-  int first[2], last[2];         // of each Q tile's (last < first: none)
-  int in_sinks, in_a[2], in_b[2];  // a Q tile takes tiles below in_sinks, and from in_a to in_b
-  __device__ __forceinline__ bool takes(int x, int j) const {
-    return j >= first[x] && j <= last[x] && (j < in_sinks || (j >= in_a[x] && j <= in_b[x]));
-  }
-};
-
-__device__ __forceinline__ void item_at(const WindowPromptParams& c, const PromptSmem& sm, int index, Item& it,
-                                        KeyTiles& k) {
+__device__ __forceinline__ void item_at(const WindowPromptParams& c, const PromptSmem& sm, int index, Item& it) {
   const WindowParams& p = c.p;
   int lo = 0, hi = p.batch;  // the sequence: begin[lo] <= index < begin[lo + 1]
   while (hi - lo > 1) {
@@ -96,80 +100,74 @@ __device__ __forceinline__ void item_at(const WindowPromptParams& c, const Promp
     if (sm.begin[mid] <= index) lo = mid; else hi = mid;
   }
   it.b = lo;
-  it.s = window_seq(p, lo);
+  const WindowSeq s = window_seq(p, lo);
   const int per = p.n_kv_heads * p.splits, i = index - sm.begin[lo];
-  const int blocks = (it.s.nq + 2 * c.tokens - 1) / (2 * c.tokens);
+  const int blocks = (s.nq + 2 * c.tokens - 1) / (2 * c.tokens);
   it.t0 = (blocks - 1 - i / per) * 2 * c.tokens;  // (the longest first)
   it.kvh = i % per / p.splits;
   it.split = i % per % p.splits;
-  const int pa = it.s.first + it.t0, pb = it.s.first + min(it.t0 + 2 * c.tokens, it.s.nq) - 1;
-  const bool ring = it.s.kept > 0;
-  int from = max(max(pa - p.window + 1, 0), it.s.kept);
-  const int end = max(pb + 1, 0), pad = (p.n_sink + 7) & ~7;
-  k.in_order = !ring && from <= pad;
-  k.sinks = p.n_sink;
-  k.whole = k.rest = k.n_a = 0;
-  k.end_a = 0;
-  k.low_a = k.low_b = it.s.kept;
-  if (k.in_order) {
+  it.n_query = s.nq;
+  it.position = s.first + it.t0;
+  const int pa = it.position, pb = s.first + min(it.t0 + 2 * c.tokens, s.nq) - 1;
+  const bool ring = s.kept > 0;
+  int from = max(max(pa - p.window + 1, 0), s.kept);
+  const int end = max(pb + 1, 0), pad = (p.n_sink + 15) & ~15;
+  it.in_order = !ring && from <= pad;
+  it.whole = it.rest = it.n_a = 0;
+  it.end_a = 0;
+  it.low_a = it.low_b = s.kept;
+  if (it.in_order) {
     from = 0;
-  } else {
-    k.whole = pad / kKeys;
-    k.rest = pad % kKeys;
+  } else if (end > 0) {
+    it.whole = pad / kKeys;
+    it.rest = pad % kKeys;
   }
+  it.firsts = it.whole + (it.rest > 0);
   int count = max(end - from, 0);
-  k.end_b = end;
-  if (end == 0) {
-    k.n = k.whole = k.rest = 0;
-    k.slot_b = 0;
-  } else {
-    k.slot_b = window_row(p, end - 1) + 1;
-    int head = k.rest;  // rows that the first part's tiles hold beside its keys
-    if (ring && count > 0) {
-      const int base = window_row(p, from);
-      if (base + count > p.n_rows) {
-        const int a = p.n_rows - base;
-        k.n_a = (a + head + kKeys - 1) / kKeys;
-        k.end_a = k.low_b = from + a;
-        count -= a;
-        head = 0;
-      }
+  it.end_b = end;
+  it.slot_b = end > 0 ? window_row(p, end - 1) + 1 : 0;
+  if (ring && count > 0) {
+    const int base = window_row(p, from);
+    if (base + count > p.n_rows) {
+      const int a = p.n_rows - base;
+      it.n_a = (a + kKeys - 1) / kKeys;
+      it.end_a = it.low_b = from + a;
+      count -= a;
     }
-    k.n = k.whole + k.n_a + (count + head + kKeys - 1) / kKeys;
   }
-  it.j0 = (int)((int64_t)k.n * it.split / p.splits);
-  it.j1 = (int)((int64_t)k.n * (it.split + 1) / p.splits);
-  if (k.in_order)
-    it.in_sinks = p.n_sink == 0 || k.n == 0 ? 0 : end <= p.n_sink ? k.n : k.n - (end - p.n_sink) / kKeys;
+  it.n = it.firsts + it.n_a + (count + kKeys - 1) / kKeys;
+  it.j0 = (int)((int64_t)it.n * it.split / p.splits);
+  it.j1 = (int)((int64_t)it.n * (it.split + 1) / p.splits);
+  if (it.in_order)
+    it.in_first = p.n_sink == 0 || it.n == 0 ? 0 : end <= p.n_sink ? it.n : it.n - (end - p.n_sink) / kKeys;
   else
-    it.in_sinks = k.whole + (k.rest > 0);
+    it.in_first = it.firsts;
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
-    const int ta = it.t0 + x * c.tokens, tb = min(ta + c.tokens, it.s.nq) - 1;
-    it.first[x] = 0;
-    it.last[x] = -1;
-    it.in_a[x] = k.whole;
-    it.in_b[x] = k.n - 1;
-    if (ta > tb || it.s.first + tb < 0) continue;
-    const int oldest = it.s.first + ta - p.window + 1, newest = it.s.first + tb;
-    while (it.in_a[x] < k.n && k.start(it.in_a[x]) + kKeys <= oldest) ++it.in_a[x];
-    while (it.in_b[x] >= k.whole && k.start(it.in_b[x]) > newest) --it.in_b[x];
-    // the first and the last that it takes of j0 .. j1 - 1
-    int first = INT_MAX, last = -1;
-    if (it.j0 < min(it.j1, it.in_sinks)) {
-      first = it.j0;
-      last = min(it.j1, it.in_sinks) - 1;
+    const int ta = it.t0 + x * c.tokens, tb = min(ta + c.tokens, s.nq) - 1;
+    int in_a = it.firsts, in_b = it.n - 1, first = INT_MAX, last = -1;
+    if (ta <= tb && s.first + tb >= 0) {
+      const int oldest = s.first + ta - p.window + 1, newest = s.first + tb;
+      while (in_a < it.n && it.start(in_a) + kKeys <= oldest) ++in_a;
+      while (in_b >= it.firsts && it.start(in_b) > newest) --in_b;
+      // the first and the last that it takes of j0 .. j1 - 1
+      if (it.j0 < min(it.j1, it.in_first)) {
+        first = it.j0;
+        last = min(it.j1, it.in_first) - 1;
+      }
+      const int a = max(it.j0, in_a), z = min(it.j1 - 1, in_b);
+      if (a <= z) {
+        first = min(first, a);
+        last = max(last, z);
+      }
     }
-    const int a = max(it.j0, it.in_a[x]), z = min(it.j1 - 1, it.in_b[x]);
-    if (a <= z) {
-      first = min(first, a);
-      last = max(last, z);
-    }
-    if (last >= 0) {
-      it.first[x] = first;
-      it.last[x] = last;
-    }
+    it.in_a[x] = in_a;
+    it.in_b[x] = in_b;
+    it.first[x] = last >= 0 ? first : 0;
+    it.last[x] = last;
   }
+  it.plain_lo = max(max(max(it.first[0], it.first[1]) + 1, max(it.in_a[0], it.in_a[1])), it.firsts);
+  it.plain_hi = min(min(it.last[0], it.last[1]) - 1, min(it.in_b[0], it.in_b[1]));
 }
 
 // Bits lo .. hi of 32 (none where hi < lo).
@@ -188,21 +186,15 @@ __device__ __forceinline__ void tma_4d(void* dst, const CUtensorMap* map, int c0
 }
 
 // A tile of the cache's rows into a slot, both halves of the channels.
-__device__ __forceinline__ void load_keys(uint8_t (*slot)[16384], const CUtensorMap* maps, const KeyTiles& k, int j,
-                                          const WindowPromptParams& c, const Item& it, uint64_t* bar) {
-  mbar_arrive_expect_tx(bar, 2 * kKeys * 128);
-  const bool a = j - k.whole < k.n_a;
-  const int row = j < k.whole ? kKeys * j : a ? c.p.n_rows - kKeys * (k.n_a - (j - k.whole)) : k.slot_b - kKeys * (k.n - j);
-  const int rest = j == k.whole ? k.rest : 0;
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    if (rest == 0) {
-      tma_4d(slot[half], &maps[0], 64 * half, row, it.kvh, it.b, bar);
-    } else {
-      tma_4d(slot[half], &maps[1], 64 * half, kKeys * k.whole, it.kvh, it.b, bar);
-      tma_4d(slot[half] + 128 * rest, &maps[2], 64 * half, row + rest, it.kvh, it.b, bar);
-    }
-  }
+__device__ __forceinline__ void load_keys(uint8_t (*slot)[16384], const CUtensorMap* maps, const Item& it, int j,
+                                          const WindowPromptParams& c, uint64_t* bar) {
+  const int width = it.width(j);
+  const int row = j < it.firsts ? kKeys * j
+                  : it.part_a(j) ? c.p.n_rows - kKeys * (it.n_a - (j - it.firsts)) : it.slot_b - kKeys * (it.n - j);
+  mbar_arrive_expect_tx(bar, 2 * width * 128);
+  const CUtensorMap* const map = width == kKeys ? &maps[0] : &maps[1];
+  tma_4d(slot[0], map, 0, row, it.kvh, it.b, bar);
+  tma_4d(slot[1], map, 64, row, it.kvh, it.b, bar);
 }
 
 __device__ __forceinline__ void store_row32(__nv_bfloat16* to, const uint32_t (&o)[32], float inv, bool wide) {
@@ -224,6 +216,12 @@ __device__ __forceinline__ void store_row32(__nv_bfloat16* to, const uint32_t (&
   }
 }
 
+// Once for the warp, what its lanes have read or written before it.
+__device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
+}
+
 __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid_constant__ WindowPromptParams c) {
   extern __shared__ uint8_t dyn[];
   PromptSmem& sm = *reinterpret_cast<PromptSmem*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -242,10 +240,14 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       mbar_init(&sm.q_full[x], 1);
       mbar_init(&sm.q_empty[x], 1);
       mbar_init(&sm.s_full[x], 1);
-      mbar_init(&sm.s_free[x], kQRows);
-      mbar_init(&sm.p_full[x], kQRows);
+      mbar_init(&sm.s_free[x], 4);
+      mbar_init(&sm.p_full[x], 4);
       mbar_init(&sm.o_full[x], 1);
-      mbar_init(&sm.o_empty[x], kQRows);
+      mbar_init(&sm.o_empty[x], 4);
+    }
+    for (int s = 0; s < kItemSlots; ++s) {
+      mbar_init(&sm.item_full[s], 1);
+      mbar_init(&sm.item_empty[s], 10);  // TMA, MMA, 8 warps of softmax
     }
     mbar_init(&sm.drain, 1);
     fence_barrier_init();
@@ -291,10 +293,10 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
     if (warp == 8 && lane == 0) {
       // -------------------------------------------------------------- TMA
       int nk = 0, nv = 0, nq[2] = {0, 0}, load = 0;
-      for (int i = blockIdx.x; i < items && !aborted; i += gridDim.x) {
-        Item it;
-        KeyTiles k;
-        item_at(c, sm, i, it, k);
+      for (uint32_t n = 0; !aborted; ++n) {
+        if (!dwait(&sm.item_full[n % kItemSlots], (n / kItemSlots) & 1, st, 79, aborted, lim)) break;
+        const Item& it = sm.item[n % kItemSlots];
+        if (it.j0 < 0) break;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           if (it.last[x] < it.first[x]) continue;
@@ -304,21 +306,23 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           tma_4d(sm.q[x][1], &c.tq, 64, it.kvh * p.group, it.t0 + x * c.tokens, it.b, &sm.q_full[x]);
           sm.loads[2 + x] = ++nq[x];
         }
-        for (int j = it.j0; j < it.j1 && !aborted; ++j) {
+        const int j1 = it.j1;
+        for (int j = it.j0; j < j1 && !aborted; ++j) {
           const int ks = nk % kKSlots, vs = nv % kVSlots;
           if (nk >= kKSlots && !dwait(&sm.k_empty[ks], (nk / kKSlots - 1) & 1, st, 81, aborted, lim)) break;
           if (load++ != c.withhold) {
-            load_keys(sm.k[ks], c.tk, k, j, c, it, &sm.k_full[ks]);
+            load_keys(sm.k[ks], c.tk, it, j, c, &sm.k_full[ks]);
             sm.loads[0] = nk + 1;
           }
           ++nk;
           if (nv >= kVSlots && !dwait(&sm.v_empty[vs], (nv / kVSlots - 1) & 1, st, 82, aborted, lim)) break;
           if (load++ != c.withhold) {
-            load_keys(sm.v[vs], c.tv, k, j, c, it, &sm.v_full[vs]);
+            load_keys(sm.v[vs], c.tv, it, j, c, &sm.v_full[vs]);
             sm.loads[1] = nv + 1;
           }
           ++nv;
         }
+        mbar_arrive(&sm.item_empty[n % kItemSlots]);
       }
     } else if (warp == 9) {
       // -------------------------------------------------------------- MMA
@@ -333,54 +337,86 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       constexpr uint32_t kSlotStep = 32768 >> 4;  // descriptor units per slot or Q tile
       int ks = 0, vs = 0;
       uint32_t kph = 0, vph = 0;
-      uint32_t q_seen[2] = {0, 0}, s_done[2] = {0, 0}, p_done[2] = {0, 0}, o_done[2] = {0, 0};  // events so far
+      // parities of the next waits by Q tile (bit x); whether O_x has been used
+      uint32_t q_par = 0, s_par = 0, p_par = 0, o_par = 0, o_any = 0;
       int s_last = -1;  // the Q tile whose S came last
-      Item cur, nxt;
-      // the first tile of the next item that has any, from item i on
-      auto find = [&](int i, Item& it) {
-        for (; i < items; i += gridDim.x) {
-          KeyTiles k;
-          item_at(c, sm, i, it, k);
-          if (it.j0 < it.j1) break;
+      // the next item that has key tiles; false: no more
+      uint32_t n_item = 0;
+      auto next_item = [&](const Item*& it) -> bool {
+        for (;;) {
+          if (!dwait_warp(&sm.item_full[n_item % kItemSlots], (n_item / kItemSlots) & 1, st, 89, aborted, lim)) return false;
+          it = &sm.item[n_item % kItemSlots];
+          if (it->j0 < 0) return false;
+          ++n_item;
+          if (it->j0 < it->j1) return true;
+          warp_arrive(&sm.item_empty[(n_item - 1) % kItemSlots], lane);
         }
-        return i;
       };
-      // S_x of tile j of an item, with K in slot ks
-      auto issue_s = [&](const Item& it, int x, int j) -> bool {
-        if (!it.takes(x, j)) return true;
-        if (j == it.first[x]) {
-          if (!dwait_warp(&sm.q_full[x], q_seen[x] & 1, st, 83, aborted, lim)) return false;
-          ++q_seen[x];
+      // What is to do for a key tile. Bit x: Q tile x takes it, 2 + x: as its first, 4 + x:
+      // as its last; from bit 8: its keys / 16
+      constexpr uint32_t kPlain = 0x803;
+      auto todo = [&](const Item& it, int j) -> uint32_t {
+        uint32_t f = (uint32_t)it.width(j) << 4;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (it.takes(x, j)) f |= (1u << x) | ((uint32_t)(j == it.first[x]) << (2 + x)) | ((uint32_t)(j == it.last[x]) << (4 + x));
+        return f;
+      };
+      // S_x of a tile, with K in slot ks
+      auto issue_s = [&](uint32_t f, int x) -> bool {
+        if (!(f >> x & 1u)) return true;
+        if (f >> (2 + x) & 1u) {
+          if (!dwait_warp(&sm.q_full[x], q_par >> x & 1u, st, 83, aborted, lim)) return false;
+          q_par ^= 1u << x;
         }
-        if (s_last >= 0 && !dwait_warp(&sm.s_free[s_last], (s_done[s_last] - 1) & 1, st, 84, aborted, lim)) return false;
-        tc_fence_after();
-        issue_qk<0>(lead, tm, q_lo + x * kSlotStep, k_lo + (uint32_t)ks * kSlotStep, dhi, id_s);
-        umma_commit_lead(lead, &sm.s_full[x]);
-        if (j == it.last[x]) umma_commit_lead(lead, &sm.q_empty[x]);
-        ++s_done[x];
+        // the S before this one has been read
+        if (s_last >= 0) {
+          if (!dwait_warp(&sm.s_free[s_last], s_par >> s_last & 1u, st, 84, aborted, lim)) return false;
+          s_par ^= 1u << s_last;
+        }
         s_last = x;
+        tc_fence_after();
+        const uint32_t q = q_lo + x * kSlotStep, k = k_lo + (uint32_t)ks * kSlotStep;
+        if (f >> 8 == 8u)  // (a constant instruction descriptor: eight of them issue in half the time)
+          issue_qk<0>(lead, tm, q, k, dhi, id_s);
+        else
+          issue_qk<0>(lead, tm, q, k, dhi, id_s - ((8u - (f >> 8)) << 18));  // (its N: the tile's keys)
+        umma_commit_lead(lead, &sm.s_full[x]);
+        if (f >> (4 + x) & 1u) umma_commit_lead(lead, &sm.q_empty[x]);
         return true;
       };
-      auto issue_pv = [&](const Item& it, int x, int j) -> bool {
-        if (!it.takes(x, j)) return true;
-        if (!dwait_warp(&sm.p_full[x], p_done[x] & 1, st, 85, aborted, lim)) return false;
-        ++p_done[x];
-        if (j == it.first[x] && o_done[x] > 0 &&
-            !dwait_warp(&sm.o_empty[x], (o_done[x] - 1) & 1, st, 86, aborted, lim))
-          return false;
-        tc_fence_after();
+      auto issue_pv = [&](uint32_t f, int x) -> bool {
+        if (!(f >> x & 1u)) return true;
+        const uint32_t again = (f >> (2 + x) & 1u) ^ 1u;
         const uint32_t d = tm + kColO + 128 * x, a = tm + kColP + 64 * x, vb = v_lo + (uint32_t)vs * kSlotStep;
-        umma_ts_lead<0>(lead, d, a, vb, dhi, id_o, j > it.first[x]);
-        umma_ts_lead<1>(lead, d, a, vb, dhi, id_o, 1u);
-        umma_ts_lead<2>(lead, d, a, vb, dhi, id_o, 1u);
-        umma_ts_lead<3>(lead, d, a, vb, dhi, id_o, 1u);
-        umma_ts_lead<4>(lead, d, a, vb, dhi, id_o, 1u);
-        umma_ts_lead<5>(lead, d, a, vb, dhi, id_o, 1u);
-        umma_ts_lead<6>(lead, d, a, vb, dhi, id_o, 1u);
-        umma_ts_lead<7>(lead, d, a, vb, dhi, id_o, 1u);
-        if (j == it.last[x]) {
+        if (!again && (o_any >> x & 1u)) {
+          if (!dwait_warp(&sm.o_empty[x], o_par >> x & 1u, st, 86, aborted, lim)) return false;
+          o_par ^= 1u << x;
+        }
+        if (!dwait_warp(&sm.p_full[x], p_par >> x & 1u, st, 85, aborted, lim)) return false;
+        p_par ^= 1u << x;
+        tc_fence_after();
+        umma_ts_lead<0>(lead, d, a, vb, dhi, id_o, again);
+        if (f >> 8 == 8u) {
+          umma_ts_lead<1>(lead, d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<2>(lead, d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<3>(lead, d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<4>(lead, d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<5>(lead, d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<6>(lead, d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<7>(lead, d, a, vb, dhi, id_o, 1u);
+        } else {
+          const uint32_t steps = f >> 8;  // of 16 keys
+          umma_ts_lead<1>(lead & (uint32_t)(steps > 1), d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<2>(lead & (uint32_t)(steps > 2), d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<3>(lead & (uint32_t)(steps > 3), d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<4>(lead & (uint32_t)(steps > 4), d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<5>(lead & (uint32_t)(steps > 5), d, a, vb, dhi, id_o, 1u);
+          umma_ts_lead<6>(lead & (uint32_t)(steps > 6), d, a, vb, dhi, id_o, 1u);
+        }
+        if (f >> (4 + x) & 1u) {
           umma_commit_lead(lead, &sm.o_full[x]);
-          ++o_done[x];
+          o_any |= 1u << x;
         }
         return true;
       };
@@ -392,50 +428,79 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           kph ^= 1u;
         }
       };
-      int i = find(blockIdx.x, cur), j = cur.j0;
-      if (i < items) {
-        if (take_k() && issue_s(cur, 0, j) && issue_s(cur, 1, j)) give_k();
-        while (!aborted) {
-          // the tile after this one
-          bool more = true, same = j + 1 < cur.j1;
-          int ni = i;
-          if (!same) {
-            ni = find(i + gridDim.x, nxt);
-            more = ni < items;
-          }
-          if (!dwait_warp(&sm.v_full[vs], vph, st, 88, aborted, lim)) break;
-          if (!issue_pv(cur, 0, j)) break;
-          if (more) {
-            if (!take_k()) break;
-            if (!(same ? issue_s(cur, 0, j + 1) : issue_s(nxt, 0, nxt.j0))) break;
-          }
-          if (!issue_pv(cur, 1, j)) break;
-          umma_commit_lead(lead, &sm.v_empty[vs]);
-          if (++vs == kVSlots) {
-            vs = 0;
-            vph ^= 1u;
-          }
-          if (!more) break;
-          if (!(same ? issue_s(cur, 1, j + 1) : issue_s(nxt, 1, nxt.j0))) break;
+      // O += P V of a tile (f), S of the one after it (nf)
+      auto step = [&](uint32_t f, uint32_t nf, bool more) -> bool {
+        if (!dwait_warp(&sm.v_full[vs], vph, st, 88, aborted, lim)) return false;
+        if (!issue_pv(f, 0)) return false;
+        if (more && !(take_k() && issue_s(nf, 0))) return false;
+        if (!issue_pv(f, 1)) return false;
+        umma_commit_lead(lead, &sm.v_empty[vs]);
+        if (++vs == kVSlots) {
+          vs = 0;
+          vph ^= 1u;
+        }
+        if (more) {
+          if (!issue_s(nf, 1)) return false;
           give_k();
-          if (same) {
-            ++j;
-          } else {
-            cur = nxt;
-            i = ni;
-            j = cur.j0;
+        }
+        return true;
+      };
+      const Item* it;
+      if (next_item(it)) {
+        int j = it->j0, j1 = it->j1, plain_lo = it->plain_lo, plain_hi = it->plain_hi;
+        uint32_t f = todo(*it, j);
+        if (take_k() && issue_s(f, 0) && issue_s(f, 1)) give_k();
+        while (!aborted) {
+          // between plain tiles there is nothing to look up (with a look at the item per
+          // tile this warp alone took 3.5K cycles a tile, its products 2K)
+          if (j >= plain_lo)
+            while (j < plain_hi && step(kPlain, kPlain, true)) ++j;
+          if (aborted) break;
+          f = todo(*it, j);
+          const uint32_t slot = (n_item - 1) % kItemSlots;  // (the present item's)
+          const bool same = ++j < j1;
+          bool more = true;
+          if (!same) {
+            more = next_item(it);
+            if (more) {
+              j = it->j0;
+              j1 = it->j1;
+              plain_lo = it->plain_lo;
+              plain_hi = it->plain_hi;
+            }
           }
+          const uint32_t nf = more ? todo(*it, j) : 0u;
+          if (!same) warp_arrive(&sm.item_empty[slot], lane);
+          if (aborted || !step(f, nf, more) || !more) break;
         }
       }
-    } else if (warp >= 10 && p.splits == 1) {
+    } else if (warp == 10) {
+      // ------------------------------------------------------------- items
+      for (uint32_t n = 0; !aborted; ++n) {
+        const uint32_t slot = n % kItemSlots;
+        if (n >= kItemSlots && !dwait_warp(&sm.item_empty[slot], (n / kItemSlots - 1) & 1, st, 78, aborted, lim)) break;
+        const int64_t index = blockIdx.x + (int64_t)n * gridDim.x;
+        Item it;
+        it.j0 = -1;
+        if (index < items) item_at(c, sm, (int)index, it);
+        if (lane == 0) sm.item[slot] = it;
+        warp_arrive(&sm.item_full[slot], lane);
+        if (index >= items) break;
+      }
+    } else if (warp == 11 && p.splits == 1) {
       // ----------------------------------------------- rows behind the queries
+      constexpr int kPiece = 32;  // tokens of a head at a time
+      const int half = lane >> 4;
       for (int b = 0; b < p.batch; ++b) {
-        const int nq = window_seq(p, b).nq;
-        const int64_t n = (int64_t)(p.n_tok - nq) * p.n_q_heads;
-        for (int64_t r = blockIdx.x * 2 + (warp - 10); r < n; r += 2 * gridDim.x) {
-          const int t = nq + (int)(r / p.n_q_heads), h = (int)(r % p.n_q_heads);
-          *reinterpret_cast<uint2*>(p.out.at(b, h, t) + 4 * lane) = make_uint2(0u, 0u);
-          if (lane == 0 && p.lse != nullptr) p.lse[((int64_t)b * p.n_q_heads + h) * p.n_tok + t] = kNone;
+        const int nq = window_seq(p, b).nq, pieces = (p.n_tok - nq + kPiece - 1) / kPiece;
+        const int64_t n = (int64_t)pieces * p.n_q_heads;
+        for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+          const int h = (int)(i / pieces), t0 = nq + (int)(i - (int64_t)h * pieces) * kPiece;
+          __nv_bfloat16* const to = p.out.at(b, h, t0) + 8 * (lane & 15);
+          const int m = min(kPiece, p.n_tok - t0);
+#pragma unroll 4
+          for (int t = half; t < m; t += 2) *reinterpret_cast<uint4*>(to + t * p.out.st) = make_uint4(0u, 0u, 0u, 0u);
+          if (lane < m && p.lse != nullptr) p.lse[((int64_t)b * p.n_q_heads + h) * p.n_tok + t0 + lane] = kNone;
         }
       }
     }
@@ -449,51 +514,66 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
     const bool is_row = token < c.tokens;
     const uint64_t sl2_2 = f2_pack(p.scale_log2, p.scale_log2);
     uint32_t n_s = 0, n_o = 0;
-    for (int i = blockIdx.x; i < items && !aborted; i += gridDim.x) {
-      Item it;
-      KeyTiles k;
-      item_at(c, sm, i, it, k);
+    for (uint32_t n = 0; !aborted; ++n) {
+      if (!dwait_warp(&sm.item_full[n % kItemSlots], (n / kItemSlots) & 1, st, 94, aborted, lim)) break;
+      const Item& it = sm.item[n % kItemSlots];
+      if (it.j0 < 0) break;
       const int t = it.t0 + x * c.tokens + token;
-      const bool row_ok = is_row && t < it.s.nq;
-      const int pos = row_ok ? it.s.first + t : -1;
-      const int pfirst = it.s.first + it.t0 + x * c.tokens;
-      const int plast = it.s.first + min(it.t0 + (x + 1) * c.tokens, it.s.nq) - 1;
+      const bool row_ok = is_row && t < it.n_query;
+      const int pos = row_ok ? it.position + x * c.tokens + token : -1;
+      const int pfirst = it.position + x * c.tokens;
+      const int plast = it.position + min((x + 1) * c.tokens, it.n_query - it.t0) - 1;
       float m_ref = kNone, l = 0.f;
-      const int first = x ? it.first[1] : it.first[0], last = x ? it.last[1] : it.last[0];
-      const int in_a = x ? it.in_a[1] : it.in_a[0], in_b = x ? it.in_b[1] : it.in_b[0];
+      const int first = it.first[x], last = it.last[x], in_a = it.in_a[x], in_b = it.in_b[x], in_first = it.in_first;
+      const int firsts = it.firsts, narrow = it.rest > 0 ? it.whole : -1, rest = it.rest;
+      const int n_a = it.n_a, a0 = it.end_a - kKeys * (n_a + firsts), b0 = it.end_b - kKeys * it.n;
+      const int low_a = it.low_a, low_b = it.low_b;
+      const bool in_order = it.in_order;
       const bool any = first <= last;
-      for (int j = first; j <= last; ++j) {
-        if (j >= it.in_sinks && (j < in_a || j > in_b)) continue;
-        if (!dwait_warp(&sm.s_full[x], n_s & 1, st, 90, aborted, lim)) break;
+      // a tile of which 32 NC columns are looked at
+      auto tile = [&](auto nc, int j) -> bool {
+        constexpr int NC = decltype(nc)::value;
+        // which of the tile's rows this row sees
+        int s1 = -1, w0 = 0, w1 = -1, e0 = 0, e1 = -1;
+        bool whole;
+        if (j < firsts) {
+          s1 = min(j == narrow ? rest : kKeys, min(p.n_sink, pos + 1) - kKeys * j) - 1;  // first tokens: rows 0 .. s1
+          whole = kKeys * (j + 1) <= min(p.n_sink, pfirst + 1);
+        } else {
+          const bool a = j - firsts < n_a;
+          const int start = (a ? a0 : b0) + kKeys * j, low = a ? low_a : low_b;
+          w0 = max(pos - p.window + 1, low) - start;
+          w1 = pos - start;
+          if (in_order) {
+            e0 = max(0, -start);
+            e1 = min(p.n_sink - 1, pos) - start;
+          }
+          whole = start >= max(plast - p.window + 1, low) && start + kKeys - 1 <= pfirst;
+        }
+        if (!dwait_warp(&sm.s_full[x], n_s & 1, st, 90, aborted, lim)) return false;
         ++n_s;
         tc_fence_after();
-        uint32_t sr[4][32];
+        uint32_t sr[NC][32];
 #pragma unroll
-        for (int cc = 0; cc < 4; ++cc) tmem_ld32(tmem + lane_off + 32 * cc, sr[cc]);
+        for (int cc = 0; cc < NC; ++cc) tmem_ld32(tmem + lane_off + 32 * cc, sr[cc]);
         tmem_wait_ld();
         tc_fence_before();
-        mbar_arrive(&sm.s_free[x]);
-        // which of the tile's rows this row sees
-        const int start = k.start(j), low = k.low(j);
-        const int head_rows = j < k.whole ? kKeys : j == k.whole ? k.rest : 0;
-        const bool whole = head_rows == 0 ? start >= max(plast - p.window + 1, low) && start + kKeys - 1 <= pfirst
-                                          : head_rows == kKeys && kKeys * (j + 1) <= min(p.n_sink, pfirst + 1);
+        warp_arrive(&sm.s_free[x], lane);
         if (!whole) {
-          const int s1 = min(head_rows, min(p.n_sink, pos + 1) - kKeys * min(j, k.whole)) - 1;  // first tokens: rows 0 .. s1
-          const int w0 = max(max(pos - p.window + 1, low) - start, head_rows), w1 = head_rows == kKeys ? -1 : pos - start;
-          const int e0 = k.in_order ? max(0, -start) : 0, e1 = k.in_order ? min(p.n_sink - 1, pos) - start : -1;
 #pragma unroll
-          for (int cc = 0; cc < 4; ++cc) {
+          for (int cc = 0; cc < NC; ++cc) {
             const uint32_t see = bits(-32 * cc, s1 - 32 * cc) | bits(w0 - 32 * cc, w1 - 32 * cc) |
                                  bits(e0 - 32 * cc, e1 - 32 * cc);
+            if (__any_sync(0xffffffffu, see != 0xffffffffu)) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (!(see >> e & 1u)) sr[cc][e] = __float_as_uint(kNone);
+              for (int e = 0; e < 32; ++e)
+                if (!(see >> e & 1u)) sr[cc][e] = __float_as_uint(kNone);
+            }
           }
         }
         float mx[4] = {kNone, kNone, kNone, kNone};
 #pragma unroll
-        for (int c2 = 0; c2 < kKeys / 2; ++c2)
+        for (int c2 = 0; c2 < 16 * NC; ++c2)
           mx[c2 & 3] = fmax3(mx[c2 & 3], __uint_as_float(sr[(2 * c2) >> 5][(2 * c2) & 31]),
                              __uint_as_float(sr[(2 * c2 + 1) >> 5][(2 * c2 + 1) & 31]));
         const float tmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
@@ -519,28 +599,41 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         }
         const float mb = m_ref == kNone ? 0.f : m_ref;
         const uint64_t nm2 = f2_pack(-mb, -mb);
-        uint32_t pk[2][32];
         uint64_t acc[2] = {0ull, 0ull};
 #pragma unroll
-        for (int c2 = 0; c2 < kKeys / 2; ++c2) {
-          float e0, e1;
-          f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[(2 * c2) >> 5][(2 * c2) & 31]),
-                                   __uint_as_float(sr[(2 * c2 + 1) >> 5][(2 * c2 + 1) & 31])),
-                           sl2_2, nm2),
-                    e0, e1);
-          const float a = ex2_approx(e0), bb = ex2_approx(e1);
-          acc[c2 & 1] = f2_add(acc[c2 & 1], f2_pack(a, bb));
-          pk[c2 >> 5][c2 & 31] = pack_bf16(a, bb);
+        for (int half = 0; half < (NC + 1) / 2; ++half) {
+          constexpr int kPairs = NC >= 2 ? 32 : 16;
+          uint32_t pk[kPairs];
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) {
+            const int c2 = 32 * half + i;
+            float e0f, e1f;
+            f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[(2 * c2) >> 5][(2 * c2) & 31]),
+                                     __uint_as_float(sr[(2 * c2 + 1) >> 5][(2 * c2 + 1) & 31])),
+                             sl2_2, nm2),
+                      e0f, e1f);
+            const float a = ex2_approx(e0f), bb = ex2_approx(e1f);
+            acc[i & 1] = f2_add(acc[i & 1], f2_pack(a, bb));
+            pk[i] = pack_bf16(a, bb);
+          }
+          if constexpr (NC >= 2)
+            tmem_st32(tmem + lane_off + p_col + 32 * half, pk);
+          else
+            tmem_st16(tmem + lane_off + p_col, pk);
         }
-        tmem_st32(tmem + lane_off + p_col, pk[0]);
-        tmem_st32(tmem + lane_off + p_col + 32, pk[1]);
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(&sm.p_full[x]);
+        warp_arrive(&sm.p_full[x], lane);
         float sum[4];
         f2_unpack(acc[0], sum[0], sum[1]);
         f2_unpack(acc[1], sum[2], sum[3]);
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        return true;
+      };
+      for (int j = first; j <= last; ++j) {
+        if (j >= in_first && (j < in_a || j > in_b)) continue;
+        if (!(j == narrow && rest <= 32 ? tile(std::integral_constant<int, 1>{}, j) : tile(std::integral_constant<int, 4>{}, j)))
+          break;
       }
       if (any && (aborted || !dwait_warp(&sm.o_full[x], n_o & 1, st, 91, aborted, lim))) break;
       if (any) ++n_o;
@@ -564,7 +657,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         }
         if (cb == 3 && any) {
           tc_fence_before();
-          mbar_arrive(&sm.o_empty[x]);
+          warp_arrive(&sm.o_empty[x], lane);
         }
         if (!row_ok) continue;
         if (p.splits == 1) {
@@ -594,6 +687,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         const float4 y = window_row_alone(p, it.b, ah, at);
         *reinterpret_cast<uint2*>(p.out.at(it.b, ah, at) + 4 * lane) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
       }
+      warp_arrive(&sm.item_empty[n % kItemSlots], lane);
     }
     tmem_wait_st();
     tc_fence_before();
