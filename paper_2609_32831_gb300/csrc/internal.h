@@ -432,6 +432,7 @@ struct WindowPromptParams {
   CUtensorMap tq;        // box 64 channels x the group's heads x tokens
   CUtensorMap tk[2], tv[2];  // box 64 channels x 128 rows; x the rows of the first tokens' last tile
   int tokens;
+  uint32_t* taken;       // items taken beyond the CTAs' first ones (0 before the launch), or null: there are none
   bool wide_out;         // rows of out start on 32 bytes
   uint64_t wait_ns;
   int withhold;          // test hook: the load of a CTA (K and V in turn) that is never made (-1: none)

@@ -512,7 +512,13 @@ uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32
   c.wait_ns = wait_limit_ns();
   c.withhold = take_withhold_pos();
   const int64_t items = (int64_t)batch * hkv * w.row_blocks * w.splits;
-  launch_window_prompt(c, (int)std::min<int64_t>(items, num_sms()), reinterpret_cast<cudaStream_t>(stream));
+  const int grid = (int)std::min<int64_t>(items, num_sms());
+  const cudaStream_t cs = reinterpret_cast<cudaStream_t>(stream);
+  if (items > grid) {
+    c.taken = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + 128);
+    cudaMemsetAsync(c.taken, 0, sizeof(uint32_t), cs);
+  }
+  launch_window_prompt(c, grid, cs);
   return cuda_check(fn);
 }
 

@@ -67,7 +67,11 @@ __device__ __forceinline__ bool window_sees(const WindowParams& p, int pos, int 
 // does not see, by a warp: lane l has channels 4 l .. 4 l + 3. For rows that a
 // product over whole tiles left NaN or infinite: 0 times what a masked row of v
 // holds is not 0 there.
-static __device__ __noinline__ float4 window_row_alone(const WindowParams& p, int b, int h, int t) {
+struct WindowRow {
+  float4 o;
+  float lse;
+};
+static __device__ __noinline__ WindowRow window_row_alone(const WindowParams& p, int b, int h, int t) {
   const int lane = threadIdx.x & 31, kvh = h / p.group;
   const WindowSeq s = window_seq(p, b);
   const int pos = s.first + t;
@@ -94,21 +98,28 @@ static __device__ __noinline__ float4 window_row_alone(const WindowParams& p, in
     m = top;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  return make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+  return WindowRow{make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv),
+                   l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2};
 }
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 
-// A finished row, by a warp: o (lane l: channels 4 l ..) and l relative to 2^m.
+// A finished row, by a warp: o (lane l: channels 4 l ..) and l relative to 2^m. An
+// infinite l: neither is known.
 __device__ __forceinline__ void window_store_row(const WindowParams& p, int b, int h, int t, float4 o, float m, float l) {
   const int lane = threadIdx.x & 31;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   float4 y = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
   const bool bad = !(finite(y.x) && finite(y.y) && finite(y.z) && finite(y.w));
-  if (__any_sync(0xffffffffu, bad) && finite(l)) y = window_row_alone(p, b, h, t);
+  float lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  if (__any_sync(0xffffffffu, bad) && l == l) {
+    const WindowRow w = window_row_alone(p, b, h, t);
+    y = w.o;
+    if (!finite(l)) lse = w.lse;
+  }
   *reinterpret_cast<uint2*>(p.out.at(b, h, t) + 4 * lane) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
   if (lane == 0 && p.lse != nullptr)
-    p.lse[((int64_t)b * p.n_q_heads + h) * p.n_tok + t] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    p.lse[((int64_t)b * p.n_q_heads + h) * p.n_tok + t] = lse;
 }
 
 }  // namespace uc

@@ -1,14 +1,18 @@
 // Attention with a sliding window and first tokens for prompts: many queries, on
 // the 5th-generation tensor cores.
 //
-// A CTA takes items one after the other: 2 tiles of up to 128 query rows of a KV
+// A CTA takes items one after the other, as they come (in equal numbers some got a fifth
+// more key tiles than the average of a ragged batch): 2 tiles of up to 128 query rows of a KV
 // head (consecutive tokens x the group's query heads, so that a tile spans few
 // tokens and reads each key tile once for all heads), over the key tiles that the
 // two have in reach, all or a range of them. Roles:
 //   warps 0-3, 4-7  softmax of Q tile 0 / 1: a row per thread (= TMEM lane). S is read
-//                   into registers, P = 2^(S - m) goes back to TMEM as bf16 pairs; the
-//                   reference m moves only when a row's maximum passes it by 2^8, and
-//                   O is scaled then; l, m and O are fp32. Then the rows' outputs.
+//                   into registers, P = 2^(S - m) goes back to TMEM as bf16 pairs, by
+//                   halves. Any reference m will do that keeps P and its sums in range
+//                   (bf16's is fp32's): the maximum of a row's first tile, moved by the
+//                   power of two that a tile's sum of P shows once that passes 2^15, O
+//                   with it. So no maximum stands between S and P. l, m and O are fp32.
+//                   Then the rows' outputs.
 //   warp 8          TMA: Q tiles, K tiles (3 slots), V tiles (2 slots)
 //   warp 9          every tcgen05.mma: S_x = Q_x K^T, O_x += P_x V (P from TMEM), the
 //                   two Q tiles in turn, across items too
@@ -39,7 +43,8 @@ constexpr int kThreads = 384;
 constexpr int kQRows = 128;   // rows of a Q tile
 constexpr int kKeys = 128;    // keys of a tile
 constexpr int kKSlots = 3, kVSlots = 2;
-// Registers per thread after the warpgroups rebalance (launch: 168 each).
+// Registers per thread after the warpgroups rebalance (launch: 168 each). A fourth
+// warpgroup for the outputs would leave the softmax 192, and took a tenth longer.
 constexpr int kRegSoftmax = 216, kRegOther = 56;
 static_assert(2 * 128 * kRegSoftmax + 128 * kRegOther <= kThreads * 168, "register split");
 // Tensor memory: one S for both Q tiles (a row is in registers long before the other
@@ -47,7 +52,8 @@ static_assert(2 * 128 * kRegSoftmax + 128 * kRegOther <= kThreads * 168, "regist
 constexpr uint32_t kColP = 128, kColO = 256;
 constexpr float kNone = -INFINITY;
 
-constexpr int kItemSlots = 4;
+constexpr int kItemSlots = 2;
+constexpr int kLooked = 8;
 
 // What the roles need to know of an item: 2 Q tiles from token t0 on, key tiles j0 ..
 // j1 - 1 of those in reach. Tiles below `firsts` hold first tokens (row i of tile j is token
@@ -67,6 +73,7 @@ struct Item {
   int slot_b;              // the cache's row behind the last
   int in_order;            // the tiles hold every position from 0 on
   int plain_lo, plain_hi;  // tiles of 128 that both Q tiles take, neither as its first or last
+  uint16_t head[kLooked], tail[kLooked];  // todo() of the first and (from behind) the last tiles
   __device__ __forceinline__ bool takes(int x, int j) const {
     return j >= first[x] && j <= last[x] && (j < in_first || (j >= in_a[x] && j <= in_b[x]));
   }
@@ -75,6 +82,15 @@ struct Item {
     return part_a(j) ? end_a - kKeys * (n_a - (j - firsts)) : end_b - kKeys * (n - j);
   }
   __device__ __forceinline__ int width(int j) const { return j == whole && rest > 0 ? rest : kKeys; }
+  // What is to do for a key tile. Bit x: Q tile x takes it, 2 + x: as its first, 4 + x: as
+  // its last; from bit 8: its keys / 16
+  __device__ __forceinline__ uint32_t todo(int j) const {
+    uint32_t f = (uint32_t)width(j) << 4;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      if (takes(x, j)) f |= (1u << x) | ((uint32_t)(j == first[x]) << (2 + x)) | ((uint32_t)(j == last[x]) << (4 + x));
+    return f;
+  }
 };
 
 struct PromptSmem {
@@ -82,7 +98,7 @@ struct PromptSmem {
   uint8_t k[kKSlots][2][16384];
   uint8_t v[kVSlots][2][16384];  // (the MN-major B operand)
   uint64_t k_full[kKSlots], k_empty[kKSlots], v_full[kVSlots], v_empty[kVSlots];
-  uint64_t q_full[2], q_empty[2], s_full[2], s_free[2], p_full[2], o_full[2], o_empty[2], drain;
+  uint64_t q_full[2], q_empty[2], s_full[2], s_free[2], p_full[2][2], o_full[2], o_empty[2], drain;
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   Item item[kItemSlots];
   DevStatus status;              // of this CTA's waits
@@ -90,7 +106,7 @@ struct PromptSmem {
   uint32_t tmem_base;
   int begin[kWindowSeqs + 1];    // items before a sequence's
 };
-static_assert(sizeof(PromptSmem) + 1024 <= 232448, "shared memory");
+static_assert(sizeof(PromptSmem) <= 232448, "shared memory");
 
 __device__ __forceinline__ void item_at(const WindowPromptParams& c, const PromptSmem& sm, int index, Item& it) {
   const WindowParams& p = c.p;
@@ -197,6 +213,11 @@ __device__ __forceinline__ void load_keys(uint8_t (*slot)[16384], const CUtensor
   tma_4d(slot[1], map, 64, row, it.kvh, it.b, bar);
 }
 
+// Where a row's part of an item's split goes.
+__device__ __forceinline__ float* part_of(const WindowParams& p, const Item& it, int row) {
+  return p.part + (((int64_t)(it.b * p.n_kv_heads + it.kvh) * p.splits + it.split) * p.group * p.n_tok + row) * (kHeadDim + 4);
+}
+
 __device__ __forceinline__ void store_row32(__nv_bfloat16* to, const uint32_t (&o)[32], float inv, bool wide) {
   // 32 values of a row: 64 bytes, in pieces of 32 where they are aligned to them
 #pragma unroll
@@ -216,6 +237,40 @@ __device__ __forceinline__ void store_row32(__nv_bfloat16* to, const uint32_t (&
   }
 }
 
+// The bounded waits, in as little code as they take (`aborted`: where one ran out; the
+// role's end reports it): the roles' loops are what the instruction caches should hold.
+// With the general ones in place 30 % of the warps' time went by fetching.
+__device__ __forceinline__ bool wait_some(uint64_t* bar, uint32_t parity, uint64_t lim) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = global_ns();
+#pragma unroll 1
+  for (uint32_t it = 1; !mbar_try_wait(bar, parity); ++it)
+    if ((it & 15u) == 0u && global_ns() - t0 > lim) return false;
+  return true;
+}
+__device__ __forceinline__ bool wait_lane(uint64_t* bar, uint32_t parity, int where, int& aborted, uint64_t lim) {
+  if (wait_some(bar, parity, lim)) return true;
+  aborted = where;
+  return false;
+}
+// The same for a converged warp, with one outcome: a vote's, which the compiler knows to
+// be the same in every lane (what depends on it may stay in uniform registers).
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, int where, int& aborted, uint64_t lim) {
+  const bool ok = __all_sync(0xffffffffu, wait_some(bar, parity, lim));
+  if (!ok) aborted = where;
+  return ok;
+}
+
+// Nothing that reads these is moved in front of this.
+__device__ __forceinline__ void tie32(uint32_t (&r)[32]) {
+  asm volatile(""
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                 "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
+                 "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                 "+r"(r[30]), "+r"(r[31]));
+}
+
 // Once for the warp, what its lanes have read or written before it.
 __device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
   __syncwarp();
@@ -223,9 +278,13 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
 }
 
 __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid_constant__ WindowPromptParams c) {
-  extern __shared__ uint8_t dyn[];
-  PromptSmem& sm = *reinterpret_cast<PromptSmem*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~static_cast<uintptr_t>(1023));
+  extern __shared__ __align__(1024) uint8_t dyn[];
+  PromptSmem& sm = *reinterpret_cast<PromptSmem*>(dyn);
   const WindowParams& p = c.p;
+  if ((smem_u32(dyn) & 1023u) != 0) {  // (the swizzled tiles need it)
+    if (threadIdx.x == 0) set_status(p.status, UC_ERR_CUDA, 77);
+    return;
+  }
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kKSlots; ++s) {
@@ -241,7 +300,8 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       mbar_init(&sm.q_empty[x], 1);
       mbar_init(&sm.s_full[x], 1);
       mbar_init(&sm.s_free[x], 4);
-      mbar_init(&sm.p_full[x], 4);
+      mbar_init(&sm.p_full[x][0], 4);
+      mbar_init(&sm.p_full[x][1], 4);
       mbar_init(&sm.o_full[x], 1);
       mbar_init(&sm.o_empty[x], 4);
     }
@@ -284,9 +344,8 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
   tc_fence_after();
   const uint32_t tmem = sm.tmem_base;
   const int items = sm.begin[p.batch];
-  DevStatus* const st = &sm.status;
   const uint64_t lim = c.wait_ns;
-  bool aborted = false;
+  int aborted = 0;
 
   if (warp >= 8) {
     setmaxnreg_dec<kRegOther>();
@@ -294,33 +353,41 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       // -------------------------------------------------------------- TMA
       int nk = 0, nv = 0, nq[2] = {0, 0}, load = 0;
       for (uint32_t n = 0; !aborted; ++n) {
-        if (!dwait(&sm.item_full[n % kItemSlots], (n / kItemSlots) & 1, st, 79, aborted, lim)) break;
+        if (!wait_lane(&sm.item_full[n % kItemSlots], (n / kItemSlots) & 1, 79, aborted, lim)) break;
         const Item& it = sm.item[n % kItemSlots];
         if (it.j0 < 0) break;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (it.last[x] < it.first[x]) continue;
-          if (nq[x] > 0 && !dwait(&sm.q_empty[x], (nq[x] - 1) & 1, st, 80, aborted, lim)) break;
-          mbar_arrive_expect_tx(&sm.q_full[x], 2 * 128 * p.group * c.tokens);
-          tma_4d(sm.q[x][0], &c.tq, 0, it.kvh * p.group, it.t0 + x * c.tokens, it.b, &sm.q_full[x]);
-          tma_4d(sm.q[x][1], &c.tq, 64, it.kvh * p.group, it.t0 + x * c.tokens, it.b, &sm.q_full[x]);
-          sm.loads[2 + x] = ++nq[x];
-        }
-        const int j1 = it.j1;
-        for (int j = it.j0; j < j1 && !aborted; ++j) {
+        // (the first K ahead of Q, whose places come free with the last S of the item before)
+        const int j0 = it.j0, j1 = it.j1;
+        for (int j = j0; j < max(j1, j0 + 1) && !aborted; ++j) {
           const int ks = nk % kKSlots, vs = nv % kVSlots;
-          if (nk >= kKSlots && !dwait(&sm.k_empty[ks], (nk / kKSlots - 1) & 1, st, 81, aborted, lim)) break;
-          if (load++ != c.withhold) {
-            load_keys(sm.k[ks], c.tk, it, j, c, &sm.k_full[ks]);
-            sm.loads[0] = nk + 1;
+          if (j < j1) {
+            if (nk >= kKSlots && !wait_lane(&sm.k_empty[ks], (nk / kKSlots - 1) & 1, 81, aborted, lim)) break;
+            if (load++ != c.withhold) {
+              load_keys(sm.k[ks], c.tk, it, j, c, &sm.k_full[ks]);
+              sm.loads[0] = nk + 1;
+            }
+            ++nk;
           }
-          ++nk;
-          if (nv >= kVSlots && !dwait(&sm.v_empty[vs], (nv / kVSlots - 1) & 1, st, 82, aborted, lim)) break;
-          if (load++ != c.withhold) {
-            load_keys(sm.v[vs], c.tv, it, j, c, &sm.v_full[vs]);
-            sm.loads[1] = nv + 1;
+          if (j == j0) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              if (it.last[x] < it.first[x]) continue;
+              if (nq[x] > 0 && !wait_lane(&sm.q_empty[x], (nq[x] - 1) & 1, 80, aborted, lim)) break;
+              mbar_arrive_expect_tx(&sm.q_full[x], 2 * 128 * p.group * c.tokens);
+              tma_4d(sm.q[x][0], &c.tq, 0, it.kvh * p.group, it.t0 + x * c.tokens, it.b, &sm.q_full[x]);
+              tma_4d(sm.q[x][1], &c.tq, 64, it.kvh * p.group, it.t0 + x * c.tokens, it.b, &sm.q_full[x]);
+              sm.loads[2 + x] = ++nq[x];
+            }
+            if (aborted) break;
           }
-          ++nv;
+          if (j < j1) {
+            if (nv >= kVSlots && !wait_lane(&sm.v_empty[vs], (nv / kVSlots - 1) & 1, 82, aborted, lim)) break;
+            if (load++ != c.withhold) {
+              load_keys(sm.v[vs], c.tv, it, j, c, &sm.v_full[vs]);
+              sm.loads[1] = nv + 1;
+            }
+            ++nv;
+          }
         }
         mbar_arrive(&sm.item_empty[n % kItemSlots]);
       }
@@ -344,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       uint32_t n_item = 0;
       auto next_item = [&](const Item*& it) -> bool {
         for (;;) {
-          if (!dwait_warp(&sm.item_full[n_item % kItemSlots], (n_item / kItemSlots) & 1, st, 89, aborted, lim)) return false;
+          if (!wait_warp(&sm.item_full[n_item % kItemSlots], (n_item / kItemSlots) & 1, 89, aborted, lim)) return false;
           it = &sm.item[n_item % kItemSlots];
           if (it->j0 < 0) return false;
           ++n_item;
@@ -352,75 +419,84 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           warp_arrive(&sm.item_empty[(n_item - 1) % kItemSlots], lane);
         }
       };
-      // What is to do for a key tile. Bit x: Q tile x takes it, 2 + x: as its first, 4 + x:
-      // as its last; from bit 8: its keys / 16
-      constexpr uint32_t kPlain = 0x803;
-      auto todo = [&](const Item& it, int j) -> uint32_t {
-        uint32_t f = (uint32_t)it.width(j) << 4;
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-          if (it.takes(x, j)) f |= (1u << x) | ((uint32_t)(j == it.first[x]) << (2 + x)) | ((uint32_t)(j == it.last[x]) << (4 + x));
-        return f;
+      auto todo = [&](const Item& it, int j, int j0, int j1) -> uint32_t {
+        const uint32_t a = (uint32_t)(j - j0), z = (uint32_t)(j1 - 1 - j);
+        return a < kLooked ? it.head[a] : z < kLooked ? it.tail[z] : it.todo(j);
       };
       // S_x of a tile, with K in slot ks
-      auto issue_s = [&](uint32_t f, int x) -> bool {
-        if (!(f >> x & 1u)) return true;
-        if (f >> (2 + x) & 1u) {
-          if (!dwait_warp(&sm.q_full[x], q_par >> x & 1u, st, 83, aborted, lim)) return false;
+      auto issue_s = [&](auto plain, uint32_t f, int x) -> bool {
+        constexpr bool kIsPlain = decltype(plain)::value;
+        if (!kIsPlain && !(f >> x & 1u)) return true;
+        if (!kIsPlain && (f >> (2 + x) & 1u)) {
+          if (!wait_warp(&sm.q_full[x], q_par >> x & 1u, 83, aborted, lim)) return false;
           q_par ^= 1u << x;
         }
         // the S before this one has been read
-        if (s_last >= 0) {
-          if (!dwait_warp(&sm.s_free[s_last], s_par >> s_last & 1u, st, 84, aborted, lim)) return false;
+        if ((s_last >= 0)) {
+          if (!wait_warp(&sm.s_free[s_last], s_par >> s_last & 1u, 84, aborted, lim)) return false;
           s_par ^= 1u << s_last;
         }
         s_last = x;
         tc_fence_after();
         const uint32_t q = q_lo + x * kSlotStep, k = k_lo + (uint32_t)ks * kSlotStep;
-        if (f >> 8 == 8u)  // (a constant instruction descriptor: eight of them issue in half the time)
+        if (kIsPlain || (f >> 8 == 8u)) {  // (with constant descriptors and offsets eight of them issue in half the time)
           issue_qk<0>(lead, tm, q, k, dhi, id_s);
-        else
-          issue_qk<0>(lead, tm, q, k, dhi, id_s - ((8u - (f >> 8)) << 18));  // (its N: the tile's keys)
+        } else {
+          const uint32_t id = id_s - ((8u - (f >> 8)) << 18);  // (its N: the tile's keys)
+#pragma unroll 1
+          for (uint32_t e = 0; e < 8; ++e) {
+            const uint32_t at = (e >> 2) * 1024u + (e & 3u) * 2u;
+            if (e == 0)
+              umma_ss_lead<0, 0, 0>(lead, tm, q, k, dhi, id);
+            else
+              umma_ss_lead<0, 0, 1>(lead, tm, q + at, k + at, dhi, id);
+          }
+        }
         umma_commit_lead(lead, &sm.s_full[x]);
-        if (f >> (4 + x) & 1u) umma_commit_lead(lead, &sm.q_empty[x]);
+        if (!kIsPlain && (f >> (4 + x) & 1u)) umma_commit_lead(lead, &sm.q_empty[x]);
         return true;
       };
-      auto issue_pv = [&](uint32_t f, int x) -> bool {
-        if (!(f >> x & 1u)) return true;
-        const uint32_t again = (f >> (2 + x) & 1u) ^ 1u;
+      auto issue_pv = [&](auto plain, uint32_t f, int x) -> bool {
+        constexpr bool kIsPlain = decltype(plain)::value;
+        if (!kIsPlain && !(f >> x & 1u)) return true;
+        const uint32_t again = kIsPlain || !(f >> (2 + x) & 1u);
         const uint32_t d = tm + kColO + 128 * x, a = tm + kColP + 64 * x, vb = v_lo + (uint32_t)vs * kSlotStep;
         if (!again && (o_any >> x & 1u)) {
-          if (!dwait_warp(&sm.o_empty[x], o_par >> x & 1u, st, 86, aborted, lim)) return false;
+          if (!wait_warp(&sm.o_empty[x], o_par >> x & 1u, 86, aborted, lim)) return false;
           o_par ^= 1u << x;
         }
-        if (!dwait_warp(&sm.p_full[x], p_par >> x & 1u, st, 85, aborted, lim)) return false;
+        const uint32_t par = p_par >> x & 1u;
         p_par ^= 1u << x;
+        if (!wait_warp(&sm.p_full[x][0], par, 85, aborted, lim)) return false;
         tc_fence_after();
-        umma_ts_lead<0>(lead, d, a, vb, dhi, id_o, again);
-        if (f >> 8 == 8u) {
+        if (kIsPlain || (f >> 8 == 8u)) {
+          umma_ts_lead<0>(lead, d, a, vb, dhi, id_o, again);
           umma_ts_lead<1>(lead, d, a, vb, dhi, id_o, 1u);
           umma_ts_lead<2>(lead, d, a, vb, dhi, id_o, 1u);
           umma_ts_lead<3>(lead, d, a, vb, dhi, id_o, 1u);
+          if (!wait_warp(&sm.p_full[x][1], par, 85, aborted, lim)) return false;
+          tc_fence_after();
           umma_ts_lead<4>(lead, d, a, vb, dhi, id_o, 1u);
           umma_ts_lead<5>(lead, d, a, vb, dhi, id_o, 1u);
           umma_ts_lead<6>(lead, d, a, vb, dhi, id_o, 1u);
           umma_ts_lead<7>(lead, d, a, vb, dhi, id_o, 1u);
         } else {
-          const uint32_t steps = f >> 8;  // of 16 keys
-          umma_ts_lead<1>(lead & (uint32_t)(steps > 1), d, a, vb, dhi, id_o, 1u);
-          umma_ts_lead<2>(lead & (uint32_t)(steps > 2), d, a, vb, dhi, id_o, 1u);
-          umma_ts_lead<3>(lead & (uint32_t)(steps > 3), d, a, vb, dhi, id_o, 1u);
-          umma_ts_lead<4>(lead & (uint32_t)(steps > 4), d, a, vb, dhi, id_o, 1u);
-          umma_ts_lead<5>(lead & (uint32_t)(steps > 5), d, a, vb, dhi, id_o, 1u);
-          umma_ts_lead<6>(lead & (uint32_t)(steps > 6), d, a, vb, dhi, id_o, 1u);
+#pragma unroll 1
+          for (uint32_t e = 0; e < 8; ++e) {
+            if (e == 4) {
+              if (!wait_warp(&sm.p_full[x][1], par, 85, aborted, lim)) return false;
+              tc_fence_after();
+            }
+            umma_ts_lead<0>(lead & (uint32_t)(e < f >> 8), d, a + 8 * e, vb + 128 * e, dhi, id_o, again | (uint32_t)(e > 0));
+          }
         }
-        if (f >> (4 + x) & 1u) {
+        if (!kIsPlain && (f >> (4 + x) & 1u)) {
           umma_commit_lead(lead, &sm.o_full[x]);
           o_any |= 1u << x;
         }
         return true;
       };
-      auto take_k = [&]() { return dwait_warp(&sm.k_full[ks], kph, st, 87, aborted, lim); };
+      auto take_k = [&]() { return wait_warp(&sm.k_full[ks], kph, 87, aborted, lim); };
       auto give_k = [&]() {
         umma_commit_lead(lead, &sm.k_empty[ks]);
         if (++ks == kKSlots) {
@@ -428,62 +504,76 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           kph ^= 1u;
         }
       };
-      // O += P V of a tile (f), S of the one after it (nf)
-      auto step = [&](uint32_t f, uint32_t nf, bool more) -> bool {
-        if (!dwait_warp(&sm.v_full[vs], vph, st, 88, aborted, lim)) return false;
-        if (!issue_pv(f, 0)) return false;
-        if (more && !(take_k() && issue_s(nf, 0))) return false;
-        if (!issue_pv(f, 1)) return false;
+      auto give_v = [&]() {
         umma_commit_lead(lead, &sm.v_empty[vs]);
         if (++vs == kVSlots) {
           vs = 0;
           vph ^= 1u;
         }
-        if (more) {
-          if (!issue_s(nf, 1)) return false;
-          give_k();
-        }
-        return true;
       };
+      auto take_v = [&]() { return wait_warp(&sm.v_full[vs], vph, 88, aborted, lim); };
+      constexpr std::true_type kPlain{};
+      constexpr std::false_type kAny{};
       const Item* it;
       if (next_item(it)) {
-        int j = it->j0, j1 = it->j1, plain_lo = it->plain_lo, plain_hi = it->plain_hi;
-        uint32_t f = todo(*it, j);
-        if (take_k() && issue_s(f, 0) && issue_s(f, 1)) give_k();
+        int j0 = it->j0, j = j0, j1 = it->j1, plain_lo = it->plain_lo, plain_hi = it->plain_hi;
+        uint32_t f = todo(*it, j, j0, j1);
+        if (take_k() && issue_s(kAny, f, 0) && issue_s(kAny, f, 1)) give_k();
+        // O += P V of a tile, S of the one after it. Between plain tiles there is nothing to
+        // look up, and elsewhere it is looked up behind the first product: with a look at
+        // the item in front of it this warp alone took 3.5K cycles a tile, its products 2K.
         while (!aborted) {
-          // between plain tiles there is nothing to look up (with a look at the item per
-          // tile this warp alone took 3.5K cycles a tile, its products 2K)
           if (j >= plain_lo)
-            while (j < plain_hi && step(kPlain, kPlain, true)) ++j;
-          if (aborted) break;
-          f = todo(*it, j);
+            while (j < plain_hi) {
+              if (!take_v() || !issue_pv(kPlain, 0, 0) || !take_k() || !issue_s(kPlain, 0, 0) || !issue_pv(kPlain, 0, 1)) break;
+              give_v();
+              if (!issue_s(kPlain, 0, 1)) break;
+              give_k();
+              f = 0x803;
+              ++j;
+            }
+          if (aborted || !take_v() || !issue_pv(kAny, f, 0)) break;
           const uint32_t slot = (n_item - 1) % kItemSlots;  // (the present item's)
           const bool same = ++j < j1;
           bool more = true;
           if (!same) {
             more = next_item(it);
+            warp_arrive(&sm.item_empty[slot], lane);
             if (more) {
-              j = it->j0;
+              j = j0 = it->j0;
               j1 = it->j1;
               plain_lo = it->plain_lo;
               plain_hi = it->plain_hi;
             }
           }
-          const uint32_t nf = more ? todo(*it, j) : 0u;
-          if (!same) warp_arrive(&sm.item_empty[slot], lane);
-          if (aborted || !step(f, nf, more) || !more) break;
+          const uint32_t nf = more ? todo(*it, j, j0, j1) : 0u;
+          if (more && !(take_k() && issue_s(kAny, nf, 0))) break;
+          if (aborted || !issue_pv(kAny, f, 1)) break;
+          give_v();
+          if (!more || !issue_s(kAny, nf, 1)) break;
+          give_k();
+          f = nf;
         }
       }
     } else if (warp == 10) {
       // ------------------------------------------------------------- items
       for (uint32_t n = 0; !aborted; ++n) {
         const uint32_t slot = n % kItemSlots;
-        if (n >= kItemSlots && !dwait_warp(&sm.item_empty[slot], (n / kItemSlots - 1) & 1, st, 78, aborted, lim)) break;
-        const int64_t index = blockIdx.x + (int64_t)n * gridDim.x;
+        if (n >= kItemSlots && !wait_warp(&sm.item_empty[slot], (n / kItemSlots - 1) & 1, 78, aborted, lim)) break;
+        // the first is its own, the others as they come
+        uint32_t taken = 0;
+        if (n > 0 && lane == 0) taken = c.taken ? atomicAdd(c.taken, 1u) : n - 1;
+        taken = __shfl_sync(0xffffffffu, taken, 0);
+        const int64_t index = n == 0 ? blockIdx.x : (int64_t)gridDim.x + (c.taken ? (int64_t)taken : (int64_t)items);
         Item it;
         it.j0 = -1;
         if (index < items) item_at(c, sm, (int)index, it);
         if (lane == 0) sm.item[slot] = it;
+        __syncwarp();
+        if (lane < kLooked)
+          sm.item[slot].head[lane] = (uint16_t)it.todo(it.j0 + lane);
+        else if (lane < 2 * kLooked)
+          sm.item[slot].tail[lane - kLooked] = (uint16_t)it.todo(it.j1 - 1 - (lane - kLooked));
         warp_arrive(&sm.item_full[slot], lane);
         if (index >= items) break;
       }
@@ -515,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
     const uint64_t sl2_2 = f2_pack(p.scale_log2, p.scale_log2);
     uint32_t n_s = 0, n_o = 0;
     for (uint32_t n = 0; !aborted; ++n) {
-      if (!dwait_warp(&sm.item_full[n % kItemSlots], (n / kItemSlots) & 1, st, 94, aborted, lim)) break;
+      if (!wait_warp(&sm.item_full[n % kItemSlots], (n / kItemSlots) & 1, 94, aborted, lim)) break;
       const Item& it = sm.item[n % kItemSlots];
       if (it.j0 < 0) break;
       const int t = it.t0 + x * c.tokens + token;
@@ -524,15 +614,123 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       const int pfirst = it.position + x * c.tokens;
       const int plast = it.position + min((x + 1) * c.tokens, it.n_query - it.t0) - 1;
       float m_ref = kNone, l = 0.f;
+      int shift = 0;       // the reference is to move by, before the next tile
+      bool alone = false;  // the row left what fp32 holds
       const int first = it.first[x], last = it.last[x], in_a = it.in_a[x], in_b = it.in_b[x], in_first = it.in_first;
       const int firsts = it.firsts, narrow = it.rest > 0 ? it.whole : -1, rest = it.rest;
       const int n_a = it.n_a, a0 = it.end_a - kKeys * (n_a + firsts), b0 = it.end_b - kKeys * it.n;
       const int low_a = it.low_a, low_b = it.low_b;
       const bool in_order = it.in_order;
       const bool any = first <= last;
-      // a tile of which 32 NC columns are looked at
-      auto tile = [&](auto nc, int j) -> bool {
-        constexpr int NC = decltype(nc)::value;
+      constexpr float kFar = 1.2676506e30f;  // 2^100
+      // S is complete, and with it every product of O before it
+      auto begin = [&]() -> bool {
+        if (!wait_warp(&sm.s_full[x], n_s & 1, 90, aborted, lim)) return false;
+        ++n_s;
+        tc_fence_after();
+        if (__any_sync(0xffffffffu, shift != 0)) {
+          const float alpha = __uint_as_float((uint32_t)(127 - shift) << 23);
+#pragma unroll 1
+          for (int cb = 0; cb < 8; ++cb) {
+            uint32_t o[16];
+            tmem_ld16(tmem + lane_off + o_col + cb * 16, o);
+            tmem_wait_ld16(o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            tmem_st16(tmem + lane_off + o_col + cb * 16, o);
+          }
+          l *= alpha;
+          m_ref += (float)shift;
+          shift = 0;
+        }
+        return true;
+      };
+      auto loaded = [&]() {
+        tc_fence_before();
+        warp_arrive(&sm.s_free[x], lane);
+      };
+      auto give = [&](int half) {
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(&sm.p_full[x][half], lane);
+      };
+      auto count = [&](float sum) {
+        l += sum;
+        alone |= sum > kFar;
+        if (sum > 32768.f) shift = (int)(__float_as_uint(sum) >> 23) - 127;
+      };
+      // 2^(s - m) of the first 64 columns as bf16 pairs; acc: sums
+      auto form = [&](const uint32_t (&sr)[4][32], uint32_t (&pk)[32], uint64_t (&acc)[2]) {
+        const float mb = m_ref == kNone ? 0.f : m_ref;
+        const uint64_t nm2 = f2_pack(-mb, -mb);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          float e0f, e1f;
+          f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[i >> 4][2 * (i & 15)]), __uint_as_float(sr[i >> 4][2 * (i & 15) + 1])),
+                           sl2_2, nm2),
+                    e0f, e1f);
+          const float a = ex2_approx(e0f), bb = ex2_approx(e1f);
+          acc[i & 1] = f2_add(acc[i & 1], f2_pack(a, bb));
+          pk[i] = pack_bf16(a, bb);
+        }
+      };
+      auto total = [&](const uint64_t (&acc)[2]) {
+        float x0, x1;
+        f2_unpack(f2_add(acc[0], acc[1]), x0, x1);
+        return x0 + x1;
+      };
+      // A tile. `simple`: every row sees it whole, behind its first: nothing but
+      // exponentials between S and P. One copy of the code, its halves in a rolled loop over
+      // registers: with copies for each kind of tile and half the warps waited for
+      // instructions (16 ragged prompts 233 -> 210 us).
+      auto tile = [&](bool simple, bool fresh, int s1, int w0, int w1, int e0, int e1) -> bool {
+        if (!begin()) return false;
+        uint32_t sr[4][32];
+#pragma unroll
+        for (int cc = 0; cc < 4; ++cc) tmem_ld32(tmem + lane_off + 32 * cc, sr[cc]);
+        tmem_wait_ld();
+#pragma unroll
+        for (int cc = 0; cc < 4; ++cc) tie32(sr[cc]);
+        loaded();
+        if (!simple) {
+#pragma unroll
+          for (int cc = 0; cc < 4; ++cc) {
+            const uint32_t see = bits(-32 * cc, s1 - 32 * cc) | bits(w0 - 32 * cc, w1 - 32 * cc) |
+                                 bits(e0 - 32 * cc, e1 - 32 * cc);
+            if (__any_sync(0xffffffffu, see != 0xffffffffu)) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!(see & (1u << e))) sr[cc][e] = __float_as_uint(kNone);
+            }
+          }
+          if (fresh) {
+            // a row's first tile: its maximum is the reference
+            float top[2] = {kNone, kNone};
+#pragma unroll
+            for (int e = 0; e < 128; e += 2)
+              top[(e >> 1) & 1] = fmax3(top[(e >> 1) & 1], __uint_as_float(sr[e >> 5][e & 31]),
+                                        __uint_as_float(sr[e >> 5][(e & 31) + 1]));
+            if (m_ref == kNone) m_ref = fmaxf(top[0], top[1]) * p.scale_log2;
+          }
+        }
+        uint64_t acc[2] = {0ull, 0ull};
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          uint32_t pk[32];
+          form(sr, pk, acc);
+          tmem_st32(tmem + lane_off + p_col + 32 * half, pk);
+          give(half);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            sr[0][e] = sr[2][e];
+            sr[1][e] = sr[3][e];
+          }
+        }
+        count(total(acc));
+        return true;
+      };
+      for (int j = first; j <= last; ++j) {
+        if (j >= in_first && (j < in_a || j > in_b)) continue;
         // which of the tile's rows this row sees
         int s1 = -1, w0 = 0, w1 = -1, e0 = 0, e1 = -1;
         bool whole;
@@ -550,107 +748,24 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           }
           whole = start >= max(plast - p.window + 1, low) && start + kKeys - 1 <= pfirst;
         }
-        if (!dwait_warp(&sm.s_full[x], n_s & 1, st, 90, aborted, lim)) return false;
-        ++n_s;
-        tc_fence_after();
-        uint32_t sr[NC][32];
-#pragma unroll
-        for (int cc = 0; cc < NC; ++cc) tmem_ld32(tmem + lane_off + 32 * cc, sr[cc]);
-        tmem_wait_ld();
-        tc_fence_before();
-        warp_arrive(&sm.s_free[x], lane);
-        if (!whole) {
-#pragma unroll
-          for (int cc = 0; cc < NC; ++cc) {
-            const uint32_t see = bits(-32 * cc, s1 - 32 * cc) | bits(w0 - 32 * cc, w1 - 32 * cc) |
-                                 bits(e0 - 32 * cc, e1 - 32 * cc);
-            if (__any_sync(0xffffffffu, see != 0xffffffffu)) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!(see >> e & 1u)) sr[cc][e] = __float_as_uint(kNone);
-            }
-          }
-        }
-        float mx[4] = {kNone, kNone, kNone, kNone};
-#pragma unroll
-        for (int c2 = 0; c2 < 16 * NC; ++c2)
-          mx[c2 & 3] = fmax3(mx[c2 & 3], __uint_as_float(sr[(2 * c2) >> 5][(2 * c2) & 31]),
-                             __uint_as_float(sr[(2 * c2 + 1) >> 5][(2 * c2 + 1) & 31]));
-        const float tmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
-        const bool grow = tmax > m_ref + 8.f;
-        if (__any_sync(0xffffffffu, grow)) {
-          const float m_new = grow ? tmax : m_ref;
-          const bool need_o = grow && m_ref != kNone;
-          if (__any_sync(0xffffffffu, need_o)) {
-            // O is final: its last product was issued before this S
-            const float alpha = need_o ? ex2_approx(m_ref - m_new) : 1.f;
-#pragma unroll 1
-            for (int cb = 0; cb < 8; ++cb) {
-              uint32_t o[16];
-              tmem_ld16(tmem + lane_off + o_col + cb * 16, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-              tmem_st16(tmem + lane_off + o_col + cb * 16, o);
-            }
-            l *= alpha;
-          }
-          m_ref = m_new;
-        }
-        const float mb = m_ref == kNone ? 0.f : m_ref;
-        const uint64_t nm2 = f2_pack(-mb, -mb);
-        uint64_t acc[2] = {0ull, 0ull};
-#pragma unroll
-        for (int half = 0; half < (NC + 1) / 2; ++half) {
-          constexpr int kPairs = NC >= 2 ? 32 : 16;
-          uint32_t pk[kPairs];
-#pragma unroll
-          for (int i = 0; i < kPairs; ++i) {
-            const int c2 = 32 * half + i;
-            float e0f, e1f;
-            f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[(2 * c2) >> 5][(2 * c2) & 31]),
-                                     __uint_as_float(sr[(2 * c2 + 1) >> 5][(2 * c2 + 1) & 31])),
-                             sl2_2, nm2),
-                      e0f, e1f);
-            const float a = ex2_approx(e0f), bb = ex2_approx(e1f);
-            acc[i & 1] = f2_add(acc[i & 1], f2_pack(a, bb));
-            pk[i] = pack_bf16(a, bb);
-          }
-          if constexpr (NC >= 2)
-            tmem_st32(tmem + lane_off + p_col + 32 * half, pk);
-          else
-            tmem_st16(tmem + lane_off + p_col, pk);
-        }
-        tmem_wait_st();
-        tc_fence_before();
-        warp_arrive(&sm.p_full[x], lane);
-        float sum[4];
-        f2_unpack(acc[0], sum[0], sum[1]);
-        f2_unpack(acc[1], sum[2], sum[3]);
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        return true;
-      };
-      for (int j = first; j <= last; ++j) {
-        if (j >= in_first && (j < in_a || j > in_b)) continue;
-        if (!(j == narrow && rest <= 32 ? tile(std::integral_constant<int, 1>{}, j) : tile(std::integral_constant<int, 4>{}, j)))
-          break;
+        const bool fresh = __any_sync(0xffffffffu, m_ref == kNone);
+        if (!tile(whole && !fresh, fresh, whole ? kKeys - 1 : s1, w0, w1, e0, e1)) break;
       }
-      if (any && (aborted || !dwait_warp(&sm.o_full[x], n_o & 1, st, 91, aborted, lim))) break;
+      if (any && (aborted || !wait_warp(&sm.o_full[x], n_o & 1, 91, aborted, lim))) break;
       if (any) ++n_o;
       tc_fence_after();
       // ---------------------------------------------------------- outputs
       const int h = it.kvh * p.group + head;
       const float inv = l == 0.f ? 0.f : 1.f / l;
       __nv_bfloat16* const to = p.out.at(it.b, h, t);
-      float* const part = p.part + (((int64_t)(it.b * p.n_kv_heads + it.kvh) * p.splits + it.split) * p.group * p.n_tok +
-                                    (int64_t)t * p.group + head) * (kHeadDim + 4);
+      float* const part = part_of(p, it, t * p.group + head);
       uint64_t odd = 0ull;  // sums of 0 times the outputs: NaN where one is not finite
 #pragma unroll 1
       for (int cb = 0; cb < 4; ++cb) {
         uint32_t o[32];
         if (any) {
           tmem_ld32(tmem + lane_off + o_col + cb * 32, o);
-          tmem_wait_ld();
+          tmem_wait_ld32(o);
         } else {
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0u;
@@ -673,25 +788,29 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       }
       float f0, f1;
       f2_unpack(odd, f0, f1);
-      if (row_ok && p.splits == 1) {
-        if (p.lse != nullptr)
-          p.lse[((int64_t)it.b * p.n_q_heads + h) * p.n_tok + t] = l == 0.f ? kNone : (m_ref + log2f(l)) * kLn2;
-      } else if (row_ok) {
-        *reinterpret_cast<float2*>(part + kHeadDim) = make_float2(m_ref, l);
+      if (row_ok && p.splits > 1) {  // (of a row to be taken alone: what the join sees that by)
+        if (alone) part[0] = INFINITY;
+        *reinterpret_cast<float2*>(part + kHeadDim) = alone ? make_float2(3e38f, INFINITY) : make_float2(m_ref, l);
+      } else if (row_ok && p.lse != nullptr) {
+        p.lse[((int64_t)it.b * p.n_q_heads + h) * p.n_tok + t] = l == 0.f ? kNone : (m_ref + log2f(l)) * kLn2;
       }
       // rows whose outputs are not finite by no fault of l: from the definition
-      uint32_t again = __ballot_sync(0xffffffffu, row_ok && p.splits == 1 && f0 + f1 != 0.f && finite(l));
+      uint32_t again = __ballot_sync(0xffffffffu, row_ok && p.splits == 1 && (alone || (f0 + f1 != 0.f && finite(l))));
       for (; again; again &= again - 1) {
         const int from = __ffs(again) - 1;
         const int ah = __shfl_sync(0xffffffffu, h, from), at = __shfl_sync(0xffffffffu, t, from);
-        const float4 y = window_row_alone(p, it.b, ah, at);
-        *reinterpret_cast<uint2*>(p.out.at(it.b, ah, at) + 4 * lane) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+        const WindowRow y = window_row_alone(p, it.b, ah, at);
+        *reinterpret_cast<uint2*>(p.out.at(it.b, ah, at) + 4 * lane) =
+            make_uint2(pack_bf16(y.o.x, y.o.y), pack_bf16(y.o.z, y.o.w));
+        if (__shfl_sync(0xffffffffu, alone, from) && lane == 0 && p.lse != nullptr)
+          p.lse[((int64_t)it.b * p.n_q_heads + ah) * p.n_tok + at] = y.lse;
       }
       warp_arrive(&sm.item_empty[n % kItemSlots], lane);
     }
     tmem_wait_st();
     tc_fence_before();
   }
+  if (aborted && (lane == 0 || warp == 8)) set_status(&sm.status, UC_ERR_TIMEOUT, aborted);
   __syncthreads();
   if (sm.status.code != 0) {
     // Where a wait ran out, others may have left with copies and products in
@@ -723,9 +842,9 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
 void launch_window_prompt(const WindowPromptParams& c, int grid, cudaStream_t st) {
   static std::once_flag once;
   std::call_once(once, [] {
-    cudaFuncSetAttribute(window_prompt_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PromptSmem) + 1024);
+    cudaFuncSetAttribute(window_prompt_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PromptSmem));
   });
-  window_prompt_kernel<<<grid, kThreads, sizeof(PromptSmem) + 1024, st>>>(c);
+  window_prompt_kernel<<<grid, kThreads, sizeof(PromptSmem), st>>>(c);
   count_launch();
   if (c.p.splits > 1) launch_window_join(c.p, st);
 }

@@ -220,3 +220,31 @@ def test_append_in_place_and_without_rotation():
     total2 = torch.zeros_like(total)
     got = uc.window_append(cache, kn, vn, ints([3, 50]), rotary=table, q=q, out_q=q, total=total2)
     assert got[0] is total2 and got[1] is q and torch.equal(total, total2) and torch.equal(q, oq)
+
+
+@pytest.mark.parametrize("hq,hkv,T,held", [(4, 4, 300, 0), (14, 2, 200, 700), (2, 2, 40, 3000)])
+@pytest.mark.parametrize("size", [30.0, 1000.0, 1e8])
+def test_logits_that_jump(hq, hkv, T, held, size):
+    """Logits that rise by any amount from tile to tile, within tiles and at their ends."""
+    g = torch.Generator(device=DEV).manual_seed(8)
+    n = held + T
+    k, v = make_cache(g, 1, hkv, n, [n], 3)
+    q = rows(g, 1, hq, T, "bhtd")
+    rise = torch.ones(n, device=DEV)
+    for at in (70, 127, 128, 200, 255, 300, 650, 2100, 2999):
+        rise[at:at + 1] *= size ** ((at % 7 + 1) / 7)
+    k = (k.float() * rise[:, None]).bfloat16()
+    for window in (1 << 30, 150):
+        ws = uc.Workspace(DEV)
+        out, lse = uc.window_attend(q, uc.WindowCache(k, v, window, 3), ints([n]), ws=ws)
+        o, l, spread, reach = owin.attend(q.float().cpu().numpy(), k.float().cpu().numpy(), v.float().cpu().numpy(), [n], [T],
+                                          window, 3)
+        assert ws.status() == _lib.UC_OK
+        # as check(); where the logits' own rounding, 2^-19 of sum |q k|, is no small share of 1 the weights say
+        # nothing: those rows' outputs are only within what they are made of
+        d = 2.0 ** -19 * reach + 2.0 ** -20
+        err = np.where(d[..., None] < 0.1, (2.5 * d[..., None] + 2.0 ** -8) * spread, 2 * np.abs(v.float().cpu().numpy()).max())
+        got = out.double().cpu().numpy()
+        assert np.isfinite(got).all()
+        assert (np.abs(got - o) <= err + 2.0 ** -8 * (np.abs(o) + err)).all()
+        assert (np.abs(lse.double().cpu().numpy() - l) <= d + 2.0 ** -19 + 2.0 ** -22 * np.abs(l)).all()
