@@ -419,7 +419,9 @@ struct WindowParams {
   int batch, n_q_heads, n_kv_heads, group, n_tok;
   int n_rows, window, n_sink;
   float scale_log2;        // log2(e) / sqrt(128)
-  int row_blocks, cluster, splits;
+  int row_blocks, cluster, splits, row_warps, key_warps;
+  uint64_t wait_ns;        // limit of the bounded waits
+  int withhold;            // test hook: the load of a CTA (prompts: K and V in turn; steps: a tile's of a key warp) that is never made
 };
 constexpr int kWindowRows = 64;  // query rows (tokens x heads of a KV head) that a step's CTA takes at most
 void launch_window_step(const WindowParams& p, cudaStream_t st);
@@ -434,8 +436,6 @@ struct WindowPromptParams {
   int tokens;
   uint32_t* taken;       // items taken beyond the CTAs' first ones (0 before the launch), or null: there are none
   bool wide_out;         // rows of out start on 32 bytes
-  uint64_t wait_ns;
-  int withhold;          // test hook: the load of a CTA (K and V in turn) that is never made (-1: none)
 };
 void launch_window_prompt(const WindowPromptParams& c, int grid, cudaStream_t st);
 

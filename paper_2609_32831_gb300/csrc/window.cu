@@ -1,19 +1,20 @@
 // Attention with a sliding window and first tokens over a cache whose rows may
 // be a ring, for few queries: single tokens, drafts, short pieces of a prompt.
 //
-// Keys and values in reach are read once, by mma.sync warps that hold them in
-// registers alone: K rows are B operands of S = Q K^T as they lie in memory
-// (16 bytes of a row per lane, the channels of the k steps taken in that order on
-// both sides), and S's accumulators are P's A operand of O += P V after the softmax.
-// The V operand wants two keys' elements side by side: rows of two keys per lane,
-// interleaved by byte permutation, output channels in the order in which they
-// come. P enters as two bf16 parts, so outputs carry their own rounding and no
+// Keys and values in reach are read once, 32 keys at a time, by bulk copies into shared
+// memory some tiles ahead (rows loaded to registers cost a tile its latency, 2.4K
+// cycles; cp.async 1.1K to issue). mma.sync, eight query rows a warp, both products with the keys or channels
+// as the 16 rows, so that few query rows waste little: S^T = K Q^T, the channels of the
+// k steps in the order of 16-byte pieces on both sides; O^T += V^T P^T with two keys'
+// elements brought side by side by byte permutation, the channels in the order in
+// which they come, and P^T from S^T's accumulators by a transposition of 8 x 8
+// registers. P enters as two bf16 parts, so outputs carry their own rounding and no
 // other; sums and the online softmax are fp32.
 //
-// A CTA of four warps takes up to 64 query rows (tokens x heads of a KV head, 16
-// a warp) and a range of keys; the ranges of a row block go to the CTAs of a
-// cluster, which joins them through distributed shared memory, and where that is
-// not enough to several clusters, joined by a second kernel.
+// A CTA takes up to 64 query rows (tokens x heads of a KV head, 8 a warp) and a
+// share of the keys, tile by tile over its warps; the shares of a row block go to the
+// CTAs of a cluster, which joins them through distributed shared memory, and
+// where that is not enough to several clusters, joined by a second kernel.
 #include <climits>
 #include <cmath>
 #include <cstring>
@@ -28,13 +29,28 @@ namespace uc {
 
 namespace {
 
-constexpr int kStepWarps = 4;
-constexpr int kTileKeys = 16;
+constexpr int kTileKeys = 32;
 
-struct StepSmem {
-  float o[kStepWarps][16][kHeadDim + 4];  // (rows 16 bytes apart in banks)
-  float m[kStepWarps][16], l[kStepWarps][16];
+constexpr int kWarpRows = 8;
+constexpr int kStages = 2;
+constexpr int kMostWarps = 12;
+constexpr int kMostCluster = 8;
+
+struct StepPart {  // of a warp
+  float o[kWarpRows][kHeadDim + 4];  // (rows 16 bytes apart in banks)
+  float m[kWarpRows], l[kWarpRows];
 };
+// Tiles of the warps that share keys: 16-byte pieces of K and V rows. (Rows lie 256 bytes
+// apart, so that K's reads take two turns and V's four: 190 of a tile's 1000 cycles.)
+struct StepRing {
+  uint4 k[kStages][kTileKeys][16], v[kStages][kTileKeys][16];
+};
+// Shared memory of a CTA: barriers; rings, and in their place the parts once the keys are through.
+constexpr int kStepHeader = 8 * kStages * 8;
+__host__ __device__ constexpr size_t step_smem(int row_warps, int key_warps) {
+  const size_t rings = key_warps * sizeof(StepRing), parts = row_warps * key_warps * sizeof(StepPart);
+  return kStepHeader + (rings > parts ? rings : parts);
+}
 
 __device__ __forceinline__ uint32_t rank_addr(const void* local, int rank) {
   uint32_t a;
@@ -43,73 +59,82 @@ __device__ __forceinline__ uint32_t rank_addr(const void* local, int rank) {
 }
 __device__ __forceinline__ float ld_rank(uint32_t a) {
   float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a));
   return v;
 }
 __device__ __forceinline__ float4 ld_rank4(uint32_t a) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
                : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-               : "r"(a)
-               : "memory");
+               : "r"(a));
   return v;
+}
+__device__ __forceinline__ int cluster_register_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return (int)r;
+}
+__device__ __forceinline__ int cluster_register_id() {
+  uint32_t r;
+  asm("mov.u32 %0, %%clusterid.x;" : "=r"(r));
+  return (int)r;
 }
 __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// RG: warps side by side over a block's rows (16 each); the others take keys.
-template <int RG>
-__global__ void __launch_bounds__(32 * kStepWarps) window_step_kernel(const __grid_constant__ WindowParams p) {
-  constexpr int kKeyWarps = kStepWarps / RG;
+// p.row_warps side by side over a block's rows (8 each) times p.key_warps over its keys.
+__global__ void __launch_bounds__(32 * kMostWarps, 1) window_step_kernel(const __grid_constant__ WindowParams p) {
   extern __shared__ __align__(16) uint8_t dyn[];
-  StepSmem& sm = *reinterpret_cast<StepSmem*>(dyn);
+  uint64_t* const bars = reinterpret_cast<uint64_t*>(dyn);  // [key warp][stage]: a tile has arrived
+  StepPart* const sm = reinterpret_cast<StepPart*>(dyn + kStepHeader);
+  StepRing* const rings = reinterpret_cast<StepRing*>(dyn + kStepHeader);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
-  const int rank = blockIdx.x % p.cluster;
-  int at = blockIdx.x / p.cluster;
-  const int split = at % p.splits;
-  at /= p.splits;
-  const int block = at % p.row_blocks;
-  at /= p.row_blocks;
-  const int kvh = at % p.n_kv_heads, b = at / p.n_kv_heads;
-  const int rg = warp % RG, kw = warp / RG;
+  // (runtime divisions take 100 cycles each: none where a register or a comparison does)
+  const int rank = cluster_register_rank();
+  int block = cluster_register_id(), split = 0;
+  if (p.splits > 1) {
+    split = block % p.splits;
+    block /= p.splits;
+  }
+  const int kvh = blockIdx.y, b = blockIdx.z;
+  const int kw = p.row_warps == 1 ? warp : warp / p.row_warps, rg = warp - kw * p.row_warps;
   const int rows = p.group * p.n_tok, row0 = block * kWindowRows;
+  // token and head of the block's r-th row
+  const int t_first = row0 == 0 ? 0 : row0 / p.group, h_first = row0 - t_first * p.group;
+  const float per_group = 1.f / (float)p.group;
+  auto token_of = [&](int r) { return (int)(((float)(h_first + r) + 0.5f) * per_group); };  // (exact: below 2^17)
   const WindowSeq s = window_seq(p, b);
   if (threadIdx.x == 0) window_check(p, b);
   // positions of the block's rows that are queries
-  const int ta = row0 / p.group, tb = min(min(row0 + kWindowRows, rows) - 1, p.group * s.nq - 1) / p.group;
+  const int last = min(min(row0 + kWindowRows, rows), p.group * s.nq) - 1 - row0;
   WindowKeys keys = {0, 0, 0};
-  if (p.group * s.nq > row0) keys = window_keys(p, s, s.first + ta, s.first + tb);
+  if (last >= 0) keys = window_keys(p, s, s.first + t_first, s.first + t_first + token_of(last));
   const int n = keys.count();
   const int base = window_row(p, keys.lo);
-  // this warp's 16 rows: r0 + g and r0 + g + 8
-  const int r0 = row0 + 16 * rg;
-  const int rr[2] = {r0 + g, r0 + g + 8};
-  int pos[2];
-  uint32_t q[8][4];  // A operands of the 8 k steps
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int t = rr[i] / p.group, h = kvh * p.group + rr[i] % p.group;
-    const bool is = rr[i] < rows && t < s.nq;
-    pos[i] = is ? s.first + t : INT_MIN;  // (sees nothing)
+  // this warp's rows of the block: as a B operand row g; of S^T's and O^T's accumulators rows 2 j and 2 j + 1
+  const int r0 = kWarpRows * rg;
+  const bool active = r0 <= last;
+  uint4 q[4];
+  {
+    const int dt = token_of(r0 + g), h = kvh * p.group + h_first + r0 + g - dt * p.group;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      uint4 w = make_uint4(0u, 0u, 0u, 0u);
-      if (is) w = *reinterpret_cast<const uint4*>(p.q.at(b, h, t) + 32 * c + 8 * j);
-      q[2 * c][i] = w.x;
-      q[2 * c][2 + i] = w.y;
-      q[2 * c + 1][i] = w.z;
-      q[2 * c + 1][2 + i] = w.w;
+      q[c] = make_uint4(0u, 0u, 0u, 0u);
+      if (r0 + g <= last) q[c] = *reinterpret_cast<const uint4*>(p.q.at(b, h, t_first + dt) + 32 * c + 8 * j);
     }
   }
-  // (of the warp's queries: a tile of keys up to the first of them and inside the last's window needs no mask)
-  const int pfirst = s.first + r0 / p.group, plast = s.first + min(r0 + 15, rows - 1) / p.group;
-  const bool active = r0 < rows && r0 / p.group < s.nq;
-
-  float o[16][4];
+  int pos[2];
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
+  for (int i = 0; i < 2; ++i)
+    pos[i] = r0 + 2 * j + i <= last ? s.first + t_first + token_of(r0 + 2 * j + i) : INT_MIN;  // (sees nothing)
+  // (of the warp's queries: a tile of keys up to the first of them and inside the last's window needs no mask)
+  const int pfirst = s.first + t_first + token_of(r0), plast = s.first + t_first + token_of(min(r0 + kWarpRows - 1, last));
+
+  float o[8][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
@@ -122,68 +147,105 @@ __global__ void __launch_bounds__(32 * kStepWarps) window_step_kernel(const __gr
     if (i >= keys.sinks && r >= p.n_rows) r -= p.n_rows - p.n_sink;
     return r;
   };
-  uint4 kr[2][4];
-  auto load_k = [&](int i0) {
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int i = i0 + g + 8 * x;
-      const uint4* const src = reinterpret_cast<const uint4*>(kb + (int64_t)row_of(min(i, n - 1)) * p.k.st) + j;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) kr[x][c] = src[4 * c];
-    }
-  };
-  uint4 vr[4][2];
-  auto load_v = [&](int i0) {
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int i = i0 + 2 * j + (x & 1) + 8 * (x >> 1);
-      const uint4* const src = reinterpret_cast<const uint4*>(vb + (int64_t)row_of(min(i, n - 1)) * p.v.st) + g;
-      vr[x][0] = src[0];
-      vr[x][1] = src[8];
-    }
-  };
-  // tiles of 16 keys in turn over the splits, the cluster's CTAs and the key warps
-  const int stride = kTileKeys * kKeyWarps * p.cluster * p.splits;
-  int i0 = kTileKeys * ((split * p.cluster + rank) * kKeyWarps + kw);
-  if (!active) i0 = n;
-  if (i0 < n) {
-    load_k(i0);
-    load_v(i0);
+  // tiles of keys in turn over the splits, the cluster's CTAs and the key warps; the
+  // rows of a tile in turn over the warps that share it
+  const int stride = kTileKeys * p.key_warps * p.cluster * p.splits;
+  int i0 = kTileKeys * ((split * p.cluster + rank) * p.key_warps + kw);
+  StepRing& ring = rings[kw];
+  uint64_t* const full = bars + kw * kStages;
+  if (rg == 0) {
+    if (lane < kStages) mbar_init(&full[lane], 1);
+    // (rows of V that no copy fills are multiplied by 0)
+    for (int x = lane; x < kStages * kTileKeys * 16; x += 32) (&ring.v[0][0][0])[x] = make_uint4(0u, 0u, 0u, 0u);
+    fence_barrier_init();
+    fence_proxy_async_smem();
   }
-  for (; i0 < n; i0 += stride) {
-    float x[2][4];
-#pragma unroll
-    for (int y = 0; y < 2; ++y)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[y][e] = 0.f;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      mma_bf16(x[0], q[2 * c], kr[0][c].x, kr[0][c].y);
-      mma_bf16(x[1], q[2 * c], kr[1][c].x, kr[1][c].y);
-      mma_bf16(x[0], q[2 * c + 1], kr[0][c].z, kr[0][c].w);
-      mma_bf16(x[1], q[2 * c + 1], kr[1][c].z, kr[1][c].w);
+  __syncthreads();
+  // The copies of a tile: of rows that lie one behind another in the cache, as far as they do.
+  const bool dense = p.k.st == kHeadDim && p.v.st == kHeadDim;
+  int loads = 0;
+  auto copy = [&](int first, int slot) {
+    if (first >= n || loads++ == p.withhold) return;
+    const int end = min(first + kTileKeys, n);
+    mbar_arrive_expect_tx(&full[slot], 2 * (end - first) * kHeadDim * 2);
+    for (int i = first; i < end;) {
+      const int row = row_of(i);
+      const int len = dense ? min(end, i < keys.sinks ? keys.sinks : i + p.n_rows - row) - i : 1;
+      bulk_load(&ring.k[slot][i - first][0], kb + (int64_t)row * p.k.st, len * kHeadDim * 2, &full[slot]);
+      bulk_load(&ring.v[slot][i - first][0], vb + (int64_t)row * p.v.st, len * kHeadDim * 2, &full[slot]);
+      i += len;
     }
-    if (i0 + stride < n) load_k(i0 + stride);
+  };
+  if (rg == 0 && lane == 0)
+    for (int x = 0; x < kStages; ++x) copy(i0 + x * stride, x);
+  // every warp that shares a tile is through with it: its place is free for another
+  auto done = [&]() {
+    if (p.row_warps == 1)
+      __syncwarp();
+    else
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + kw), "r"(32 * p.row_warps) : "memory");
+  };
+  uint32_t parity = 0;
+  bool aborted = false;  // a wait ran out: nothing more is copied or computed
+  int slot = 0, seen = 0;
+  auto next = [&]() {
+    done();
+    if (rg == 0 && lane == 0 && !aborted) copy(i0 + kStages * stride, slot);
+    if (++slot == kStages) {
+      slot = 0;
+      parity ^= 1u;
+    }
+    i0 += stride;
+  };
+  for (; i0 < n; next()) {
+    if (!aborted && !mbar_wait(&full[slot], parity, p.status, 100, p.wait_ns)) aborted = true;
+    aborted = __any_sync(0xffffffffu, aborted);
+    if (aborted) continue;
+    ++seen;
+    if (!active) continue;
+    // x[u]: keys 16 u + g (0, 1) and 16 u + g + 8 (2, 3), rows 2 j (0, 2) and 2 j + 1 (1, 3)
+    constexpr int kU = kTileKeys / 16;
+    float x[kU][4];
     const int ka = keys.position(i0), kz = keys.position(i0 + kTileKeys - 1);
     const bool whole = i0 + kTileKeys <= n && kz <= pfirst && (plast - ka < p.window || kz < p.n_sink);
-    // x[y][e]: row rr[e / 2], key i0 + 8 y + 2 j + e % 2
-    float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
+    for (int u = 0; u < kU; ++u) {
+      float y[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[y][e] *= p.scale_log2;
-        if (!whole) {
-          const int i = i0 + 8 * y + 2 * j + (e & 1);
-          if (i >= n || !window_sees(p, pos[e >> 1], keys.position(i))) x[y][e] = -INFINITY;
-        }
-        top[e >> 1] = fmaxf(top[e >> 1], x[y][e]);
+      for (int e = 0; e < 4; ++e) x[u][e] = y[e] = 0.f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint4 k0 = ring.k[slot][16 * u + g][4 * c + j], k1 = ring.k[slot][16 * u + g + 8][4 * c + j];
+        const uint32_t a0[4] = {k0.x, k1.x, k0.y, k1.y}, a1[4] = {k0.z, k1.z, k0.w, k1.w};
+        mma_bf16(x[u], a0, q[c].x, q[c].y);
+        mma_bf16(y, a1, q[c].z, q[c].w);
       }
-    float old[2];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[u][e] = (x[u][e] + y[e]) * p.scale_log2;
+    }
+    if (!whole) {
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = i0 + 16 * u + g + 8 * (e >> 1);
+          if (i >= n || !window_sees(p, pos[e & 1], keys.position(i))) x[u][e] = -INFINITY;
+        }
+    }
+    float old[2], top[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-      top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+      top[i] = fmaxf(x[0][i], x[0][2 + i]);
+#pragma unroll
+      for (int u = 1; u < kU; ++u) top[i] = fmaxf(top[i], fmaxf(x[u][i], x[u][2 + i]));
+    }
+#pragma unroll
+    for (int d = 4; d <= 16; d <<= 1) {
+      top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], d));
+      top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], d));
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
       old[i] = m[i];
       m[i] = fmaxf(m[i], top[i]);
     }
@@ -193,97 +255,122 @@ __global__ void __launch_bounds__(32 * kStepWarps) window_step_kernel(const __gr
         const float a = m[i] > old[i] ? ex2_approx(old[i] - m[i]) : 1.f;
         l[i] *= a;
 #pragma unroll
-        for (int y = 0; y < 16; ++y) {
-          o[y][2 * i] *= a;
-          o[y][2 * i + 1] *= a;
+        for (int z = 0; z < 8; ++z) {
+          o[z][i] *= a;
+          o[z][2 + i] *= a;
         }
       }
     }
-    uint32_t hi[4], lo[4];
+    const float mb[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+    uint32_t hi[kU][2], lo[kU][2];
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
+    for (int u = 0; u < kU; ++u)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float mb = m[i] == -INFINITY ? 0.f : m[i];
-        const float a = ex2_approx(x[y][2 * i] - mb), c = ex2_approx(x[y][2 * i + 1] - mb);
-        l[i] += a + c;
+      for (int k = 0; k < 2; ++k) {
+        const float a = ex2_approx(x[u][2 * k] - mb[0]), c = ex2_approx(x[u][2 * k + 1] - mb[1]);
+        l[0] += a;
+        l[1] += c;
         const uint32_t w = pack_bf16(a, c);
-        hi[2 * y + i] = w;
-        lo[2 * y + i] = pack_bf16(a - bf16_lo(w), c - bf16_hi(w));
+        hi[u][k] = movmatrix_t(w);
+        lo[u][k] = movmatrix_t(pack_bf16(a - bf16_lo(w), c - bf16_hi(w)));
       }
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const uint32_t* const v0 = &vr[0][half].x;
-      const uint32_t* const v1 = &vr[1][half].x;
-      const uint32_t* const v2 = &vr[2][half].x;
-      const uint32_t* const v3 = &vr[3][half].x;
+    for (int u = 0; u < kU; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t sel = e & 1 ? 0x7632u : 0x5410u;
-        const uint32_t b0 = __byte_perm(v0[e >> 1], v1[e >> 1], sel), b1 = __byte_perm(v2[e >> 1], v3[e >> 1], sel);
-        mma_bf16(o[8 * half + e], hi, b0, b1);
-        mma_bf16(o[8 * half + e], lo, b0, b1);
+      for (int half = 0; half < 2; ++half) {
+        uint4 w[4];  // keys 2 j, 2 j + 1, 2 j + 8, 2 j + 9
+#pragma unroll
+        for (int z = 0; z < 4; ++z) w[z] = ring.v[slot][16 * u + 2 * j + (z & 1) + 8 * (z >> 1)][g + 8 * half];
+        const uint32_t* const v0 = &w[0].x;
+        const uint32_t* const v1 = &w[1].x;
+        const uint32_t* const v2 = &w[2].x;
+        const uint32_t* const v3 = &w[3].x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t a[4] = {__byte_perm(v0[e], v1[e], 0x5410), __byte_perm(v0[e], v1[e], 0x7632),
+                                 __byte_perm(v2[e], v3[e], 0x5410), __byte_perm(v2[e], v3[e], 0x7632)};
+          mma_bf16(o[4 * half + e], a, hi[u][0], hi[u][1]);
+          mma_bf16(o[4 * half + e], a, lo[u][0], lo[u][1]);
+        }
       }
-    }
-    if (i0 + stride < n) load_v(i0 + stride);
   }
-  // this warp's part: o[8 half + e][2 i + c]: row g + 8 i, channel 64 half + 16 j + 8 c + e
+  // (the parts lie where the tiles did: all copies have arrived, or are waited for now)
+  if (aborted && rg == 0 && lane == 0)
+    for (int x = seen; x < loads; ++x)
+      if (x != p.withhold) mbar_wait(&full[x % kStages], (x / kStages) & 1, p.status, 101);
+  __syncthreads();
+  // this warp's part: o[4 half + e][2 c + i]: row 2 j + i, channel 64 half + 8 g + 2 e + c
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-    if (j == 0) {
-      sm.m[warp][g + 8 * i] = m[i];
-      sm.l[warp][g + 8 * i] = l[i];
+#pragma unroll
+    for (int d = 4; d <= 16; d <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+    if (g == 0) {
+      sm[warp].m[2 * j + i] = m[i];
+      sm[warp].l[2 * j + i] = l[i];
     }
 #pragma unroll
-    for (int y = 0; y < 16; y += 4)
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-        *reinterpret_cast<float4*>(&sm.o[warp][g + 8 * i][64 * (y >> 3) + 16 * j + 8 * c + (y & 7)]) =
-            make_float4(o[y][2 * i + c], o[y + 1][2 * i + c], o[y + 2][2 * i + c], o[y + 3][2 * i + c]);
+    for (int z = 0; z < 8; z += 2)
+      *reinterpret_cast<float4*>(&sm[warp].o[2 * j + i][64 * (z >> 2) + 8 * g + 2 * (z & 3)]) =
+          make_float4(o[z][i], o[z][2 + i], o[z + 1][i], o[z + 1][2 + i]);
+  }
+  // a warp per row: first the CTA's own parts, in place of the first one, then the cluster's
+  const int live = min(kWindowRows, rows - row0), warps = p.row_warps * p.key_warps;
+  if (p.key_warps > 1) {
+    __syncthreads();
+    for (int r = warp; r < live; r += warps) {
+      StepPart* const part = sm + r / kWarpRows;
+      const int ri = r % kWarpRows;
+      float top = -INFINITY;
+      for (int w = 0; w < p.key_warps; ++w) top = fmaxf(top, part[w * p.row_warps].m[ri]);
+      const float mb = top == -INFINITY ? 0.f : top;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+      float sum = 0.f;
+#pragma unroll 4
+      for (int w = 0; w < p.key_warps; ++w) {
+        const StepPart& from = part[w * p.row_warps];
+        const float a = ex2_approx(from.m[ri] - mb);
+        const float4 z = *reinterpret_cast<const float4*>(&from.o[ri][4 * lane]);
+        sum += a * from.l[ri];
+        y = make_float4(y.x + a * z.x, y.y + a * z.y, y.z + a * z.z, y.w + a * z.w);
+      }
+      *reinterpret_cast<float4*>(&part->o[ri][4 * lane]) = y;
+      __syncwarp();
+      if (lane == 0) {
+        part->m[ri] = top;
+        part->l[ri] = sum;
+      }
+    }
   }
   cluster_barrier();
-  // a warp per row: rows in turn over the cluster's warps
-  const int live = min(kWindowRows, rows - row0);
-  const int parts = p.cluster * kKeyWarps;  // part c * kKeyWarps + w: warp w * RG + (row / 16) of CTA c
-  for (int r = rank + p.cluster * warp; r < live; r += p.cluster * kStepWarps) {
-    const int rgr = r >> 4, ri = r & 15;
-    auto part_m = [&](int i) {
-      return ld_rank(rank_addr(&sm.m[(i % kKeyWarps) * RG + rgr][ri], i / kKeyWarps));
-    };
-    auto part_l = [&](int i) {
-      return ld_rank(rank_addr(&sm.l[(i % kKeyWarps) * RG + rgr][ri], i / kKeyWarps));
-    };
-    float pm[2], top = -INFINITY, sum = 0.f;
+  for (int r = rank + p.cluster * warp; r < live; r += p.cluster * warps) {
+    const int ri = r % kWarpRows;
+    const StepPart* const part = sm + r / kWarpRows;
+    float top = -INFINITY, sum = 0.f;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    // all loads before the first use
+    float pm[kMostCluster], pl[kMostCluster];
+    float4 z[kMostCluster];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int i = lane + 32 * x;
-      pm[x] = i < parts ? part_m(i) : -INFINITY;
-      top = fmaxf(top, pm[x]);
+    for (int c = 0; c < kMostCluster; ++c) {
+      pm[c] = -INFINITY;
+      pl[c] = 0.f;
+      z[c] = y;
+      if (c < p.cluster) {
+        pm[c] = ld_rank(rank_addr(&part->m[ri], c));
+        pl[c] = ld_rank(rank_addr(&part->l[ri], c));
+        z[c] = ld_rank4(rank_addr(&part->o[ri][4 * lane], c));
+      }
     }
 #pragma unroll
-    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    for (int c = 0; c < kMostCluster; ++c) top = fmaxf(top, pm[c]);
     const float mb = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int i = lane + 32 * x;
-      pm[x] = ex2_approx(pm[x] - mb);
-      if (i < parts) sum += pm[x] * part_l(i);
+    for (int c = 0; c < kMostCluster; ++c) {
+      const float a = ex2_approx(pm[c] - mb);
+      sum += a * pl[c];
+      y = make_float4(y.x + a * z[c].x, y.y + a * z[c].y, y.z + a * z[c].z, y.w + a * z[c].w);
     }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int i = 0; i < parts; ++i) {
-      const float w = __shfl_sync(0xffffffffu, i < 32 ? pm[0] : pm[1], i & 31);
-      const float4 z = ld_rank4(rank_addr(&sm.o[(i % kKeyWarps) * RG + rgr][ri][4 * lane], i / kKeyWarps));
-      y.x += w * z.x;
-      y.y += w * z.y;
-      y.z += w * z.z;
-      y.w += w * z.w;
-    }
-    const int row = row0 + r, t = row / p.group, h = kvh * p.group + row % p.group;
+    const int dt = token_of(r), t = t_first + dt, row = row0 + r, h = kvh * p.group + h_first + r - dt * p.group;
     if (p.splits == 1) {
       if (t < s.nq)
         window_store_row(p, b, h, t, y, top, sum);
@@ -326,39 +413,28 @@ __global__ void __launch_bounds__(128) window_join_kernel(const __grid_constant_
   window_store_row(p, b, h, t, y, m, l);
 }
 
-template <int RG>
-void step_launch(const WindowParams& p, cudaStream_t st) {
+}  // namespace
+
+void launch_window_step(const WindowParams& p, cudaStream_t st) {
   static std::once_flag once;
   std::call_once(once, [] {
-    cudaFuncSetAttribute(window_step_kernel<RG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(StepSmem));
-    cudaFuncSetAttribute(window_step_kernel<RG>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    cudaFuncSetAttribute(window_step_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)step_smem(1, 7));
   });
+  const int warps = p.row_warps * p.key_warps;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)p.cluster;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = (unsigned)((int64_t)p.batch * p.n_kv_heads * p.row_blocks * p.splits * p.cluster);
-  cfg.blockDim = 32 * kStepWarps;
-  cfg.dynamicSmemBytes = sizeof(StepSmem);
+  cfg.gridDim = dim3((unsigned)((int64_t)p.row_blocks * p.splits * p.cluster), (unsigned)p.n_kv_heads, (unsigned)p.batch);
+  cfg.blockDim = 32 * warps;
+  cfg.dynamicSmemBytes = step_smem(p.row_warps, p.key_warps);
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  cudaLaunchKernelEx(&cfg, window_step_kernel<RG>, p);
+  cudaLaunchKernelEx(&cfg, window_step_kernel, p);
   count_launch();
-}
-
-}  // namespace
-
-void launch_window_step(const WindowParams& p, cudaStream_t st) {
-  const int rows = std::min(p.group * p.n_tok, kWindowRows);
-  if (rows <= 16)
-    step_launch<1>(p, st);
-  else if (rows <= 32)
-    step_launch<2>(p, st);
-  else
-    step_launch<4>(p, st);
   if (p.splits > 1) launch_window_join(p, st);
 }
 
@@ -370,9 +446,11 @@ void launch_window_join(const WindowParams& p, cudaStream_t st) {
 
 namespace {
 
+constexpr int64_t kSmBytes = 228 << 10;  // of shared memory
+
 struct WindowPlan {
   bool prompt;
-  int row_blocks, cluster, splits;  // (prompt: row_blocks are pairs of Q tiles)
+  int row_blocks, cluster, splits, row_warps, key_warps;  // (prompt: row_blocks are pairs of Q tiles)
 };
 
 // Keys that a block of rows may have in reach.
@@ -399,12 +477,26 @@ WindowPlan plan_window(const uc_window_cache& c, int n_q_heads, int n_tok) {
     w.splits = (int)std::max<int64_t>(1, std::min<int64_t>(num_sms() / all, tiles / 4));
     return w;
   }
-  const int rg = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  // CTAs with at least one tile a warp, up to what the SMs hold of them
-  const int64_t tiles = (most_keys(c, n_tok, group) + kTileKeys * (kStepWarps / rg) - 1) / (kTileKeys * (kStepWarps / rg));
-  const int64_t want = std::max<int64_t>(1, std::min(tiles, 2 * (int64_t)num_sms() / items));
-  w.cluster = 1;
-  while (2 * w.cluster <= std::min<int64_t>(want, 8)) w.cluster *= 2;
+  // A step: keys in tiles over the warps of a cluster of up to 8 CTAs. The size that the
+  // SMs are through with first, with a CTA's start and end as long as kStart tiles of a
+  // warp; where even 8 leave a warp many tiles and SMs idle, several clusters and a join.
+  constexpr int64_t kStart = 6;
+  const int64_t tiles = (most_keys(c, n_tok, group) + kTileKeys - 1) / kTileKeys;
+  w.row_warps = (int)std::min<int64_t>((rows + kWarpRows - 1) / kWarpRows, kWindowRows / kWarpRows);
+  w.key_warps = w.row_warps == 1 && 16 * items <= num_sms() ? 7 : w.row_warps == 1 ? 3 : w.row_warps <= 5 ? 2 : 1;
+  const int64_t slots = (int64_t)std::min<int64_t>(kSmBytes / ((int64_t)step_smem(w.row_warps, w.key_warps) + 1024), kMostWarps / (w.row_warps * w.key_warps)) * num_sms();
+  int64_t least = INT64_MAX;
+  for (int n = 1; n <= kMostCluster; ++n) {
+    const int64_t per = (tiles + n * w.key_warps - 1) / (n * w.key_warps);
+    const int64_t cost = ((items * n + slots - 1) / slots) * (kStart + per);
+    if (cost < least) {
+      least = cost;
+      w.cluster = n;
+    }
+  }
+  const int64_t per = (tiles + w.cluster * w.key_warps - 1) / (w.cluster * w.key_warps);
+  if (per > 2 * kStart)
+    w.splits = (int)std::max<int64_t>(1, std::min<int64_t>(slots / (items * w.cluster), per / kStart));
   return w;
 }
 
@@ -491,6 +583,10 @@ uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32
   p.row_blocks = w.row_blocks;
   p.cluster = w.cluster;
   p.splits = w.splits;
+  p.row_warps = w.row_warps;
+  p.key_warps = w.key_warps;
+  p.wait_ns = wait_limit_ns();
+  p.withhold = take_withhold_pos();
   if (!w.prompt) {
     launch_window_step(p, reinterpret_cast<cudaStream_t>(stream));
     return cuda_check(fn);
@@ -509,8 +605,6 @@ uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32
   }
   if (st != UC_OK) return st;
   c.wide_out = aligned(p.out.base, 32) && p.out.sb % 16 == 0 && p.out.sh % 16 == 0 && p.out.st % 16 == 0;
-  c.wait_ns = wait_limit_ns();
-  c.withhold = take_withhold_pos();
   const int64_t items = (int64_t)batch * hkv * w.row_blocks * w.splits;
   const int grid = (int)std::min<int64_t>(items, num_sms());
   const cudaStream_t cs = reinterpret_cast<cudaStream_t>(stream);

@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
   tc_fence_after();
   const uint32_t tmem = sm.tmem_base;
   const int items = sm.begin[p.batch];
-  const uint64_t lim = c.wait_ns;
+  const uint64_t lim = c.p.wait_ns;
   int aborted = 0;
 
   if (warp >= 8) {
@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           const int ks = nk % kKSlots, vs = nv % kVSlots;
           if (j < j1) {
             if (nk >= kKSlots && !wait_lane(&sm.k_empty[ks], (nk / kKSlots - 1) & 1, 81, aborted, lim)) break;
-            if (load++ != c.withhold) {
+            if (load++ != c.p.withhold) {
               load_keys(sm.k[ks], c.tk, it, j, c, &sm.k_full[ks]);
               sm.loads[0] = nk + 1;
             }
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           }
           if (j < j1) {
             if (nv >= kVSlots && !wait_lane(&sm.v_empty[vs], (nv / kVSlots - 1) & 1, 82, aborted, lim)) break;
-            if (load++ != c.withhold) {
+            if (load++ != c.p.withhold) {
               load_keys(sm.v[vs], c.tv, it, j, c, &sm.v_full[vs]);
               sm.loads[1] = nv + 1;
             }
@@ -819,9 +819,9 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
     bool gone = false;
     if (warp == 8) {
       for (int i = max(0, sm.loads[0] - kKSlots); i < sm.loads[0]; ++i)
-        if (2 * i != c.withhold) dwait_warp(&sm.k_full[i % kKSlots], (i / kKSlots) & 1, p.status, 92, gone);
+        if (2 * i != c.p.withhold) dwait_warp(&sm.k_full[i % kKSlots], (i / kKSlots) & 1, p.status, 92, gone);
       for (int i = max(0, sm.loads[1] - kVSlots); i < sm.loads[1]; ++i)
-        if (2 * i + 1 != c.withhold) dwait_warp(&sm.v_full[i % kVSlots], (i / kVSlots) & 1, p.status, 92, gone);
+        if (2 * i + 1 != c.p.withhold) dwait_warp(&sm.v_full[i % kVSlots], (i / kVSlots) & 1, p.status, 92, gone);
       for (int x = 0; x < 2; ++x)
         if (sm.loads[2 + x] > 0) dwait_warp(&sm.q_full[x], (sm.loads[2 + x] - 1) & 1, p.status, 92, gone);
     } else if (warp == 9) {
