@@ -28,7 +28,10 @@ namespace {
 
 constexpr int kVerifyThreads = 256;
 constexpr int kVerifyWarps = kVerifyThreads / 32;
-constexpr int kVerifyVecs = 4;  // 16-byte vectors of a thread in flight
+constexpr int kVerifyVecs = 2;  // 16-byte vectors of a thread in flight, and as many worked on
+constexpr int kRowsPerSm = 8;   // CTAs that an SM holds (with four of twice the vectors 22.6 us instead of 20)
+constexpr int kPickPerSm = 4;
+constexpr int kDeep = 8;         // tokens of a thread in flight
 constexpr float kNone = -INFINITY;
 
 __device__ __forceinline__ int drafts_of(const VerifyParams& p, int b) {
@@ -51,7 +54,7 @@ __device__ __forceinline__ const T* draft_row(const VerifyParams& p, int b, int 
 
 // Rows are the target's [B, n_tok + 1], then the drafter's [B, n_tok].
 template <typename T>
-__global__ void __launch_bounds__(kVerifyThreads) verify_rows_kernel(const __grid_constant__ VerifyParams p) {
+__global__ void __launch_bounds__(kVerifyThreads, kRowsPerSm) verify_rows_kernel(const __grid_constant__ VerifyParams p) {
   using L = Logits<T>;
   constexpr int kE = L::kE;
   __shared__ float s_m[kVerifyWarps], s_s[kVerifyWarps];
@@ -80,12 +83,19 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_rows_kernel(const __gri
   float m = kNone, sum = 0.f;
   int at = INT_MAX;
   bool bad = false;
-  for (int from = vec0 + tid; from < vec1; from += kVerifyThreads * kVerifyVecs) {
-    uint4 v[kVerifyVecs];
+  constexpr int kRound = kVerifyThreads * kVerifyVecs;
+  const int last = min(whole1, vec1);
+  auto load = [&](uint4(&v)[kVerifyVecs], int from) {
+    if (from - tid >= whole0 && from - tid + kRound <= last) {
+#pragma unroll
+      for (int k = 0; k < kVerifyVecs; ++k) v[k] = xv[from + k * kVerifyThreads];
+      return;
+    }
+    // a row's ends: only what the row has
 #pragma unroll
     for (int k = 0; k < kVerifyVecs; ++k) {
       const int i = from + k * kVerifyThreads;
-      if (i >= whole0 && i < min(whole1, vec1)) {
+      if (i >= whole0 && i < last) {
         v[k] = xv[i];
       } else {
         v[k] = make_vector<T>([&](int e) {
@@ -94,6 +104,13 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_rows_kernel(const __gri
         });
       }
     }
+  };
+  uint4 v[kVerifyVecs], next[kVerifyVecs];
+  if (vec0 + tid < vec1) load(next, vec0 + tid);
+  for (int from = vec0 + tid; from < vec1; from += kRound) {
+#pragma unroll
+    for (int k = 0; k < kVerifyVecs; ++k) v[k] = next[k];
+    if (from + kRound < vec1) load(next, from + kRound);
     float best = kNone;
 #pragma unroll
     for (int k = 0; k < kVerifyVecs; ++k) {
@@ -174,16 +191,31 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_rows_kernel(const __gri
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kVerifyThreads) verify_pick_kernel(const __grid_constant__ VerifyParams p) {
+__global__ void __launch_bounds__(kVerifyThreads, kPickPerSm) verify_pick_kernel(const __grid_constant__ VerifyParams p) {
   __shared__ float s_m[2][UC_MAX_DRAFTS + 1], s_s[2][UC_MAX_DRAFTS + 1];
   __shared__ int s_at[UC_MAX_DRAFTS + 1], s_bad[2];
   __shared__ int s_a, s_last;
   __shared__ uint64_t s_key[kVerifyWarps];
-  griddep_wait();
   const int tile = blockIdx.x % p.pick_tiles, b = blockIdx.x / p.pick_tiles;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n = drafts_of(p, b), targets = p.batch * (p.n_tok + 1);
   const bool model = p.draft != nullptr;
+  // what the caller gave is read while the rows are still at work: a draft's logits, the first noise
+  int drafted = -1;
+  float xd = kNone, yd = kNone, ud = 0.f, es[kDeep];
+  if (tid < n) {
+    drafted = p.tokens[b * p.n_tok + tid];
+    if (drafted >= 0 && drafted < p.vocab && !p.greedy) {
+      xd = to_float(target_row<T>(p, b, tid)[drafted]);
+      if (model) yd = to_float(draft_row<T>(p, b, tid)[drafted]);
+      ud = p.u[b * p.n_tok + tid];
+    }
+  }
+  const int v_first = tile * p.pick_span + tid;
+  const float* const noise = p.noise + (int64_t)b * p.vocab;
+#pragma unroll
+  for (int k = 0; k < kDeep; ++k) es[k] = p.greedy ? 1.f : noise[min(v_first + k * kVerifyThreads, p.vocab - 1)];
+  griddep_wait();
   if (tid == 0) s_a = n;
   if (tid < 2) s_bad[tid] = 0;
   // the rows' statistics: a warp per row
@@ -226,28 +258,20 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_pick_kernel(const __gri
     return x < INFINITY && s_m[0][t] != kNone ? (x - s_m[0][t]) * p.inv_temperature - logf(s_s[0][t]) : kNone;
   };
   // the decisions: a thread per draft
-  for (int t = tid; t <= n; t += kVerifyThreads) {
+  if (tid <= n) {
+    const int t = tid;
     if (s_m[0][t] == kNone || (model && t < n && s_m[1][t] == kNone)) s_bad[0] = 1;
-    if (t == n) break;
-    const int d = p.tokens[b * p.n_tok + t];
-    bool good = d >= 0 && d < p.vocab;
-    if (!good) {
-      s_bad[1] = 1;
-    } else if (p.greedy) {
-      good = s_m[0][t] != kNone && d == s_at[t];
-    } else {
+    bool good = drafted >= 0 && drafted < p.vocab;
+    if (t < n && !good) s_bad[1] = 1;
+    if (p.greedy) {
+      good = good && s_m[0][t] != kNone && drafted == s_at[t];
+    } else if (t < n) {
       // u q < p, with both sides times the two sums
-      const float x = to_float(target_row<T>(p, b, t)[d]);
-      const float px = x < INFINITY && s_m[0][t] != kNone ? weight(p, x - s_m[0][t]) : 0.f;
-      float q = 1.f, sq = 1.f;
-      if (model) {
-        const float y = to_float(draft_row<T>(p, b, t)[d]);
-        q = y < INFINITY && s_m[1][t] != kNone ? weight(p, y - s_m[1][t]) : 0.f;
-        sq = s_s[1][t];
-      }
-      good = p.u[b * p.n_tok + t] * (q * s_s[0][t]) < px * sq;
+      const float px = xd < INFINITY && s_m[0][t] != kNone ? weight(p, xd - s_m[0][t]) : 0.f;
+      const float q = !model ? 1.f : yd < INFINITY && s_m[1][t] != kNone ? weight(p, yd - s_m[1][t]) : 0.f;
+      good = good && ud * (q * s_s[0][t]) < px * (model ? s_s[1][t] : 1.f);
     }
-    if (!good) atomicMin(&s_a, t);
+    if (t < n && !good) atomicMin(&s_a, t);
   }
   __syncthreads();
   const int a = s_a;
@@ -259,33 +283,32 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_pick_kernel(const __gri
     const T* const x = target_row<T>(p, b, a);
     const bool rest = a < n;
     const T* const y = model && rest ? draft_row<T>(p, b, a) : x;
-    const float* const e = p.noise + (int64_t)b * p.vocab;
     const float pm = s_m[0][a], ps = 1.f / s_s[0][a];
     const float qm = model && rest ? s_m[1][a] : 0.f, qs = model && rest ? 1.f / s_s[1][a] : 0.f;
     const int taken = !model && rest ? p.tokens[b * p.n_tok + a] : -1;
     const int v1 = min(p.vocab, (tile + 1) * p.pick_span);
     float best = -1.f;
     int best_at = 0;
-    constexpr int kDeep = 8;
-    for (int v0 = tile * p.pick_span + tid; v0 < v1; v0 += kVerifyThreads * kDeep) {
-      float xs[kDeep], ys[kDeep], es[kDeep];
+    for (int v0 = v_first; v0 < v1; v0 += kVerifyThreads * kDeep) {
+      float xs[kDeep], ys[kDeep];
 #pragma unroll
       for (int k = 0; k < kDeep; ++k) {
-        const int v = v0 + k * kVerifyThreads, w = min(v, p.vocab - 1);
+        const int w = min(v0 + k * kVerifyThreads, p.vocab - 1);
         xs[k] = to_float(x[w]);
         ys[k] = model && rest ? to_float(y[w]) : kNone;
-        es[k] = e[w];
+        if (v0 != v_first) es[k] = noise[w];
       }
 #pragma unroll
       for (int k = 0; k < kDeep; ++k) {
         const int v = v0 + k * kVerifyThreads;
-        if (v >= v1) break;
-        float w = xs[k] < INFINITY && xs[k] != kNone ? weight(p, xs[k] - pm) * ps : 0.f;
-        if (ys[k] < INFINITY && ys[k] != kNone) w -= weight(p, ys[k] - qm) * qs;
+        // (as the sums were formed; a difference above 0 is that of +inf)
+        const float dx = xs[k] - pm, dy = ys[k] - qm;
+        float w = dx <= 0.f ? ex2_approx(dx * p.scale.x) * ps : 0.f;
+        if (dy <= 0.f) w = fmaf(ex2_approx(dy * p.scale.x), -qs, w);
         if (v == taken) w -= 1.f;
-        w = fmaxf(w, 0.f) / es[k];
+        w = __fdividef(fmaxf(w, 0.f), es[k]);
         if (!(w >= 0.f)) w = 0.f;  // (a noise of 0 or NaN)
-        if (w > best) {  // (the first of equal ones: v ascends)
+        if (v < v1 && w > best) {  // (the first of equal ones: v ascends)
           best = w;
           best_at = v;
         }
@@ -342,7 +365,7 @@ int64_t row_vecs(int32_t vocab, int element) {
 constexpr int kMostTiles = 64;
 constexpr int kMinSpan = 512;       // vectors of a tile, where the row has them
 constexpr int kPickMost = 256;      // parts of a vocabulary
-constexpr int kPickMinSpan = 2048;  // tokens of one
+constexpr int kPickMinSpan = 512;   // tokens of one
 
 size_t verify_bytes(int64_t rows, int batch, int tiles) {
   return 256 + rows * tiles * (sizeof(float2) + sizeof(int32_t)) + batch * (sizeof(uint64_t) + sizeof(int32_t)) + 16;
@@ -456,13 +479,21 @@ uc_status uc_verify_draft(const void* target, int64_t target_b, int64_t target_t
   p.inv_temperature = (float)inv;
   p.scale = make_float2((float)scale, (float)(scale - (double)(float)scale));
   const int64_t rows = (int64_t)batch * (n_tok + 1 + (draft ? n_tok : 0)), vecs = row_vecs(vocab, element);
-  const int64_t slots = 4 * (int64_t)num_sms();
+  const int64_t slots = kRowsPerSm * (int64_t)num_sms();
+  // tiles of a row: the split that the SMs are through with first, a CTA's start and end as long as kStart vectors
+  constexpr int64_t kStart = 2048;
   const int64_t most = std::min<int64_t>(kMostTiles, (vecs + kMinSpan - 1) / kMinSpan);
-  const int64_t tiles = std::max<int64_t>(1, std::min(most, (slots + rows - 1) / rows));
-  p.span = (int)((vecs + tiles - 1) / tiles);
+  int64_t least = INT64_MAX;
+  for (int64_t t = 1; t <= most; ++t) {
+    const int64_t span = (vecs + t - 1) / t, cost = (rows * t + slots - 1) / slots * (kStart + span);
+    if (cost < least) {
+      least = cost;
+      p.span = (int)span;
+    }
+  }
   p.tiles = (int)((vecs + p.span - 1) / p.span);
   const int64_t pick = greedy ? 1 : std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(kPickMost, vocab / kPickMinSpan),
-                                                                         slots / batch));
+                                                                         kPickPerSm * (int64_t)num_sms() / batch));
   p.pick_span = (int)((vocab + pick - 1) / pick);
   p.pick_tiles = (int)((vocab + p.pick_span - 1) / p.pick_span);
   uint8_t* const w = static_cast<uint8_t*>(workspace);
