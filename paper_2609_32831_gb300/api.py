@@ -779,29 +779,35 @@ def reorder(pairs, parent: torch.Tensor, ws: Optional[Workspace] = None, stream=
 
 # ------------------------------------------------- positions of tokens (rotary)
 
-def _on_device(fn: str, *tensors) -> None:
-    """The library takes plain addresses: what it cannot see of a tensor."""
-    at = -1
-    for t in tensors:
-        if t is None:
-            continue
-        if at < 0 and t.is_cuda:
-            at = torch._C._cuda_getDevice()
-        if t.get_device() != at or at < 0:
+_BF16 = torch.bfloat16
+
+
+def _device_of(fn: str, first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    """The library takes plain addresses: what it cannot see of tensors."""
+    at = first.get_device()
+    if at < 0 or at != torch._C._cuda_getDevice():
+        raise ValueError(f"{fn}: every tensor is on the current CUDA device")
+    for t in others:
+        if t is not None and t.get_device() != at:
             raise ValueError(f"{fn}: every tensor is on the current CUDA device")
 
 
-def _head_rows(fn: str, name: str, x: torch.Tensor, shape, dtype) -> bytes:
-    """uc_rows of x [batch, heads, tokens, 128]."""
+def _head_rows(fn: str, name: str, x: torch.Tensor, like, dtype) -> bytes:
+    """uc_rows of x [batch, heads, tokens, 128] of the shape ``like``."""
     s = x.stride()
-    if x.shape != shape or x.dtype is not dtype or s[3] != 1:
-        raise ValueError(f"{fn}: {name} is {dtype} {list(shape)}, every row contiguous")
+    if x.shape != like or x.dtype is not dtype or s[-1] != 1:
+        raise ValueError(f"{fn}: {name} is {dtype} {list(like)}, every row contiguous")
     return _pack_rows(x.data_ptr(), s[0], s[1], s[2])
 
 
-def _counts(fn: str, name: str, x: Optional[torch.Tensor], batch: int) -> None:
-    if x is not None and (x.dtype is not torch.int32 or x.shape != (batch,) or not x.is_contiguous()):
+def _counts(fn: str, name: str, x: torch.Tensor, batch: int) -> int:
+    if x.dtype is not torch.int32 or x.dim() != 1 or x.shape[0] != batch or not x.is_contiguous():
         raise ValueError(f"{fn}: {name} is contiguous int32 [{batch}]")
+    return x.data_ptr()
+
+
+def _like(x: torch.Tensor, stream) -> torch.Tensor:
+    return torch.empty_like(x) if stream is None else _new(stream, lambda: torch.empty_like(x))[0]
 
 
 class Rotary:
@@ -827,26 +833,33 @@ def rotary(table: Rotary, positions: torch.Tensor, q: torch.Tensor, k: Optional[
     takes them. positions int32: [B, T], or [B, 1] for the first token's.
     out_q, out_k: where they go (may be q and k themselves: in place). Returns (out_q, out_k),
     with the strides of q and k where these have no gaps."""
-    kind = _LOGIT_TYPES.get(q.dtype)
-    if kind is None or q.dim() != 4 or q.shape[3] != HEAD_DIM:
+    dtype, shape = q.dtype, q.shape
+    kind = _LOGIT_TYPES.get(dtype)
+    if kind is None or len(shape) != 4 or shape[3] != HEAD_DIM:
         raise ValueError("rotary: q is fp32, bf16 or fp16 [B, Hq, T, 128]")
-    B, hq, T, d = q.shape
-    if positions.dtype is not torch.int32 or positions.shape not in ((B, T), (B, 1)) or not positions.is_contiguous():
+    B, hq, T, d = shape
+    at = positions.shape
+    if positions.dtype is not torch.int32 or len(at) != 2 or at[0] != B or at[1] not in (1, T) \
+            or not positions.is_contiguous():
         raise ValueError("rotary: positions are contiguous int32 [B, T] or [B, 1]")
-    if k is None and out_k is not None or k is not None and k.dim() != 4:
-        raise ValueError("rotary: k is [B, Hkv, T, 128], and out_k its result")
-    hkv = 0 if k is None else k.shape[1]
-    rq = _head_rows("rotary", "q", q, (B, hq, T, d), q.dtype)
-    rk = None if k is None else _head_rows("rotary", "k", k, (B, hkv, T, d), q.dtype)
-    _on_device("rotary", q, k, positions, out_q, out_k)
+    rq, rk, ok, hkv = _head_rows("rotary", "q", q, shape, dtype), None, None, 0
+    if k is not None:
+        if k.dim() != 4:
+            raise ValueError("rotary: k is [B, Hkv, T, 128]")
+        hkv = k.shape[1]
+        rk = _head_rows("rotary", "k", k, (B, hkv, T, d), dtype)
+    elif out_k is not None:
+        raise ValueError("rotary: out_k is the result for k")
+    _device_of("rotary", q, k, positions, out_q, out_k)
     if out_q is None:
-        out_q = torch.empty_like(q) if stream is None else _new(stream, lambda: torch.empty_like(q))[0]
-    if k is not None and out_k is None:
-        out_k = torch.empty_like(k) if stream is None else _new(stream, lambda: torch.empty_like(k))[0]
-    oq = _head_rows("rotary", "out_q", out_q, (B, hq, T, d), q.dtype)
-    ok = None if k is None else _head_rows("rotary", "out_k", out_k, (B, hkv, T, d), q.dtype)
-    check("uc_rotary", lib().uc_rotary(table._at, positions.data_ptr(), int(positions.shape[1] == T), kind, B, T, rq, oq,
-                                       hq, rk, ok, hkv, _stream(stream)))
+        out_q = _like(q, stream)
+    oq = _head_rows("rotary", "out_q", out_q, shape, dtype)
+    if k is not None:
+        if out_k is None:
+            out_k = _like(k, stream)
+        ok = _head_rows("rotary", "out_k", out_k, k.shape, dtype)
+    check("uc_rotary", lib().uc_rotary(table._at, positions.data_ptr(), at[1] == T, kind, B, T, rq, oq, hq, rk, ok, hkv,
+                                       _stream(stream)))
     return out_q, out_k
 
 
@@ -886,30 +899,33 @@ def window_append(cache: WindowCache, k: torch.Tensor, v: torch.Tensor, held: to
     where that is given. q [B, Hq, T, 128]: turned beside them, into out_q (may
     be q). held, n_new: device int32 [B] (None: T each). Returns (total, out_q),
     total = held + n_new (another array than held)."""
-    B, hkv, d = cache.batch, cache.n_kv_heads, HEAD_DIM
-    if k.dim() != 4:
+    fn, shape = "window_append", k.shape
+    if len(shape) != 4 or shape[0] != cache.batch or shape[1] != cache.n_kv_heads or shape[3] != HEAD_DIM:
         raise ValueError("window_append: k and v are bf16 [B, Hkv, T, 128]")
-    T = k.shape[2]
-    rk, rv = (_head_rows("window_append", name, x, (B, hkv, T, d), torch.bfloat16) for x, name in ((k, "k"), (v, "v")))
-    _counts("window_append", "held", held, B)
-    _counts("window_append", "n_new", n_new, B)
-    _counts("window_append", "total", total, B)
-    if held is None or (q is None and out_q is not None) or (q is not None and (rotary is None or q.dim() != 4)):
+    B, T = shape[0], shape[2]
+    rk, rv = _head_rows(fn, "k", k, shape, _BF16), _head_rows(fn, "v", v, shape, _BF16)
+    if held is None or (out_q is not None if q is None else rotary is None or q.dim() != 4):
         raise ValueError("window_append: held is needed, and a rotary where there is a q [B, Hq, T, 128]")
-    hq = 0 if q is None else q.shape[1]
-    rq = None if q is None else _head_rows("window_append", "q", q, (B, hq, T, d), torch.bfloat16)
-    _on_device("window_append", cache.k, k, v, held, n_new, q, out_q, total)
+    n_held = _counts(fn, "held", held, B)
+    n_add = None if n_new is None else _counts(fn, "n_new", n_new, B)
+    rq = oq = None
+    hq = 0
+    if q is not None:
+        hq = q.shape[1]
+        rq = _head_rows(fn, "q", q, (B, hq, T, HEAD_DIM), _BF16)
+    _device_of(fn, k, v, cache.k, held, n_new, q, out_q, total)
     if total is None:
-        total = torch.empty_like(held) if stream is None else _new(stream, lambda: torch.empty_like(held))[0]
-    if q is not None and out_q is None:
-        out_q = torch.empty_like(q) if stream is None else _new(stream, lambda: torch.empty_like(q))[0]
-    oq = None if q is None else _head_rows("window_append", "out_q", out_q, (B, hq, T, d), torch.bfloat16)
+        total = _like(held, stream)
+    if q is not None:
+        if out_q is None:
+            out_q = _like(q, stream)
+        oq = _head_rows(fn, "out_q", out_q, q.shape, _BF16)
     ws = ws or default_workspace(k.device)
     st = _stream(stream)
     wp, wn = ws.get(256, "scratch", stream, st)
     check("uc_window_append", lib().uc_window_append(
-        cache._at, rk, rv, T, held.data_ptr(), _ptr(n_new), None if rotary is None else rotary._at, rq, oq, hq,
-        total.data_ptr(), wp, wn, st))
+        cache._at, rk, rv, T, n_held, n_add, None if rotary is None else rotary._at, rq, oq, hq,
+        _counts(fn, "total", total, B), wp, wn, st))
     return total, out_q
 
 
@@ -921,25 +937,25 @@ def window_attend(q: torch.Tensor, cache: WindowCache, lengths: torch.Tensor, n_
     lengths[b] tokens that sequence b holds in ``cache``, their own among them;
     device int32 [B]. Returns (out, lse): out with q's shape (and its strides
     where q has no gaps), 0 behind a sequence's last query; lse fp32 [B, Hq, T] or None."""
-    B, hkv = cache.batch, cache.n_kv_heads
-    if q.dim() != 4 or lengths is None:
+    fn, shape = "window_attend", q.shape
+    if len(shape) != 4 or shape[0] != cache.batch or shape[3] != HEAD_DIM or lengths is None:
         raise ValueError("window_attend: lengths are needed, and q is bf16 [B, Hq, T, 128]")
-    hq, T = q.shape[1], q.shape[2]
-    rq = _head_rows("window_attend", "q", q, (B, hq, T, HEAD_DIM), torch.bfloat16)
-    _counts("window_attend", "lengths", lengths, B)
-    _counts("window_attend", "n_query", n_query, B)
+    B, hq, T, _ = shape
+    rq = _head_rows(fn, "q", q, shape, _BF16)
+    n = _counts(fn, "lengths", lengths, B)
+    n_last = None if n_query is None else _counts(fn, "n_query", n_query, B)
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (B, hq, T) or not lse.is_contiguous()):
         raise ValueError("window_attend: lse is contiguous fp32 [B, Hq, T]")
-    _on_device("window_attend", cache.k, q, lengths, n_query, out, lse)
+    _device_of(fn, q, cache.k, lengths, n_query, out, lse)
     if out is None:
-        out = torch.empty_like(q) if stream is None else _new(stream, lambda: torch.empty_like(q))[0]
-    ro = _head_rows("window_attend", "out", out, (B, hq, T, HEAD_DIM), torch.bfloat16)
+        out = _like(q, stream)
+    ro = _head_rows(fn, "out", out, shape, _BF16)
     if want_lse and lse is None:
         lse = _new(stream, lambda: torch.empty((B, hq, T), dtype=torch.float32, device=q.device))[0]
     ws = ws or default_workspace(q.device)
     L = lib()
     st = _stream(stream)
-    args = (cache._at, rq, hq, T, lengths.data_ptr(), _ptr(n_query), ro, _ptr(lse))
+    args = (cache._at, rq, hq, T, n, n_last, ro, None if lse is None else lse.data_ptr())
     code = L.uc_window_attend(*args, *ws.get(256, "scratch", stream, st), st)
     if code == _lib.UC_ERR_OOM:   # nothing is launched then: only now is the size asked for
         code = L.uc_window_attend(*args, *ws.get(L.uc_window_workspace_size(cache._at, hq, T), "scratch", stream, st), st)
@@ -960,32 +976,46 @@ def verify_draft(logits: torch.Tensor, tokens: torch.Tensor, u: Optional[torch.T
     [B, T] uniform in [0, 1), noise fp32 [B, V] exponential variates; neither is
     needed at temperature 0. Returns (accepted int32 [B], tokens int32 [B, T + 1]:
     the accepted drafts, the next token, then -1; log probabilities fp32 [B, T + 1])."""
+    fn, shape, strides = "verify_draft", logits.shape, logits.stride()
     kind = _LOGIT_TYPES.get(logits.dtype)
-    if kind is None or logits.dim() != 3 or logits.stride(2) != 1:
+    if kind is None or len(shape) != 3 or strides[2] != 1:
         raise ValueError("verify_draft: logits are fp32, bf16 or fp16 [B, T + 1, V] with contiguous rows")
-    B, T, V = logits.shape[0], logits.shape[1] - 1, logits.shape[2]
+    B, T1, V = shape
+    T = T1 - 1
     if tokens.dtype is not torch.int32 or tokens.shape != (B, T) or not tokens.is_contiguous():
         raise ValueError("verify_draft: tokens are contiguous int32 [B, T]")
-    if draft_logits is not None and (draft_logits.dtype is not logits.dtype or draft_logits.shape != (B, T, V)
-                                     or draft_logits.stride(2) != 1):
-        raise ValueError("verify_draft: draft_logits are [B, T, V] of the logits' type with contiguous rows")
-    for x, shape, name in ((u, (B, T), "u"), (noise, (B, V), "noise")):
-        if x is None and temperature != 0:
-            raise ValueError(f"verify_draft: {name} is needed unless temperature is 0")
-        if x is not None and (x.dtype is not torch.float32 or x.shape != shape or not x.is_contiguous()):
-            raise ValueError(f"verify_draft: {name} is contiguous fp32 {list(shape)}")
-    _counts("verify_draft", "n_draft", n_draft, B)
-    _on_device("verify_draft", logits, tokens, draft_logits, u, noise, n_draft)
+    pd, db, dt = None, 0, 0
+    if draft_logits is not None:
+        db, dt, dv = draft_logits.stride() if draft_logits.dim() == 3 else (0, 0, 0)
+        if draft_logits.dtype is not logits.dtype or draft_logits.shape != (B, T, V) or dv != 1:
+            raise ValueError("verify_draft: draft_logits are [B, T, V] of the logits' type with contiguous rows")
+        pd = draft_logits.data_ptr()
+    pu = pe = None
+    if u is not None:
+        if u.dtype is not torch.float32 or u.shape != (B, T) or not u.is_contiguous():
+            raise ValueError("verify_draft: u is contiguous fp32 [B, T]")
+        pu = u.data_ptr()
+    if noise is not None:
+        if noise.dtype is not torch.float32 or noise.shape != (B, V) or not noise.is_contiguous():
+            raise ValueError("verify_draft: noise is contiguous fp32 [B, V]")
+        pe = noise.data_ptr()
+    if temperature != 0 and (pu is None or pe is None):
+        raise ValueError("verify_draft: u and noise are needed unless temperature is 0")
+    n = None if n_draft is None else _counts(fn, "n_draft", n_draft, B)
+    _device_of(fn, logits, tokens, draft_logits, u, noise, n_draft)
     dev = logits.device
-    accepted, out, logprob = _new(stream, partial(torch.empty, (B,), dtype=torch.int32, device=dev),
-                                  partial(torch.empty, (B, T + 1), dtype=torch.int32, device=dev),
-                                  partial(torch.empty, (B, T + 1), dtype=torch.float32, device=dev))
+    if stream is None:
+        accepted = torch.empty((B,), dtype=torch.int32, device=dev)
+        out = torch.empty((B, T1), dtype=torch.int32, device=dev)
+        logprob = torch.empty((B, T1), dtype=torch.float32, device=dev)
+    else:
+        accepted, out, logprob = _new(stream, partial(torch.empty, (B,), dtype=torch.int32, device=dev),
+                                      partial(torch.empty, (B, T1), dtype=torch.int32, device=dev),
+                                      partial(torch.empty, (B, T1), dtype=torch.float32, device=dev))
     ws = ws or default_workspace(dev)
     L = lib()
-    db, dt = (0, 0) if draft_logits is None else draft_logits.stride()[:2]
-    args = (logits.data_ptr(), *logits.stride()[:2], _ptr(draft_logits), db, dt, kind, B, T, V, tokens.data_ptr(),
-            _ptr(n_draft), _ptr(u), _ptr(noise), float(temperature), accepted.data_ptr(), out.data_ptr(),
-            logprob.data_ptr())
+    args = (logits.data_ptr(), strides[0], strides[1], pd, db, dt, kind, B, T, V, tokens.data_ptr(), n, pu, pe,
+            temperature, accepted.data_ptr(), out.data_ptr(), logprob.data_ptr())
     st = _stream(stream)
     code = L.uc_verify_draft(*args, *ws.get(256, "scratch", stream, st), st)
     if code == _lib.UC_ERR_OOM:   # nothing is launched then: only now is the size asked for

@@ -10,8 +10,8 @@
 // Every row is read once and written once, so HBM bounds it. A thread holds the
 // sines and cosines of its 16 bytes' pairs and walks the token's heads
 // with them, four rows in flight; a token's heads go to several threads where
-// tokens are few. Pairs (i, i + P) with P no multiple of a vector's elements
-// take a warp per token, element by element.
+// tokens are few. Pairs (i, i + P) with P no multiple of a vector's elements take a
+// warp per token, partners by shuffles.
 #include <climits>
 #include <cmath>
 #include <cstring>
@@ -208,49 +208,120 @@ __global__ void __launch_bounds__(kPosThreads) positions_kernel(const __grid_con
   });
 }
 
-// Pairs (i, i + P) of any P: a warp per token, channels lane, lane + 32, ...
+// Four elements of a row: one lane's, as words.
+template <typename T>
+struct Four {
+  static constexpr int kWords = 4 * sizeof(T) / 4;
+  uint32_t w[kWords];
+};
+
+// Pairs (i, i + P) of any P: a warp per token, lane l has channels 4 l .. 4 l + 3.
+// Their partners lie P channels on or back: in two lanes' words there, brought
+// together and shifted by P mod 4 elements.
 template <typename T>
 __global__ void __launch_bounds__(kPosThreads) positions_any_kernel(const __grid_constant__ PositionParams p) {
   using V = Vec<T>;
-  constexpr int kN = kHeadDim / 32;
+  using F = Four<T>;
+  constexpr int kPer = 4 / (int)sizeof(T);  // elements of a word
   const int64_t at = (int64_t)(blockIdx.x / p.parts) * (kPosThreads / 32) + threadIdx.x / 32;
   const int part = blockIdx.x % p.parts, lane = threadIdx.x & 31;
   if (at >= (int64_t)p.batch * p.n_tok) return;
   const Token k = token_of(p, at, part == 0 && lane == 0);
   const int h0 = (int)((int64_t)p.heads * part / p.parts), h1 = (int)((int64_t)p.heads * (part + 1) / p.parts);
-  float c[kN], s[kN];
-  int partner[kN];
+  float c[4], s[4];
+  bool first[4], live[4];
 #pragma unroll
-  for (int e = 0; e < kN; ++e) {
-    const int ch = lane + 32 * e;
-    partner[e] = ch < p.n_pairs ? ch + p.n_pairs : ch < 2 * p.n_pairs ? ch - p.n_pairs : -1;
-    if (partner[e] >= 0) {
-      const float2 cs = turned(k.pos, p.turn[min(ch, partner[e])], p.scale);
-      c[e] = cs.x;
-      s[e] = ch < p.n_pairs ? -cs.y : cs.y;
-    }
+  for (int e = 0; e < 4; ++e) {
+    const int ch = 4 * lane + e;
+    first[e] = ch < p.n_pairs;
+    live[e] = ch < 2 * p.n_pairs;
+    const float2 cs = live[e] ? turned(k.pos, p.turn[first[e] ? ch : ch - p.n_pairs], p.scale) : make_float2(1.f, 0.f);
+    c[e] = cs.x;
+    s[e] = first[e] ? -cs.y : cs.y;
   }
+  auto value = [](const F& f, int e) -> float {
+    if constexpr (kPer == 1) {
+      return __uint_as_float(f.w[e]);
+    } else {
+      const uint16_t x = (uint16_t)(f.w[e >> 1] >> (16 * (e & 1)));
+      return V::one(*reinterpret_cast<const T*>(&x));
+    }
+  };
+  // the four elements that begin `shift` channels behind a lane's first (any sign)
+  auto moved = [&](const F& x, int shift) -> F {
+    const int lanes = shift >> 2, rest = shift & 3;
+    F a, b, r;
+#pragma unroll
+    for (int i = 0; i < F::kWords; ++i) {
+      a.w[i] = __shfl_sync(0xffffffffu, x.w[i], (lane + lanes) & 31);
+      b.w[i] = __shfl_sync(0xffffffffu, x.w[i], (lane + lanes + 1) & 31);
+    }
+    uint32_t w[2 * F::kWords];
+#pragma unroll
+    for (int i = 0; i < F::kWords; ++i) {
+      w[i] = a.w[i];
+      w[F::kWords + i] = b.w[i];
+    }
+    const int words = rest / kPer;
+#pragma unroll
+    for (int i = 0; i < F::kWords; ++i) {
+      uint32_t lo = w[i], hi = w[i + 1];
+#pragma unroll
+      for (int y = 1; y < F::kWords; ++y)
+        if (words == y) {
+          lo = w[i + y];
+          hi = i + y + 1 < 2 * F::kWords ? w[i + y + 1] : 0u;
+        }
+      r.w[i] = kPer == 2 && (rest & 1) ? __funnelshift_r(lo, hi, 16) : lo;
+    }
+    return r;
+  };
   groups_in(p, h0, h1, [&](const PositionGroup& g, int h, int n) {
     if (g.role != kTurn && !k.keep) return;
-    const T* const src0 = reinterpret_cast<const T*>(g.src.base) + k.b * g.src.sb + k.t * g.src.st;
-    T* const dst0 = reinterpret_cast<T*>(g.dst.base) + k.b * g.dst.sb + (g.role == kTurn ? k.t : k.slot) * g.dst.st;
-    const bool turns = g.role != kStore;
-#pragma unroll 2
-    for (int i = h; i < h + n; ++i) {
-      const T* const src = src0 + i * g.src.sh;
-      T* const dst = dst0 + i * g.dst.sh;
-      T x[kN], y[kN];
+    const T* const src0 = reinterpret_cast<const T*>(g.src.base) + k.b * g.src.sb + k.t * g.src.st + 4 * lane;
+    T* const dst0 = reinterpret_cast<T*>(g.dst.base) + k.b * g.dst.sb + (g.role == kTurn ? k.t : k.slot) * g.dst.st + 4 * lane;
+    constexpr int kRowsInFlight = 4;  // (eight took a tenth longer: what bounds it is instructions, 150 a row)
+#pragma unroll 1
+    for (int i = h; i < h + n; i += kRowsInFlight) {
+      F x[kRowsInFlight];
 #pragma unroll
-      for (int e = 0; e < kN; ++e) {
-        x[e] = src[lane + 32 * e];
-        y[e] = turns && partner[e] >= 0 ? src[partner[e]] : x[e];
-      }
-      __syncwarp();  // (in place, other lanes' elements are overwritten below)
+      for (int r = 0; r < kRowsInFlight; ++r)
+        if (i + r < h + n) {
+          if constexpr (kPer == 1) {
+            const uint4 w = *reinterpret_cast<const uint4*>(src0 + (i + r) * g.src.sh);
+            x[r].w[0] = w.x; x[r].w[1] = w.y; x[r].w[2] = w.z; x[r].w[3] = w.w;
+          } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(src0 + (i + r) * g.src.sh);
+            x[r].w[0] = w.x; x[r].w[1] = w.y;
+          }
+        }
 #pragma unroll
-      for (int e = 0; e < kN; ++e) {
-        const float z = fmaf(V::one(x[e]), c[e], V::one(y[e]) * s[e]);
-        dst[lane + 32 * e] = turns && partner[e] >= 0 ? V::back(z) : x[e];
-      }
+      for (int r = 0; r < kRowsInFlight; ++r)
+        if (i + r < h + n) {
+          if (g.role != kStore) {
+            const F on = moved(x[r], p.n_pairs), back = moved(x[r], -p.n_pairs);
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              y[e] = fmaf(value(x[r], e), c[e], (first[e] ? value(on, e) : value(back, e)) * s[e]);
+#pragma unroll
+            for (int w = 0; w < F::kWords; ++w) {
+              if constexpr (kPer == 1) {
+                if (live[w]) x[r].w[w] = __float_as_uint(y[w]);
+              } else {
+                const T lo = V::back(y[2 * w]), hi = V::back(y[2 * w + 1]);
+                uint32_t z = *reinterpret_cast<const uint16_t*>(&lo) | (uint32_t)*reinterpret_cast<const uint16_t*>(&hi) << 16;
+                if (!live[2 * w]) z = (z & 0xffff0000u) | (x[r].w[w] & 0xffffu);
+                if (!live[2 * w + 1]) z = (z & 0xffffu) | (x[r].w[w] & 0xffff0000u);
+                x[r].w[w] = z;
+              }
+            }
+          }
+          if constexpr (kPer == 1)
+            *reinterpret_cast<uint4*>(dst0 + (i + r) * g.dst.sh) = make_uint4(x[r].w[0], x[r].w[1], x[r].w[2], x[r].w[3]);
+          else
+            *reinterpret_cast<uint2*>(dst0 + (i + r) * g.dst.sh) = make_uint2(x[r].w[0], x[r].w[1]);
+        }
     }
   });
 }
@@ -279,9 +350,9 @@ void launch_typed(PositionParams p, cudaStream_t st) {
 uint64_t turns_of(double freq) {
   constexpr double kHi = 0x1.45f306dc9c883p-3, kLo = -0x1.6b01ec5417056p-57;
   const double p = freq * kHi, rest = std::fma(freq, kHi, -p) + freq * kLo;
-  const double f = p - std::floor(p);  // [0, 1)
-  const uint64_t whole = f < 0.5 ? (uint64_t)std::ldexp(f, 64) : (uint64_t)(int64_t)std::ldexp(f - 1.0, 64);
-  return whole + (uint64_t)(int64_t)std::nearbyint(std::ldexp(rest - std::floor(rest + 0.5), 64));
+  // (both parts modulo one: [-1/2, 1/2), times 2^64 exactly; |p| < 2^29)
+  auto part = [](double x) { return (uint64_t)std::llrint((x - (double)(int64_t)std::floor(x + 0.5)) * 0x1p64); };
+  return part(p) + part(rest);
 }
 
 uc_status set_table(const uc_rotary_table* t, const char* fn, PositionParams* p) {
