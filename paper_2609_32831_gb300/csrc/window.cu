@@ -1,5 +1,6 @@
-// Attention with a sliding window and first tokens over a cache whose rows may
-// be a ring, for few queries: single tokens, drafts, short pieces of a prompt.
+// Attention with a sliding window and first tokens over a cache whose rows may be a
+// ring, for few query rows of a KV head: single tokens, short drafts. (More rows, and
+// what plans and joins calls of either kind: plan_window, window_join_kernel.)
 //
 // Keys and values in reach are read once, 32 keys at a time, by bulk copies into shared
 // memory some tiles ahead (rows loaded to registers cost a tile its latency, 2.4K
@@ -446,6 +447,7 @@ void launch_window_join(const WindowParams& p, cudaStream_t st) {
 
 namespace {
 
+constexpr int kQTileRows = 128;  // query rows of a prompt's tile
 constexpr int64_t kSmBytes = 228 << 10;  // of shared memory
 
 struct WindowPlan {
@@ -459,44 +461,69 @@ int64_t most_keys(const uc_window_cache& c, int n_tok, int group) {
   return std::min<int64_t>(c.n_rows, (int64_t)c.window + c.n_sink + tokens);
 }
 
-WindowPlan plan_window(const uc_window_cache& c, int n_q_heads, int n_tok) {
+// Steps: keys in tiles over the warps of a cluster of up to 8 CTAs. The size that the
+// SMs are through with first, with a CTA's start and end as long as kStart tiles of a
+// warp; where even 8 leave a warp many tiles and SMs idle, several clusters and a join.
+// *turns: tiles that a warp takes one after the other, over the rounds of CTAs.
+WindowPlan plan_step(const uc_window_cache& c, int64_t rows, int group, int n_tok, int64_t* turns) {
+  constexpr int64_t kStart = 6;
   WindowPlan w;
-  const int group = n_q_heads / c.n_kv_heads;
-  const int64_t rows = (int64_t)group * n_tok;
+  w.prompt = false;
+  w.splits = 1;
   w.row_blocks = (int)((rows + kWindowRows - 1) / kWindowRows);
   const int64_t items = (int64_t)c.batch * c.n_kv_heads * w.row_blocks;
-  w.splits = 1;
-  w.prompt = rows > kWindowRows && group <= 128 && c.batch <= kWindowSeqs;
-  if (w.prompt) {
-    // key ranges of a tile or more where there are too few pairs of Q tiles for the SMs
-    const int tokens = 128 / group;
-    w.row_blocks = (n_tok + 2 * tokens - 1) / (2 * tokens);
-    w.cluster = 1;
-    const int64_t all = (int64_t)c.batch * c.n_kv_heads * w.row_blocks;
-    const int64_t tiles = (std::min<int64_t>(c.n_rows, (int64_t)c.window + c.n_sink + std::min(n_tok, 2 * tokens)) + 127) / 128;
-    w.splits = (int)std::max<int64_t>(1, std::min<int64_t>(num_sms() / all, tiles / 4));
-    return w;
-  }
-  // A step: keys in tiles over the warps of a cluster of up to 8 CTAs. The size that the
-  // SMs are through with first, with a CTA's start and end as long as kStart tiles of a
-  // warp; where even 8 leave a warp many tiles and SMs idle, several clusters and a join.
-  constexpr int64_t kStart = 6;
   const int64_t tiles = (most_keys(c, n_tok, group) + kTileKeys - 1) / kTileKeys;
   w.row_warps = (int)std::min<int64_t>((rows + kWarpRows - 1) / kWarpRows, kWindowRows / kWarpRows);
   w.key_warps = w.row_warps == 1 && 16 * items <= num_sms() ? 7 : w.row_warps == 1 ? 3 : w.row_warps <= 5 ? 2 : 1;
-  const int64_t slots = (int64_t)std::min<int64_t>(kSmBytes / ((int64_t)step_smem(w.row_warps, w.key_warps) + 1024), kMostWarps / (w.row_warps * w.key_warps)) * num_sms();
-  int64_t least = INT64_MAX;
+  const int64_t ctas = std::min<int64_t>(kSmBytes / ((int64_t)step_smem(w.row_warps, w.key_warps) + 1024),
+                                         kMostWarps / (w.row_warps * w.key_warps));
+  const int64_t slots = ctas * num_sms();
+  int64_t least = INT64_MAX, per = 0;
   for (int n = 1; n <= kMostCluster; ++n) {
-    const int64_t per = (tiles + n * w.key_warps - 1) / (n * w.key_warps);
-    const int64_t cost = ((items * n + slots - 1) / slots) * (kStart + per);
-    if (cost < least) {
-      least = cost;
+    const int64_t k = (tiles + n * w.key_warps - 1) / (n * w.key_warps), rounds = (items * n + slots - 1) / slots;
+    if (rounds * (kStart + k) < least) {
+      least = rounds * (kStart + k);
       w.cluster = n;
+      per = k;
+      *turns = rounds * k;
     }
   }
-  const int64_t per = (tiles + w.cluster * w.key_warps - 1) / (w.cluster * w.key_warps);
   if (per > 2 * kStart)
     w.splits = (int)std::max<int64_t>(1, std::min<int64_t>(slots / (items * w.cluster), per / kStart));
+  return w;
+}
+
+// Up to 8 query rows of a KV head go step by step: keys and values are read at 93 % of
+// the copy rate. More rows wait for a warp's products and softmax there (64 sequences of
+// 35 rows over 4100 keys: 312 us, 109 on the tensor cores), unless there are few keys as well
+// (8 sequences of 14 rows over 1030 keys: 12 us instead of 17).
+WindowPlan plan_window(const uc_window_cache& c, int n_q_heads, int n_tok) {
+  const int group = n_q_heads / c.n_kv_heads;
+  const int64_t rows = (int64_t)group * n_tok;
+  if (rows <= 2 * kWarpRows || group > kQTileRows || c.batch > kWindowSeqs) {
+    int64_t turns = 0;
+    const WindowPlan w = plan_step(c, rows, group, n_tok, &turns);
+    if (rows <= kWarpRows || turns <= 4 || group > kQTileRows || c.batch > kWindowSeqs) return w;
+  }
+  // Pairs of Q tiles; ranges of key tiles where these are too few for the SMs, an item's
+  // start and end and the join as long as kItem and kJoin tiles.
+  constexpr int64_t kItem = 3, kJoin = 3;
+  WindowPlan w;
+  w.prompt = true;
+  w.cluster = w.row_warps = w.key_warps = 1;
+  const int tokens = kQTileRows / group;
+  w.row_blocks = (n_tok + 2 * tokens - 1) / (2 * tokens);
+  const int64_t all = (int64_t)c.batch * c.n_kv_heads * w.row_blocks;
+  const int64_t tiles = (std::min<int64_t>(c.n_rows, (int64_t)c.window + c.n_sink + std::min(n_tok, 2 * tokens)) + 127) / 128;
+  int64_t least = INT64_MAX;
+  w.splits = 1;
+  for (int64_t r = 1; r <= std::min<int64_t>(32, std::max<int64_t>(1, tiles / 2)) && (r == 1 || all < 2 * num_sms()); ++r) {
+    const int64_t cost = (all * r + num_sms() - 1) / num_sms() * (kItem + (tiles + r - 1) / r) + (r > 1 ? kJoin : 0);
+    if (cost < least) {
+      least = cost;
+      w.splits = (int)r;
+    }
+  }
   return w;
 }
 
@@ -594,7 +621,7 @@ uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32
   WindowPromptParams c;
   memset(&c, 0, sizeof(c));
   c.p = p;
-  c.tokens = 128 / p.group;
+  c.tokens = kQTileRows / p.group;
   st = encode_heads_4d(&c.tq, p.q, n_tok, n_q_heads, batch, p.group, c.tokens);
   const int rest = (cache->n_sink + 15) / 16 * 16 % 128;
   for (int i = 0; i < 2 && st == UC_OK; ++i) {

@@ -72,7 +72,8 @@ struct Item {
   int low_a, low_b;        // positions from which on their rows are what they seem
   int slot_b;              // the cache's row behind the last
   int in_order;            // the tiles hold every position from 0 on
-  int plain_lo, plain_hi;  // tiles of 128 that both Q tiles take, neither as its first or last
+  int plain_lo, plain_hi;  // tiles of 128 that both Q tiles (or alone: the first) take, neither as its first or last
+  int alone;               // the second Q tile takes none
   uint16_t head[kLooked], tail[kLooked];  // todo() of the first and (from behind) the last tiles
   __device__ __forceinline__ bool takes(int x, int j) const {
     return j >= first[x] && j <= last[x] && (j < in_first || (j >= in_a[x] && j <= in_b[x]));
@@ -182,8 +183,13 @@ __device__ __forceinline__ void item_at(const WindowPromptParams& c, const Promp
     it.first[x] = last >= 0 ? first : 0;
     it.last[x] = last;
   }
-  it.plain_lo = max(max(max(it.first[0], it.first[1]) + 1, max(it.in_a[0], it.in_a[1])), it.firsts);
-  it.plain_hi = min(min(it.last[0], it.last[1]) - 1, min(it.in_b[0], it.in_b[1]));
+  it.alone = it.last[1] < it.first[1];
+  it.plain_lo = max(max(it.first[0] + 1, it.in_a[0]), it.firsts);
+  it.plain_hi = min(it.last[0] - 1, it.in_b[0]);
+  if (!it.alone) {
+    it.plain_lo = max(it.plain_lo, max(it.first[1] + 1, it.in_a[1]));
+    it.plain_hi = min(it.plain_hi, min(it.last[1] - 1, it.in_b[1]));
+  }
 }
 
 // Bits lo .. hi of 32 (none where hi < lo).
@@ -516,14 +522,23 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       constexpr std::false_type kAny{};
       const Item* it;
       if (next_item(it)) {
-        int j0 = it->j0, j = j0, j1 = it->j1, plain_lo = it->plain_lo, plain_hi = it->plain_hi;
+        int j0 = it->j0, j = j0, j1 = it->j1, plain_lo = it->plain_lo, plain_hi = it->plain_hi, alone = it->alone;
         uint32_t f = todo(*it, j, j0, j1);
         if (take_k() && issue_s(kAny, f, 0) && issue_s(kAny, f, 1)) give_k();
         // O += P V of a tile, S of the one after it. Between plain tiles there is nothing to
         // look up, and elsewhere it is looked up behind the first product: with a look at
         // the item in front of it this warp alone took 3.5K cycles a tile, its products 2K.
         while (!aborted) {
-          if (j >= plain_lo)
+          if (j >= plain_lo && alone)
+            while (j < plain_hi) {
+              if (!take_v() || !issue_pv(kPlain, 0, 0)) break;
+              give_v();
+              if (!take_k() || !issue_s(kPlain, 0, 0)) break;
+              give_k();
+              f = 0x801;
+              ++j;
+            }
+          else if (j >= plain_lo)
             while (j < plain_hi) {
               if (!take_v() || !issue_pv(kPlain, 0, 0) || !take_k() || !issue_s(kPlain, 0, 0) || !issue_pv(kPlain, 0, 1)) break;
               give_v();
@@ -544,6 +559,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
               j1 = it->j1;
               plain_lo = it->plain_lo;
               plain_hi = it->plain_hi;
+              alone = it->alone;
             }
           }
           const uint32_t nf = more ? todo(*it, j, j0, j1) : 0u;
