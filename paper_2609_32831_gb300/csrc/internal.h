@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include <nvtx3/nvToolsExt.h>
 
 #include "../../include/unicache.h"
@@ -467,6 +469,17 @@ void launch_verify(const VerifyParams& p, int dtype, cudaStream_t st);
 uc_status cuda_check(const char* where);
 uc_status check_segment(const uc_segment* s, const char* fn);
 int num_sms();
+
+// A kernel's dynamic shared memory beyond 48 KB, once for each device (`set`: which have it).
+template <typename K>
+inline void allow_smem(K kernel, size_t bytes, std::atomic<uint64_t>* set) {
+  int dev = 0;
+  cudaGetDevice(&dev);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (set->load(std::memory_order_acquire) & bit) return;
+  cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  set->fetch_or(bit, std::memory_order_release);
+}
 // bf16 rows as a 4D tensor map [128, T, H, B], box 64 x `rows`.
 uc_status encode_rows_4d(CUtensorMap* map, const RowsDev& r, int n_tok, int heads, int batch, int rows);
 // The same as [128, H, T, B], box 64 x `box_heads` x `box_tok`.

@@ -11,7 +11,9 @@
 //    decisions, and looks through a part of the vocabulary for the next token; the
 //    last CTA of a sequence writes its results.
 // Bytes bound it where batches are large: all rows once (the second look finds
-// them in L2).
+// them in L2). 32 sequences of five drafts, 150001 tokens, bf16: 33 us, of which the
+// first kernel 20 (the rows' bytes 15.6), the second the noise's bytes and its own start; small
+// batches 6 to 8 us, two kernels' latency.
 #include <climits>
 #include <cmath>
 #include <cstring>

@@ -16,10 +16,10 @@
 // share of the keys, tile by tile over its warps; the shares of a row block go to the
 // CTAs of a cluster, which joins them through distributed shared memory, and
 // where that is not enough to several clusters, joined by a second kernel.
+#include <atomic>
 #include <climits>
 #include <cmath>
 #include <cstring>
-#include <mutex>
 
 #include "args.h"
 #include "common.cuh"
@@ -417,10 +417,8 @@ __global__ void __launch_bounds__(128) window_join_kernel(const __grid_constant_
 }  // namespace
 
 void launch_window_step(const WindowParams& p, cudaStream_t st) {
-  static std::once_flag once;
-  std::call_once(once, [] {
-    cudaFuncSetAttribute(window_step_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)step_smem(1, 7));
-  });
+  static std::atomic<uint64_t> set{0};
+  allow_smem(window_step_kernel, step_smem(1, 7), &set);
   const int warps = p.row_warps * p.key_warps;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;

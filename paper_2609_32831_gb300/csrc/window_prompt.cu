@@ -16,7 +16,7 @@
 //   warp 8          TMA: Q tiles, K tiles (3 slots), V tiles (2 slots)
 //   warp 9          every tcgen05.mma: S_x = Q_x K^T, O_x += P_x V (P from TMEM), the
 //                   two Q tiles in turn, across items too
-//   warp 10         what the items are, a few ahead of the others
+//   warp 10         what the items are, one ahead of the others
 //   warp 11         zeros in the rows behind the sequences' last queries
 // P enters its product as one bf16 part, rounded by at most 2^-8 of itself: an output
 // carries that beside its own rounding.
@@ -25,9 +25,14 @@
 // the ring) ends, so that the only rows in front of the first key are older ones, or
 // none, which TMA fills with zeros: no row that never held a token is read. First
 // tokens that the window has left make tiles of their own, the last of them as wide
-// as they need (in 16s): its products and its softmax take that share of a tile's.
+// as they need (in 16s): its products take that share of a tile's.
+//
+// The products bound it on long windows: 28 heads of 65536 tokens, 4096 in reach, take
+// 2.61 ms, 1.43 PFLOP/s, and 2.06 ms with no softmax between the products. With few key
+// tiles to an item its start and end weigh more: 16 prompts of up to 4097 tokens, 512 in
+// reach, 205 us where the bytes take 90 and the products 70.
+#include <atomic>
 #include <climits>
-#include <mutex>
 #include <type_traits>
 
 #include "common.cuh"
@@ -816,6 +821,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         const int from = __ffs(again) - 1;
         const int ah = __shfl_sync(0xffffffffu, h, from), at = __shfl_sync(0xffffffffu, t, from);
         const WindowRow y = window_row_alone(p, it.b, ah, at);
+        __syncwarp();  // (behind the row's first stores)
         *reinterpret_cast<uint2*>(p.out.at(it.b, ah, at) + 4 * lane) =
             make_uint2(pack_bf16(y.o.x, y.o.y), pack_bf16(y.o.z, y.o.w));
         if (__shfl_sync(0xffffffffu, alone, from) && lane == 0 && p.lse != nullptr)
@@ -856,10 +862,8 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
 }  // namespace
 
 void launch_window_prompt(const WindowPromptParams& c, int grid, cudaStream_t st) {
-  static std::once_flag once;
-  std::call_once(once, [] {
-    cudaFuncSetAttribute(window_prompt_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PromptSmem));
-  });
+  static std::atomic<uint64_t> set{0};
+  allow_smem(window_prompt_kernel, sizeof(PromptSmem), &set);
   window_prompt_kernel<<<grid, kThreads, sizeof(PromptSmem), st>>>(c);
   count_launch();
   if (c.p.splits > 1) launch_window_join(c.p, st);
