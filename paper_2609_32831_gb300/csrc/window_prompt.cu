@@ -52,9 +52,10 @@ constexpr int kKSlots = 3, kVSlots = 2;
 // warpgroup for the outputs would leave the softmax 192, and took a tenth longer.
 constexpr int kRegSoftmax = 216, kRegOther = 56;
 static_assert(2 * 128 * kRegSoftmax + 128 * kRegOther <= kThreads * 168, "register split");
-// Tensor memory: one S for both Q tiles (a row is in registers long before the other
-// tile's S is due), P and O of each.
-constexpr uint32_t kColP = 128, kColO = 256;
+// Tensor memory of Q tile x: S from column 128 x on, and P in its place once its rows are in
+// registers (S is written again behind the product that reads P: of one thread's products
+// none overtakes another); O.
+constexpr uint32_t kColO = 256;
 constexpr float kNone = -INFINITY;
 
 constexpr int kItemSlots = 2;
@@ -99,12 +100,14 @@ struct Item {
   }
 };
 
+__device__ __noinline__ uint32_t todo_of(const Item& it, int j) { return it.todo(j); }
+
 struct PromptSmem {
   uint8_t q[2][2][16384];        // [128 rows][2 x 64 channels], K-major, 128B swizzle
   uint8_t k[kKSlots][2][16384];
   uint8_t v[kVSlots][2][16384];  // (the MN-major B operand)
   uint64_t k_full[kKSlots], k_empty[kKSlots], v_full[kVSlots], v_empty[kVSlots];
-  uint64_t q_full[2], q_empty[2], s_full[2], s_free[2], p_full[2][2], o_full[2], o_empty[2], drain;
+  uint64_t q_full[2], q_empty[2], s_full[2], p_full[2][2], o_full[2], o_empty[2], drain;
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   Item item[kItemSlots];
   DevStatus status;              // of this CTA's waits
@@ -310,7 +313,6 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       mbar_init(&sm.q_full[x], 1);
       mbar_init(&sm.q_empty[x], 1);
       mbar_init(&sm.s_full[x], 1);
-      mbar_init(&sm.s_free[x], 4);
       mbar_init(&sm.p_full[x][0], 4);
       mbar_init(&sm.p_full[x][1], 4);
       mbar_init(&sm.o_full[x], 1);
@@ -416,8 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       int ks = 0, vs = 0;
       uint32_t kph = 0, vph = 0;
       // parities of the next waits by Q tile (bit x); whether O_x has been used
-      uint32_t q_par = 0, s_par = 0, p_par = 0, o_par = 0, o_any = 0;
-      int s_last = -1;  // the Q tile whose S came last
+      uint32_t q_par = 0, p_par = 0, o_par = 0, o_any = 0;
       // the next item that has key tiles; false: no more
       uint32_t n_item = 0;
       auto next_item = [&](const Item*& it) -> bool {
@@ -432,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       };
       auto todo = [&](const Item& it, int j, int j0, int j1) -> uint32_t {
         const uint32_t a = (uint32_t)(j - j0), z = (uint32_t)(j1 - 1 - j);
-        return a < kLooked ? it.head[a] : z < kLooked ? it.tail[z] : it.todo(j);
+        return a < kLooked ? it.head[a] : z < kLooked ? it.tail[z] : todo_of(it, j);
       };
       // S_x of a tile, with K in slot ks
       auto issue_s = [&](auto plain, uint32_t f, int x) -> bool {
@@ -442,25 +443,18 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           if (!wait_warp(&sm.q_full[x], q_par >> x & 1u, 83, aborted, lim)) return false;
           q_par ^= 1u << x;
         }
-        // the S before this one has been read
-        if ((s_last >= 0)) {
-          if (!wait_warp(&sm.s_free[s_last], s_par >> s_last & 1u, 84, aborted, lim)) return false;
-          s_par ^= 1u << s_last;
-        }
-        s_last = x;
-        tc_fence_after();
         const uint32_t q = q_lo + x * kSlotStep, k = k_lo + (uint32_t)ks * kSlotStep;
         if (kIsPlain || (f >> 8 == 8u)) {  // (with constant descriptors and offsets eight of them issue in half the time)
-          issue_qk<0>(lead, tm, q, k, dhi, id_s);
+          issue_qk<0>(lead, tm + 128 * x, q, k, dhi, id_s);
         } else {
           const uint32_t id = id_s - ((8u - (f >> 8)) << 18);  // (its N: the tile's keys)
 #pragma unroll 1
           for (uint32_t e = 0; e < 8; ++e) {
             const uint32_t at = (e >> 2) * 1024u + (e & 3u) * 2u;
             if (e == 0)
-              umma_ss_lead<0, 0, 0>(lead, tm, q, k, dhi, id);
+              umma_ss_lead<0, 0, 0>(lead, tm + 128 * x, q, k, dhi, id);
             else
-              umma_ss_lead<0, 0, 1>(lead, tm, q + at, k + at, dhi, id);
+              umma_ss_lead<0, 0, 1>(lead, tm + 128 * x, q + at, k + at, dhi, id);
           }
         }
         umma_commit_lead(lead, &sm.s_full[x]);
@@ -471,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         constexpr bool kIsPlain = decltype(plain)::value;
         if (!kIsPlain && !(f >> x & 1u)) return true;
         const uint32_t again = kIsPlain || !(f >> (2 + x) & 1u);
-        const uint32_t d = tm + kColO + 128 * x, a = tm + kColP + 64 * x, vb = v_lo + (uint32_t)vs * kSlotStep;
+        const uint32_t d = tm + kColO + 128 * x, a = tm + 128 * x, vb = v_lo + (uint32_t)vs * kSlotStep;
         if (!again && (o_any >> x & 1u)) {
           if (!wait_warp(&sm.o_empty[x], o_par >> x & 1u, 86, aborted, lim)) return false;
           o_par ^= 1u << x;
@@ -492,13 +486,14 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           umma_ts_lead<6>(lead, d, a, vb, dhi, id_o, 1u);
           umma_ts_lead<7>(lead, d, a, vb, dhi, id_o, 1u);
         } else {
+          const uint32_t w = f >> 8;
 #pragma unroll 1
-          for (uint32_t e = 0; e < 8; ++e) {
+          for (uint32_t e = 0; e < max(w, 5u); ++e) {
             if (e == 4) {
               if (!wait_warp(&sm.p_full[x][1], par, 85, aborted, lim)) return false;
               tc_fence_after();
             }
-            umma_ts_lead<0>(lead & (uint32_t)(e < f >> 8), d, a + 8 * e, vb + 128 * e, dhi, id_o, again | (uint32_t)(e > 0));
+            if (e < w) umma_ts_lead<0>(lead, d, a + 8 * e, vb + 128 * e, dhi, id_o, again | (uint32_t)(e > 0));
           }
         }
         if (!kIsPlain && (f >> (4 + x) & 1u)) {
@@ -525,56 +520,57 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       auto take_v = [&]() { return wait_warp(&sm.v_full[vs], vph, 88, aborted, lim); };
       constexpr std::true_type kPlain{};
       constexpr std::false_type kAny{};
+      // O += P V of a tile, S of the one after it (of the next item, where it was the last).
+      // Between plain tiles there is nothing to look up, and elsewhere the next is looked up
+      // ahead: with a look at the item in front of each product this warp alone took 3.5K cycles
+      // a tile, its products 2K.
       const Item* it;
-      if (next_item(it)) {
-        int j0 = it->j0, j = j0, j1 = it->j1, plain_lo = it->plain_lo, plain_hi = it->plain_hi, alone = it->alone;
-        uint32_t f = todo(*it, j, j0, j1);
-        if (take_k() && issue_s(kAny, f, 0) && issue_s(kAny, f, 1)) give_k();
-        // O += P V of a tile, S of the one after it. Between plain tiles there is nothing to
-        // look up, and elsewhere it is looked up behind the first product: with a look at
-        // the item in front of it this warp alone took 3.5K cycles a tile, its products 2K.
-        while (!aborted) {
-          if (j >= plain_lo && alone)
-            while (j < plain_hi) {
-              if (!take_v() || !issue_pv(kPlain, 0, 0)) break;
-              give_v();
-              if (!take_k() || !issue_s(kPlain, 0, 0)) break;
-              give_k();
-              f = 0x801;
-              ++j;
-            }
-          else if (j >= plain_lo)
-            while (j < plain_hi) {
-              if (!take_v() || !issue_pv(kPlain, 0, 0) || !take_k() || !issue_s(kPlain, 0, 0) || !issue_pv(kPlain, 0, 1)) break;
-              give_v();
-              if (!issue_s(kPlain, 0, 1)) break;
-              give_k();
-              f = 0x803;
-              ++j;
-            }
-          if (aborted || !take_v() || !issue_pv(kAny, f, 0)) break;
-          const uint32_t slot = (n_item - 1) % kItemSlots;  // (the present item's)
-          const bool same = ++j < j1;
-          bool more = true;
-          if (!same) {
-            more = next_item(it);
-            warp_arrive(&sm.item_empty[slot], lane);
-            if (more) {
-              j = j0 = it->j0;
-              j1 = it->j1;
-              plain_lo = it->plain_lo;
-              plain_hi = it->plain_hi;
-              alone = it->alone;
-            }
+      int j0 = 0, j = 0, j1 = 0, plain_lo = INT_MAX, plain_hi = 0, alone = 0;
+      uint32_t f = 0;  // of tile j; 0: there has been none
+      while (!aborted) {
+        if (j >= plain_lo && alone) {
+          while (j < plain_hi) {
+            if (!take_v() || !issue_pv(kPlain, 0, 0)) break;
+            give_v();
+            if (!take_k() || !issue_s(kPlain, 0, 0)) break;
+            give_k();
+            f = 0x801;
+            ++j;
           }
-          const uint32_t nf = more ? todo(*it, j, j0, j1) : 0u;
-          if (more && !(take_k() && issue_s(kAny, nf, 0))) break;
-          if (aborted || !issue_pv(kAny, f, 1)) break;
-          give_v();
-          if (!more || !issue_s(kAny, nf, 1)) break;
-          give_k();
-          f = nf;
+        } else if (j >= plain_lo) {
+          while (j < plain_hi) {
+            if (!take_v() || !issue_pv(kPlain, 0, 0) || !take_k() || !issue_s(kPlain, 0, 0) || !issue_pv(kPlain, 0, 1)) break;
+            give_v();
+            if (!issue_s(kPlain, 0, 1)) break;
+            give_k();
+            f = 0x803;
+            ++j;
+          }
         }
+        const bool same = j + 1 < j1;
+        uint32_t nf = same ? todo(*it, j + 1, j0, j1) : 0u;
+        if (aborted || (f && (!take_v() || !issue_pv(kAny, f, 0)))) break;
+        if (same) {
+          ++j;
+        } else {
+          const uint32_t slot = (n_item - 1) % kItemSlots;  // (the present item's)
+          const bool more = next_item(it);
+          if (f) warp_arrive(&sm.item_empty[slot], lane);
+          if (more) {
+            j = j0 = it->j0;
+            j1 = it->j1;
+            plain_lo = it->plain_lo;
+            plain_hi = it->plain_hi;
+            alone = it->alone;
+            nf = todo(*it, j0, j0, j1);
+          }
+        }
+        if (nf && (!take_k() || !issue_s(kAny, nf, 0))) break;
+        if (aborted || (f && !issue_pv(kAny, f, 1))) break;
+        if (f) give_v();
+        if (!nf || !issue_s(kAny, nf, 1)) break;
+        give_k();
+        f = nf;
       }
     } else if (warp == 10) {
       // ------------------------------------------------------------- items
@@ -620,7 +616,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
     // ------------------------------------------------------------ softmax
     const int x = warp >> 2, r = threadIdx.x & 127;
     const uint32_t lane_off = (uint32_t)(32 * (warp & 3)) << 16;
-    const uint32_t p_col = kColP + 64 * x, o_col = kColO + 128 * x;
+    const uint32_t s_col = 128 * x, o_col = kColO + 128 * x;
     const int token = r / p.group, head = r - token * p.group;
     const bool is_row = token < c.tokens;
     const uint64_t sl2_2 = f2_pack(p.scale_log2, p.scale_log2);
@@ -666,10 +662,6 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         }
         return true;
       };
-      auto loaded = [&]() {
-        tc_fence_before();
-        warp_arrive(&sm.s_free[x], lane);
-      };
       auto give = [&](int half) {
         tmem_wait_st();
         tc_fence_before();
@@ -708,11 +700,10 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         if (!begin()) return false;
         uint32_t sr[4][32];
 #pragma unroll
-        for (int cc = 0; cc < 4; ++cc) tmem_ld32(tmem + lane_off + 32 * cc, sr[cc]);
+        for (int cc = 0; cc < 4; ++cc) tmem_ld32(tmem + lane_off + s_col + 32 * cc, sr[cc]);
         tmem_wait_ld();
 #pragma unroll
         for (int cc = 0; cc < 4; ++cc) tie32(sr[cc]);
-        loaded();
         if (!simple) {
 #pragma unroll
           for (int cc = 0; cc < 4; ++cc) {
@@ -739,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         for (int half = 0; half < 2; ++half) {
           uint32_t pk[32];
           form(sr, pk, acc);
-          tmem_st32(tmem + lane_off + p_col + 32 * half, pk);
+          tmem_st32(tmem + lane_off + s_col + 32 * half, pk);
           give(half);
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
