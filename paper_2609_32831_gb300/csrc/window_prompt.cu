@@ -27,10 +27,13 @@
 // tokens that the window has left make tiles of their own, the last of them as wide
 // as they need (in 16s): its products take that share of a tile's.
 //
-// The products bound it on long windows: 28 heads of 65536 tokens, 4096 in reach, take
-// 2.61 ms, 1.43 PFLOP/s, and 2.06 ms with no softmax between the products. With few key
-// tiles to an item its start and end weigh more: 16 prompts of up to 4097 tokens, 512 in
-// reach, 205 us where the bytes take 90 and the products 70.
+// The products bound it on long windows, under the power limit: 28 heads of 65536 tokens,
+// 4096 in reach, take 2.28 ms once (1.64 PFLOP/s) and 2.45 one after the other, 2.06 with no
+// softmax between the products. With few key tiles to an item its start and end and the MMA
+// warp's look-ups weigh more: 16 prompts of up to 4097 tokens, 512 in reach, 190 us where
+// the bytes take 90 and the products 70. A warp of its own for either Q tile's products
+// took longer (2.97 ms, 219 us: both tiles' products then finish late), and so did S of a
+// tile ahead of the product with P (2.71 ms, 212 us).
 #include <atomic>
 #include <climits>
 #include <type_traits>
@@ -695,7 +698,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       // A tile. `simple`: every row sees it whole, behind its first: nothing but
       // exponentials between S and P. One copy of the code, its halves in a rolled loop over
       // registers: with copies for each kind of tile and half the warps waited for
-      // instructions (16 ragged prompts 233 -> 210 us).
+      // instructions (16 ragged prompts 233 -> 210 us then).
       auto tile = [&](bool simple, bool fresh, int s1, int w0, int w1, int e0, int e1) -> bool {
         if (!begin()) return false;
         uint32_t sr[4][32];
