@@ -382,7 +382,7 @@ bool same_rows(const RowsDev& a, const RowsDev& b) {
 
 // Tokens whose rows one launch can index.
 bool fits(int batch, int n_tok, int heads) {
-  return (int64_t)batch * n_tok * std::max(heads, 1) <= (int64_t(1) << 32);
+  return (int64_t)batch * n_tok <= (int64_t(1) << 32) / std::max(heads, 1);
 }
 
 }  // namespace

@@ -42,7 +42,7 @@ def _rotary(**kw):
     (dict(table=_table(65)), "ARG"), (dict(table=_table(inter=2)), "ARG"), (dict(table=_table(scale=float("inf"))), "ARG"),
     (dict(table=_table(f=float("nan"))), "ARG"), (dict(table=_table(f=2.0 ** 31)), "ARG"), (dict(pos=None), "ARG"),
     (dict(pos=9 * FAKE + 2), "ARG"), (dict(B=0), "SHAPE"), (dict(T=0), "SHAPE"), (dict(hq=0), "SHAPE"),
-    (dict(hkv=0), "SHAPE"), (dict(B=65535, T=1 << 28), "SHAPE"), (dict(q=None), "ARG"), (dict(qo=None), "ARG"),
+    (dict(hkv=0), "SHAPE"), (dict(B=65535, T=1 << 28), "SHAPE"), (dict(B=1 << 30, T=1 << 30, hq=14), "SHAPE"), (dict(q=None), "ARG"), (dict(qo=None), "ARG"),
     (dict(ko=None), "ARG"), (dict(k=None), "ARG"), (dict(q=_rows(1, off=8)), "ARG"), (dict(q=_rows(1, st=64)), "SHAPE"),
     (dict(qo=_rows(2, sb=0)), "SHAPE"), (dict(k=_rows(3, st=132)), "SHAPE"), (dict(qo=_rows(1, off=256)), "ARG"),
     (dict(ko=_rows(2)), "ARG"), (dict(ko=_rows(1)), "ARG"), (dict(qo=_rows(9)), "ARG"),
