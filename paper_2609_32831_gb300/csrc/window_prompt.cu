@@ -30,7 +30,7 @@
 // The products bound it on long windows, under the power limit: 28 heads of 65536 tokens,
 // 4096 in reach, take 2.28 ms once (1.64 PFLOP/s) and 2.45 one after the other, 2.06 with no
 // softmax between the products. With few key tiles to an item its start and end and the MMA
-// warp's look-ups weigh more: 16 prompts of up to 4097 tokens, 512 in reach, 190 us where
+// warp's look-ups weigh more: 16 prompts of up to 4097 tokens, 512 in reach, 186 us where
 // the bytes take 90 and the products 70. A warp of its own for either Q tile's products
 // took longer (2.97 ms, 219 us: both tiles' products then finish late), and so did S of a
 // tile ahead of the product with P (2.71 ms, 212 us).
@@ -699,7 +699,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       // exponentials between S and P. One copy of the code, its halves in a rolled loop over
       // registers: with copies for each kind of tile and half the warps waited for
       // instructions (16 ragged prompts 233 -> 210 us then).
-      auto tile = [&](bool simple, bool fresh, int s1, int w0, int w1, int e0, int e1) -> bool {
+      auto tile = [&](bool simple, bool fresh, int w0, int w1, int e0, int e1) -> bool {
         if (!begin()) return false;
         uint32_t sr[4][32];
 #pragma unroll
@@ -710,8 +710,8 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         if (!simple) {
 #pragma unroll
           for (int cc = 0; cc < 4; ++cc) {
-            const uint32_t see = bits(-32 * cc, s1 - 32 * cc) | bits(w0 - 32 * cc, w1 - 32 * cc) |
-                                 bits(e0 - 32 * cc, e1 - 32 * cc);
+            uint32_t see = bits(w0 - 32 * cc, w1 - 32 * cc);
+            if (in_order) see |= bits(e0 - 32 * cc, e1 - 32 * cc);
             if (__any_sync(0xffffffffu, see != 0xffffffffu)) {
 #pragma unroll
               for (int e = 0; e < 32; ++e)
@@ -747,10 +747,10 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       for (int j = first; j <= last; ++j) {
         if (j >= in_first && (j < in_a || j > in_b)) continue;
         // which of the tile's rows this row sees
-        int s1 = -1, w0 = 0, w1 = -1, e0 = 0, e1 = -1;
+        int w0 = 0, w1, e0 = 0, e1 = -1;
         bool whole;
         if (j < firsts) {
-          s1 = min(j == narrow ? rest : kKeys, min(p.n_sink, pos + 1) - kKeys * j) - 1;  // first tokens: rows 0 .. s1
+          w1 = min(j == narrow ? rest : kKeys, min(p.n_sink, pos + 1) - kKeys * j) - 1;  // first tokens: rows 0 .. w1
           whole = kKeys * (j + 1) <= min(p.n_sink, pfirst + 1);
         } else {
           const bool a = j - firsts < n_a;
@@ -764,7 +764,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           whole = start >= max(plast - p.window + 1, low) && start + kKeys - 1 <= pfirst;
         }
         const bool fresh = __any_sync(0xffffffffu, m_ref == kNone);
-        if (!tile(whole && !fresh, fresh, whole ? kKeys - 1 : s1, w0, w1, e0, e1)) break;
+        if (!tile(whole && !fresh, fresh, whole ? 0 : w0, whole ? kKeys - 1 : w1, e0, e1)) break;
       }
       if (any && (aborted || !wait_warp(&sm.o_full[x], n_o & 1, 91, aborted, lim))) break;
       if (any) ++n_o;
