@@ -775,7 +775,8 @@ typedef struct uc_window_cache {
   uc_rows k, v;                        /* bf16 [batch, n_kv_heads, n_rows] rows */
   int32_t batch, n_kv_heads, n_rows;
   int32_t window;                      /* >= 1 */
-  int32_t n_sink;                      /* 0 .. n_rows - 1 */
+  int32_t n_sink;                      /* >= 0; n_rows and more count as n_rows - 1 (the same, for
+                                          sequences of up to n_rows tokens) */
 } uc_window_cache;
 
 /*

@@ -871,22 +871,23 @@ class WindowCache:
     rows, 128] bf16 with contiguous rows. Token p lies in row p, or, where p >=
     n_sink, in row n_sink + (p - n_sink) mod (rows - n_sink): a ring, unless the rows
     hold every token. Queries of T tokens at once need window + T - 1 rows behind the
-    first ones. How many tokens a sequence holds is the caller's, on the device."""
+    first ones; an n_sink of all rows or more counts as one less. How many tokens a
+    sequence holds is the caller's, on the device."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, window: int, n_sink: int = 0):
         if k.dim() != 4 or k.shape[3] != HEAD_DIM:
             raise ValueError("WindowCache: k and v are bf16 [B, Hkv, rows, 128]")
         for x, name in ((k, "k"), (v, "v")):
             _head_rows("WindowCache", name, x, k.shape, torch.bfloat16)
-        if window < 1 or not 0 <= n_sink < k.shape[2]:
-            raise ValueError("WindowCache: window is at least 1, n_sink at least 0 and less than the rows")
+        if window < 1 or n_sink < 0:
+            raise ValueError("WindowCache: window is at least 1, n_sink at least 0")
         if k.device != v.device:
             raise ValueError("WindowCache: k and v are on one device")
         self.k, self.v, self.window, self.n_sink = k, v, int(window), int(n_sink)
         self.batch, self.n_kv_heads, self.n_rows, _ = k.shape
         rows = [_lib.UcRows(x.data_ptr(), *x.stride()[:3]) for x in (k, v)]
         self.c = _lib.UcWindowCache(*rows, self.batch, self.n_kv_heads, self.n_rows, min(self.window, 1 << 30),
-                                    self.n_sink)
+                                    min(self.n_sink, 1 << 30))
         self._at = C.addressof(self.c)
 
 

@@ -131,7 +131,7 @@ inline uc_status check_window_cache(const uc_window_cache* c, const char* fn, Ro
     return UC_ERR_ARG;
   }
   if (c->batch < 1 || c->batch > 65535 || c->n_kv_heads < 1 || c->n_kv_heads > 65535 || c->n_rows < 1 ||
-      c->n_rows > (1 << 30) || c->window < 1 || c->n_sink < 0 || c->n_sink >= c->n_rows) {
+      c->n_rows > (1 << 30) || c->window < 1 || c->n_sink < 0) {
     set_error("%s: unsupported cache (batch %d, kv heads %d, %d rows, window %d, %d first tokens)", fn, c->batch,
               c->n_kv_heads, c->n_rows, c->window, c->n_sink);
     return UC_ERR_SHAPE;
@@ -139,6 +139,14 @@ inline uc_status check_window_cache(const uc_window_cache* c, const char* fn, Ro
   uc_status st = check_rows(&c->k, fn, "the cache's k", c->batch, c->n_kv_heads, c->n_rows, k, nk);
   if (st == UC_OK) st = check_rows(&c->v, fn, "the cache's v", c->batch, c->n_kv_heads, c->n_rows, v, nv);
   return st;
+}
+
+// n_sink below n_rows, as the kernels need it: of sequences that the rows hold, the last
+// row's token is then seen by its own query alone, which has it in its window.
+inline uc_window_cache within_rows(const uc_window_cache& c) {
+  uc_window_cache r = c;
+  r.n_sink = std::min(c.n_sink, c.n_rows - 1);
+  return r;
 }
 
 }  // namespace uc

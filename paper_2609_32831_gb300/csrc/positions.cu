@@ -475,6 +475,8 @@ uc_status uc_window_append(const uc_window_cache* cache, const uc_rows* k, const
   uint64_t nck, ncv;
   uc_status st = check_window_cache(cache, fn, &ck, &cv, &nck, &ncv);
   if (st != UC_OK) return st;
+  const uc_window_cache cut = within_rows(*cache);
+  cache = &cut;
   const int batch = cache->batch, hkv = cache->n_kv_heads;
   if (n_tok < 1 || (q != nullptr && (n_q_heads < 1 || n_q_heads > 65535)) ||
       !fits(batch, n_tok, 2 * hkv + (q != nullptr ? n_q_heads : 0))) {

@@ -554,7 +554,8 @@ size_t uc_window_workspace_size(const uc_window_cache* cache, int32_t n_q_heads,
       cache->n_kv_heads > 65535 || cache->n_rows < 1 || cache->n_rows > (1 << 30) || cache->window < 1 ||
       cache->n_sink < 0 || check_window_shape(*cache, n_q_heads, n_tok, "uc_window_workspace_size") != UC_OK)
     return 0;
-  return window_bytes(*cache, n_q_heads, n_tok, plan_window(*cache, n_q_heads, n_tok));
+  const uc_window_cache cut = within_rows(*cache);
+  return window_bytes(cut, n_q_heads, n_tok, plan_window(cut, n_q_heads, n_tok));
 }
 
 uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32_t n_q_heads, int32_t n_tok,
@@ -570,6 +571,8 @@ uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32
   if (st == UC_OK) st = check_rows(q, fn, "q", cache->batch, n_q_heads, n_tok, &p.q, &nq);
   if (st == UC_OK) st = check_rows(out, fn, "out", cache->batch, n_q_heads, n_tok, &p.out, &no);
   if (st != UC_OK) return st;
+  const uc_window_cache cut = within_rows(*cache);
+  cache = &cut;
   if (lengths == nullptr || !aligned(lengths, 4) || !aligned(n_query, 4) || !aligned(lse, 4)) {
     set_error("uc_window_attend: null or misaligned argument");
     return UC_ERR_ARG;

@@ -60,7 +60,7 @@ def _cache(k=1, v=2, B=2, hkv=2, rows=64, window=16, sinks=4, sb=2 * 64 * 128, k
 
 CACHES = [(dict(cache=None), "ARG"), (dict(cache=_cache(B=0)), "SHAPE"), (dict(cache=_cache(hkv=0)), "SHAPE"),
           (dict(cache=_cache(rows=0)), "SHAPE"), (dict(cache=_cache(window=0)), "SHAPE"),
-          (dict(cache=_cache(sinks=-1)), "SHAPE"), (dict(cache=_cache(sinks=64)), "SHAPE"),
+          (dict(cache=_cache(sinks=-1)), "SHAPE"),
           (dict(cache=_cache(sb=0)), "SHAPE"), (dict(cache=_cache(koff=8)), "ARG"),
           (dict(cache=_cache(rows=(1 << 30) + 1)), "SHAPE")]
 
@@ -150,7 +150,7 @@ def test_binding_refuses_what_the_library_cannot_see():
                      (bf, bf, p[:, :3]), (cut, bf, p), (bf, cut, p), (bf, bf, p)):      # (the last: not on a GPU)
         with pytest.raises(ValueError):
             api.rotary(turn, at, q, k)
-    for bad in (dict(k=bf.float()), dict(v=bf[:, :1]), dict(k=cut), dict(window=0), dict(n_sink=4), dict(n_sink=-1)):
+    for bad in (dict(k=bf.float()), dict(v=bf[:, :1]), dict(k=cut), dict(window=0), dict(n_sink=-1)):
         with pytest.raises(ValueError):
             api.WindowCache(**{**dict(k=bf, v=bf.clone(), window=2, n_sink=1), **bad})
     c = api.WindowCache(bf, bf.clone(), 2, 1)
