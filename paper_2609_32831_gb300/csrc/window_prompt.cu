@@ -422,16 +422,20 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       uint32_t kph = 0, vph = 0;
       // parities of the next waits by Q tile (bit x); whether O_x has been used
       uint32_t q_par = 0, p_par = 0, o_par = 0, o_any = 0;
-      // the next item that has key tiles; false: no more
+      // The next item that has key tiles. With a product of the present one `pending` no
+      // item without tiles is looked past: what comes behind it takes the present one's
+      // place, which comes free with its last product.
       uint32_t n_item = 0;
-      auto next_item = [&](const Item*& it) -> bool {
+      enum { kEnd, kNoTiles, kTiles };
+      auto next_item = [&](const Item*& it, bool pending) -> int {
         for (;;) {
-          if (!wait_warp(&sm.item_full[n_item % kItemSlots], (n_item / kItemSlots) & 1, 89, aborted, lim)) return false;
+          if (!wait_warp(&sm.item_full[n_item % kItemSlots], (n_item / kItemSlots) & 1, 89, aborted, lim)) return kEnd;
           it = &sm.item[n_item % kItemSlots];
-          if (it->j0 < 0) return false;
+          if (it->j0 < 0) return kEnd;
           ++n_item;
-          if (it->j0 < it->j1) return true;
+          if (it->j0 < it->j1) return kTiles;
           warp_arrive(&sm.item_empty[(n_item - 1) % kItemSlots], lane);
+          if (pending) return kNoTiles;
         }
       };
       auto todo = [&](const Item& it, int j, int j0, int j1) -> uint32_t {
@@ -553,13 +557,14 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         const bool same = j + 1 < j1;
         uint32_t nf = same ? todo(*it, j + 1, j0, j1) : 0u;
         if (aborted || (f && (!take_v() || !issue_pv(kAny, f, 0)))) break;
+        int got = kEnd;
         if (same) {
           ++j;
         } else {
           const uint32_t slot = (n_item - 1) % kItemSlots;  // (the present item's)
-          const bool more = next_item(it);
+          got = next_item(it, f != 0);
           if (f) warp_arrive(&sm.item_empty[slot], lane);
-          if (more) {
+          if (got == kTiles) {
             j = j0 = it->j0;
             j1 = it->j1;
             plain_lo = it->plain_lo;
@@ -571,7 +576,12 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         if (nf && (!take_k() || !issue_s(kAny, nf, 0))) break;
         if (aborted || (f && !issue_pv(kAny, f, 1))) break;
         if (f) give_v();
-        if (!nf || !issue_s(kAny, nf, 1)) break;
+        if (!nf) {
+          f = 0;
+          if (got == kNoTiles) continue;
+          break;
+        }
+        if (!issue_s(kAny, nf, 1)) break;
         give_k();
         f = nf;
       }
