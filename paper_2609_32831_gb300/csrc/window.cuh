@@ -2,6 +2,8 @@
 // and a row from its definition.
 #pragma once
 
+#include <climits>
+
 #include "common.cuh"
 #include "internal.h"
 
@@ -64,42 +66,77 @@ __device__ __forceinline__ bool window_sees(const WindowParams& p, int pos, int 
 }
 
 // The output of one query from its definition, key by key and with none that it
-// does not see, by a warp: lane l has channels 4 l .. 4 l + 3. For rows that a
-// product over whole tiles left NaN or infinite: 0 times what a masked row of v
-// holds is not 0 there.
-struct WindowRow {
+// does not see: for rows that a product over whole tiles left NaN or infinite (0 times what
+// a masked row of v holds is not 0 there). A warp takes every `shares`-th run of four keys from
+// `share` on; lane l has channels 4 l .. 4 l + 3. Sums relative to 2^m.
+struct WindowPart {
   float4 o;
-  float lse;
+  float m, l;
 };
-static __device__ __noinline__ WindowRow window_row_alone(const WindowParams& p, int b, int h, int t) {
+static __device__ __noinline__ WindowPart window_row_part(const WindowParams& p, int b, int h, int t, int share,
+                                                          int shares) {
+  constexpr int kRun = 4;
   const int lane = threadIdx.x & 31, kvh = h / p.group;
   const WindowSeq s = window_seq(p, b);
   const int pos = s.first + t;
   const WindowKeys keys = window_keys(p, s, pos, pos);
+  const int n = keys.count();
   const uint2 qw = *reinterpret_cast<const uint2*>(p.q.at(b, h, t) + 4 * lane);
   const float q[4] = {bf16_lo(qw.x), bf16_hi(qw.x), bf16_lo(qw.y), bf16_hi(qw.y)};
   float o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-  for (int i = 0; i < keys.count(); ++i) {
-    const int key = keys.position(i);
-    if (!window_sees(p, pos, key)) continue;
-    const int row = window_row(p, key);
-    const uint2 kw = *reinterpret_cast<const uint2*>(p.k.at(b, kvh, row) + 4 * lane);
-    const uint2 vw = *reinterpret_cast<const uint2*>(p.v.at(b, kvh, row) + 4 * lane);
-    float x = q[0] * bf16_lo(kw.x) + q[1] * bf16_hi(kw.x) + q[2] * bf16_lo(kw.y) + q[3] * bf16_hi(kw.y);
+  for (int64_t i = (int64_t)kRun * share; i < n; i += kRun * shares) {
+    bool see[kRun];
+    uint2 kw[kRun], vw[kRun];
+    float x[kRun];
 #pragma unroll
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    x *= p.scale_log2;
-    const float top = fmaxf(m, x), base = top == -INFINITY ? 0.f : top;
-    const float shrink = ex2_approx(m - base), e = ex2_approx(x - base);
-    l = l * shrink + e;
-    const float v[4] = {bf16_lo(vw.x), bf16_hi(vw.x), bf16_lo(vw.y), bf16_hi(vw.y)};
+    for (int u = 0; u < kRun; ++u) {
+      const int key = i + u < n ? keys.position((int)i + u) : INT_MAX;
+      see[u] = window_sees(p, pos, key);
+      kw[u] = vw[u] = make_uint2(0u, 0u);
+      if (see[u]) {
+        const int row = window_row(p, key);
+        kw[u] = *reinterpret_cast<const uint2*>(p.k.at(b, kvh, row) + 4 * lane);
+        vw[u] = *reinterpret_cast<const uint2*>(p.v.at(b, kvh, row) + 4 * lane);
+      }
+    }
 #pragma unroll
-    for (int c = 0; c < 4; ++c) o[c] = o[c] * shrink + e * v[c];
+    for (int u = 0; u < kRun; ++u)
+      x[u] = q[0] * bf16_lo(kw[u].x) + q[1] * bf16_hi(kw[u].x) + q[2] * bf16_lo(kw[u].y) + q[3] * bf16_hi(kw[u].y);
+#pragma unroll
+    for (int d = 16; d; d >>= 1)
+#pragma unroll
+      for (int u = 0; u < kRun; ++u) x[u] += __shfl_xor_sync(0xffffffffu, x[u], d);
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < kRun; ++u) {
+      x[u] = see[u] ? x[u] * p.scale_log2 : -INFINITY;
+      top = fmaxf(top, x[u]);
+    }
+    const float base = top == -INFINITY ? 0.f : top, shrink = ex2_approx(m - base);
+    l *= shrink;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] *= shrink;
+#pragma unroll
+    for (int u = 0; u < kRun; ++u) {
+      const float e = ex2_approx(x[u] - base);
+      const float v[4] = {bf16_lo(vw[u].x), bf16_hi(vw[u].x), bf16_lo(vw[u].y), bf16_hi(vw[u].y)};
+      l += e;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] = fmaf(e, v[c], o[c]);
+    }
     m = top;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  return WindowRow{make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv),
-                   l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2};
+  return WindowPart{make_float4(o[0], o[1], o[2], o[3]), m, l};
+}
+
+struct WindowRow {
+  float4 o;
+  float lse;
+};
+__device__ __forceinline__ WindowRow window_row_of(const WindowPart& w) {
+  const float inv = w.l == 0.f ? 0.f : 1.f / w.l;
+  return WindowRow{make_float4(w.o.x * inv, w.o.y * inv, w.o.z * inv, w.o.w * inv),
+                   w.l == 0.f ? -INFINITY : (w.m + log2f(w.l)) * kLn2};
 }
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
@@ -113,7 +150,7 @@ __device__ __forceinline__ void window_store_row(const WindowParams& p, int b, i
   const bool bad = !(finite(y.x) && finite(y.y) && finite(y.z) && finite(y.w));
   float lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
   if (__any_sync(0xffffffffu, bad) && l == l) {
-    const WindowRow w = window_row_alone(p, b, h, t);
+    const WindowRow w = window_row_of(window_row_part(p, b, h, t, 0, 1));
     y = w.o;
     if (!finite(l)) lse = w.lse;
   }

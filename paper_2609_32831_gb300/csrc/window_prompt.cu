@@ -91,6 +91,10 @@ struct Item {
   __device__ __forceinline__ int start(int j) const {
     return part_a(j) ? end_a - kKeys * (n_a - (j - firsts)) : end_b - kKeys * (n - j);
   }
+  // the cache's row of a tile's first key (below 0: rows in front of the cache, taken as zeros)
+  __device__ __forceinline__ int row(const WindowParams& p, int j) const {
+    return j < firsts ? kKeys * j : part_a(j) ? p.n_rows - kKeys * (n_a - (j - firsts)) : slot_b - kKeys * (n - j);
+  }
   __device__ __forceinline__ int width(int j) const { return j == whole && rest > 0 ? rest : kKeys; }
   // What is to do for a key tile. Bit x: Q tile x takes it, 2 + x: as its first, 4 + x: as
   // its last; from bit 8: its keys / 16
@@ -115,6 +119,7 @@ struct PromptSmem {
   Item item[kItemSlots];
   DevStatus status;              // of this CTA's waits
   int loads[4];                  // K, V, Q tile 0 and 1 loads begun
+  uint32_t again;                // the last row put aside (of_again), 0: none
   uint32_t tmem_base;
   int begin[kWindowSeqs + 1];    // items before a sequence's
 };
@@ -222,8 +227,7 @@ __device__ __forceinline__ void tma_4d(void* dst, const CUtensorMap* map, int c0
 __device__ __forceinline__ void load_keys(uint8_t (*slot)[16384], const CUtensorMap* maps, const Item& it, int j,
                                           const WindowPromptParams& c, uint64_t* bar) {
   const int width = it.width(j);
-  const int row = j < it.firsts ? kKeys * j
-                  : it.part_a(j) ? c.p.n_rows - kKeys * (it.n_a - (j - it.firsts)) : it.slot_b - kKeys * (it.n - j);
+  const int row = it.row(c.p, j);
   mbar_arrive_expect_tx(bar, 2 * width * 128);
   const CUtensorMap* const map = width == kKeys ? &maps[0] : &maps[1];
   tma_4d(slot[0], map, 0, row, it.kvh, it.b, bar);
@@ -294,6 +298,110 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
   if (lane == 0) mbar_arrive(bar);
 }
 
+// Is a row whose outputs are not finite (this lane's query at pos; row_ok: there is one) to be
+// computed again? Not where values that it sees are not finite either, in every channel in
+// which ones that it does not see, from the same tiles, are: those outputs are its own. Looked at: the
+// tiles that the warp's rows see in part, the first and the last kWhole of the others. (Where those hold
+// nothing of the kind, sums may have left fp32.)
+static __device__ __noinline__ bool not_its_own(const WindowParams& p, const Item& it, int x, int pos, bool row_ok) {
+  constexpr int kRun = 8;  // rows in flight
+  constexpr int kWhole = 32;
+  const int lane = threadIdx.x & 31;
+  uint32_t seen[4] = {0u, 0u, 0u, 0u}, unseen[4] = {0u, 0u, 0u, 0u};  // channels 4 l + i: bit l
+#pragma unroll 1
+  for (int j = it.first[x]; j <= it.last[x]; ++j) {
+    if (!it.takes(x, j)) continue;
+    const int width = it.width(j), row0 = it.row(p, j);
+    int w0 = 0, w1, e0 = 0, e1 = -1;  // the rows that are seen, as in the kernel
+    if (j < it.firsts) {
+      w1 = min(p.n_sink, pos + 1) - kKeys * j - 1;
+    } else {
+      const int start = it.start(j);
+      w0 = max(pos - p.window + 1, it.part_a(j) ? it.low_a : it.low_b) - start;
+      w1 = pos - start;
+      if (it.in_order) {
+        e0 = -start;
+        e1 = min(p.n_sink - 1, pos) - start;
+      }
+    }
+    const bool whole = __all_sync(0xffffffffu, !row_ok || (w0 <= 0 && w1 >= width - 1));
+    if (whole && j != it.first[x] && j <= it.last[x] - kWhole) continue;
+#pragma unroll 1
+    for (int i = 0; i < width; i += kRun) {  // (widths are multiples of 16)
+      uint2 w[kRun];
+#pragma unroll
+      for (int u = 0; u < kRun; ++u) {
+        const int row = row0 + i + u;
+        w[u] = make_uint2(0u, 0u);
+        if (row >= 0 && row < p.n_rows) w[u] = *reinterpret_cast<const uint2*>(p.v.at(it.b, it.kvh, row) + 4 * lane);
+      }
+#pragma unroll
+      for (int u = 0; u < kRun; ++u) {
+        const float f[4] = {bf16_lo(w[u].x), bf16_hi(w[u].x), bf16_lo(w[u].y), bf16_hi(w[u].y)};
+        if (__all_sync(0xffffffffu, finite(f[0]) && finite(f[1]) && finite(f[2]) && finite(f[3]))) continue;
+        const int at = i + u;
+        const bool sees = (at >= w0 && at <= w1) || (at >= e0 && at <= e1);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t odd = __ballot_sync(0xffffffffu, !finite(f[c]));
+          if (sees)
+            seen[c] |= odd;
+          else
+            unseen[c] |= odd;
+        }
+      }
+    }
+  }
+  uint32_t any = 0u, alone = 0u;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    any |= seen[c];
+    alone |= unseen[c] & ~seen[c];
+  }
+  return row_ok && (any == 0u || alone != 0u);
+}
+
+// Rows that are computed again wait for the end of their CTA's items: key by key they may take
+// longer than the waits of its roles for one another do at most (16 heads of 5120 queries behind
+// 20000 tokens, one of which takes half of the rows out of range: 129 ms, 0.84 without it). They form
+// a list: a row's index and whether its lse is new, plus one, 0 behind the last; the row's first four
+// bytes hold the one before it.
+constexpr uint32_t kNewLse = 1u << 31;
+__device__ __forceinline__ uint32_t of_again(const WindowParams& p, int b, int h, int t, bool new_lse) {
+  return (uint32_t)(((int64_t)b * p.n_q_heads + h) * p.n_tok + t + 1) | (new_lse ? kNewLse : 0u);  // (at most 2^30 rows)
+}
+// By the 8 warps of the softmax, which share a row's keys.
+static __device__ __noinline__ void rows_again(const WindowParams& p, uint32_t list, float (*parts)[kHeadDim + 4]) {
+  constexpr int kWarps = 8;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll 1
+  while (list != 0) {
+    const int at = (int)((list & ~kNewLse) - 1), bh = at / p.n_tok, t = at - bh * p.n_tok;
+    const int b = bh / p.n_q_heads, h = bh - b * p.n_q_heads;
+    const uint32_t before = *reinterpret_cast<const volatile uint32_t*>(p.out.at(b, h, t));
+    const WindowPart w = window_row_part(p, b, h, t, warp, kWarps);
+    *reinterpret_cast<float4*>(&parts[warp][4 * lane]) = w.o;
+    if (lane == 0) *reinterpret_cast<float2*>(&parts[warp][kHeadDim]) = make_float2(w.m, w.l);
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");
+    if (warp == 0) {
+      WindowPart sum{make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
+      for (int i = 0; i < kWarps; ++i) sum.m = fmaxf(sum.m, parts[i][kHeadDim]);
+      const float base = sum.m == -INFINITY ? 0.f : sum.m;
+      for (int i = 0; i < kWarps; ++i) {
+        const float a = ex2_approx(parts[i][kHeadDim] - base);
+        const float4 o = *reinterpret_cast<const float4*>(&parts[i][4 * lane]);
+        sum.l = fmaf(a, parts[i][kHeadDim + 1], sum.l);
+        sum.o = make_float4(fmaf(a, o.x, sum.o.x), fmaf(a, o.y, sum.o.y), fmaf(a, o.z, sum.o.z), fmaf(a, o.w, sum.o.w));
+      }
+      const WindowRow y = window_row_of(sum);
+      *reinterpret_cast<uint2*>(p.out.at(b, h, t) + 4 * lane) = make_uint2(pack_bf16(y.o.x, y.o.y), pack_bf16(y.o.z, y.o.w));
+      if ((list & kNewLse) && lane == 0 && p.lse != nullptr) p.lse[at] = y.lse;
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");
+    list = before;
+  }
+}
+
 __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid_constant__ WindowPromptParams c) {
   extern __shared__ __align__(1024) uint8_t dyn[];
   PromptSmem& sm = *reinterpret_cast<PromptSmem*>(dyn);
@@ -328,6 +436,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
     mbar_init(&sm.drain, 1);
     fence_barrier_init();
     sm.status.code = 0;
+    sm.again = 0;
     sm.loads[0] = sm.loads[1] = sm.loads[2] = sm.loads[3] = 0;
   }
   if (warp == 9) tmem_alloc(&sm.tmem_base, 512);
@@ -819,18 +928,11 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       } else if (row_ok && p.lse != nullptr) {
         p.lse[((int64_t)it.b * p.n_q_heads + h) * p.n_tok + t] = l == 0.f ? kNone : (m_ref + log2f(l)) * kLn2;
       }
-      // rows whose outputs are not finite by no fault of l: from the definition
-      uint32_t again = __ballot_sync(0xffffffffu, row_ok && p.splits == 1 && (alone || (f0 + f1 != 0.f && finite(l))));
-      for (; again; again &= again - 1) {
-        const int from = __ffs(again) - 1;
-        const int ah = __shfl_sync(0xffffffffu, h, from), at = __shfl_sync(0xffffffffu, t, from);
-        const WindowRow y = window_row_alone(p, it.b, ah, at);
-        __syncwarp();  // (behind the row's first stores)
-        *reinterpret_cast<uint2*>(p.out.at(it.b, ah, at) + 4 * lane) =
-            make_uint2(pack_bf16(y.o.x, y.o.y), pack_bf16(y.o.z, y.o.w));
-        if (__shfl_sync(0xffffffffu, alone, from) && lane == 0 && p.lse != nullptr)
-          p.lse[((int64_t)it.b * p.n_q_heads + ah) * p.n_tok + at] = y.lse;
-      }
+      // rows whose outputs are not finite by no fault of l, nor by what they see: put aside
+      bool odd_row = row_ok && p.splits == 1 && !alone && f0 + f1 != 0.f && finite(l);
+      if (__any_sync(0xffffffffu, odd_row)) odd_row &= not_its_own(p, it, x, pos, row_ok);
+      if (odd_row || (row_ok && p.splits == 1 && alone))
+        *reinterpret_cast<uint32_t*>(to) = atomicExch(&sm.again, of_again(p, it.b, h, t, alone));
       warp_arrive(&sm.item_empty[n % kItemSlots], lane);
     }
     tmem_wait_st();
@@ -855,6 +957,8 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       dwait_warp(&sm.drain, 0, p.status, 93, gone);
     }
     __syncthreads();
+  } else if (warp < 8 && sm.again != 0) {
+    rows_again(p, sm.again, reinterpret_cast<float(*)[kHeadDim + 4]>(sm.q));
   }
   if (warp == 9) {
     __syncwarp();
