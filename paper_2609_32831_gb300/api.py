@@ -40,6 +40,14 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _capturing(stream=None) -> bool:
+    """Whether what is launched on ``stream`` (the current one if None) goes into a graph."""
+    if stream is None:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 _STATUS_BYTES = 16   # of a workspace's first bytes (see uc_workspace_status)
 
 
@@ -48,21 +56,25 @@ class Workspace:
 
     ``uc_attend`` and ``uc_attend_batch`` keep self-resetting counters
     in their workspaces, so each gets a buffer of its own ("attend",
-    "attend_batch"); every other entry point shares the "scratch" buffer."""
+    "attend_batch"); every other entry point shares the "scratch" buffer. Calls
+    that may run at the same time, on two streams or in two graphs, need a Workspace
+    each. A buffer that a graph's launches work in stays as long as the Workspace does."""
 
     def __init__(self, device=None):
         self.device = torch.device(device or "cuda")
         self.bufs = {}
         self._at = {}     # (kind, stream handle) -> (address, bytes), for the streams that have worked in the buffer
         self._kept = []   # buffers replaced during a graph's capture, for their status words
+        self._graphs = {}  # address -> buffer, of captured launches: replays use them whatever the next calls need
 
     def get(self, nbytes: int, kind: str = "scratch", stream=None, handle: Optional[int] = None) -> Tuple[int, int]:
         """(address, bytes) of a buffer of at least ``nbytes`` for a launch on
         ``stream`` (the current one if None; its handle, where the caller has it)."""
         if handle is None and self.device.type == "cuda":
             handle = _stream(stream)
+        in_graph = bool(handle) and _capturing(stream)   # (the default stream, 0, is in no capture)
         at = self._at.get((kind, handle))
-        if at is not None and at[1] >= nbytes:
+        if at is not None and at[1] >= nbytes and not in_graph:
             return at
         nbytes = max(256, int(nbytes))
         buf = self.bufs.get(kind)
@@ -71,6 +83,8 @@ class Workspace:
         elif self.device.type == "cuda":
             self._record(buf, stream)
         at = self._at[kind, handle] = buf.data_ptr(), buf.numel()
+        if in_graph:
+            self._graphs[at[0]] = buf
         return at
 
     @staticmethod
@@ -91,7 +105,7 @@ class Workspace:
             with torch.cuda.stream(stream):
                 buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
                 if old is not None:
-                    if torch.cuda.is_current_stream_capturing():
+                    if _capturing():
                         self._kept.append(old)   # (a captured copy would read it at every replay)
                     else:
                         buf[:_STATUS_BYTES].copy_(old[:_STATUS_BYTES])
@@ -102,7 +116,7 @@ class Workspace:
     def status(self, stream=None) -> int:
         """Synchronise and read (then clear) the device status words."""
         code = 0
-        for buf in [*self.bufs.values(), *self._kept]:
+        for buf in {b.data_ptr(): b for b in [*self.bufs.values(), *self._kept, *self._graphs.values()]}.values():
             c = lib().uc_workspace_status(C.c_void_p(buf.data_ptr()), _stream(stream))
             code = code or c
         self._kept.clear()
