@@ -26,6 +26,11 @@
  *  - Conditions only the device can see (a non-finite value to quantize, a
  *    bounded wait that ran out) are recorded in the first 16 bytes of the
  *    call's workspace and read with uc_workspace_status().
+ *  - A workspace is one call's at a time: besides its status word it holds what
+ *    the call's kernels hand to one another (partial results, counters), whatever
+ *    its size. Calls that may run at the same time, on two streams or in
+ *    two replayed graphs, need one each; where they share one, outputs are
+ *    wrong and nothing reports it.
  *  - No entry point ever falls back to a CPU implementation.
  */
 #ifndef UNICACHE_H
@@ -821,7 +826,8 @@ uc_status uc_window_append(const uc_window_cache* cache, const uc_rows* k, const
  * Sums and the softmax are fp32; probabilities enter the product with v with 16 bits
  * where a KV head has up to 8 query rows (Hq / Hkv * n_tok), else rounded to bf16 or better.
  * out and lse share no memory with one another or with what is read. workspace:
- * uc_window_workspace_size() bytes, 16-byte aligned.
+ * uc_window_workspace_size() bytes, 16-byte aligned; of 256 bytes the first are the
+ * status word and the others count the items that a prompt's CTAs have taken.
  */
 uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32_t n_q_heads, int32_t n_tok,
                            const int32_t* lengths, const int32_t* n_query, const uc_rows* out, float* lse,
@@ -857,7 +863,8 @@ size_t uc_window_workspace_size(const uc_window_cache* cache, int32_t n_q_heads,
  * n_draft out of range (taken as the nearest) set UC_ERR_RANGE in the
  * status word; NaN and +inf count as -inf. 1 <= n_tok <= UC_MAX_DRAFTS,
  * B * (n_tok + 1) <= 65535, temperature finite and >= 0. Outputs share no memory with one another or with
- * inputs. workspace: uc_verify_workspace_size() bytes, 16-byte aligned.
+ * inputs. workspace: uc_verify_workspace_size() bytes, 16-byte aligned (the rows'
+ * sums and the best tokens so far).
  */
 #define UC_MAX_DRAFTS 64
 uc_status uc_verify_draft(const void* target, int64_t target_b, int64_t target_t, const void* draft, int64_t draft_b,

@@ -58,10 +58,12 @@ class Workspace:
     in their workspaces, so each gets a buffer of its own ("attend",
     "attend_batch"); every other entry point shares the "scratch" buffer. Calls
     that may run at the same time, on two streams or in two graphs, need a Workspace
-    each. A buffer that a graph's launches work in stays as long as the Workspace does."""
+    each, or, on streams, one that keeps its buffers ``per_stream``. A buffer that a graph's
+    launches work in stays as long as the Workspace does."""
 
-    def __init__(self, device=None):
+    def __init__(self, device=None, per_stream: bool = False):
         self.device = torch.device(device or "cuda")
+        self.per_stream = per_stream   # then the streams other than the default one have buffers (kind, handle)
         self.bufs = {}
         self._at = {}     # (kind, stream handle) -> (address, bytes), for the streams that have worked in the buffer
         self._kept = []   # buffers replaced during a graph's capture, for their status words
@@ -77,22 +79,33 @@ class Workspace:
         if at is not None and at[1] >= nbytes and not in_graph:
             return at
         nbytes = max(256, int(nbytes))
-        buf = self.bufs.get(kind)
+        key = self._key(kind, handle, nbytes, in_graph) if self.per_stream and handle else kind
+        buf = self.bufs.get(key)
         if buf is None or buf.numel() < nbytes:
-            buf = self._grow(buf, nbytes, kind, stream)
+            buf = self._grow(buf, nbytes, key, stream)
         elif self.device.type == "cuda":
             self._record(buf, stream)
-        at = self._at[kind, handle] = buf.data_ptr(), buf.numel()
+        at = buf.data_ptr(), buf.numel()
         if in_graph:
             self._graphs[at[0]] = buf
+        else:
+            self._at[kind, handle] = at
         return at
+
+    def _key(self, kind: str, handle: int, nbytes: int, in_graph: bool):
+        """Under capture a buffer that is large enough already, whichever stream it is of, the default
+        one's first: a new one would lie in the graph's memory, and be cleared by every replay."""
+        if not in_graph:
+            return kind, handle
+        keys = [kind, *(k for k in self.bufs if k[0] == kind)]
+        return next((k for k in keys if k in self.bufs and self.bufs[k].numel() >= nbytes), kind)
 
     @staticmethod
     def _record(buf: torch.Tensor, stream) -> None:
         """The allocator gives ``buf`` to nobody else before ``stream`` is done with it."""
         buf.record_stream(stream or torch.cuda.current_stream())
 
-    def _grow(self, old: Optional[torch.Tensor], nbytes: int, kind: str, stream) -> torch.Tensor:
+    def _grow(self, old: Optional[torch.Tensor], nbytes: int, key, stream) -> torch.Tensor:
         """A larger buffer, cleared on the launch's own stream (a fill on another
         one could run beside the launch); it takes the status word over."""
         if self.device.type != "cuda":
@@ -109,13 +122,16 @@ class Workspace:
                         self._kept.append(old)   # (a captured copy would read it at every replay)
                     else:
                         buf[:_STATUS_BYTES].copy_(old[:_STATUS_BYTES])
-        self._at = {key: at for key, at in self._at.items() if key[0] != kind}
-        self.bufs[kind] = buf
+        kind = key if isinstance(key, str) else key[0]
+        self._at = {k: at for k, at in self._at.items() if k[0] != kind}
+        self.bufs[key] = buf
         return buf
 
     def status(self, stream=None) -> int:
         """Synchronise and read (then clear) the device status words."""
         code = 0
+        if self.per_stream and self.device.type == "cuda":
+            torch.cuda.synchronize(self.device)   # (buffers of any stream)
         for buf in {b.data_ptr(): b for b in [*self.bufs.values(), *self._kept, *self._graphs.values()]}.values():
             c = lib().uc_workspace_status(C.c_void_p(buf.data_ptr()), _stream(stream))
             code = code or c
@@ -127,9 +143,11 @@ _default_ws = {}
 
 
 def default_workspace(device) -> Workspace:
+    """What calls that are given no workspace use: buffers for each stream, so that calls on several
+    streams may run at the same time. (Graphs captured with it share buffers.)"""
     key = torch.device(device).index or 0
     if key not in _default_ws:
-        _default_ws[key] = Workspace(device)
+        _default_ws[key] = Workspace(device, per_stream=True)
     return _default_ws[key]
 
 
