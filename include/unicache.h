@@ -843,7 +843,8 @@ size_t uc_window_workspace_size(const uc_window_cache* cache, int32_t n_q_heads,
  * temperature), or q_t = 1 at d_t where draft is NULL:
  *   draft t is accepted while u[b, t] q_t(d_t) < p_t(d_t); a = the first that is not
  *   the next token is argmax_v w_v / noise[b, v], the lowest v of equal ones, with
- *   w = max(p_a - q_a, 0) where a < n and w = p_n where all were accepted
+ *   w = max(p_a - q_a, 0) where a < n and w = p_n where all were accepted, or where
+ *   p_a - q_a is nowhere above 2^-20 p_a: a draft refused by rounding alone
  * so that with uniform u and noise from the exponential distribution the tokens
  * are distributed as the target's own. temperature 0: a draft is accepted while it
  * is the target's best (the lowest of equal ones), and the next token is that;

@@ -2,7 +2,7 @@
 //
 // A draft d_t is accepted while u_t q_t(d_t) < p_t(d_t); the next token is the
 // argmax of w_v / e_v with w = max(p_a - q_a, 0) behind a rejected draft and w = p_n
-// behind the last. Softmax statistics need whole rows, the choice a second look at
+// behind the last (and where p_a - q_a leaves nothing but rounding). Softmax statistics need whole rows, the choice a second look at
 // two of them:
 // 1. verify_rows_kernel: one CTA per tile of a row (target's and drafter's): its
 //    maximum and the sum of exp((x - max) / temperature), at temperature 0 the
@@ -289,8 +289,9 @@ __global__ void __launch_bounds__(kVerifyThreads, kPickPerSm) verify_pick_kernel
     const float qm = model && rest ? s_m[1][a] : 0.f, qs = model && rest ? 1.f / s_s[1][a] : 0.f;
     const int taken = !model && rest ? p.tokens[b * p.n_tok + a] : -1;
     const int v1 = min(p.vocab, (tile + 1) * p.pick_span);
-    float best = -1.f;
-    int best_at = 0;
+    constexpr float kKnown = 0x1p-20f;  // what p and q are known to, at least
+    float best = 0.f;
+    int best_at = v_first;
     for (int v0 = v_first; v0 < v1; v0 += kVerifyThreads * kDeep) {
       float xs[kDeep], ys[kDeep];
 #pragma unroll
@@ -305,18 +306,34 @@ __global__ void __launch_bounds__(kVerifyThreads, kPickPerSm) verify_pick_kernel
         const int v = v0 + k * kVerifyThreads;
         // (as the sums were formed; a difference above 0 is that of +inf)
         const float dx = xs[k] - pm, dy = ys[k] - qm;
-        float w = dx <= 0.f ? ex2_approx(dx * p.scale.x) * ps : 0.f;
+        const float own = dx <= 0.f ? ex2_approx(dx * p.scale.x) * ps : 0.f;
+        float w = own;
         if (dy <= 0.f) w = fmaf(ex2_approx(dy * p.scale.x), -qs, w);
         if (v == taken) w -= 1.f;
-        w = __fdividef(fmaxf(w, 0.f), es[k]);
-        if (!(w >= 0.f)) w = 0.f;  // (a noise of 0 or NaN)
-        if (v < v1 && w > best) {  // (the first of equal ones: v ascends)
+        w = __fdividef(w > kKnown * own ? w : 0.f, es[k]);
+        if (v < v1 && w > best) {  // (the first of equal ones: v ascends; a noise of 0 or NaN: none)
           best = w;
           best_at = v;
         }
       }
     }
-    if (best >= 0.f) key = ((uint64_t)__float_as_uint(best) << 32) | (0xffffffffu - (uint32_t)best_at);
+    // A weight's rank: its bits, the top one set. A CTA that has found nothing left of p - q
+    // gives p's own best instead, without that bit: it counts where none has found any.
+    uint32_t top_bit = 0x80000000u;
+    if (!__syncthreads_or(best > 0.f)) {
+      top_bit = 0u;
+#pragma unroll 1
+      for (int v = v_first; v < v1; v += kVerifyThreads) {
+        const float dx = to_float(x[v]) - pm;
+        const float w = dx <= 0.f ? __fdividef(ex2_approx(dx * p.scale.x) * ps, noise[v]) : 0.f;
+        if (w > best) {
+          best = w;
+          best_at = v;
+        }
+      }
+    }
+    const uint32_t rank = __float_as_uint(best) | (best > 0.f ? top_bit : 0u);
+    if (v_first < v1) key = ((uint64_t)rank << 32) | (0xffffffffu - (uint32_t)best_at);
   }
 #pragma unroll
   for (int d = 16; d; d >>= 1) {
