@@ -812,7 +812,9 @@ uc_status uc_window_append(const uc_window_cache* cache, const uc_rows* k, const
  *   o = softmax(q . k / sqrt(128)) v
  * to the tokens j <= p of KV head h / (Hq / Hkv) with p - j < window or
  * j < n_sink, as far as the cache holds them: a ring that is shorter than
- * window + n_query - 1 has lost some to later tokens.
+ * window + n_query - 1 has lost some to later tokens, which is not reported
+ * (prompts beyond that attend over their own rows as a cache, and are appended
+ * afterwards, k turned by uc_rotary and without a table).
  *   q, out     bf16 [B, n_q_heads, n_tok] rows
  *   lengths    device int32 [B], >= 0: tokens held, the queries' own among them
  *   n_query    device int32 [B], 0 .. n_tok; NULL: n_tok each

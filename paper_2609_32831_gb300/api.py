@@ -902,9 +902,12 @@ class WindowCache:
     first ``n_sink`` ones (uc_window_cache), over caller tensors k, v [B, Hkv,
     rows, 128] bf16 with contiguous rows. Token p lies in row p, or, where p >=
     n_sink, in row n_sink + (p - n_sink) mod (rows - n_sink): a ring, unless the rows
-    hold every token. Queries of T tokens at once need window + T - 1 rows behind the
-    first ones; an n_sink of all rows or more counts as one less. How many tokens a
-    sequence holds is the caller's, on the device."""
+    hold every token. T tokens that are appended and then attend at once need window +
+    T - 1 rows behind the first ones: with fewer their first queries miss tokens that
+    the last of them replaced, which nothing reports. (A longer prompt attends over a
+    WindowCache of its own k and v, turned by ``rotary``, and is appended afterwards.)
+    An n_sink of all rows or more counts as one less. How many tokens a sequence holds
+    is the caller's, on the device."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, window: int, n_sink: int = 0):
         if k.dim() != 4 or k.shape[3] != HEAD_DIM:
@@ -967,8 +970,8 @@ def window_attend(q: torch.Tensor, cache: WindowCache, lengths: torch.Tensor, n_
                   ws: Optional[Workspace] = None, stream=None):
     """Attention with a sliding window and first tokens (uc_window_attend): the
     queries q bf16 [B, Hq, T, 128] are the last n_query[b] (None: T) of the
-    lengths[b] tokens that sequence b holds in ``cache``, their own among them;
-    device int32 [B]. Returns (out, lse): out with q's shape (and its strides
+    lengths[b] tokens that sequence b holds in ``cache``, their own among them (as
+    far as a ring still has what they see: see WindowCache); device int32 [B]. Returns (out, lse): out with q's shape (and its strides
     where q has no gaps), 0 behind a sequence's last query; lse fp32 [B, Hq, T] or None."""
     fn, shape = "window_attend", q.shape
     if len(shape) != 4 or shape[0] != cache.batch or shape[3] != HEAD_DIM or lengths is None:
