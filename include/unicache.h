@@ -826,7 +826,8 @@ uc_status uc_window_append(const uc_window_cache* cache, const uc_rows* k, const
  * n_query out of range sets UC_ERR_RANGE in the status word; it is then taken
  * as the nearest in range.
  * Sums and the softmax are fp32; probabilities enter the product with v with 16 bits
- * where a KV head has up to 8 query rows (Hq / Hkv * n_tok), else rounded to bf16 or better.
+ * where a KV head has up to 128 query rows (Hq / Hkv * n_tok: single tokens, drafts), else
+ * rounded to bf16 or better.
  * out and lse share no memory with one another or with what is read. workspace:
  * uc_window_workspace_size() bytes, 16-byte aligned; of 256 bytes the first are the
  * status word and the others count the items that a prompt's CTAs have taken.

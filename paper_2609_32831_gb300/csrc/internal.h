@@ -438,6 +438,7 @@ struct WindowPromptParams {
   int tokens;
   uint32_t* taken;       // items taken beyond the CTAs' first ones (0 before the launch), or null: there are none
   bool wide_out;         // rows of out start on 32 bytes
+  bool two_parts;        // P in two bf16 parts: outputs carry their own rounding only
 };
 void launch_window_prompt(const WindowPromptParams& c, int grid, cudaStream_t st);
 

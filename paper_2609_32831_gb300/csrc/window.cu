@@ -494,7 +494,7 @@ WindowPlan plan_step(const uc_window_cache& c, int64_t rows, int group, int n_to
 // Up to 8 query rows of a KV head go step by step: keys and values are read at 93 % of
 // the copy rate. More rows wait for a warp's products and softmax there (64 sequences of
 // 35 rows over 4100 keys: 312 us, 109 on the tensor cores), unless there are few keys as well
-// (8 sequences of 14 rows over 1030 keys: 12 us instead of 17).
+// (8 sequences of 14 rows over 1030 keys: 12 us instead of 17, with P in one part there).
 WindowPlan plan_window(const uc_window_cache& c, int n_q_heads, int n_tok) {
   const int group = n_q_heads / c.n_kv_heads;
   const int64_t rows = (int64_t)group * n_tok;
@@ -633,6 +633,7 @@ uc_status uc_window_attend(const uc_window_cache* cache, const uc_rows* q, int32
   }
   if (st != UC_OK) return st;
   c.wide_out = aligned(p.out.base, 32) && p.out.sb % 16 == 0 && p.out.sh % 16 == 0 && p.out.st % 16 == 0;
+  c.two_parts = (int64_t)p.group * n_tok <= kQTileRows;
   const int64_t items = (int64_t)batch * hkv * w.row_blocks * w.splits;
   const int grid = (int)std::min<int64_t>(items, num_sms());
   const cudaStream_t cs = reinterpret_cast<cudaStream_t>(stream);

@@ -19,7 +19,12 @@
 //   warp 10         what the items are, one ahead of the others
 //   warp 11         zeros in the rows behind the sequences' last queries
 // P enters its product as one bf16 part, rounded by at most 2^-8 of itself: an output
-// carries that beside its own rounding.
+// carries that beside its own rounding. A second part would add half of the products, which bound
+// prompts. Calls of one Q tile (up to 128 query rows of a KV head: drafts) have two, so
+// that a token is attended as exactly among drafts as alone: their key tiles come from HBM once
+// each, 2.8K cycles a tile at the copy rate beside 1.5K of one Q tile's products (1K with one
+// part). 64 sequences of 35 rows over 4100 keys take 109 us so, 104 with one part; 256 of 40 over
+// 517 keys 63 and 57.7.
 //
 // Key tiles are 128 rows of the cache. They end where the last query's own key (or
 // the ring) ends, so that the only rows in front of the first key are older ones, or
@@ -59,6 +64,11 @@ static_assert(2 * 128 * kRegSoftmax + 128 * kRegOther <= kThreads * 168, "regist
 // registers (S is written again behind the product that reads P: of one thread's products
 // none overtakes another); O.
 constexpr uint32_t kColO = 256;
+// With P in two parts (one Q tile) P has columns of its own, those that the second tile would have,
+// two places in turn: S of a tile is written while the product with P of the one before it
+// goes on. The first 64 keys' parts, then the others'.
+constexpr uint32_t kColLow = 32;  // (the second part, from the first)
+__device__ __forceinline__ uint32_t col_p(int half, uint32_t turn) { return (turn == 0 ? 128u : 384u) + 64 * half; }
 constexpr float kNone = -INFINITY;
 
 constexpr int kItemSlots = 2;
@@ -402,6 +412,11 @@ static __device__ __noinline__ void rows_again(const WindowParams& p, uint32_t l
   }
 }
 
+// kTwo: one Q tile, P in two bf16 parts. The second Q tile's barriers then serve the first: p_full[t]
+// is that of every second tile, t its place of P (a tile's P may be complete before the MMA warp
+// asks for that of the one before it: two phases of one barrier could not be told apart), and s_full[1]
+// says that a tile's product with P is complete.
+template <bool kTwo>
 __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid_constant__ WindowPromptParams c) {
   extern __shared__ __align__(1024) uint8_t dyn[];
   PromptSmem& sm = *reinterpret_cast<PromptSmem*>(dyn);
@@ -554,7 +569,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       // S_x of a tile, with K in slot ks
       auto issue_s = [&](auto plain, uint32_t f, int x) -> bool {
         constexpr bool kIsPlain = decltype(plain)::value;
-        if (!kIsPlain && !(f >> x & 1u)) return true;
+        if ((kTwo && x == 1) || (!kIsPlain && !(f >> x & 1u))) return true;
         if (!kIsPlain && (f >> (2 + x) & 1u)) {
           if (!wait_warp(&sm.q_full[x], q_par >> x & 1u, 83, aborted, lim)) return false;
           q_par ^= 1u << x;
@@ -577,44 +592,79 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         if (!kIsPlain && (f >> (4 + x) & 1u)) umma_commit_lead(lead, &sm.q_empty[x]);
         return true;
       };
+      // Two parts: the first or second half of P of the next tile, by its place's barrier.
+      uint32_t n_p = 0;  // tiles whose products with P have been issued
+      auto wait_p = [&](int half) -> bool {
+        if (!wait_warp(&sm.p_full[n_p & 1u][half], n_p >> 1 & 1u, 85, aborted, lim)) return false;
+        tc_fence_after();
+        return true;
+      };
+      // O_x += P_x V of a tile. Two parts: of its first and its second 64 keys, x the half. S of the next tile
+      // comes between them, as between two Q tiles: it has been read where the first half of P is there.
       auto issue_pv = [&](auto plain, uint32_t f, int x) -> bool {
         constexpr bool kIsPlain = decltype(plain)::value;
-        if (!kIsPlain && !(f >> x & 1u)) return true;
-        const uint32_t again = kIsPlain || !(f >> (2 + x) & 1u);
-        const uint32_t d = tm + kColO + 128 * x, a = tm + 128 * x, vb = v_lo + (uint32_t)vs * kSlotStep;
-        if (!again && (o_any >> x & 1u)) {
-          if (!wait_warp(&sm.o_empty[x], o_par >> x & 1u, 86, aborted, lim)) return false;
-          o_par ^= 1u << x;
+        const int qt = kTwo ? 0 : x;
+        if (!kIsPlain && !(f >> qt & 1u)) return true;
+        const uint32_t again = kIsPlain || !(f >> (2 + qt) & 1u);
+        const uint32_t d = tm + kColO + 128 * qt, vb = v_lo + (uint32_t)vs * kSlotStep;
+        if (!again && (!kTwo || x == 0) && (o_any >> qt & 1u)) {
+          if (!wait_warp(&sm.o_empty[qt], o_par >> qt & 1u, 86, aborted, lim)) return false;
+          o_par ^= 1u << qt;
         }
-        const uint32_t par = p_par >> x & 1u;
-        p_par ^= 1u << x;
-        if (!wait_warp(&sm.p_full[x][0], par, 85, aborted, lim)) return false;
-        tc_fence_after();
-        if (kIsPlain || (f >> 8 == 8u)) {
-          umma_ts_lead<0>(lead, d, a, vb, dhi, id_o, again);
-          umma_ts_lead<1>(lead, d, a, vb, dhi, id_o, 1u);
-          umma_ts_lead<2>(lead, d, a, vb, dhi, id_o, 1u);
-          umma_ts_lead<3>(lead, d, a, vb, dhi, id_o, 1u);
-          if (!wait_warp(&sm.p_full[x][1], par, 85, aborted, lim)) return false;
-          tc_fence_after();
-          umma_ts_lead<4>(lead, d, a, vb, dhi, id_o, 1u);
-          umma_ts_lead<5>(lead, d, a, vb, dhi, id_o, 1u);
-          umma_ts_lead<6>(lead, d, a, vb, dhi, id_o, 1u);
-          umma_ts_lead<7>(lead, d, a, vb, dhi, id_o, 1u);
-        } else {
-          const uint32_t w = f >> 8;
+        const uint32_t w = kIsPlain ? 8u : f >> 8;
+        if constexpr (kTwo) {
+          if (!wait_p(x)) return false;
+          const uint32_t a = tm + col_p(x, n_p & 1u), v = vb + 512 * x, n = min(max((int)w - 4 * x, 0), 4);
+          const uint32_t acc = again | (uint32_t)x;
+          if (n == 4) {
+            umma_ts_lead<0>(lead, d, a, v, dhi, id_o, acc);
+            umma_ts_lead<1>(lead, d, a, v, dhi, id_o, 1u);
+            umma_ts_lead<2>(lead, d, a, v, dhi, id_o, 1u);
+            umma_ts_lead<3>(lead, d, a, v, dhi, id_o, 1u);
+            umma_ts_lead<0>(lead, d, a + kColLow, v, dhi, id_o, 1u);
+            umma_ts_lead<1>(lead, d, a + kColLow, v, dhi, id_o, 1u);
+            umma_ts_lead<2>(lead, d, a + kColLow, v, dhi, id_o, 1u);
+            umma_ts_lead<3>(lead, d, a + kColLow, v, dhi, id_o, 1u);
+          } else {
 #pragma unroll 1
-          for (uint32_t e = 0; e < max(w, 5u); ++e) {
-            if (e == 4) {
-              if (!wait_warp(&sm.p_full[x][1], par, 85, aborted, lim)) return false;
-              tc_fence_after();
+            for (uint32_t e = 0; e < n; ++e) {
+              umma_ts_lead<0>(lead, d, a + 8 * e, v + 128 * e, dhi, id_o, acc | (uint32_t)(e > 0));
+              umma_ts_lead<0>(lead, d, a + kColLow + 8 * e, v + 128 * e, dhi, id_o, 1u);
             }
-            if (e < w) umma_ts_lead<0>(lead, d, a + 8 * e, vb + 128 * e, dhi, id_o, again | (uint32_t)(e > 0));
+          }
+          if (x == 0) return true;
+          ++n_p;
+          umma_commit_lead(lead, &sm.s_full[1]);
+        } else {
+          const uint32_t a = tm + 128 * x, par = p_par >> x & 1u;
+          p_par ^= 1u << x;
+          if (!wait_warp(&sm.p_full[x][0], par, 85, aborted, lim)) return false;
+          tc_fence_after();
+          if (w == 8u) {
+            umma_ts_lead<0>(lead, d, a, vb, dhi, id_o, again);
+            umma_ts_lead<1>(lead, d, a, vb, dhi, id_o, 1u);
+            umma_ts_lead<2>(lead, d, a, vb, dhi, id_o, 1u);
+            umma_ts_lead<3>(lead, d, a, vb, dhi, id_o, 1u);
+            if (!wait_warp(&sm.p_full[x][1], par, 85, aborted, lim)) return false;
+            tc_fence_after();
+            umma_ts_lead<4>(lead, d, a, vb, dhi, id_o, 1u);
+            umma_ts_lead<5>(lead, d, a, vb, dhi, id_o, 1u);
+            umma_ts_lead<6>(lead, d, a, vb, dhi, id_o, 1u);
+            umma_ts_lead<7>(lead, d, a, vb, dhi, id_o, 1u);
+          } else {
+#pragma unroll 1
+            for (uint32_t e = 0; e < max(w, 5u); ++e) {
+              if (e == 4) {
+                if (!wait_warp(&sm.p_full[x][1], par, 85, aborted, lim)) return false;
+                tc_fence_after();
+              }
+              if (e < w) umma_ts_lead<0>(lead, d, a + 8 * e, vb + 128 * e, dhi, id_o, again | (uint32_t)(e > 0));
+            }
           }
         }
-        if (!kIsPlain && (f >> (4 + x) & 1u)) {
-          umma_commit_lead(lead, &sm.o_full[x]);
-          o_any |= 1u << x;
+        if (!kIsPlain && (f >> (4 + qt) & 1u)) {
+          umma_commit_lead(lead, &sm.o_full[qt]);
+          o_any |= 1u << qt;
         }
         return true;
       };
@@ -644,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       int j0 = 0, j = 0, j1 = 0, plain_lo = INT_MAX, plain_hi = 0, alone = 0;
       uint32_t f = 0;  // of tile j; 0: there has been none
       while (!aborted) {
-        if (j >= plain_lo && alone) {
+        if (!kTwo && j >= plain_lo && alone) {
           while (j < plain_hi) {
             if (!take_v() || !issue_pv(kPlain, 0, 0)) break;
             give_v();
@@ -659,7 +709,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
             give_v();
             if (!issue_s(kPlain, 0, 1)) break;
             give_k();
-            f = 0x803;
+            f = kTwo ? 0x801 : 0x803;
             ++j;
           }
         }
@@ -762,12 +812,16 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       const bool in_order = it.in_order;
       const bool any = first <= last;
       constexpr float kFar = 1.2676506e30f;  // 2^100
-      // S is complete, and with it every product of O before it
+      // S is complete, and with it every product of O before it (two parts: but the last tile's second half)
       auto begin = [&]() -> bool {
         if (!wait_warp(&sm.s_full[x], n_s & 1, 90, aborted, lim)) return false;
         ++n_s;
         tc_fence_after();
         if (__any_sync(0xffffffffu, shift != 0)) {
+          if constexpr (kTwo) {
+            if (!wait_warp(&sm.s_full[1], n_s & 1, 95, aborted, lim)) return false;  // (of the tile before, n_s - 2)
+            tc_fence_after();
+          }
           const float alpha = __uint_as_float((uint32_t)(127 - shift) << 23);
 #pragma unroll 1
           for (int cb = 0; cb < 8; ++cb) {
@@ -787,15 +841,15 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
       auto give = [&](int half) {
         tmem_wait_st();
         tc_fence_before();
-        warp_arrive(&sm.p_full[x][half], lane);
+        warp_arrive(&sm.p_full[kTwo ? (n_s - 1) & 1 : x][half], lane);
       };
       auto count = [&](float sum) {
         l += sum;
         alone |= sum > kFar;
         if (sum > 32768.f) shift = (int)(__float_as_uint(sum) >> 23) - 127;
       };
-      // 2^(s - m) of the first 64 columns as bf16 pairs; acc: sums
-      auto form = [&](const uint32_t (&sr)[4][32], uint32_t (&pk)[32], uint64_t (&acc)[2]) {
+      // 2^(s - m) of the first 64 columns as bf16 pairs (low: what they leave of it); acc: sums
+      auto form = [&](const uint32_t (&sr)[4][32], uint32_t (&pk)[32], uint32_t (&low)[32], uint64_t (&acc)[2]) {
         const float mb = m_ref == kNone ? 0.f : m_ref;
         const uint64_t nm2 = f2_pack(-mb, -mb);
 #pragma unroll
@@ -807,6 +861,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
           const float a = ex2_approx(e0f), bb = ex2_approx(e1f);
           acc[i & 1] = f2_add(acc[i & 1], f2_pack(a, bb));
           pk[i] = pack_bf16(a, bb);
+          if constexpr (kTwo) low[i] = pack_bf16(a - bf16_lo(pk[i]), bb - bf16_hi(pk[i]));
         }
       };
       auto total = [&](const uint64_t (&acc)[2]) {
@@ -850,9 +905,15 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
         uint64_t acc[2] = {0ull, 0ull};
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
-          uint32_t pk[32];
-          form(sr, pk, acc);
-          tmem_st32(tmem + lane_off + s_col + 32 * half, pk);
+          uint32_t pk[32], low[32];
+          form(sr, pk, low, acc);
+          if constexpr (kTwo) {
+            const uint32_t to = tmem + lane_off + col_p(half, (n_s - 1) & 1);
+            tmem_st32(to, pk);
+            tmem_st32(to + kColLow, low);
+          } else {
+            tmem_st32(tmem + lane_off + s_col + 32 * half, pk);
+          }
           give(half);
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
@@ -970,9 +1031,10 @@ __global__ void __launch_bounds__(kThreads, 1) window_prompt_kernel(const __grid
 }  // namespace
 
 void launch_window_prompt(const WindowPromptParams& c, int grid, cudaStream_t st) {
-  static std::atomic<uint64_t> set{0};
-  allow_smem(window_prompt_kernel, sizeof(PromptSmem), &set);
-  window_prompt_kernel<<<grid, kThreads, sizeof(PromptSmem), st>>>(c);
+  static std::atomic<uint64_t> set[2];
+  const auto kernel = c.two_parts ? window_prompt_kernel<true> : window_prompt_kernel<false>;
+  allow_smem(kernel, sizeof(PromptSmem), &set[c.two_parts]);
+  kernel<<<grid, kThreads, sizeof(PromptSmem), st>>>(c);
   count_launch();
   if (c.p.splits > 1) launch_window_join(c.p, st);
 }
