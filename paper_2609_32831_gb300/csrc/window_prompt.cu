@@ -334,7 +334,7 @@ static __device__ __noinline__ bool not_its_own(const WindowParams& p, const Ite
         e1 = min(p.n_sink - 1, pos) - start;
       }
     }
-    const bool whole = __all_sync(0xffffffffu, !row_ok || (w0 <= 0 && w1 >= width - 1));
+    const bool whole = __all_sync(0xffffffffu, !row_ok || (w0 <= 0 && w1 >= width - 1) || (e0 <= 0 && e1 >= width - 1));
     if (whole && j != it.first[x] && j <= it.last[x] - kWhole) continue;
 #pragma unroll 1
     for (int i = 0; i < width; i += kRun) {  // (widths are multiples of 16)

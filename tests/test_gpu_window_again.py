@@ -108,3 +108,24 @@ def test_values_that_are_not_seen(window):
         err = (2 * d + 2.0 ** -8) * spread
         far = (out[0, h, at].double() - o).abs() - (err + 2.0 ** -8 * (o.abs() + err))
         assert bool((far[keep] <= 0).all())
+
+
+def test_first_tokens_that_are_seen():
+    """Tens of thousands of first tokens, one of whose values is bad: seen in every tile, window or not."""
+    q, k, v = make(4)
+    n = ints([N])
+    ws = uc.Workspace(DEV)
+    cache = uc.WindowCache(k, v, 500, 24000)
+    want, l0 = uc.window_attend(q, cache, n, ws=ws)
+    v[:, :, 11000, 3] = float("nan")
+    prev = uc.set_wait_limit(20_000_000)
+    try:
+        out, lse = uc.window_attend(q, cache, n, ws=ws)
+        assert ws.status() == _lib.UC_OK
+    finally:
+        uc.set_wait_limit(prev)
+    hit = torch.zeros(128, dtype=torch.bool, device=DEV)
+    hit[3] = True
+    assert torch.equal(lse, l0) and not bool(torch.isfinite(out[..., hit]).any())
+    # (one bad value beyond the tiles that are looked at: the rows are computed again, p not rounded)
+    assert float((out[..., ~hit].float() - want[..., ~hit].float()).abs().max()) <= 3 * 2.0 ** -8 * float(v[:, :, :11000].abs().max())
