@@ -430,7 +430,7 @@ void launch_window_step(const WindowParams& p, cudaStream_t st);
 void launch_window_join(const WindowParams& p, cudaStream_t st);
 
 // Prompts: tiles of `tokens` tokens x the heads of a KV head, up to 128 rows.
-constexpr int kWindowSeqs = 256;  // sequences of a call at most
+constexpr int kWindowSeqs = 256;  // sequences of a call at most: their first items lie in what the tiles leave of shared memory
 struct WindowPromptParams {
   WindowParams p;
   CUtensorMap tq;        // box 64 channels x the group's heads x tokens

@@ -33,7 +33,7 @@
 // as they need (in 16s): its products take that share of a tile's.
 //
 // The products bound it on long windows, under the power limit: 28 heads of 65536 tokens,
-// 4096 in reach, take 2.28 ms once (1.64 PFLOP/s) and 2.45 one after the other, 2.06 with no
+// 4096 in reach, take 2.29 ms once (1.63 PFLOP/s) and 2.45 to 2.52 one after the other, 2.06 with no
 // softmax between the products. With few key tiles to an item its start and end and the MMA
 // warp's look-ups weigh more: 16 prompts of up to 4097 tokens, 512 in reach, 186 us where
 // the bytes take 90 and the products 70. A warp of its own for either Q tile's products
