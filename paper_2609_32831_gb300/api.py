@@ -144,7 +144,8 @@ _default_ws = {}
 
 def default_workspace(device) -> Workspace:
     """What calls that are given no workspace use: buffers for each stream, so that calls on several
-    streams may run at the same time. (Graphs captured with it share buffers.)"""
+    streams may run at the same time. (Graphs captured with it share buffers, with one another
+    and with calls that are not captured.)"""
     key = torch.device(device).index or 0
     if key not in _default_ws:
         _default_ws[key] = Workspace(device, per_stream=True)
